@@ -314,6 +314,34 @@ xconv_status xconv_sketch_wgrad_host(const xconv_desc* desc, const void* hX, con
 xconv_status xconv_sketch_static(const xconv_desc* desc, const void* X, const void* Z, float* sketch,
                                  void* cuda_stream);
 
+/* ---- Around the layers.  The method leaves these to "standard" training; they have no counterpart in the paper.
+ *
+ * Layer norm over the channels: of every pixel of a channels-last tensor, or over the last axis of a matrix of tokens.  Row i (of `rows`) has C values,
+ *   mean[i] = sum_c x[i,c] / C,   rstd[i] = 1 / sqrt(sum_c (x[i,c] - mean[i])^2 / C + eps),   y[i,c] = (x[i,c] - mean[i]) * rstd[i] * weight[c] + bias[c]
+ * and its gradients, with xh = (x - mean) * rstd and g = dY * weight,
+ *   dX[i,c] = rstd[i] * (g[i,c] - sum_c g / C - xh[i,c] * sum_c (g * xh) / C),   dweight[c] = sum_i dY[i,c] * xh[i,c],   dbias[c] = sum_i dY[i,c].
+ * X, Y, dY, dX are stored in `dtype`, weight and bias in `param_dtype` (XCONV_F32, or `dtype`); mean, rstd, dweight and dbias are float, and so are all sums.
+ * Element (i, c) of X lies at i * x_stride + c, of Y and dY at i * y_stride + c, of dX at i * dx_stride + c (strides in elements: views of some of the channels of a
+ * wider tensor; inputs may have a stride below C, outputs not).  Pointers need the alignment of their elements only; where all rows lie on 16-byte boundaries
+ * they are read and written 16 bytes at a time.  Outputs overlap neither inputs nor each other. */
+typedef struct {
+  int64_t rows;
+  int32_t C;
+  int32_t dtype, param_dtype;
+  float eps;                          /* not negative */
+  int64_t x_stride, y_stride, dx_stride;
+} xconv_norm_desc;
+
+/* weight and bias may be NULL (1 and 0), and so may mean and rstd, both together.  desc.dx_stride is ignored.  No scratch. */
+xconv_status xconv_layernorm_forward(const xconv_norm_desc* desc, const void* X, const void* weight, const void* bias, void* Y, float* mean, float* rstd,
+                                     void* cuda_stream);
+
+/* mean and rstd as the forward call left them (desc.eps is ignored).  weight may be NULL (1), dweight and dbias too: what is NULL is not computed, and with both
+ * NULL `ws` may be.  ws: xconv_layernorm_workspace_bytes(desc) bytes, 16-byte aligned (0 for an invalid descriptor). */
+size_t xconv_layernorm_workspace_bytes(const xconv_norm_desc* desc);
+xconv_status xconv_layernorm_backward(const xconv_norm_desc* desc, const void* dY, const void* X, const float* mean, const float* rstd, const void* weight, void* dX,
+                                      float* dweight, float* dbias, void* ws, size_t ws_bytes, void* cuda_stream);
+
 /* Reads the status the kernels of the last call left in the header of `ws` (synchronises
  * `cuda_stream`).  XCONV_OK, or XCONV_ERR_TIMEOUT if a bounded device-side wait ran out in that call.
  * The header never needs clearing: every call tags it afresh, so a later call on the same `ws`

@@ -12,7 +12,7 @@ import ctypes
 import os
 import threading
 import warnings
-from ctypes import POINTER, Structure, c_char_p, c_float, c_int, c_int32, c_size_t, c_void_p
+from ctypes import POINTER, Structure, c_char_p, c_float, c_int, c_int32, c_int64, c_size_t, c_void_p
 
 import torch
 
@@ -35,6 +35,7 @@ EXPORTS = ("xconv_workspace_bytes", "xconv_engine_for", "xconv_variants_for", "x
            "xconv_sketch_independent", "xconv_wgrad_independent", "xconv_zero_blocks", "xconv_zero_blocks_used",
            "xconv_gaussian_probes_from_seed", "xconv_sketch_seeded_gaussian", "xconv_wgrad_seeded_gaussian",
            "xconv_block_sparse_probes_from_seed",
+           "xconv_layernorm_workspace_bytes", "xconv_layernorm_forward", "xconv_layernorm_backward",
            "xconv_last_launch_count", "xconv_last_cuda_error", "xconv_status_string")
 
 
@@ -43,6 +44,11 @@ class XConvDesc(Structure):
                 ("KH", c_int32), ("KW", c_int32), ("pad_h", c_int32), ("pad_w", c_int32), ("r", c_int32),
                 ("dtype", c_int32), ("circular", c_int32), ("chan_scale", c_void_p),
                 ("D", c_int32), ("KD", c_int32), ("pad_d", c_int32), ("zero_blocks", c_void_p)]
+
+
+class NormDesc(Structure):
+    _fields_ = [("rows", c_int64), ("C", c_int32), ("dtype", c_int32), ("param_dtype", c_int32), ("eps", c_float),
+                ("x_stride", c_int64), ("y_stride", c_int64), ("dx_stride", c_int64)]
 
 
 class XConvError(RuntimeError):
@@ -115,6 +121,12 @@ def lib() -> ctypes.CDLL:
     L.xconv_selftest_wait_limit.restype = c_int
     L.xconv_measure_fma_rate.argtypes = [c_void_p, c_size_t, POINTER(ctypes.c_double), c_void_p]
     L.xconv_measure_fma_rate.restype = c_int
+    N = POINTER(NormDesc)
+    L.xconv_layernorm_workspace_bytes.argtypes = [N]; L.xconv_layernorm_workspace_bytes.restype = c_size_t
+    L.xconv_layernorm_forward.argtypes = [N, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]
+    L.xconv_layernorm_forward.restype = c_int
+    L.xconv_layernorm_backward.argtypes = [N] + [c_void_p] * 9 + [c_size_t, c_void_p]
+    L.xconv_layernorm_backward.restype = c_int
     L.xconv_workspace_status.argtypes = [c_void_p, c_void_p]; L.xconv_workspace_status.restype = c_int
     L.xconv_last_launch_count.argtypes = []; L.xconv_last_launch_count.restype = c_int
     L.xconv_last_cuda_error.argtypes = []; L.xconv_last_cuda_error.restype = c_int
@@ -608,6 +620,112 @@ def xconv_dgrad(dY: torch.Tensor, W: torch.Tensor, circular: bool = False) -> to
     ws = workspace(workspace_bytes(desc, OP_DGRAD), dY.device)
     dgrad_into(desc, dY, W, dX, ws)
     return dX
+
+
+# ------------------------------------------------------------------ around the layers
+
+def _rows(t: torch.Tensor, name: str):
+    """(shape of the rows, C, row stride) of a tensor whose last axis -- of images and volumes (4-d, 5-d): whose channel axis -- has neighbouring values, and
+    whose rows lie at one distance from each other: dense channels-last or row-major tensors, and views of some of their channels."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    shape, strides = list(t.shape), list(t.stride())
+    if t.dim() >= 4:
+        shape.append(shape.pop(1)); strides.append(strides.pop(1))
+    if not 1 <= t.dim() <= 5:
+        raise ValueError(f"{name} must have one to five dimensions")
+    C, unit = shape.pop(), strides.pop()
+    if C > 1 and unit != 1:
+        raise ValueError(f"{name}: the values of a row must be neighbours (4-d and 5-d tensors in torch.channels_last(_3d) memory format)")
+    row, span = None, None
+    for n, s in zip(reversed(shape), reversed(strides)):
+        if n == 1:
+            continue
+        if row is None:
+            row, span = s, s * n
+        elif s == span:
+            span *= n
+        else:
+            raise ValueError(f"{name}: its rows must lie at one distance from each other")
+    if row is None:
+        row = C
+    return shape, C, row
+
+
+def _norm_params(C, X, **params):
+    """The code of the parameters' type (that of X, or float32); contiguous vectors of C values."""
+    code = None
+    for name, p in params.items():
+        if p is None:
+            continue
+        if not p.is_cuda or p.device != X.device or tuple(p.shape) != (C,) or not p.is_contiguous() or p.dtype not in (torch.float32, X.dtype):
+            raise ValueError(f"{name} must be a contiguous vector of {C} values in X's dtype or float32 on X's device")
+        if code is not None and code != _dtype_code(p.dtype):
+            raise ValueError("weight and bias must have one dtype")
+        code = _dtype_code(p.dtype)
+    return XCONV_F32 if code is None else code
+
+
+def _norm_stats(shape, X, mean, rstd):
+    for name, t in (("mean", mean), ("rstd", rstd)):
+        if not t.is_cuda or t.device != X.device or t.dtype != torch.float32 or list(t.shape) != shape or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous float32 CUDA tensor of shape {tuple(shape)}: the forward call's")
+
+
+def _on_device(t: torch.Tensor):
+    """The device of `t` made the current one."""
+    return torch.cuda.device(t.device)
+
+
+def _elsewhere(t: torch.Tensor) -> bool:
+    return t.is_cuda and t.device.index != torch._C._cuda_getDevice()
+
+
+def xconv_layernorm(X: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None, eps: float = 1e-5):
+    """Layer norm over the channels: (Y, mean, rstd).  X: (B, C, H, W) or (B, C, D, H, W) channels-last, normalised pixel by pixel over C, or (..., C) with up to three
+    dimensions, normalised over the last.  Views of some of the channels of such a tensor are taken as they are.  weight, bias: C values in X's dtype or
+    float32 (1 and 0 where None).  Y is dense in X's dtype and format; mean and rstd are float32, (B, [D,] H, W) or (...)."""
+    if _elsewhere(X):
+        with _on_device(X):
+            return xconv_layernorm(X, weight, bias, eps)
+    shape, C, row = _rows(X, "X")
+    code = _norm_params(C, X, weight=weight, bias=bias)
+    mean, rstd = torch.empty(shape, dtype=torch.float32, device=X.device), torch.empty(shape, dtype=torch.float32, device=X.device)
+    Y = _dense_like(X)
+    desc = NormDesc(mean.numel(), C, _dtype_code(X.dtype), code, eps, row, C, C)
+    _check(lib().xconv_layernorm_forward(ctypes.byref(desc), X.data_ptr(), _ptr(weight), _ptr(bias), Y.data_ptr(), mean.data_ptr(), rstd.data_ptr(), _stream()),
+           "xconv_layernorm_forward")
+    return Y, mean, rstd
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _dense_like(t: torch.Tensor) -> torch.Tensor:
+    fmt = {4: torch.channels_last, 5: torch.channels_last_3d}.get(t.dim(), torch.contiguous_format)
+    return torch.empty(t.shape, dtype=t.dtype, device=t.device, memory_format=fmt)
+
+
+def xconv_layernorm_backward(dY: torch.Tensor, X: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor, weight: torch.Tensor | None = None):
+    """Gradients of xconv_layernorm: (dX, dweight, dbias), dX dense in X's dtype and format, dweight and dbias float32 (the same bits every time).  mean and rstd
+    are the forward call's, weight what it got.  dweight and dbias are what a weight and a bias would get where the layer has none."""
+    if _elsewhere(X):
+        with _on_device(X):
+            return xconv_layernorm_backward(dY, X, mean, rstd, weight)
+    shape, C, row = _rows(X, "X")
+    if dY.shape != X.shape or dY.dtype != X.dtype or dY.device != X.device:
+        raise ValueError("shape, dtype or device mismatch between dY and X")
+    _, _, dy_row = _rows(dY, "dY")
+    _norm_stats(shape, X, mean, rstd)
+    code = _norm_params(C, X, weight=weight)
+    dX = _dense_like(X)
+    dweight, dbias = torch.empty((2, C), dtype=torch.float32, device=X.device).unbind()
+    desc = NormDesc(mean.numel(), C, _dtype_code(X.dtype), code, 0.0, row, dy_row, C)
+    ws = workspace(lib().xconv_layernorm_workspace_bytes(ctypes.byref(desc)), X.device)
+    _check(lib().xconv_layernorm_backward(ctypes.byref(desc), dY.data_ptr(), X.data_ptr(), mean.data_ptr(), rstd.data_ptr(), _ptr(weight), dX.data_ptr(),
+                                          dweight.data_ptr(), dbias.data_ptr(), ws.data_ptr(), ws.numel(), _stream()), "xconv_layernorm_backward")
+    return dX, dweight, dbias
 
 
 def host_arena_bytes(desc: XConvDesc) -> int:

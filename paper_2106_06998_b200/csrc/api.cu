@@ -36,7 +36,7 @@ static xconv_status check_launch() {
 // A fresh non-zero tag per API call (see the workspace header in common.cuh).
 static std::atomic<unsigned int> g_call_tag{0x51u};
 thread_local unsigned int g_tag = 1u;
-static void new_call() {
+void new_call() {
   g_launches = 0;
   g_tag = g_call_tag.fetch_add(2u) | 1u;
 }
