@@ -342,6 +342,47 @@ size_t xconv_layernorm_workspace_bytes(const xconv_norm_desc* desc);
 xconv_status xconv_layernorm_backward(const xconv_norm_desc* desc, const void* dY, const void* X, const float* mean, const float* rstd, const void* weight, void* dX,
                                       float* dweight, float* dbias, void* ws, size_t ws_bytes, void* cuda_stream);
 
+/* Orthogonalisation of gradients by Newton-Schulz products, and the step of the weights by orthogonalised momenta (the Muon optimiser's).
+ *
+ * A tensor of gradients is `batch` matrices [rows][cols] behind one another, each dense and row-major: the weights of a convolution are one of Cout rows and
+ * KH*KW*Cin (volumes KD*KH*KW*Cin) columns in the layout above; the order of the columns does not matter, it comes back as it went in.  For every matrix U
+ *   X = U / max(|U|, eps)   (|U|: the root of the sum of its squares; transposed where rows > cols),
+ *   `steps` times   A = X X^T,  X = (a I + b A + c A A) X,
+ *   orthogonalize(U) = X    (transposed back),
+ * that is, the singular vectors of U with every singular value s / max(|U|, eps) mapped `steps` times by s -> a s + b s^3 + c s^5.
+ * The products are as exact as products of floats whatever the storage types; what is below 2^-38 in X is lost, which only matters to a matrix whose
+ * norm is far below eps.  A matrix with a value that is not finite becomes NaN; the others keep their bits.
+ *
+ * xconv_orthogonalize: O = orthogonalize(G).  G [batch][rows][cols] in g_dtype, O in o_dtype; M is ignored, and so is what follows `eps` in the descriptor.
+ * xconv_muon_step, in place: with g = G (in g_dtype) and m = M (float)
+ *   m = m + (1 - momentum) (g - m),   u = nesterov ? g + momentum (m - g) : m,
+ *   O = (1 - lr * weight_decay) O - lr * scale * orthogonalize(u),   O: the weights, in o_dtype, rounded to it once,
+ * scale = sqrt(max(1, rows / cols)) (XCONV_ADJUST_SPECTRAL) or 0.2 sqrt(max(rows, cols)) (XCONV_ADJUST_RMS).
+ *
+ * All items of a call are worked on together: a network's weights in one call take little longer than its largest ones.  Pointers are 16-byte aligned; what is
+ * written (O, and M) overlaps neither anything else that is written nor any G (XCONV_ERR_INVALID_ARG).  steps: 1 to 64; a, b, c: XCONV_ERR_UNSUPPORTED where singular
+ * values could pass 1.9 or |a + b s^2 + c s^4| 7.5 (the range in which the operands are held).  ws: xconv_update_workspace_bytes(items, count) bytes (0 where an
+ * item's sizes are invalid or a matrix would need more than 128 GB; pointers and types are not looked at), at most 2 GB and a little where no single matrix needs more. */
+typedef enum { XCONV_ADJUST_SPECTRAL = 0, XCONV_ADJUST_RMS = 1 } xconv_adjust;
+typedef struct {
+  int32_t steps;
+  float a, b, c;
+  float eps;
+  float lr, momentum, weight_decay;   /* momentum between 0 and 1 */
+  int32_t nesterov;                   /* 0 or 1 */
+  int32_t adjust;                     /* xconv_adjust */
+} xconv_update_desc;
+typedef struct {
+  const void* G;
+  float* M;
+  void* O;
+  int32_t rows, cols, batch;
+  int32_t g_dtype, o_dtype;           /* xconv_dtype */
+} xconv_matrices;
+size_t xconv_update_workspace_bytes(const xconv_matrices* items, int count);
+xconv_status xconv_orthogonalize(const xconv_update_desc* desc, const xconv_matrices* items, int count, void* ws, size_t ws_bytes, void* cuda_stream);
+xconv_status xconv_muon_step(const xconv_update_desc* desc, const xconv_matrices* items, int count, void* ws, size_t ws_bytes, void* cuda_stream);
+
 /* Reads the status the kernels of the last call left in the header of `ws` (synchronises
  * `cuda_stream`).  XCONV_OK, or XCONV_ERR_TIMEOUT if a bounded device-side wait ran out in that call.
  * The header never needs clearing: every call tags it afresh, so a later call on the same `ws`

@@ -36,6 +36,7 @@ EXPORTS = ("xconv_workspace_bytes", "xconv_engine_for", "xconv_variants_for", "x
            "xconv_gaussian_probes_from_seed", "xconv_sketch_seeded_gaussian", "xconv_wgrad_seeded_gaussian",
            "xconv_block_sparse_probes_from_seed",
            "xconv_layernorm_workspace_bytes", "xconv_layernorm_forward", "xconv_layernorm_backward",
+           "xconv_update_workspace_bytes", "xconv_orthogonalize", "xconv_muon_step",
            "xconv_last_launch_count", "xconv_last_cuda_error", "xconv_status_string")
 
 
@@ -49,6 +50,16 @@ class XConvDesc(Structure):
 class NormDesc(Structure):
     _fields_ = [("rows", c_int64), ("C", c_int32), ("dtype", c_int32), ("param_dtype", c_int32), ("eps", c_float),
                 ("x_stride", c_int64), ("y_stride", c_int64), ("dx_stride", c_int64)]
+
+
+class UpdateDesc(Structure):
+    _fields_ = [("steps", c_int32), ("a", c_float), ("b", c_float), ("c", c_float), ("eps", c_float),
+                ("lr", c_float), ("momentum", c_float), ("weight_decay", c_float), ("nesterov", c_int32), ("adjust", c_int32)]
+
+
+class Matrices(Structure):
+    _fields_ = [("G", c_void_p), ("M", c_void_p), ("O", c_void_p), ("rows", c_int32), ("cols", c_int32), ("batch", c_int32),
+                ("g_dtype", c_int32), ("o_dtype", c_int32)]
 
 
 class XConvError(RuntimeError):
@@ -127,6 +138,11 @@ def lib() -> ctypes.CDLL:
     L.xconv_layernorm_forward.restype = c_int
     L.xconv_layernorm_backward.argtypes = [N] + [c_void_p] * 9 + [c_size_t, c_void_p]
     L.xconv_layernorm_backward.restype = c_int
+    L.xconv_update_workspace_bytes.argtypes = [POINTER(Matrices), c_int]; L.xconv_update_workspace_bytes.restype = c_size_t
+    L.xconv_orthogonalize.argtypes = [POINTER(UpdateDesc), POINTER(Matrices), c_int, c_void_p, c_size_t, c_void_p]
+    L.xconv_orthogonalize.restype = c_int
+    L.xconv_muon_step.argtypes = L.xconv_orthogonalize.argtypes
+    L.xconv_muon_step.restype = c_int
     L.xconv_workspace_status.argtypes = [c_void_p, c_void_p]; L.xconv_workspace_status.restype = c_int
     L.xconv_last_launch_count.argtypes = []; L.xconv_last_launch_count.restype = c_int
     L.xconv_last_cuda_error.argtypes = []; L.xconv_last_cuda_error.restype = c_int
@@ -726,6 +742,97 @@ def xconv_layernorm_backward(dY: torch.Tensor, X: torch.Tensor, mean: torch.Tens
     _check(lib().xconv_layernorm_backward(ctypes.byref(desc), dY.data_ptr(), X.data_ptr(), mean.data_ptr(), rstd.data_ptr(), _ptr(weight), dX.data_ptr(),
                                           dweight.data_ptr(), dbias.data_ptr(), ws.data_ptr(), ws.numel(), _stream()), "xconv_layernorm_backward")
     return dX, dweight, dbias
+
+
+# The steps' polynomial a x + b x^3 + c x^5 that the Muon optimiser uses: singular values of a hundredth come near 1 in five steps.
+NEWTON_SCHULZ = (3.4445, -4.7750, 2.0315)
+_ADJUST = {"spectral": 0, "rms": 1}
+
+
+def _matrices(t: torch.Tensor, name: str):
+    """(rows, columns, batch) of a tensor of weights: a matrix, a batch of matrices (3-d), or the weights of a convolution (4-d, 5-d) with a row per output channel."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if t.dim() in (2, 3):
+        if not t.is_contiguous():
+            raise ValueError(f"{name}: matrices must be contiguous")
+        rows, cols = t.shape[-2:]
+        batch = t.shape[0] if t.dim() == 3 else 1
+    else:
+        _cl(t, name)
+        rows, batch = t.shape[0], 1
+        cols = t.numel() // rows if rows else 0
+    if t.numel() == 0:
+        raise ValueError(f"{name} is empty")
+    return rows, cols, batch
+
+
+def _same_layout(a: torch.Tensor, b: torch.Tensor, names: str):
+    if a.shape != b.shape or a.device != b.device:
+        raise ValueError(f"shape or device mismatch between {names}")
+
+
+def _update(fn, where, desc, items, device):
+    array = (Matrices * len(items))(*items)
+    ws = workspace(lib().xconv_update_workspace_bytes(array, len(items)), device)
+    _check(fn(ctypes.byref(desc), array, len(items), ws.data_ptr(), ws.numel(), _stream()), where)
+
+
+def xconv_orthogonalize(G, steps: int = 5, coefficients=NEWTON_SCHULZ, eps: float = 1e-7):
+    """The gradients in G orthogonalised by Newton-Schulz products (include/xconv.h has the formulas), in G's dtype and layout.  G: a matrix, a batch of matrices
+    (3-d), the channels-last weights of a convolution (4-d, 5-d: a row per output channel) -- or a list of such tensors, which are worked on together and
+    come back as a list."""
+    many = isinstance(G, (list, tuple))
+    tensors = list(G) if many else [G]
+    if not tensors:
+        return []
+    if _elsewhere(tensors[0]):
+        with _on_device(tensors[0]):
+            return xconv_orthogonalize(G, steps, coefficients, eps)
+    items, outs = [], []
+    for t in tensors:
+        rows, cols, batch = _matrices(t, "G")
+        if t.device != tensors[0].device:
+            raise ValueError("the tensors of a call must be on one device")
+        code = _dtype_code(t.dtype)
+        O = _dense_like(t)
+        outs.append(O)
+        items.append((t.data_ptr(), None, O.data_ptr(), rows, cols, batch, code, code))
+    a, b, c = coefficients
+    _update(lib().xconv_orthogonalize, "xconv_orthogonalize", UpdateDesc(steps, a, b, c, eps), items, tensors[0].device)
+    return outs if many else outs[0]
+
+
+def xconv_muon_step(W, dW, M, lr: float, momentum: float = 0.95, nesterov: bool = True, weight_decay: float = 0.0, steps: int = 5, coefficients=NEWTON_SCHULZ,
+                    eps: float = 1e-7, adjust: str = "spectral"):
+    """One step of the Muon optimiser, in place: the momenta M (float32) take in the gradients dW, the weights W (any of the library's dtypes) move against the
+    orthogonalised momenta (include/xconv.h has the formulas).  W, dW, M: tensors of one shape and layout as xconv_orthogonalize takes them, or lists of them: a
+    whole network's weights in one call take little longer than the largest of them.  Returns W."""
+    many = isinstance(W, (list, tuple))
+    Ws, dWs, Ms = (list(t) if isinstance(t, (list, tuple)) else [t] for t in (W, dW, M))
+    if not len(Ws) == len(dWs) == len(Ms):
+        raise ValueError("W, dW and M must have the same length")
+    if adjust not in _ADJUST:
+        raise ValueError(f"adjust must be one of {sorted(_ADJUST)}")
+    if not Ws:
+        return W
+    if _elsewhere(Ws[0]):
+        with _on_device(Ws[0]):
+            return xconv_muon_step(W, dW, M, lr, momentum, nesterov, weight_decay, steps, coefficients, eps, adjust)
+    items = []
+    for w, g, m in zip(Ws, dWs, Ms):
+        rows, cols, batch = _matrices(w, "W")
+        if w.device != Ws[0].device:
+            raise ValueError("the tensors of a call must be on one device")
+        _same_layout(w, g, "W and dW"); _same_layout(w, m, "W and M")
+        _matrices(g, "dW"); _matrices(m, "M")
+        if m.dtype != torch.float32:
+            raise ValueError("M must be float32")
+        items.append((g.data_ptr(), m.data_ptr(), w.data_ptr(), rows, cols, batch, _dtype_code(g.dtype), _dtype_code(w.dtype)))
+    a, b, c = coefficients
+    desc = UpdateDesc(steps, a, b, c, eps, lr, momentum, weight_decay, 1 if nesterov else 0, _ADJUST[adjust])
+    _update(lib().xconv_muon_step, "xconv_muon_step", desc, items, Ws[0].device)
+    return W
 
 
 def host_arena_bytes(desc: XConvDesc) -> int:

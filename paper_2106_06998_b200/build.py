@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libxconv.so")
 MARSHAL, MARSHAL_SOURCE = os.path.join(HERE, "_marshal.so"), os.path.join(HERE, "csrc", "marshal.cpp")
 SOURCES = ["api.cu", "tc_kernels.cu", "conv_tc.cu", "contract_tc.cu", "stream_tc.cu", "conv_fma.cu", "small_f32.cu", "conv_split.cu", "contract_split.cu", "gemm_split.cu",
-           "static_scratch.cu", "layer_norm.cu", "api_norm.cu"]
+           "static_scratch.cu", "layer_norm.cu", "api_norm.cu", "update/newton_schulz.cu", "api_update.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "--use_fast_math=false", "-Xcompiler", "-fPIC,-O2", "-cudart", "static"]
 
@@ -27,7 +27,7 @@ def _stale() -> bool:
     if not os.path.exists(LIB):
         return True
     t = os.path.getmtime(LIB)
-    deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if not f.endswith(".cpp")] + [os.path.join(HERE, "..", "include", "xconv.h")]
+    deps = [os.path.join(top, f) for top, _, names in os.walk(CSRC) for f in names if f.endswith((".cu", ".cuh", ".h"))] + [os.path.join(HERE, "..", "include", "xconv.h")]
     return any(os.path.getmtime(d) > t for d in deps)
 
 
