@@ -393,7 +393,7 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_product_kernel(const __grid_
         if (!mbar_wait_warp(&full[slot], lap, p.status, p.tag)) { ok = false; break; }
         if (used >= NS_SETS && !mbar_wait_warp(&acc_empty[set], set_lap ^ 1u, p.status, p.tag)) { ok = false; break; }
         tc_fence_after();
-        const uint32_t at = smem + slot * NS_STAGE;
+        const uint32_t at = (smem + slot * NS_STAGE) & 0x3FFFFu;      // (in a cluster an address has the CTA's rank above these bits)
         const uint32_t a = A_LO | (at >> 4), b = B_LO | ((at + (same ? 0u : NS_OPERAND)) >> 4), d = tmem + set * 128;
         constexpr uint32_t L = NS_PART >> 4;
 #pragma unroll
