@@ -3,22 +3,26 @@
 //   A = X X^T,   B = a I + b A + c A A,   X <- B X
 //
 // which maps every singular value s to a s + b s^3 + c s^5 and leaves the singular vectors.  Any number of matrices of any shapes goes through the same launches: the
-// unit of work is a 128 x 128 tile of some matrix's product.
+// unit of work is a 256 x 256 tile of some matrix's product.
 //
 // Arithmetic.  A step multiplies small singular values by a (3.4): an error of the operands' roundings grows by 485 in five steps where X has large singular
 // values beside small ones.  With operands rounded to bfloat16 the result is off by 1e-2 (normal values) to 0.3 (eight directions above noise), with one float16 part
 // by 1e-3 to 4e-2; with float arithmetic by 1e-7 to 5e-6.  So every operand is two float16 parts here, x 2^13 = h + l (11 + 11 bits and the sign between
 // them; |X| < 2, |A| < 4, |B| < 8: nothing overflows, and what is lost is below 2^-38), and a product is l h + h l + h h on the tensor cores, as exact as one of floats.
-// The tensor cores' accumulator is not rounded to nearest; a chain is one stage (64 terms: eight MMAs of the small products, then four of h h), and the chains
-// are added in float registers.
+// The tensor cores' accumulator is not rounded to nearest; a chain is 32 terms (four MMAs of the small products, then two of h h), and the
+// chains are added in float registers.
 //
 // Layout.  X, A and B lie in the scratch memory as blocks of 128 x 64 values, each part 16 KB in the order that the MMA wants in shared memory (rows of 128
-// bytes, 16-byte pieces exchanged by the row's last three bits): one untiled bulk copy fetches a block, whatever the matrix's sizes, and the same block serves as
+// bytes, 16-byte pieces exchanged by the row's last three bits): whatever the matrices' sizes one tensor map describes them all, and the same block serves as
 // a tile whose rows run along the result (X X^T, A A, B of B X) and as one whose rows run along the sum (X of B X).  Behind a matrix's last row and column lie zeros.
-// A and A A are symmetric: the tiles on and below the diagonal are computed and written twice, and rows of A serve as its columns.
+// A and B are symmetric: only tiles of 256 x 256 on and below the diagonal are computed and kept, and what lies above is read as the transposed of a tile below:
+// the same memory with its rows along the sum.
 //
-// A block of threads: a warp that copies, one that issues MMAs, eight that add chains and write results.  Where there are fewer tiles than SMs, a cluster of
-// 2, 4 or 8 shares the terms of a tile; each then has a part of the tile's columns, and reads the others' sums of them over the SMs' network.
+// A pair of CTAs works on a tile of 256 x 256: each brings 128 rows of either operand, 64 terms (64 KB) a stage, and the two tensor cores read both halves of the second
+// one.  The copies' latency bounds smaller tiles: 192 KB of ring, 2800 clocks from a copy to its arrival, 768 clocks of MMAs for the 64 KB of a
+// tile of 128 x 128 by one CTA (measured there: 1250 clocks a stage), 1536 here.  In a CTA a warp copies, one (of the first CTA) issues the MMAs, sixteen add
+// chains and write results.  Where there are fewer tiles than pairs, a cluster of two or four pairs shares the terms of a tile; each then has a part of the tile's
+// columns, and reads the others' sums of them over the SMs' network.
 #include "newton_schulz.h"
 
 #include <algorithm>
@@ -30,15 +34,17 @@ namespace xconv {
 namespace {
 
 constexpr int NS_SMS = 148;
-constexpr int NS_STAGES = 3, NS_SETS = 4;
-constexpr uint32_t NS_OPERAND = 32 * 1024, NS_STAGE = 2 * NS_OPERAND, NS_PART = NS_OPERAND / 2;
-constexpr int NS_ADDERS = 8, NS_THREADS = 32 * (2 + NS_ADDERS);
+constexpr int NS_STAGES = 3, NS_SETS = 2, NS_CHAIN = 2;      // NS_CHAIN: steps of 16 terms
+constexpr uint32_t NS_OPERAND = 32 * 1024, NS_STAGE = 2 * NS_OPERAND, NS_PART = NS_OPERAND / 2, NS_HALF = NS_PART / 2;
+constexpr int NS_ADDERS = 16, NS_THREADS = 32 * (2 + NS_ADDERS);
+constexpr int NS_TILE = 256;
 constexpr float NS_SCALE = 8192.f, NS_UNSCALE = 1.f / 8192.f;
 constexpr size_t NS_HEADER = 256;
 
 enum { NS_GRAM, NS_SQUARE, NS_APPLY, NS_LAST };
 
 struct NsArgs {
+  CUtensorMap whole, half;     // the blocks' rows of 2 KB: 16 (both parts of a block), 4 at a time
   NsTable t;
   char* blocks;                // the blocks of the scratch memory
   double* sums;                // partial sums of squares, NS_CHUNK values each
@@ -46,7 +52,7 @@ struct NsArgs {
   float a, b, c, momentum, keep;
   double eps;
   int muon, nesterov, which;   // which: the buffer that X is in
-  int cs;                      // CTAs a tile
+  int cs;                      // pairs of CTAs a tile
 };
 
 __device__ __forceinline__ float load_as_float(const void* p, int dtype, size_t i) {
@@ -63,7 +69,9 @@ __device__ __forceinline__ void store_from_float(void* p, int dtype, size_t i, f
 __host__ __device__ __forceinline__ int chunks_of(const NsEntry& e) { return (int)(((long)e.n * e.m + NS_CHUNK - 1) / NS_CHUNK); }
 __host__ __device__ __forceinline__ int row_blocks(const NsEntry& e) { return (e.n + NS_ROWS - 1) / NS_ROWS; }
 __host__ __device__ __forceinline__ int x_cols(const NsEntry& e) { return (e.m + NS_COLS - 1) / NS_COLS; }
-__host__ __device__ __forceinline__ int a_cols(const NsEntry& e) { return (e.n + NS_COLS - 1) / NS_COLS; }
+__host__ __device__ __forceinline__ int a_cols(const NsEntry& e) { return 2 * row_blocks(e); }
+__host__ __device__ __forceinline__ int a_terms(const NsEntry& e) { return (e.n + NS_COLS - 1) / NS_COLS; }      // blocks of A's columns that hold anything
+__host__ __device__ __forceinline__ int tiles(int blocks, int per) { return (blocks + per - 1) / per; }
 
 // The parts of eight values that are scaled already, packed.
 __device__ __forceinline__ void parts8(const float (&v)[8], uint4& hi, uint4& lo) {
@@ -188,85 +196,106 @@ __device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr, uint32_t rank) {
                : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr), "r"(rank) : "memory");
   return v;
 }
+__device__ __forceinline__ void arrive_at(uint64_t* bar, uint32_t rank) {      // ... of the same barrier in another CTA of the cluster
+  asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %0, %1;\n\tmbarrier.arrive.shared::cluster.b64 _, [a];\n\t}"
+               ::"r"(smem_u32(bar)), "r"(rank) : "memory");
+}
+// Tensor memory of a pair: a warp of either CTA allocates, behind it the go-ahead for the next kernel is given.
+__device__ __forceinline__ void pair_alloc_then_trigger(uint32_t* slot) {
+  asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(slot)) : "memory");
+  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  pdl_trigger();
+}
+__device__ __forceinline__ void pair_dealloc(uint32_t tmem) {
+  asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+}
+// Rows of the blocks into this CTA's shared memory; the bytes count at the barrier of the pair's first CTA.
+__device__ __forceinline__ void pair_load(uint32_t dst, const CUtensorMap* map, uint32_t row, uint64_t* bar) {
+  asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+               ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(row), "r"(smem_u32(bar) & 0xFEFFFFFFu) : "memory");
+}
+__device__ __forceinline__ void pair_mma(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, e;\n\t.reg .b64 da, db;\n\t"
+      "elect.sync _|e, 0xffffffff;\n\t"
+      "mov.b64 da, {%1, %3};\n\t"
+      "mov.b64 db, {%2, %3};\n\t"
+      "setp.ne.b32 p, %5, 0;\n\t"
+      "@e tcgen05.mma.cta_group::2.kind::f16 [%0], da, db, %4, p;\n\t}"
+      ::"r"(d), "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(accumulate) : "memory");
+}
+// An arrival at the barrier in the CTAs of `mask` once every MMA issued so far has finished.
+__device__ __forceinline__ void pair_commit(uint64_t* bar, uint32_t mask) {
+  asm volatile("{\n\t.reg .pred e;\n\t.reg .b16 m;\n\tcvt.u16.u32 m, %1;\n\telect.sync _|e, 0xffffffff;\n\t"
+               "@e tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], m;\n\t}" ::"r"(smem_u32(bar)), "r"(mask) : "memory");
+}
 
-// A unit of work: tile (i, j) of matrix `mat` of an entry, and the stages (64 terms each) that its sums have.
-struct NsUnit { const NsEntry* e; int mat, i, j, stages; };
+// A unit of work: tile (I, J) of matrix `mat` of an entry, and the stages (64 terms each) that its sums have.
+struct NsUnit { int k, mat, I, J, stages; };
 template <int MODE>
-__device__ __forceinline__ NsUnit ns_unit(const NsArgs& p, int u, int& k) {
+__device__ __forceinline__ NsUnit ns_unit(const NsEntry* es, int entries, int u, int& k) {
   constexpr bool SYM = MODE == NS_GRAM || MODE == NS_SQUARE;
-  while (k + 1 < p.t.entries && u >= (SYM ? p.t.e[k + 1].sym0 : p.t.e[k + 1].prod0)) ++k;
+  while (k + 1 < entries && u >= (SYM ? es[k + 1].sym0 : es[k + 1].prod0)) ++k;
+  const NsEntry& e = es[k];
   NsUnit w;
-  w.e = &p.t.e[k];
-  const int nt = row_blocks(*w.e);
+  w.k = k;
+  const int rows = tiles(row_blocks(e), 2);
   if (SYM) {
-    const int per = nt * (nt + 1) / 2, local = u - w.e->sym0;
+    const int per = rows * (rows + 1) / 2, local = u - e.sym0;
     w.mat = local / per;
     const int t = local - w.mat * per;
     int i = (int)((sqrtf(8.f * (float)t + 1.f) - 1.f) * 0.5f);
     while (i * (i + 1) / 2 > t) --i;
     while ((i + 1) * (i + 2) / 2 <= t) ++i;
-    w.i = i;
-    w.j = t - i * (i + 1) / 2;
-    w.stages = MODE == NS_GRAM ? x_cols(*w.e) : a_cols(*w.e);
+    w.I = i;
+    w.J = t - i * (i + 1) / 2;
+    w.stages = MODE == NS_GRAM ? x_cols(e) : a_terms(e);
   } else {
-    const int per_row = (x_cols(*w.e) + 1) / 2, per = nt * per_row, local = u - w.e->prod0;
+    const int per = rows * tiles(x_cols(e), 4), local = u - e.prod0;
     w.mat = local / per;
     const int t = local - w.mat * per;
-    w.j = t / nt;                                    // (neighbouring units read the same columns of X)
-    w.i = t - w.j * nt;
-    w.stages = a_cols(*w.e);
+    w.J = t / rows;                                  // (neighbouring units read the same columns of X)
+    w.I = t - w.J * rows;
+    w.stages = a_terms(e);
   }
   return w;
 }
 
-// Eight neighbouring sums of a row of a tile, columns 8 * q8 on.
+// Eight neighbouring sums of a row of this CTA's half of a tile, columns 8 * q8 on.
 template <int MODE>
-__device__ __forceinline__ void ns_emit(const NsArgs& p, const NsUnit& w, int row, int q8, float (&v)[8]) {
-  const NsEntry& e = *w.e;
-  const int nt = row_blocks(e), ka = a_cols(e);
+__device__ __forceinline__ void ns_emit(const NsArgs& p, const NsEntry& e, const NsUnit& w, int half, int row, int q8, float (&v)[8]) {
+  const int nt = row_blocks(e), i = 2 * w.I + half, cb = 4 * w.J + (q8 >> 3);
+  if (i >= nt) return;
   if (MODE == NS_GRAM || MODE == NS_SQUARE) {
-    char* to = p.blocks + ((size_t)(MODE == NS_GRAM ? e.a : e.b) + (size_t)w.mat * nt * ka) * NS_BLOCK;
-    const int cb = 2 * w.j + (q8 >> 3), r0 = w.i * NS_ROWS + row;
-    if (cb < ka) {
-      const size_t at = ((size_t)w.i * ka + cb) * NS_BLOCK + piece_at(row, q8 & 7);
-      if (MODE == NS_GRAM) {
+    if (cb >= 2 * nt) return;
+    const size_t at = (((size_t)w.mat * nt + i) * 2 * nt + cb) * NS_BLOCK + piece_at(row, q8 & 7);
+    char* to = p.blocks + (size_t)(MODE == NS_GRAM ? e.a : e.b) * NS_BLOCK + at;
+    if (MODE == NS_GRAM) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] *= NS_UNSCALE;
-      } else {
-        const char* from = p.blocks + ((size_t)e.a + (size_t)w.mat * nt * ka) * NS_BLOCK + at;
-        const uint4 hi = __ldcg(reinterpret_cast<const uint4*>(from)), lo = __ldcg(reinterpret_cast<const uint4*>(from + NS_PART));
-        const uint32_t h[4] = {hi.x, hi.y, hi.z, hi.w}, l[4] = {lo.x, lo.y, lo.z, lo.w};
+      for (int k = 0; k < 8; ++k) v[k] *= NS_UNSCALE;
+    } else {
+      const char* from = p.blocks + (size_t)e.a * NS_BLOCK + at;
+      const uint4 hi = __ldcg(reinterpret_cast<const uint4*>(from)), lo = __ldcg(reinterpret_cast<const uint4*>(from + NS_PART));
+      const uint32_t h[4] = {hi.x, hi.y, hi.z, hi.w}, l[4] = {lo.x, lo.y, lo.z, lo.w};
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&h[k])), b = __half22float2(*reinterpret_cast<const __half2*>(&l[k]));
-          v[2 * k] = fmaf(p.c * NS_UNSCALE, v[2 * k], p.b * (a.x + b.x));
-          v[2 * k + 1] = fmaf(p.c * NS_UNSCALE, v[2 * k + 1], p.b * (a.y + b.y));
-        }
-        const int d = r0 - (w.j * NS_ROWS + q8 * 8);
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-          if (k == d && r0 < e.n) v[k] += p.a * NS_SCALE;
+      for (int k = 0; k < 4; ++k) {
+        const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&h[k])), b = __half22float2(*reinterpret_cast<const __half2*>(&l[k]));
+        v[2 * k] = fmaf(p.c * NS_UNSCALE, v[2 * k], p.b * (a.x + b.x));
+        v[2 * k + 1] = fmaf(p.c * NS_UNSCALE, v[2 * k + 1], p.b * (a.y + b.y));
       }
-      uint4 hi, lo;
-      parts8(v, hi, lo);
-      *reinterpret_cast<uint4*>(to + at) = hi;
-      *reinterpret_cast<uint4*>(to + at + NS_PART) = lo;
-      const int mb = 2 * w.i + (row >> 6);
-      if (w.i != w.j && mb < ka) {                   // the tile's mirror image: column `row` of it
-        char* m = to + ((size_t)w.j * ka + mb) * NS_BLOCK;
-        const uint32_t h[4] = {hi.x, hi.y, hi.z, hi.w}, l[4] = {lo.x, lo.y, lo.z, lo.w};
+      const int r = i * NS_ROWS + row, d = r - (w.J * NS_TILE + q8 * 8);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const uint32_t b = piece_at(q8 * 8 + k, (row & 63) >> 3) + (row & 7) * 2;
-          *reinterpret_cast<unsigned short*>(m + b) = (unsigned short)(h[k >> 1] >> (16 * (k & 1)));
-          *reinterpret_cast<unsigned short*>(m + b + NS_PART) = (unsigned short)(l[k >> 1] >> (16 * (k & 1)));
-        }
-      }
+      for (int k = 0; k < 8; ++k)
+        if (k == d && r < e.n) v[k] += p.a * NS_SCALE;
     }
+    uint4 hi, lo;
+    parts8(v, hi, lo);
+    *reinterpret_cast<uint4*>(to) = hi;
+    *reinterpret_cast<uint4*>(to + NS_PART) = lo;
   } else if (MODE == NS_APPLY) {
-    const int kt = x_cols(e), cb = 2 * w.j + (q8 >> 3);
+    const int kt = x_cols(e);
     if (cb >= kt) return;
-    char* to = p.blocks + ((size_t)(p.which ? e.x0 : e.x1) + ((size_t)w.mat * nt + w.i) * kt + cb) * NS_BLOCK + piece_at(row, q8 & 7);
+    char* to = p.blocks + ((size_t)(p.which ? e.x0 : e.x1) + ((size_t)w.mat * nt + i) * kt + cb) * NS_BLOCK + piece_at(row, q8 & 7);
 #pragma unroll
     for (int k = 0; k < 8; ++k) v[k] *= NS_UNSCALE;
     uint4 hi, lo;
@@ -274,7 +303,7 @@ __device__ __forceinline__ void ns_emit(const NsArgs& p, const NsUnit& w, int ro
     *reinterpret_cast<uint4*>(to) = hi;
     *reinterpret_cast<uint4*>(to + NS_PART) = lo;
   } else {
-    const long r = (long)w.i * NS_ROWS + row, c0 = (long)w.j * NS_ROWS + q8 * 8;
+    const long r = (long)i * NS_ROWS + row, c0 = (long)w.J * NS_TILE + q8 * 8;
     if (r >= e.n) return;
     const bool tall = e.rows > e.cols;
     const size_t base = (size_t)w.mat * e.n * e.m;
@@ -295,16 +324,24 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_product_kernel(const __grid_
   constexpr bool SYM = MODE == NS_GRAM || MODE == NS_SQUARE;
   extern __shared__ uint8_t raw[];
   __shared__ uint64_t full[NS_STAGES], empty[NS_STAGES], acc_full[NS_SETS], acc_empty[NS_SETS];
+  __shared__ NsEntry es[NS_MOST];
   __shared__ uint32_t tmem_slot;
   __shared__ int go;
   const uint32_t smem = (smem_u32(raw) + 1023u) & ~1023u;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, entries = p.t.entries;
+  const uint32_t rank = cluster_rank(), half = rank & 1u, leader = rank & ~1u;
   if (threadIdx.x == 0) {
     for (int i = 0; i < NS_STAGES; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); }
-    for (int i = 0; i < NS_SETS; ++i) { mbar_init(&acc_full[i], 1); mbar_init(&acc_empty[i], NS_ADDERS); }
+    for (int i = 0; i < NS_SETS; ++i) { mbar_init(&acc_full[i], 1); mbar_init(&acc_empty[i], 2 * NS_ADDERS); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    prefetch_tmap(&p.whole);
+    prefetch_tmap(&p.half);
   }
-  if (warp == 1) tmem_alloc_then_trigger(&tmem_slot, 512);
+  for (int i = threadIdx.x; i < entries * (int)(sizeof(NsEntry) / 4); i += NS_THREADS)
+    reinterpret_cast<uint32_t*>(es)[i] = reinterpret_cast<const uint32_t*>(p.t.e)[i];
+  if (warp == 1) pair_alloc_then_trigger(&tmem_slot);
+  __syncwarp();
+  cluster_sync();                                    // (the other CTAs' barriers are there)
   pdl_wait();
   if (threadIdx.x == 0) {
     go = (*reinterpret_cast<volatile unsigned*>(p.status) != p.tag) ? 1 : 0;
@@ -314,8 +351,8 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_product_kernel(const __grid_
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&tmem_slot);
-  const int rank = p.cs > 1 ? (int)cluster_rank() : 0;
-  const int units = SYM ? p.t.syms : p.t.prods, u0 = (int)blockIdx.x / p.cs, step = (int)gridDim.x / p.cs;
+  const int part = (int)(rank >> 1);                 // of the tile's terms
+  const int units = SYM ? p.t.syms : p.t.prods, per = 2 * p.cs, u0 = (int)blockIdx.x / per, step = (int)gridDim.x / per;
 
   if (go && warp == 0) {
     if (lane == 0) {
@@ -324,48 +361,52 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_product_kernel(const __grid_
       int k = 0;
       bool ok = true;
       for (int u = u0; u < units && ok; u += step) {
-        const NsUnit w = ns_unit<MODE>(p, u, k);
-        const NsEntry& e = *w.e;
-        const int nt = row_blocks(e), ka = a_cols(e), kt = x_cols(e);
-        const uint32_t xb = p.which ? e.x1 : e.x0;
-        const char *A, *B;
-        uint32_t b_bytes = NS_OPERAND;
-        const bool same = SYM && w.i == w.j;
-        int halves = 2;
-        if (SYM) {
-          const int kk = MODE == NS_GRAM ? kt : ka;
-          const char* top = p.blocks + ((size_t)(MODE == NS_GRAM ? xb : e.a) + (size_t)w.mat * nt * kk) * NS_BLOCK;
-          A = top + (size_t)w.i * kk * NS_BLOCK;
-          B = top + (size_t)w.j * kk * NS_BLOCK;
-          if (same) b_bytes = 0;
-        } else {
-          A = p.blocks + ((size_t)e.b + ((size_t)w.mat * nt + w.i) * ka) * NS_BLOCK;
-          B = p.blocks + ((size_t)xb + (size_t)w.mat * nt * kt + 2 * w.j) * NS_BLOCK;
-          halves = min(2, kt - 2 * w.j);
-          b_bytes = (uint32_t)halves * (NS_OPERAND / 2);
-        }
-        const int s0 = w.stages * rank / p.cs, s1 = w.stages * (rank + 1) / p.cs;
+        const NsUnit w = ns_unit<MODE>(es, entries, u, k);
+        const NsEntry& e = es[w.k];
+        const int nt = row_blocks(e), kt = x_cols(e), i = 2 * w.I + (int)half, j = 2 * w.J + (int)half;
+        const uint32_t xb = (p.which ? e.x1 : e.x0) + (uint32_t)w.mat * nt * kt, sb = (MODE == NS_SQUARE ? e.a : e.b) + (uint32_t)w.mat * nt * 2 * nt;
+        const bool same = SYM && w.I == w.J;
+        // What both CTAs of the pair copy a stage: rows of the first operand, rows (columns) of the second.
+        uint32_t bytes = (uint32_t)min(2, nt - 2 * w.I) * NS_OPERAND;
+        if (SYM) bytes += same ? 0u : (uint32_t)min(2, nt - 2 * w.J) * NS_OPERAND;
+        else bytes += (uint32_t)min(4, kt - 4 * w.J) * NS_PART;
+        const int s0 = w.stages * part / p.cs, s1 = w.stages * (part + 1) / p.cs;
         for (int s = s0; s < s1; ++s) {
           if (issued >= NS_STAGES && !mbar_wait(&empty[slot], lap ^ 1u, p.status, p.tag)) { ok = false; break; }
           const uint32_t to = smem + slot * NS_STAGE;
-          mbar_arrive_expect_tx(&full[slot], NS_OPERAND + b_bytes);
-          bulk_load(to, A + (size_t)s * NS_BLOCK, NS_OPERAND, &full[slot]);
-          if (SYM) {
-            if (!same) bulk_load(to + NS_OPERAND, B + (size_t)s * NS_BLOCK, NS_OPERAND, &full[slot]);
+          uint64_t* bar = &full[slot];
+          if (half == 0) mbar_arrive_expect_tx(bar, bytes);
+          // 64 rows of two neighbouring blocks, both parts of each: a tile with its rows along the sum
+          const auto load_across = [&](uint32_t dst, uint32_t block, int count) {
+            const uint32_t row = block * 16u + (uint32_t)(s & 1) * 4u;
+            for (int h = 0; h < count; ++h) {
+              pair_load(dst + h * NS_HALF, &p.half, row + h * 16u, bar);
+              pair_load(dst + NS_PART + h * NS_HALF, &p.half, row + h * 16u + 8u, bar);
+            }
+          };
+          // block (i, s) of a symmetric matrix
+          const auto load_symmetric = [&](uint32_t dst, int row_block) {
+            if (s / 4 <= row_block / 2) pair_load(dst, &p.whole, (sb + (uint32_t)row_block * 2 * nt + s) * 16u, bar);
+            else load_across(dst, sb + (uint32_t)(s >> 1) * 2 * nt + 2 * row_block, 2);
+          };
+          if (MODE == NS_GRAM) {
+            if (i < nt) pair_load(to, &p.whole, (xb + (uint32_t)i * kt + s) * 16u, bar);
+            if (!same && j < nt) pair_load(to + NS_OPERAND, &p.whole, (xb + (uint32_t)j * kt + s) * 16u, bar);
           } else {
-            // 64 rows of X: the upper or the lower half of a block's rows, in both column blocks
-            const char* from = B + (size_t)(s >> 1) * kt * NS_BLOCK + (s & 1) * (NS_PART / 2);
-            for (int h = 0; h < halves; ++h) {
-              bulk_load(to + NS_OPERAND + h * (NS_PART / 2), from + h * NS_BLOCK, NS_PART / 2, &full[slot]);
-              bulk_load(to + NS_OPERAND + NS_PART + h * (NS_PART / 2), from + h * NS_BLOCK + NS_PART, NS_PART / 2, &full[slot]);
+            if (i < nt) load_symmetric(to, i);
+            if (MODE == NS_SQUARE) {
+              if (!same && j < nt) load_symmetric(to + NS_OPERAND, j);
+            } else {
+              const int c = 4 * w.J + 2 * (int)half;
+              load_across(to + NS_OPERAND, xb + (uint32_t)(s >> 1) * kt + c, min(2, kt - c));
             }
           }
           ++issued;
           if (++slot == NS_STAGES) { slot = 0; lap ^= 1u; }
         }
       }
-      // Behind an error: no copy is under way when the block ends.
-      if (!ok)
+      // Behind an error: no copy is under way when the block ends (the first CTA's barriers count both CTAs' copies; the second one ends behind it).
+      if (!ok && half == 0)
         for (uint32_t i = 0; i < NS_STAGES && i < issued; ++i) {
           if (slot == 0) { slot = NS_STAGES; lap ^= 1u; }
           --slot;
@@ -374,77 +415,85 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_product_kernel(const __grid_
     }
     __syncwarp();
   } else if (go && warp == 1) {
-    uint32_t slot = 0, lap = 0, set = 0, set_lap = 0, used = 0;
-    int k = 0;
-    bool ok = true;
-    // Shared-memory descriptors: rows along the result (groups of eight 1024 bytes apart, 32 bytes a step of 16 terms), or along the sum (2048
-    // bytes a step, column blocks 8 KB apart).
-    constexpr uint32_t HI = (1024u >> 4) | (1u << 14) | (2u << 29);
-    constexpr uint32_t A_LO = (16u >> 4) << 16, B_LO = ((SYM ? 16u : NS_PART / 2) >> 4) << 16;
-    constexpr uint32_t A_STEP = 32u >> 4, B_STEP = (SYM ? 32u : 2048u) >> 4;
-    constexpr uint32_t IDESC = (1u << 4) | (SYM ? 0u : (1u << 16)) | ((uint32_t)(TILE_M >> 4) << 24);
-    for (int u = u0; u < units && ok; u += step) {
-      const NsUnit w = ns_unit<MODE>(p, u, k);
-      const bool same = SYM && w.i == w.j;
-      const int halves = SYM ? 2 : min(2, x_cols(*w.e) - 2 * w.j);
-      const uint32_t idesc = IDESC | ((uint32_t)(halves * 64 >> 3) << 17);
-      const int s0 = w.stages * rank / p.cs, s1 = w.stages * (rank + 1) / p.cs;
-      for (int s = s0; s < s1; ++s) {
-        if (!mbar_wait_warp(&full[slot], lap, p.status, p.tag)) { ok = false; break; }
-        if (used >= NS_SETS && !mbar_wait_warp(&acc_empty[set], set_lap ^ 1u, p.status, p.tag)) { ok = false; break; }
-        tc_fence_after();
-        const uint32_t at = (smem + slot * NS_STAGE) & 0x3FFFFu;      // (in a cluster an address has the CTA's rank above these bits)
-        const uint32_t a = A_LO | (at >> 4), b = B_LO | ((at + (same ? 0u : NS_OPERAND)) >> 4), d = tmem + set * 128;
-        constexpr uint32_t L = NS_PART >> 4;
+    if (half == 0) {
+      uint32_t slot = 0, lap = 0, set = 0, set_lap = 0, used = 0;
+      int k = 0;
+      bool ok = true;
+      // Shared-memory descriptors: rows along the result (groups of eight 1024 bytes apart, 32 bytes a step of 16 terms), or along the sum (2048
+      // bytes a step, column blocks 8 KB apart).
+      constexpr uint32_t HI = (1024u >> 4) | (1u << 14) | (2u << 29);
+      constexpr uint32_t ACROSS = (NS_HALF >> 4) << 16, ALONG_STEP = 32u >> 4, ACROSS_STEP = 2048u >> 4;
+      constexpr uint32_t IDESC = (1u << 4) | ((uint32_t)(NS_TILE >> 3) << 17) | ((uint32_t)(NS_TILE >> 4) << 24);
+      const uint32_t pair_mask = 3u << leader;
+      for (int u = u0; u < units && ok; u += step) {
+        const NsUnit w = ns_unit<MODE>(es, entries, u, k);
+        const bool same = SYM && w.I == w.J;
+        const int s0 = w.stages * part / p.cs, s1 = w.stages * (part + 1) / p.cs;
+        for (int s = s0; s < s1 && ok; ++s) {
+          if (!mbar_wait_warp(&full[slot], lap, p.status, p.tag)) { ok = false; break; }
+          tc_fence_after();
+          const bool a_across = MODE != NS_GRAM && s / 4 > w.I, b_across = MODE == NS_SQUARE ? s / 4 > w.J : !SYM;
+          const uint32_t at = (smem + slot * NS_STAGE) & 0x3FFFFu;      // (in a cluster an address has the CTA's rank above these bits)
+          const uint32_t a = (a_across ? ACROSS : 1u << 16) | (at >> 4), b = (b_across ? ACROSS : 1u << 16) | ((at + (same ? 0u : NS_OPERAND)) >> 4);
+          const uint32_t a_step = a_across ? ACROSS_STEP : ALONG_STEP, b_step = b_across ? ACROSS_STEP : ALONG_STEP;
+          const uint32_t idesc = IDESC | (a_across ? 1u << 15 : 0u) | (b_across ? 1u << 16 : 0u);
+          constexpr uint32_t L = NS_PART >> 4;
 #pragma unroll
-        for (int t = 0; t < 4; ++t) umma_warp(d, a + L + t * A_STEP, HI, b + t * B_STEP, HI, idesc, t > 0);
+          for (int c = 0; c < 4; c += NS_CHAIN) {
+            if (used >= NS_SETS && !mbar_wait_warp(&acc_empty[set], set_lap ^ 1u, p.status, p.tag)) { ok = false; break; }
+            tc_fence_after();
+            const uint32_t d = tmem + set * NS_TILE;
 #pragma unroll
-        for (int t = 0; t < 4; ++t) umma_warp(d, a + t * A_STEP, HI, b + L + t * B_STEP, HI, idesc, 1u);
+            for (int t = c; t < c + NS_CHAIN; ++t) pair_mma(d, a + L + t * a_step, b + t * b_step, HI, idesc, t > c);
 #pragma unroll
-        for (int t = 0; t < 4; ++t) umma_warp(d, a + t * A_STEP, HI, b + t * B_STEP, HI, idesc, 1u);
-        umma_commit_warp(&empty[slot]);
-        umma_commit_warp(&acc_full[set]);
-        ++used;
-        if (++slot == NS_STAGES) { slot = 0; lap ^= 1u; }
-        if (++set == NS_SETS) { set = 0; set_lap ^= 1u; }
+            for (int t = c; t < c + NS_CHAIN; ++t) pair_mma(d, a + t * a_step, b + L + t * b_step, HI, idesc, 1u);
+#pragma unroll
+            for (int t = c; t < c + NS_CHAIN; ++t) pair_mma(d, a + t * a_step, b + t * b_step, HI, idesc, 1u);
+            if (c + NS_CHAIN == 4) pair_commit(&empty[slot], pair_mask);
+            pair_commit(&acc_full[set], pair_mask);
+            ++used;
+            if (++set == NS_SETS) { set = 0; set_lap ^= 1u; }
+          }
+          if (++slot == NS_STAGES) { slot = 0; lap ^= 1u; }
+        }
       }
+      // Behind an error: no MMA is under way when its tensor memory is given back.
+      if (!ok)
+        for (uint32_t i = 0; i < NS_SETS && i < used; ++i) {
+          if (set == 0) { set = NS_SETS; set_lap ^= 1u; }
+          --set;
+          mbar_wait_warp(&acc_full[set], set_lap, p.status, p.tag);
+        }
     }
-    // Behind an error: no MMA is under way when its tensor memory is given back.
-    if (!ok)
-      for (uint32_t i = 0; i < NS_SETS && i < used; ++i) {
-        if (set == 0) { set = NS_SETS; set_lap ^= 1u; }
-        --set;
-        mbar_wait_warp(&acc_full[set], set_lap, p.status, p.tag);
-      }
   } else if (go) {
-    const int quadrant = warp & 3, half = (warp - 2) >> 2, row = quadrant * 32 + lane;
+    const int quadrant = warp & 3, quarter = (warp - 2) >> 2, row = quadrant * 32 + lane;
     uint32_t set = 0, set_lap = 0;
     int k = 0;
     bool ok = true;
     for (int u = u0; u < units && ok; u += step) {
-      const NsUnit w = ns_unit<MODE>(p, u, k);
+      const NsUnit w = ns_unit<MODE>(es, entries, u, k);
       float sum[64];
 #pragma unroll
       for (int i = 0; i < 64; ++i) sum[i] = 0.f;
-      const int s0 = w.stages * rank / p.cs, s1 = w.stages * (rank + 1) / p.cs;
-      for (int s = s0; s < s1; ++s) {
+      const int s0 = w.stages * part / p.cs, s1 = w.stages * (part + 1) / p.cs;
+      for (int s = s0 * (4 / NS_CHAIN); s < s1 * (4 / NS_CHAIN); ++s) {
         if (!mbar_wait_warp(&acc_full[set], set_lap, p.status, p.tag)) { ok = false; break; }
         tc_fence_after();
-        const uint32_t from = tmem + set * 128 + half * 64 + ((uint32_t)(quadrant * 32) << 16);
-        if (SYM || half == 0 || 2 * w.j + 1 < x_cols(*w.e)) {
+        const uint32_t from = tmem + set * NS_TILE + quarter * 64 + ((uint32_t)(quadrant * 32) << 16);
 #pragma unroll
-          for (int q = 0; q < 2; ++q) {
-            uint32_t x[16], y[16];
-            tmem_ld16_issue(from + q * 32, x);
-            tmem_ld16_issue(from + q * 32 + 16, y);
-            tmem_ld_wait(x); tmem_ld_wait(y);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) { sum[q * 32 + i] += __uint_as_float(x[i]); sum[q * 32 + 16 + i] += __uint_as_float(y[i]); }
+        for (int q = 0; q < 2; ++q) {
+          uint32_t x[16], y[16];
+          tmem_ld16_issue(from + q * 32, x);
+          tmem_ld16_issue(from + q * 32 + 16, y);
+          tmem_ld_wait(x); tmem_ld_wait(y);
+          if (q == 1) {                              // all of the set's columns are read
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) arrive_at(&acc_empty[set], leader);
           }
+#pragma unroll
+          for (int i = 0; i < 16; ++i) { sum[q * 32 + i] += __uint_as_float(x[i]); sum[q * 32 + 16 + i] += __uint_as_float(y[i]); }
         }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&acc_empty[set]);
         if (++set == NS_SETS) { set = 0; set_lap ^= 1u; }
       }
       if (!ok) break;
@@ -454,43 +503,42 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_product_kernel(const __grid_
           float v[8];
 #pragma unroll
           for (int i = 0; i < 8; ++i) v[i] = sum[q * 8 + i];
-          ns_emit<MODE>(p, w, row, half * 8 + q, v);
+          ns_emit<MODE>(p, es[w.k], w, (int)half, row, quarter * 8 + q, v);
         }
       } else {
-        // (one unit a cluster: every stage of this CTA has been multiplied, and the ring's memory is free)
+        // (one unit a cluster: every stage of this pair has been multiplied, and the ring's memory is free)
 #pragma unroll
         for (int q = 0; q < 16; ++q)
-          asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(smem + (uint32_t)(((half * 16 + q) * 128 + row) * 16)), "f"(sum[4 * q]), "f"(sum[4 * q + 1]),
+          asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(smem + (uint32_t)(((quarter * 16 + q) * 128 + row) * 16)), "f"(sum[4 * q]), "f"(sum[4 * q + 1]),
                        "f"(sum[4 * q + 2]), "f"(sum[4 * q + 3]) : "memory");
       }
     }
   }
+  __syncwarp();
+  tc_fence_before();
+  cluster_sync();                                    // (no arrival and no copy of the pair comes behind this)
   if (p.cs > 1) {
-    __syncwarp();
-    cluster_sync();
     if (go && warp >= 2 && u0 < units) {
       int k = 0;
-      const NsUnit w = ns_unit<MODE>(p, u0, k);
-      const int t = threadIdx.x - 64, row = t & 127, per = 16 / p.cs;      // this CTA's groups of eight columns
-      for (int g = t >> 7; g < per; g += 2) {
-        const int q8 = rank * per + g;
+      const NsUnit w = ns_unit<MODE>(es, entries, u0, k);
+      const int t = threadIdx.x - 64, row = t & 127, groups = 32 / p.cs;      // this CTA's groups of eight columns
+      for (int g = t >> 7; g < groups; g += 4) {
+        const int q8 = part * groups + g;
         float v[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = 0.f;
         for (int c = 0; c < p.cs; ++c) {
-          const float4 x = ld_cluster_f4(smem + (uint32_t)((2 * q8 * 128 + row) * 16), (uint32_t)c);
-          const float4 y = ld_cluster_f4(smem + (uint32_t)(((2 * q8 + 1) * 128 + row) * 16), (uint32_t)c);
+          const uint32_t from = smem + (uint32_t)((2 * q8 * 128 + row) * 16), other = 2u * c + half;
+          const float4 x = ld_cluster_f4(from, other), y = ld_cluster_f4(from + 128 * 16, other);
           v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w; v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
         }
-        ns_emit<MODE>(p, w, row, q8, v);
+        ns_emit<MODE>(p, es[w.k], w, (int)half, row, q8, v);
       }
     }
     __syncwarp();
     cluster_sync();                                  // (no CTA ends while its sums are read)
   }
-  tc_fence_before();
-  __syncthreads();
-  if (warp == 1) tmem_dealloc(tmem, 512);
+  if (warp == 1) pair_dealloc(tmem);
 }
 
 template <int MODE>
@@ -498,15 +546,15 @@ cudaError_t launch_product(NsArgs& p, cudaStream_t st) {
   constexpr bool SYM = MODE == NS_GRAM || MODE == NS_SQUARE;
   constexpr size_t smem = NS_STAGES * NS_STAGE + 1024;
   const int units = SYM ? p.t.syms : p.t.prods;
-  // A cluster's CTAs have a stage each at least where the longest sum has that many.
+  // A pair has a stage at least where the longest sum has that many.
   int stages = 1;
-  for (int k = 0; k < p.t.entries; ++k) stages = std::max(stages, MODE == NS_GRAM ? x_cols(p.t.e[k]) : a_cols(p.t.e[k]));
+  for (int k = 0; k < p.t.entries; ++k) stages = std::max(stages, MODE == NS_GRAM ? x_cols(p.t.e[k]) : a_terms(p.t.e[k]));
   p.cs = 1;
-  while (p.cs < 8 && units * p.cs * 2 <= NS_SMS && p.cs * 2 <= stages) p.cs *= 2;
+  while (p.cs < 4 && units * p.cs * 4 <= NS_SMS && p.cs * 2 <= stages) p.cs *= 2;
   cudaError_t e = cudaFuncSetAttribute(ns_product_kernel<MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(p.cs > 1 ? units * p.cs : std::min(units, NS_SMS)));
+  cfg.gridDim = dim3((unsigned)(p.cs > 1 ? units * p.cs * 2 : std::min(2 * units, NS_SMS)));
   cfg.blockDim = dim3(NS_THREADS);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
@@ -514,11 +562,22 @@ cudaError_t launch_product(NsArgs& p, cudaStream_t st) {
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = (unsigned)p.cs;
+  attr[1].val.clusterDim.x = (unsigned)(2 * p.cs);
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = p.cs > 1 ? 2 : 1;
+  cfg.numAttrs = 2;
   return cudaLaunchKernelEx(&cfg, ns_product_kernel<MODE>, p);
+}
+
+// The scratch memory's blocks as rows of 256 values of 8 bytes, 16 of them a block; `rows` of them a copy.  (The copy engine fetches a box row by row: with
+// rows of 128 bytes it was what bounded the products.)
+bool map_blocks(CUtensorMap* m, const void* blocks, size_t count, uint32_t rows) {
+  PFN_cuTensorMapEncodeTiled_v12000 fn = encode_fn();
+  if (!fn) return false;
+  cuuint64_t dims[2] = {256, count * 16}, strides[1] = {2048};
+  cuuint32_t box[2] = {256, rows}, steps[2] = {1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_INT64, 2, const_cast<void*>(blocks), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 size_t sums_bytes(const NsTable& t) { return ((size_t)t.chunks * sizeof(double) + 1023) / 1024 * 1024; }
@@ -528,21 +587,22 @@ size_t sums_bytes(const NsTable& t) { return ((size_t)t.chunks * sizeof(double) 
 size_t ns_blocks_of(long rows, long cols) {
   const long n = std::min(rows, cols), m = std::max(rows, cols);
   const size_t nt = (size_t)((n + NS_ROWS - 1) / NS_ROWS);
-  return 2 * nt * (size_t)((m + NS_COLS - 1) / NS_COLS) + 2 * nt * (size_t)((n + NS_COLS - 1) / NS_COLS);
+  return 2 * nt * (size_t)((m + NS_COLS - 1) / NS_COLS) + 2 * nt * 2 * nt;
 }
 
 void ns_add(NsTable* t, NsEntry e) {
   e.n = std::min(e.rows, e.cols);
   e.m = std::max(e.rows, e.cols);
   const int nt = row_blocks(e);
+  const int tall = tiles(nt, 2);
   const uint32_t x = (uint32_t)e.count * nt * x_cols(e), a = (uint32_t)e.count * nt * a_cols(e);
   e.x0 = t->ws_blocks; e.x1 = e.x0 + x; e.a = e.x1 + x; e.b = e.a + a;
   t->ws_blocks = e.b + a;
   e.chunk0 = t->chunks; e.block0 = t->blocks; e.sym0 = t->syms; e.prod0 = t->prods;
   t->chunks += e.count * chunks_of(e);
   t->blocks += (int)x;
-  t->syms += e.count * (nt * (nt + 1) / 2);
-  t->prods += e.count * nt * ((x_cols(e) + 1) / 2);
+  t->syms += e.count * (tall * (tall + 1) / 2);
+  t->prods += e.count * tall * tiles(x_cols(e), 4);
   t->e[t->entries++] = e;
 }
 
@@ -556,6 +616,7 @@ cudaError_t launch_newton_schulz(const NsTable& t, const NsOptions& o, void* ws,
   p.sums = reinterpret_cast<double*>(static_cast<char*>(ws) + NS_HEADER);
   p.blocks = static_cast<char*>(ws) + NS_HEADER + sums_bytes(t);
   p.a = o.a; p.b = o.b; p.c = o.c; p.eps = o.eps; p.momentum = o.momentum; p.keep = o.keep; p.muon = o.muon; p.nesterov = o.nesterov;
+  if (!map_blocks(&p.whole, p.blocks, t.ws_blocks, 16) || !map_blocks(&p.half, p.blocks, t.ws_blocks, 4)) return cudaErrorInvalidValue;
   cudaError_t e = launch_pdl(ns_squares_kernel, dim3((unsigned)t.chunks), dim3(256), 0, st, p);
   if (e != cudaSuccess) return e;
   ++*launches;

@@ -99,9 +99,11 @@ def test_the_binding_refuses_what_it_cannot_read(lib):
 def test_kernels_that_take_tensor_memory_do_so_before_they_let_the_next_one_start():
     """The rule of the layers' kernels (test_split_sources.py) for those of this folder: one allocation, by one warp, the go-ahead behind it and nowhere else."""
     code = "".join(re.sub(r"//[^\n]*", "", open(os.path.join(UPDATE, f)).read()) for f in sorted(os.listdir(UPDATE)) if f.endswith((".cu", ".cuh")))
-    assert "tmem_alloc(" not in code and "tcgen05.alloc" not in code
-    kernels = [c for c in code.split("\n}\n") if "tmem_alloc_then_trigger(" in c]
-    assert kernels and code.count("tmem_alloc_then_trigger(") == len(kernels)
+    assert "tmem_alloc" not in code and code.count("tcgen05.alloc") == 1
+    alloc = code.split("void pair_alloc_then_trigger(")[1].split("\n}\n")[0]
+    assert alloc.index("tcgen05.alloc") < alloc.index("pdl_trigger()") and alloc.count("pdl_trigger()") == 1
+    kernels = [c for c in code.split("\n}\n") if "pair_alloc_then_trigger(&" in c]
+    assert kernels and code.count("pair_alloc_then_trigger(&") == len(kernels)
     for k in kernels:
-        assert re.search(r"if \(warp == 1\) tmem_alloc_then_trigger\(", k) and "pdl_trigger(" not in k and k.count("tmem_dealloc(") == 1
+        assert re.search(r"if \(warp == 1\) pair_alloc_then_trigger\(", k) and "pdl_trigger(" not in k and k.count("pair_dealloc(") == 1
     assert "__ldg" not in code and "ld.global.nc" not in code      # (what the kernel before writes is not read through the read-only cache)
