@@ -12,9 +12,9 @@
 // The tensor cores' accumulator is not rounded to nearest; a chain is 32 terms (four MMAs of the small products, then two of h h), and the
 // chains are added in float registers.
 //
-// Layout.  X, A and B lie in the scratch memory as blocks of 128 x 64 values, each part 16 KB in the order that the MMA wants in shared memory (rows of 128
-// bytes, 16-byte pieces exchanged by the row's last three bits): whatever the matrices' sizes one tensor map describes them all, and the same block serves as
-// a tile whose rows run along the result (X X^T, A A, B of B X) and as one whose rows run along the sum (X of B X).  Behind a matrix's last row and column lie zeros.
+// Layout.  X, A and B lie in the scratch memory as blocks of 128 x 64 values, each part 16 KB in the order that the MMA wants in shared memory without a swizzle
+// (eight rows' 16-byte pieces side by side): whatever the matrices' sizes one tensor map describes them all, eight lanes with a row each write whole lines, and the
+// same block serves as a tile whose rows run along the result (X X^T, A A, B of B X) and as one whose rows run along the sum (X of B X).  Behind a matrix's last row and column lie zeros.
 // A and B are symmetric: only tiles of 256 x 256 on and below the diagonal are computed and kept, and what lies above is read as the transposed of a tile below:
 // the same memory with its rows along the sum.
 //
@@ -35,16 +35,17 @@ namespace {
 
 constexpr int NS_SMS = 148;
 constexpr int NS_STAGES = 3, NS_SETS = 2, NS_CHAIN = 2;      // NS_CHAIN: steps of 16 terms
-constexpr uint32_t NS_OPERAND = 32 * 1024, NS_STAGE = 2 * NS_OPERAND, NS_PART = NS_OPERAND / 2, NS_HALF = NS_PART / 2;
+constexpr uint32_t NS_OPERAND = 32 * 1024, NS_STAGE = 2 * NS_OPERAND, NS_PART = NS_OPERAND / 2;
 constexpr int NS_ADDERS = 16, NS_THREADS = 32 * (2 + NS_ADDERS);
 constexpr int NS_TILE = 256;
+constexpr int NS_PITCH = 129;                            // rows of a column group of the sums that pairs exchange, and one
 constexpr float NS_SCALE = 8192.f, NS_UNSCALE = 1.f / 8192.f;
 constexpr size_t NS_HEADER = 256;
 
 enum { NS_GRAM, NS_SQUARE, NS_APPLY, NS_LAST };
 
 struct NsArgs {
-  CUtensorMap whole, half;     // the blocks' rows of 2 KB: 16 (both parts of a block), 4 at a time
+  CUtensorMap whole, across;   // the blocks as rows of 2 KB, 16 (both parts of a block) a copy; as rows of 1 KB, 8 of two neighbouring blocks a copy
   NsTable t;
   char* blocks;                // the blocks of the scratch memory
   double* sums;                // partial sums of squares, NS_CHUNK values each
@@ -88,36 +89,67 @@ __device__ __forceinline__ void parts8(const float (&v)[8], uint4& hi, uint4& lo
   lo = make_uint4(l[0], l[1], l[2], l[3]);
 }
 // Byte of a block's first part at which the 16-byte piece `piece` of `row` lies.
-__device__ __forceinline__ uint32_t piece_at(int row, int piece) { return (uint32_t)row * 128u + (uint32_t)((piece ^ (row & 7)) << 4); }
+__device__ __forceinline__ uint32_t piece_at(int row, int piece) { return (uint32_t)((row >> 3) * 1024 + piece * 128 + (row & 7) * 16); }
 
 // ---- momenta and sums of squares: a block of threads per NS_CHUNK values
 
 __device__ __forceinline__ float update_of(float g, float m, float mu, int nesterov) { return nesterov ? fmaf(mu, m - g, g) : m; }
 
+template <typename G>
+__device__ __forceinline__ double squares_of(const NsArgs& p, const NsEntry& e, size_t first, size_t last) {
+  const G* g = static_cast<const G*>(e.g);
+  double s = 0.0;
+  if ((first | last) % 4 == 0) {                             // (every pointer is aligned to 16 bytes)
+    constexpr int DEEP = 4;                                  // loads that are under way together
+#pragma unroll
+    for (int k0 = 0; k0 < NS_CHUNK / 1024; k0 += DEEP) {
+      float4 u[DEEP], m[DEEP];
+#pragma unroll
+      for (int k = 0; k < DEEP; ++k) {
+        const size_t i = first + (size_t)((k0 + k) * 256 + threadIdx.x) * 4;
+        u[k] = i < last ? ld4(g + i) : make_float4(0.f, 0.f, 0.f, 0.f);
+        if (p.muon) m[k] = i < last ? ld4(e.mom + i) : make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+#pragma unroll
+      for (int k = 0; k < DEEP; ++k) {
+        if (p.muon) {
+          const float f = 1.f - p.momentum;
+          m[k] = make_float4(fmaf(f, u[k].x - m[k].x, m[k].x), fmaf(f, u[k].y - m[k].y, m[k].y), fmaf(f, u[k].z - m[k].z, m[k].z), fmaf(f, u[k].w - m[k].w, m[k].w));
+          const size_t i = first + (size_t)((k0 + k) * 256 + threadIdx.x) * 4;
+          if (i < last) st4(e.mom + i, m[k]);
+          u[k] = make_float4(update_of(u[k].x, m[k].x, p.momentum, p.nesterov), update_of(u[k].y, m[k].y, p.momentum, p.nesterov),
+                             update_of(u[k].z, m[k].z, p.momentum, p.nesterov), update_of(u[k].w, m[k].w, p.momentum, p.nesterov));
+        }
+        s += ((double)u[k].x * u[k].x + (double)u[k].y * u[k].y) + ((double)u[k].z * u[k].z + (double)u[k].w * u[k].w);
+      }
+    }
+  } else {
+#pragma unroll 8
+    for (int k = 0; k < NS_CHUNK / 256; ++k) {
+      const size_t i = first + (size_t)(k * 256 + threadIdx.x);
+      if (i >= last) break;
+      float u = to_f(g[i]);
+      if (p.muon) {
+        const float m = fmaf(1.f - p.momentum, u - e.mom[i], e.mom[i]);
+        e.mom[i] = m;
+        u = update_of(u, m, p.momentum, p.nesterov);
+      }
+      s += (double)u * u;
+    }
+  }
+  return s;
+}
+
 __global__ void __launch_bounds__(256) ns_squares_kernel(const __grid_constant__ NsArgs p) {
   __shared__ double sums[8];
-  pdl_wait();
   int k = 0;
   while (k + 1 < p.t.entries && (int)blockIdx.x >= p.t.e[k + 1].chunk0) ++k;
   const NsEntry& e = p.t.e[k];
   const int local = (int)blockIdx.x - e.chunk0, per = chunks_of(e), mat = local / per;
-  const long size = (long)e.n * e.m, first = (long)(local - mat * per) * NS_CHUNK, last = min(size, first + NS_CHUNK), base = (long)mat * size;
-  double s = 0.0;
-  if (p.muon) {
-    float* mom = e.mom + base;
-    for (long i = first + threadIdx.x; i < last; i += 256) {
-      const float g = load_as_float(e.g, e.g_dtype, (size_t)(base + i));
-      const float m = fmaf(1.f - p.momentum, g - mom[i], mom[i]);
-      mom[i] = m;
-      const double u = (double)update_of(g, m, p.momentum, p.nesterov);
-      s += u * u;
-    }
-  } else {
-    for (long i = first + threadIdx.x; i < last; i += 256) {
-      const double u = (double)load_as_float(e.g, e.g_dtype, (size_t)(base + i));
-      s += u * u;
-    }
-  }
+  const size_t size = (size_t)e.n * e.m, base = (size_t)mat * size, first = base + (size_t)(local - mat * per) * NS_CHUNK;
+  const size_t last = first + NS_CHUNK < base + size ? first + NS_CHUNK : base + size;
+  pdl_wait();
+  double s = e.g_dtype == XCONV_F32 ? squares_of<float>(p, e, first, last) : e.g_dtype == XCONV_BF16 ? squares_of<bf16>(p, e, first, last) : squares_of<f16>(p, e, first, last);
   pdl_trigger();
   for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
   if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = s;
@@ -133,13 +165,13 @@ __global__ void __launch_bounds__(256) ns_squares_kernel(const __grid_constant__
 __global__ void __launch_bounds__(256) ns_blocks_kernel(const __grid_constant__ NsArgs p) {
   __shared__ float tile[NS_ROWS][NS_COLS + 1];
   __shared__ double sums[8];
-  pdl_wait();
-  pdl_trigger();
   int k = 0;
   while (k + 1 < p.t.entries && (int)blockIdx.x >= p.t.e[k + 1].block0) ++k;
   const NsEntry& e = p.t.e[k];
   const int kt = x_cols(e), per = row_blocks(e) * kt, local = (int)blockIdx.x - e.block0, mat = local / per, at = local - mat * per;
   const int rb = at / kt, cb = at - rb * kt, tid = threadIdx.x;
+  pdl_wait();
+  pdl_trigger();
   // the norm, from the matrix's partial sums in fixed order
   const int chunks = chunks_of(e);
   double s = 0.0;
@@ -172,7 +204,7 @@ __global__ void __launch_bounds__(256) ns_blocks_kernel(const __grid_constant__ 
   const float s1 = __int_as_float((e1 + 127) << 23), s2 = __int_as_float((e2 + 127) << 23);
   char* out = p.blocks + ((size_t)e.x0 + (size_t)mat * per + at) * NS_BLOCK;
   for (int i = tid; i < NS_ROWS * 8; i += 256) {
-    const int r = i >> 3, q = i & 7;
+    const int r = i & (NS_ROWS - 1), q = i / NS_ROWS;
     float v[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = tile[r][q * 8 + j] * s1 * f * s2;
@@ -214,15 +246,19 @@ __device__ __forceinline__ void pair_load(uint32_t dst, const CUtensorMap* map, 
   asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
                ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(row), "r"(smem_u32(bar) & 0xFEFFFFFFu) : "memory");
 }
-__device__ __forceinline__ void pair_mma(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t accumulate) {
+__device__ __forceinline__ void pair_load_across(uint32_t dst, const CUtensorMap* map, uint32_t block, uint32_t row, uint64_t* bar) {
+  asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+               ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(block), "r"(row), "r"(smem_u32(bar) & 0xFEFFFFFFu) : "memory");
+}
+__device__ __forceinline__ void pair_mma(uint32_t d, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
       "{\n\t.reg .pred p, e;\n\t.reg .b64 da, db;\n\t"
       "elect.sync _|e, 0xffffffff;\n\t"
-      "mov.b64 da, {%1, %3};\n\t"
-      "mov.b64 db, {%2, %3};\n\t"
-      "setp.ne.b32 p, %5, 0;\n\t"
-      "@e tcgen05.mma.cta_group::2.kind::f16 [%0], da, db, %4, p;\n\t}"
-      ::"r"(d), "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(accumulate) : "memory");
+      "mov.b64 da, {%1, %2};\n\t"
+      "mov.b64 db, {%3, %4};\n\t"
+      "setp.ne.b32 p, %6, 0;\n\t"
+      "@e tcgen05.mma.cta_group::2.kind::f16 [%0], da, db, %5, p;\n\t}"
+      ::"r"(d), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate) : "memory");
 }
 // An arrival at the barrier in the CTAs of `mask` once every MMA issued so far has finished.
 __device__ __forceinline__ void pair_commit(uint64_t* bar, uint32_t mask) {
@@ -259,6 +295,38 @@ __device__ __forceinline__ NsUnit ns_unit(const NsEntry* es, int entries, int u,
     w.stages = a_terms(e);
   }
   return w;
+}
+
+// An element of the result, from its sum: the orthogonalised matrix's, or the weight that it moves.
+__device__ __forceinline__ void ns_finish(const NsArgs& p, const NsEntry& e, size_t at, float sum) {
+  float o = sum * (NS_UNSCALE * NS_UNSCALE);
+  if (p.muon) o = fmaf(-e.scale, o, p.keep * load_as_float(e.out, e.out_dtype, at));
+  store_from_float(e.out, e.out_dtype, at, o);
+}
+template <typename T>
+__device__ __forceinline__ void ns_finish4_of(const NsArgs& p, const NsEntry& e, size_t at, float4 v) {
+  T* out = static_cast<T*>(e.out) + at;
+  constexpr float S = NS_UNSCALE * NS_UNSCALE;
+  float4 o = make_float4(v.x * S, v.y * S, v.z * S, v.w * S);
+  if (p.muon) {
+    const float4 w = ld4(out);
+    o = make_float4(fmaf(-e.scale, o.x, p.keep * w.x), fmaf(-e.scale, o.y, p.keep * w.y), fmaf(-e.scale, o.z, p.keep * w.z), fmaf(-e.scale, o.w, p.keep * w.w));
+  }
+  st4(out, o);
+}
+// ... and four neighbouring ones of a row, of which `left` are there.
+__device__ __forceinline__ void ns_finish4(const NsArgs& p, const NsEntry& e, size_t at, long left, float4 v) {
+  if (e.m % 4 == 0) {
+    if (left <= 0) return;
+    if (e.out_dtype == XCONV_F32) ns_finish4_of<float>(p, e, at, v);
+    else if (e.out_dtype == XCONV_BF16) ns_finish4_of<bf16>(p, e, at, v);
+    else ns_finish4_of<f16>(p, e, at, v);
+    return;
+  }
+  if (left > 0) ns_finish(p, e, at, v.x);
+  if (left > 1) ns_finish(p, e, at + 1, v.y);
+  if (left > 2) ns_finish(p, e, at + 2, v.z);
+  if (left > 3) ns_finish(p, e, at + 3, v.w);
 }
 
 // Eight neighbouring sums of a row of this CTA's half of a tile, columns 8 * q8 on.
@@ -307,15 +375,45 @@ __device__ __forceinline__ void ns_emit(const NsArgs& p, const NsEntry& e, const
     if (r >= e.n) return;
     const bool tall = e.rows > e.cols;
     const size_t base = (size_t)w.mat * e.n * e.m;
+    if (tall) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const long c = c0 + k;
-      if (c >= e.m) break;
-      const size_t at = base + (tall ? (size_t)c * e.n + r : (size_t)r * e.m + c);
-      float o = v[k] * (NS_UNSCALE * NS_UNSCALE);
-      if (p.muon) o = fmaf(-e.scale, o, p.keep * load_as_float(e.out, e.out_dtype, at));
-      store_from_float(e.out, e.out_dtype, at, o);
+      for (int k = 0; k < 8; ++k)
+        if (c0 + k < e.m) ns_finish(p, e, base + (size_t)(c0 + k) * e.n + r, v[k]);
+    } else {
+      ns_finish4(p, e, base + (size_t)r * e.m + c0, e.m - c0, make_float4(v[0], v[1], v[2], v[3]));
+      ns_finish4(p, e, base + (size_t)r * e.m + c0 + 4, e.m - c0 - 4, make_float4(v[4], v[5], v[6], v[7]));
     }
+  }
+}
+
+// The last product of a matrix that is not tall, 64 columns of a row each lane: eight lanes exchange pieces of four columns, so that together they have 32 of a row.
+__device__ __forceinline__ void ns_emit_rows(const NsArgs& p, const NsEntry& e, const NsUnit& w, int half, int row, int quarter, const float (&sum)[64]) {
+  const int lane = threadIdx.x & 7;
+  const long r0 = (long)(2 * w.I + half) * NS_ROWS + (row & ~7), c0 = (long)w.J * NS_TILE + quarter * 64 + lane * 4;
+  const size_t base = (size_t)w.mat * e.n * e.m;
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    float v[8][4];
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[u][k] = sum[b * 32 + u * 4 + k];
+#pragma unroll
+    for (int d = 1; d < 8; d *= 2)
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        if (u & d) continue;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float got = __shfl_xor_sync(0xffffffffu, lane & d ? v[u][k] : v[u | d][k], d);
+          if (lane & d) v[u][k] = got;
+          else v[u | d][k] = got;
+        }
+      }
+    const long c = c0 + b * 32;
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      if (r0 + u < e.n) ns_finish4(p, e, base + (size_t)(r0 + u) * e.m + c, e.m - c, make_float4(v[u][0], v[u][1], v[u][2], v[u][3]));
   }
 }
 
@@ -326,7 +424,6 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_product_kernel(const __grid_
   __shared__ uint64_t full[NS_STAGES], empty[NS_STAGES], acc_full[NS_SETS], acc_empty[NS_SETS];
   __shared__ NsEntry es[NS_MOST];
   __shared__ uint32_t tmem_slot;
-  __shared__ int go;
   const uint32_t smem = (smem_u32(raw) + 1023u) & ~1023u;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, entries = p.t.entries;
   const uint32_t rank = cluster_rank(), half = rank & 1u, leader = rank & ~1u;
@@ -335,26 +432,23 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_product_kernel(const __grid_
     for (int i = 0; i < NS_SETS; ++i) { mbar_init(&acc_full[i], 1); mbar_init(&acc_empty[i], 2 * NS_ADDERS); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     prefetch_tmap(&p.whole);
-    prefetch_tmap(&p.half);
+    prefetch_tmap(&p.across);
   }
   for (int i = threadIdx.x; i < entries * (int)(sizeof(NsEntry) / 4); i += NS_THREADS)
     reinterpret_cast<uint32_t*>(es)[i] = reinterpret_cast<const uint32_t*>(p.t.e)[i];
   if (warp == 1) pair_alloc_then_trigger(&tmem_slot);
   __syncwarp();
   cluster_sync();                                    // (the other CTAs' barriers are there)
-  pdl_wait();
-  if (threadIdx.x == 0) {
-    go = (*reinterpret_cast<volatile unsigned*>(p.status) != p.tag) ? 1 : 0;
-    if (blockIdx.x == 0) reinterpret_cast<volatile unsigned*>(p.status)[1] = p.tag;
-  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  pdl_wait();
+  if (blockIdx.x == 0 && threadIdx.x == 64) reinterpret_cast<volatile unsigned*>(p.status)[1] = p.tag;
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&tmem_slot);
   const int part = (int)(rank >> 1);                 // of the tile's terms
   const int units = SYM ? p.t.syms : p.t.prods, per = 2 * p.cs, u0 = (int)blockIdx.x / per, step = (int)gridDim.x / per;
 
-  if (go && warp == 0) {
+  if (warp == 0) {
     if (lane == 0) {
       asm volatile("fence.proxy.async;" ::: "memory");       // (the kernels before wrote the blocks by ordinary stores)
       uint32_t slot = 0, lap = 0, issued = 0;
@@ -369,25 +463,23 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_product_kernel(const __grid_
         // What both CTAs of the pair copy a stage: rows of the first operand, rows (columns) of the second.
         uint32_t bytes = (uint32_t)min(2, nt - 2 * w.I) * NS_OPERAND;
         if (SYM) bytes += same ? 0u : (uint32_t)min(2, nt - 2 * w.J) * NS_OPERAND;
-        else bytes += (uint32_t)min(4, kt - 4 * w.J) * NS_PART;
+        else bytes += kt - 4 * w.J > 2 ? 2 * NS_OPERAND : NS_OPERAND;
         const int s0 = w.stages * part / p.cs, s1 = w.stages * (part + 1) / p.cs;
         for (int s = s0; s < s1; ++s) {
           if (issued >= NS_STAGES && !mbar_wait(&empty[slot], lap ^ 1u, p.status, p.tag)) { ok = false; break; }
           const uint32_t to = smem + slot * NS_STAGE;
           uint64_t* bar = &full[slot];
           if (half == 0) mbar_arrive_expect_tx(bar, bytes);
-          // 64 rows of two neighbouring blocks, both parts of each: a tile with its rows along the sum
-          const auto load_across = [&](uint32_t dst, uint32_t block, int count) {
-            const uint32_t row = block * 16u + (uint32_t)(s & 1) * 4u;
-            for (int h = 0; h < count; ++h) {
-              pair_load(dst + h * NS_HALF, &p.half, row + h * 16u, bar);
-              pair_load(dst + NS_PART + h * NS_HALF, &p.half, row + h * 16u + 8u, bar);
-            }
+          // 64 rows of two neighbouring blocks, both parts of each: a tile with its rows along the sum (behind a matrix's last block another's, for columns that
+          // nothing reads)
+          const auto load_across = [&](uint32_t dst, uint32_t block) {
+            pair_load_across(dst, &p.across, block, (uint32_t)(s & 1) * 8u, bar);
+            pair_load_across(dst + NS_PART, &p.across, block, (uint32_t)(s & 1) * 8u + 16u, bar);
           };
           // block (i, s) of a symmetric matrix
           const auto load_symmetric = [&](uint32_t dst, int row_block) {
             if (s / 4 <= row_block / 2) pair_load(dst, &p.whole, (sb + (uint32_t)row_block * 2 * nt + s) * 16u, bar);
-            else load_across(dst, sb + (uint32_t)(s >> 1) * 2 * nt + 2 * row_block, 2);
+            else load_across(dst, sb + (uint32_t)(s >> 1) * 2 * nt + 2 * row_block);
           };
           if (MODE == NS_GRAM) {
             if (i < nt) pair_load(to, &p.whole, (xb + (uint32_t)i * kt + s) * 16u, bar);
@@ -398,7 +490,7 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_product_kernel(const __grid_
               if (!same && j < nt) load_symmetric(to + NS_OPERAND, j);
             } else {
               const int c = 4 * w.J + 2 * (int)half;
-              load_across(to + NS_OPERAND, xb + (uint32_t)(s >> 1) * kt + c, min(2, kt - c));
+              if (c < kt) load_across(to + NS_OPERAND, xb + (uint32_t)(s >> 1) * kt + c);
             }
           }
           ++issued;
@@ -414,15 +506,15 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_product_kernel(const __grid_
         }
     }
     __syncwarp();
-  } else if (go && warp == 1) {
+  } else if (warp == 1) {
     if (half == 0) {
       uint32_t slot = 0, lap = 0, set = 0, set_lap = 0, used = 0;
       int k = 0;
       bool ok = true;
-      // Shared-memory descriptors: rows along the result (groups of eight 1024 bytes apart, 32 bytes a step of 16 terms), or along the sum (2048
-      // bytes a step, column blocks 8 KB apart).
-      constexpr uint32_t HI = (1024u >> 4) | (1u << 14) | (2u << 29);
-      constexpr uint32_t ACROSS = (NS_HALF >> 4) << 16, ALONG_STEP = 32u >> 4, ACROSS_STEP = 2048u >> 4;
+      // Shared-memory descriptors, no swizzle.  Rows along the result: a row's pieces 128 bytes apart, groups of eight rows 1024, a step of 16 terms 256.
+      // Rows along the sum: groups of eight rows 2048 bytes apart (of both blocks), columns' pieces 128, a step 4096.
+      constexpr uint32_t ALONG = (128u >> 4) << 16, ALONG_HI = (1024u >> 4) | (1u << 14), ALONG_STEP = 256u >> 4;
+      constexpr uint32_t ACROSS = (2048u >> 4) << 16, ACROSS_HI = (128u >> 4) | (1u << 14), ACROSS_STEP = 4096u >> 4;
       constexpr uint32_t IDESC = (1u << 4) | ((uint32_t)(NS_TILE >> 3) << 17) | ((uint32_t)(NS_TILE >> 4) << 24);
       const uint32_t pair_mask = 3u << leader;
       for (int u = u0; u < units && ok; u += step) {
@@ -434,7 +526,8 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_product_kernel(const __grid_
           tc_fence_after();
           const bool a_across = MODE != NS_GRAM && s / 4 > w.I, b_across = MODE == NS_SQUARE ? s / 4 > w.J : !SYM;
           const uint32_t at = (smem + slot * NS_STAGE) & 0x3FFFFu;      // (in a cluster an address has the CTA's rank above these bits)
-          const uint32_t a = (a_across ? ACROSS : 1u << 16) | (at >> 4), b = (b_across ? ACROSS : 1u << 16) | ((at + (same ? 0u : NS_OPERAND)) >> 4);
+          const uint32_t a = (a_across ? ACROSS : ALONG) | (at >> 4), b = (b_across ? ACROSS : ALONG) | ((at + (same ? 0u : NS_OPERAND)) >> 4);
+          const uint32_t a_hi = a_across ? ACROSS_HI : ALONG_HI, b_hi = b_across ? ACROSS_HI : ALONG_HI;
           const uint32_t a_step = a_across ? ACROSS_STEP : ALONG_STEP, b_step = b_across ? ACROSS_STEP : ALONG_STEP;
           const uint32_t idesc = IDESC | (a_across ? 1u << 15 : 0u) | (b_across ? 1u << 16 : 0u);
           constexpr uint32_t L = NS_PART >> 4;
@@ -444,11 +537,11 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_product_kernel(const __grid_
             tc_fence_after();
             const uint32_t d = tmem + set * NS_TILE;
 #pragma unroll
-            for (int t = c; t < c + NS_CHAIN; ++t) pair_mma(d, a + L + t * a_step, b + t * b_step, HI, idesc, t > c);
+            for (int t = c; t < c + NS_CHAIN; ++t) pair_mma(d, a + L + t * a_step, a_hi, b + t * b_step, b_hi, idesc, t > c);
 #pragma unroll
-            for (int t = c; t < c + NS_CHAIN; ++t) pair_mma(d, a + t * a_step, b + L + t * b_step, HI, idesc, 1u);
+            for (int t = c; t < c + NS_CHAIN; ++t) pair_mma(d, a + t * a_step, a_hi, b + L + t * b_step, b_hi, idesc, 1u);
 #pragma unroll
-            for (int t = c; t < c + NS_CHAIN; ++t) pair_mma(d, a + t * a_step, b + t * b_step, HI, idesc, 1u);
+            for (int t = c; t < c + NS_CHAIN; ++t) pair_mma(d, a + t * a_step, a_hi, b + t * b_step, b_hi, idesc, 1u);
             if (c + NS_CHAIN == 4) pair_commit(&empty[slot], pair_mask);
             pair_commit(&acc_full[set], pair_mask);
             ++used;
@@ -465,7 +558,7 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_product_kernel(const __grid_
           mbar_wait_warp(&acc_full[set], set_lap, p.status, p.tag);
         }
     }
-  } else if (go) {
+  } else {
     const int quadrant = warp & 3, quarter = (warp - 2) >> 2, row = quadrant * 32 + lane;
     uint32_t set = 0, set_lap = 0;
     int k = 0;
@@ -497,7 +590,9 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_product_kernel(const __grid_
         if (++set == NS_SETS) { set = 0; set_lap ^= 1u; }
       }
       if (!ok) break;
-      if (p.cs == 1) {
+      if (p.cs == 1 && MODE == NS_LAST && es[w.k].rows <= es[w.k].cols) {
+        ns_emit_rows(p, es[w.k], w, (int)half, row, quarter, sum);
+      } else if (p.cs == 1) {
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
           float v[8];
@@ -509,7 +604,7 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_product_kernel(const __grid_
         // (one unit a cluster: every stage of this pair has been multiplied, and the ring's memory is free)
 #pragma unroll
         for (int q = 0; q < 16; ++q)
-          asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(smem + (uint32_t)(((quarter * 16 + q) * 128 + row) * 16)), "f"(sum[4 * q]), "f"(sum[4 * q + 1]),
+          asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(smem + (uint32_t)(((quarter * 16 + q) * NS_PITCH + row) * 16)), "f"(sum[4 * q]), "f"(sum[4 * q + 1]),
                        "f"(sum[4 * q + 2]), "f"(sum[4 * q + 3]) : "memory");
       }
     }
@@ -518,21 +613,24 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_product_kernel(const __grid_
   tc_fence_before();
   cluster_sync();                                    // (no arrival and no copy of the pair comes behind this)
   if (p.cs > 1) {
-    if (go && warp >= 2 && u0 < units) {
+    if (warp >= 2 && u0 < units) {
       int k = 0;
       const NsUnit w = ns_unit<MODE>(es, entries, u0, k);
-      const int t = threadIdx.x - 64, row = t & 127, groups = 32 / p.cs;      // this CTA's groups of eight columns
-      for (int g = t >> 7; g < groups; g += 4) {
-        const int q8 = part * groups + g;
+      const NsEntry& e = es[w.k];
+      // This CTA's groups of eight columns; neighbouring lanes have neighbouring rows, or, where rows of the result are written, neighbouring columns.
+      const int t = threadIdx.x - 64, groups = 32 / p.cs;
+      const bool by_row = MODE == NS_LAST && e.rows <= e.cols;
+      for (int x = t; x < 128 * groups; x += 512) {
+        const int row = by_row ? x / groups : x & 127, q8 = part * groups + (by_row ? x % groups : x >> 7);
         float v[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = 0.f;
         for (int c = 0; c < p.cs; ++c) {
-          const uint32_t from = smem + (uint32_t)((2 * q8 * 128 + row) * 16), other = 2u * c + half;
-          const float4 x = ld_cluster_f4(from, other), y = ld_cluster_f4(from + 128 * 16, other);
-          v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w; v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
+          const uint32_t from = smem + (uint32_t)((2 * q8 * NS_PITCH + row) * 16), other = 2u * c + half;
+          const float4 f = ld_cluster_f4(from, other), g = ld_cluster_f4(from + NS_PITCH * 16, other);
+          v[0] += f.x; v[1] += f.y; v[2] += f.z; v[3] += f.w; v[4] += g.x; v[5] += g.y; v[6] += g.z; v[7] += g.w;
         }
-        ns_emit<MODE>(p, es[w.k], w, (int)half, row, q8, v);
+        ns_emit<MODE>(p, e, w, (int)half, row, q8, v);
       }
     }
     __syncwarp();
@@ -569,14 +667,16 @@ cudaError_t launch_product(NsArgs& p, cudaStream_t st) {
   return cudaLaunchKernelEx(&cfg, ns_product_kernel<MODE>, p);
 }
 
-// The scratch memory's blocks as rows of 256 values of 8 bytes, 16 of them a block; `rows` of them a copy.  (The copy engine fetches a box row by row: with
-// rows of 128 bytes it was what bounded the products.)
-bool map_blocks(CUtensorMap* m, const void* blocks, size_t count, uint32_t rows) {
+// The scratch memory's blocks as rows of 256 values of 8 bytes, 16 of them a block and a copy.  (The copy engine fetches a box row by row: long rows.)  And as rows
+// of 128 such values, 32 of them a block: 8 rows of two neighbouring blocks a copy, row by row.
+bool map_blocks(CUtensorMap* whole, CUtensorMap* across, void* blocks, size_t count) {
   PFN_cuTensorMapEncodeTiled_v12000 fn = encode_fn();
   if (!fn) return false;
-  cuuint64_t dims[2] = {256, count * 16}, strides[1] = {2048};
-  cuuint32_t box[2] = {256, rows}, steps[2] = {1, 1};
-  return fn(m, CU_TENSOR_MAP_DATA_TYPE_INT64, 2, const_cast<void*>(blocks), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
+  const cuuint64_t dims[2] = {256, count * 16}, strides[1] = {2048}, dims3[3] = {128, count, 32}, strides3[2] = {NS_BLOCK, 1024};
+  const cuuint32_t box[2] = {256, 16}, box3[3] = {128, 2, 8}, steps[3] = {1, 1, 1};
+  return fn(whole, CU_TENSOR_MAP_DATA_TYPE_INT64, 2, blocks, dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS &&
+         fn(across, CU_TENSOR_MAP_DATA_TYPE_INT64, 3, blocks, dims3, strides3, box3, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -616,7 +716,7 @@ cudaError_t launch_newton_schulz(const NsTable& t, const NsOptions& o, void* ws,
   p.sums = reinterpret_cast<double*>(static_cast<char*>(ws) + NS_HEADER);
   p.blocks = static_cast<char*>(ws) + NS_HEADER + sums_bytes(t);
   p.a = o.a; p.b = o.b; p.c = o.c; p.eps = o.eps; p.momentum = o.momentum; p.keep = o.keep; p.muon = o.muon; p.nesterov = o.nesterov;
-  if (!map_blocks(&p.whole, p.blocks, t.ws_blocks, 16) || !map_blocks(&p.half, p.blocks, t.ws_blocks, 4)) return cudaErrorInvalidValue;
+  if (!map_blocks(&p.whole, &p.across, p.blocks, t.ws_blocks)) return cudaErrorInvalidValue;
   cudaError_t e = launch_pdl(ns_squares_kernel, dim3((unsigned)t.chunks), dim3(256), 0, st, p);
   if (e != cudaSuccess) return e;
   ++*launches;
