@@ -222,10 +222,15 @@ __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release;" ::: "memory");
   asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
 }
-__device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr, uint32_t rank) {
+// ... that orders no memory: for what only has to outlive the other CTAs' accesses, which they have seen the end of.
+__device__ __forceinline__ void cluster_sync_relaxed() {
+  asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");
+  asm volatile("barrier.cluster.wait;" ::: "memory");
+}
+__device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr, uint32_t rank) {      // (several are under way together)
   float4 v;
   asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %4, %5;\n\tld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [a];\n\t}"
-               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr), "r"(rank) : "memory");
+               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr), "r"(rank));
   return v;
 }
 __device__ __forceinline__ void arrive_at(uint64_t* bar, uint32_t rank) {      // ... of the same barrier in another CTA of the cluster
@@ -329,59 +334,59 @@ __device__ __forceinline__ void ns_finish4(const NsArgs& p, const NsEntry& e, si
   if (left > 3) ns_finish(p, e, at + 3, v.w);
 }
 
-// Eight neighbouring sums of a row of this CTA's half of a tile, columns 8 * q8 on.
-template <int MODE>
-__device__ __forceinline__ void ns_emit(const NsArgs& p, const NsEntry& e, const NsUnit& w, int half, int row, int q8, float (&v)[8]) {
+// N groups of eight neighbouring sums of a row of this CTA's half of a tile, from column 8 * q8 on (within a block's 64 columns).
+template <int MODE, int N>
+__device__ __forceinline__ void ns_emit(const NsArgs& p, const NsEntry& e, const NsUnit& w, int half, int row, int q8, float (&v)[N][8]) {
   const int nt = row_blocks(e), i = 2 * w.I + half, cb = 4 * w.J + (q8 >> 3);
   if (i >= nt) return;
-  if (MODE == NS_GRAM || MODE == NS_SQUARE) {
-    if (cb >= 2 * nt) return;
-    const size_t at = (((size_t)w.mat * nt + i) * 2 * nt + cb) * NS_BLOCK + piece_at(row, q8 & 7);
-    char* to = p.blocks + (size_t)(MODE == NS_GRAM ? e.a : e.b) * NS_BLOCK + at;
-    if (MODE == NS_GRAM) {
+  if (MODE != NS_LAST) {
+    const int columns = MODE == NS_APPLY ? x_cols(e) : 2 * nt;
+    if (cb >= columns) return;
+    const size_t at = (((size_t)w.mat * nt + i) * columns + cb) * NS_BLOCK + piece_at(row, q8 & 7);
+    char* to = p.blocks + (size_t)(MODE == NS_GRAM ? e.a : MODE == NS_SQUARE ? e.b : p.which ? e.x0 : e.x1) * NS_BLOCK + at;
+    const char* from = p.blocks + (size_t)e.a * NS_BLOCK + at;
+    uint4 ah[N], al[N];
+    if (MODE == NS_SQUARE)
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] *= NS_UNSCALE;
-    } else {
-      const char* from = p.blocks + (size_t)e.a * NS_BLOCK + at;
-      const uint4 hi = __ldcg(reinterpret_cast<const uint4*>(from)), lo = __ldcg(reinterpret_cast<const uint4*>(from + NS_PART));
-      const uint32_t h[4] = {hi.x, hi.y, hi.z, hi.w}, l[4] = {lo.x, lo.y, lo.z, lo.w};
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&h[k])), b = __half22float2(*reinterpret_cast<const __half2*>(&l[k]));
-        v[2 * k] = fmaf(p.c * NS_UNSCALE, v[2 * k], p.b * (a.x + b.x));
-        v[2 * k + 1] = fmaf(p.c * NS_UNSCALE, v[2 * k + 1], p.b * (a.y + b.y));
+      for (int g = 0; g < N; ++g) {
+        ah[g] = __ldcg(reinterpret_cast<const uint4*>(from + g * 128));
+        al[g] = __ldcg(reinterpret_cast<const uint4*>(from + g * 128 + NS_PART));
       }
-      const int r = i * NS_ROWS + row, d = r - (w.J * NS_TILE + q8 * 8);
 #pragma unroll
-      for (int k = 0; k < 8; ++k)
-        if (k == d && r < e.n) v[k] += p.a * NS_SCALE;
+    for (int g = 0; g < N; ++g) {
+      if (MODE == NS_SQUARE) {
+        const uint32_t h[4] = {ah[g].x, ah[g].y, ah[g].z, ah[g].w}, l[4] = {al[g].x, al[g].y, al[g].z, al[g].w};
+        const int r = i * NS_ROWS + row, d = r < e.n ? r - (w.J * NS_TILE + (q8 + g) * 8) : -1;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&h[k])), y = __half22float2(*reinterpret_cast<const __half2*>(&l[k]));
+          v[g][2 * k] = fmaf(p.c * NS_UNSCALE, v[g][2 * k], p.b * (x.x + y.x)) + (d == 2 * k ? p.a * NS_SCALE : 0.f);
+          v[g][2 * k + 1] = fmaf(p.c * NS_UNSCALE, v[g][2 * k + 1], p.b * (x.y + y.y)) + (d == 2 * k + 1 ? p.a * NS_SCALE : 0.f);
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[g][k] *= NS_UNSCALE;
+      }
+      uint4 hi, lo;
+      parts8(v[g], hi, lo);
+      *reinterpret_cast<uint4*>(to + g * 128) = hi;
+      *reinterpret_cast<uint4*>(to + g * 128 + NS_PART) = lo;
     }
-    uint4 hi, lo;
-    parts8(v, hi, lo);
-    *reinterpret_cast<uint4*>(to) = hi;
-    *reinterpret_cast<uint4*>(to + NS_PART) = lo;
-  } else if (MODE == NS_APPLY) {
-    const int kt = x_cols(e);
-    if (cb >= kt) return;
-    char* to = p.blocks + ((size_t)(p.which ? e.x0 : e.x1) + ((size_t)w.mat * nt + i) * kt + cb) * NS_BLOCK + piece_at(row, q8 & 7);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] *= NS_UNSCALE;
-    uint4 hi, lo;
-    parts8(v, hi, lo);
-    *reinterpret_cast<uint4*>(to) = hi;
-    *reinterpret_cast<uint4*>(to + NS_PART) = lo;
   } else {
-    const long r = (long)i * NS_ROWS + row, c0 = (long)w.J * NS_TILE + q8 * 8;
+    const long r = (long)i * NS_ROWS + row;
     if (r >= e.n) return;
-    const bool tall = e.rows > e.cols;
     const size_t base = (size_t)w.mat * e.n * e.m;
-    if (tall) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k)
-        if (c0 + k < e.m) ns_finish(p, e, base + (size_t)(c0 + k) * e.n + r, v[k]);
-    } else {
-      ns_finish4(p, e, base + (size_t)r * e.m + c0, e.m - c0, make_float4(v[0], v[1], v[2], v[3]));
-      ns_finish4(p, e, base + (size_t)r * e.m + c0 + 4, e.m - c0 - 4, make_float4(v[4], v[5], v[6], v[7]));
+    for (int g = 0; g < N; ++g) {
+      const long c0 = (long)w.J * NS_TILE + (q8 + g) * 8;
+      if (e.rows > e.cols) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (c0 + k < e.m) ns_finish(p, e, base + (size_t)(c0 + k) * e.n + r, v[g][k]);
+      } else {
+        ns_finish4(p, e, base + (size_t)r * e.m + c0, e.m - c0, make_float4(v[g][0], v[g][1], v[g][2], v[g][3]));
+        ns_finish4(p, e, base + (size_t)r * e.m + c0 + 4, e.m - c0 - 4, make_float4(v[g][4], v[g][5], v[g][6], v[g][7]));
+      }
     }
   }
 }
@@ -423,6 +428,7 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_product_kernel(const __grid_
   extern __shared__ uint8_t raw[];
   __shared__ uint64_t full[NS_STAGES], empty[NS_STAGES], acc_full[NS_SETS], acc_empty[NS_SETS];
   __shared__ NsEntry es[NS_MOST];
+  __shared__ NsUnit first;
   __shared__ uint32_t tmem_slot;
   const uint32_t smem = (smem_u32(raw) + 1023u) & ~1023u;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, entries = p.t.entries;
@@ -434,28 +440,32 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_product_kernel(const __grid_
     prefetch_tmap(&p.whole);
     prefetch_tmap(&p.across);
   }
+  const int part = (int)(rank >> 1);                 // of the tile's terms
+  const int units = SYM ? p.t.syms : p.t.prods, per = 2 * p.cs, u0 = (int)blockIdx.x / per, step = (int)gridDim.x / per;
   for (int i = threadIdx.x; i < entries * (int)(sizeof(NsEntry) / 4); i += NS_THREADS)
     reinterpret_cast<uint32_t*>(es)[i] = reinterpret_cast<const uint32_t*>(p.t.e)[i];
   if (warp == 1) pair_alloc_then_trigger(&tmem_slot);
   __syncwarp();
   cluster_sync();                                    // (the other CTAs' barriers are there)
+  __syncthreads();
+  if (threadIdx.x == 0) {                            // (while the kernel before still runs)
+    int k = 0;
+    first = ns_unit<MODE>(es, entries, u0, k);
+  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   pdl_wait();
   if (blockIdx.x == 0 && threadIdx.x == 64) reinterpret_cast<volatile unsigned*>(p.status)[1] = p.tag;
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&tmem_slot);
-  const int part = (int)(rank >> 1);                 // of the tile's terms
-  const int units = SYM ? p.t.syms : p.t.prods, per = 2 * p.cs, u0 = (int)blockIdx.x / per, step = (int)gridDim.x / per;
 
   if (warp == 0) {
     if (lane == 0) {
-      asm volatile("fence.proxy.async;" ::: "memory");       // (the kernels before wrote the blocks by ordinary stores)
       uint32_t slot = 0, lap = 0, issued = 0;
-      int k = 0;
+      int k = first.k;
       bool ok = true;
       for (int u = u0; u < units && ok; u += step) {
-        const NsUnit w = ns_unit<MODE>(es, entries, u, k);
+        const NsUnit w = u == u0 ? first : ns_unit<MODE>(es, entries, u, k);
         const NsEntry& e = es[w.k];
         const int nt = row_blocks(e), kt = x_cols(e), i = 2 * w.I + (int)half, j = 2 * w.J + (int)half;
         const uint32_t xb = (p.which ? e.x1 : e.x0) + (uint32_t)w.mat * nt * kt, sb = (MODE == NS_SQUARE ? e.a : e.b) + (uint32_t)w.mat * nt * 2 * nt;
@@ -509,7 +519,7 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_product_kernel(const __grid_
   } else if (warp == 1) {
     if (half == 0) {
       uint32_t slot = 0, lap = 0, set = 0, set_lap = 0, used = 0;
-      int k = 0;
+      int k = first.k;
       bool ok = true;
       // Shared-memory descriptors, no swizzle.  Rows along the result: a row's pieces 128 bytes apart, groups of eight rows 1024, a step of 16 terms 256.
       // Rows along the sum: groups of eight rows 2048 bytes apart (of both blocks), columns' pieces 128, a step 4096.
@@ -518,7 +528,7 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_product_kernel(const __grid_
       constexpr uint32_t IDESC = (1u << 4) | ((uint32_t)(NS_TILE >> 3) << 17) | ((uint32_t)(NS_TILE >> 4) << 24);
       const uint32_t pair_mask = 3u << leader;
       for (int u = u0; u < units && ok; u += step) {
-        const NsUnit w = ns_unit<MODE>(es, entries, u, k);
+        const NsUnit w = u == u0 ? first : ns_unit<MODE>(es, entries, u, k);
         const bool same = SYM && w.I == w.J;
         const int s0 = w.stages * part / p.cs, s1 = w.stages * (part + 1) / p.cs;
         for (int s = s0; s < s1 && ok; ++s) {
@@ -561,10 +571,10 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_product_kernel(const __grid_
   } else {
     const int quadrant = warp & 3, quarter = (warp - 2) >> 2, row = quadrant * 32 + lane;
     uint32_t set = 0, set_lap = 0;
-    int k = 0;
+    int k = first.k;
     bool ok = true;
     for (int u = u0; u < units && ok; u += step) {
-      const NsUnit w = ns_unit<MODE>(es, entries, u, k);
+      const NsUnit w = u == u0 ? first : ns_unit<MODE>(es, entries, u, k);
       float sum[64];
 #pragma unroll
       for (int i = 0; i < 64; ++i) sum[i] = 0.f;
@@ -594,11 +604,11 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_product_kernel(const __grid_
         ns_emit_rows(p, es[w.k], w, (int)half, row, quarter, sum);
       } else if (p.cs == 1) {
 #pragma unroll
-        for (int q = 0; q < 8; ++q) {
-          float v[8];
+        for (int q = 0; q < 8; q += 2) {
+          float v[2][8];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) v[i] = sum[q * 8 + i];
-          ns_emit<MODE>(p, es[w.k], w, (int)half, row, quarter * 8 + q, v);
+          for (int i = 0; i < 16; ++i) v[i / 8][i % 8] = sum[q * 8 + i];
+          ns_emit<MODE, 2>(p, es[w.k], w, (int)half, row, quarter * 8 + q, v);
         }
       } else {
         // (one unit a cluster: every stage of this pair has been multiplied, and the ring's memory is free)
@@ -611,30 +621,39 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_product_kernel(const __grid_
   }
   __syncwarp();
   tc_fence_before();
-  cluster_sync();                                    // (no arrival and no copy of the pair comes behind this)
-  if (p.cs > 1) {
+  // No arrival and no copy of the pair comes behind this.
+  if (p.cs == 1) {
+    cluster_sync_relaxed();
+  } else {
+    cluster_sync();
     if (warp >= 2 && u0 < units) {
-      int k = 0;
-      const NsUnit w = ns_unit<MODE>(es, entries, u0, k);
+      const NsUnit& w = first;
       const NsEntry& e = es[w.k];
       // This CTA's groups of eight columns; neighbouring lanes have neighbouring rows, or, where rows of the result are written, neighbouring columns.
       const int t = threadIdx.x - 64, groups = 32 / p.cs;
       const bool by_row = MODE == NS_LAST && e.rows <= e.cols;
       for (int x = t; x < 128 * groups; x += 512) {
         const int row = by_row ? x / groups : x & 127, q8 = part * groups + (by_row ? x % groups : x >> 7);
-        float v[8];
+        float4 f[4], g[4];                             // (p.cs is 2 or 4)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = 0.f;
-        for (int c = 0; c < p.cs; ++c) {
-          const uint32_t from = smem + (uint32_t)((2 * q8 * NS_PITCH + row) * 16), other = 2u * c + half;
-          const float4 f = ld_cluster_f4(from, other), g = ld_cluster_f4(from + NS_PITCH * 16, other);
-          v[0] += f.x; v[1] += f.y; v[2] += f.z; v[3] += f.w; v[4] += g.x; v[5] += g.y; v[6] += g.z; v[7] += g.w;
-        }
-        ns_emit<MODE>(p, e, w, (int)half, row, q8, v);
+        for (int c = 0; c < 4; ++c)
+          if (c < p.cs) {
+            const uint32_t from = smem + (uint32_t)((2 * q8 * NS_PITCH + row) * 16);
+            f[c] = ld_cluster_f4(from, 2u * c + half);
+            g[c] = ld_cluster_f4(from + NS_PITCH * 16, 2u * c + half);
+          }
+        float v[1][8] = {{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          if (c < p.cs) {
+            v[0][0] += f[c].x; v[0][1] += f[c].y; v[0][2] += f[c].z; v[0][3] += f[c].w;
+            v[0][4] += g[c].x; v[0][5] += g[c].y; v[0][6] += g[c].z; v[0][7] += g[c].w;
+          }
+        ns_emit<MODE, 1>(p, e, w, (int)half, row, q8, v);
       }
     }
     __syncwarp();
-    cluster_sync();                                  // (no CTA ends while its sums are read)
+    cluster_sync_relaxed();                          // (no CTA ends while its sums are read)
   }
   if (warp == 1) pair_dealloc(tmem);
 }
