@@ -9,7 +9,10 @@
 // a block keep the same columns from row to row and carry the sums of dw and db in registers; blocks leave one partial sum a column each, which a second kernel
 // adds in fixed order (no atomics: the same bits every time).
 //
-// Rows that are not aligned to 16 bytes are read element by element; rows that do not fit the registers of a block are read again for every sum.
+// What keeps the memory busy are asynchronous copies: persistent blocks fetch the next rows of their threads into shared memory while they work on these ones, each
+// thread its own 16-byte pieces, so that no thread waits for another's.  Dense rows that do not begin on 16-byte boundaries (odd channel counts) are fetched and
+// written as runs of several rows that do, and picked apart in shared memory.  Other rows (some of the channels of a wider tensor, at odd offsets) are read element by
+// element; rows that do not fit the registers of a block are read again for every sum.
 #include "layer_norm.h"
 
 #include <algorithm>
@@ -24,7 +27,7 @@ namespace {
 constexpr int NORM_SMS = 148;
 constexpr int NORM_THREADS = 512;            // of a block whose threads hold the row
 
-template <typename T> constexpr int vec_of() { return 16 / (int)sizeof(T); }
+template <typename T> constexpr int VEC_OF = 16 / (int)sizeof(T);
 
 // VEC neighbouring elements as floats.
 template <typename T, int VEC>
@@ -70,6 +73,12 @@ __device__ __forceinline__ void store_elems(T* p, const float (&f)[VEC]) {
     *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
   }
 }
+__device__ __forceinline__ void copy16_async(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
 // VEC parameters (weight, bias): VEC elements of the activations are up to 32 bytes of them.
 template <typename P, int VEC>
 __device__ __forceinline__ void load_params(const P* p, float (&f)[VEC]) {
@@ -81,27 +90,30 @@ __device__ __forceinline__ void load_params(const P* p, float (&f)[VEC]) {
   }
 }
 
-// Sums over the `group` threads of a row, the same in each of them: within a warp by shuffles, across warps through shared memory (a buffer of
-// blockDim.x / 32 entries that no one else uses before the next barrier but one).  All threads of the block take part.
+// Sums over the `group` threads of a row, the same in each of them: within a warp by shuffles, across warps through shared memory (a buffer that
+// no one else uses before the group's next sum but one) and a barrier of the group's own: other rows of the block are elsewhere.
 template <int N>
-__device__ __forceinline__ void group_sum(float (&v)[N], int group, float (*buf)[N]) {
-  const int width = min(group, 32);
-  for (int o = width >> 1; o > 0; o >>= 1)
+__device__ __forceinline__ void group_sum(float (&v)[N], int group, float (*buf)[32]) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+  for (int o = 16; o > 0; o >>= 1)
+    if (o < group)
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
   if (group <= 32) return;
-  const int warp = threadIdx.x >> 5, per = group >> 5;
+  const int warp = threadIdx.x >> 5, per = group >> 5, first = warp & -per;
   if ((threadIdx.x & 31) == 0)
 #pragma unroll
-    for (int i = 0; i < N; ++i) buf[warp][i] = v[i];
-  __syncthreads();
-  // (each warp adds the `per` sums by shuffles too: 32 of them at most)
-  const int lane = threadIdx.x & 31, first = warp / per * per;
+    for (int i = 0; i < N; ++i) buf[i][warp] = v[i];
+  asm volatile("bar.sync %0, %1;" ::"r"(1 + first / per), "r"(group) : "memory");      // (at most eight groups of several warps)
 #pragma unroll
-  for (int i = 0; i < N; ++i) v[i] = lane < per ? buf[first + lane][i] : 0.f;
-  for (int o = 16; o > 0; o >>= 1)
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+  for (int i = 0; i < N; ++i) {
+    float s = 0.f;
+    for (int k = 0; k < per; k += 2) {
+      const float2 f = *reinterpret_cast<const float2*>(&buf[i][first + k]);
+      s += f.x + f.y;
+    }
+    v[i] = s;
+  }
 }
 
 struct NormArgs {
@@ -110,133 +122,94 @@ struct NormArgs {
   float *mean, *rstd;              // (read by the backward pass)
   float* part;
   long rows, sx, sy, sdx;          // row strides in elements
-  int C, group, shift;             // group = 2^shift threads a row
+  int C, group, shift, run;        // group = 2^shift threads a row; rows of a run
   float eps, inv_c;
 };
 
-template <typename T, typename P, int VEC, int V, int ROWS>
-__global__ void __launch_bounds__(NORM_THREADS) norm_forward_kernel(const NormArgs a) {
-  __shared__ float sums[2 * ROWS][32][1];
-  const int group = a.group, lane = threadIdx.x & (group - 1);
-  const long row0 = ((long)blockIdx.x * (blockDim.x >> a.shift) + (threadIdx.x >> a.shift)) * ROWS;
-  const T* X = static_cast<const T*>(a.X);
-  float x[ROWS][V][VEC];
+// Two values an instruction where a piece has an even number of them.
+struct Pair {
+  float2 v;
+  template <int VEC> static __device__ __forceinline__ Pair of(const float (&x)[VEC], int i) { return {VEC > 1 ? make_float2(x[i], x[i + 1]) : make_float2(x[0], 0.f)}; }
+  template <int VEC> __device__ __forceinline__ void to(float (&x)[VEC], int i) const { x[i] = v.x; if (VEC > 1) x[i + (VEC > 1)] = v.y; }
+};
+template <int VEC> __device__ __forceinline__ Pair add(Pair a, Pair b) { return {VEC > 1 ? __fadd2_rn(a.v, b.v) : make_float2(a.v.x + b.v.x, 0.f)}; }
+template <int VEC> __device__ __forceinline__ Pair mul(Pair a, Pair b) { return {VEC > 1 ? __fmul2_rn(a.v, b.v) : make_float2(a.v.x * b.v.x, 0.f)}; }
+template <int VEC> __device__ __forceinline__ Pair fma(Pair a, Pair b, Pair c) { return {VEC > 1 ? __ffma2_rn(a.v, b.v, c.v) : make_float2(fmaf(a.v.x, b.v.x, c.v.x), 0.f)}; }
+__device__ __forceinline__ Pair both(float x) { return {make_float2(x, x)}; }
+
+// A row's values less their mean in x, and y's factor.  FULL: every thread of the row has V whole vectors.
+template <int VEC, int V, bool FULL>
+__device__ __forceinline__ void norm_row(const NormArgs& a, int lane, float (&x)[V][VEC], float& mean, float& rstd, float (*sums)[1][32]) {
+  constexpr int STEP = VEC > 1 ? 2 : 1;
+  Pair t = both(0.f);
 #pragma unroll
-  for (int r = 0; r < ROWS; ++r)
+  for (int v = 0; v < V; ++v)
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const int c = (lane + v * group) * VEC;
-      if (c < a.C && row0 + r < a.rows) load_elems<T, VEC>(X + (row0 + r) * a.sx + c, x[r][v]);
-      else
+    for (int e = 0; e < VEC; e += STEP) t = add<VEC>(t, Pair::of(x[v], e));
+  float s[1] = {t.v.x + t.v.y};
+  if (VEC == 1) s[0] = t.v.x;
+  group_sum<1>(s, a.group, sums[0]);
+  mean = s[0] * a.inv_c;
+  t = both(0.f);
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) x[r][v][e] = 0.f;
-    }
-  float mean[ROWS], rstd[ROWS];
+  for (int v = 0; v < V; ++v)
+    if (FULL || (lane + v * a.group) * VEC < a.C)
 #pragma unroll
-  for (int r = 0; r < ROWS; ++r) {
-    float s[1] = {0.f};
-#pragma unroll
-    for (int v = 0; v < V; ++v)
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) s[0] += x[r][v][e];
-    group_sum<1>(s, group, sums[2 * r]);
-    mean[r] = s[0] * a.inv_c;
-  }
-#pragma unroll
-  for (int r = 0; r < ROWS; ++r) {
-    float s[1] = {0.f};
-#pragma unroll
-    for (int v = 0; v < V; ++v)
-      if ((lane + v * group) * VEC < a.C)
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-          x[r][v][e] -= mean[r];
-          s[0] = fmaf(x[r][v][e], x[r][v][e], s[0]);
-        }
-    group_sum<1>(s, group, sums[2 * r + 1]);
-    rstd[r] = 1.f / sqrtf(fmaf(s[0], a.inv_c, a.eps));
-    if (lane == 0 && row0 + r < a.rows && a.mean) { a.mean[row0 + r] = mean[r]; a.rstd[row0 + r] = rstd[r]; }
-  }
+      for (int e = 0; e < VEC; e += STEP) {
+        const Pair d = add<VEC>(Pair::of(x[v], e), both(-mean));
+        d.to(x[v], e);
+        t = fma<VEC>(d, d, t);
+      }
+  s[0] = VEC == 1 ? t.v.x : t.v.x + t.v.y;
+  group_sum<1>(s, a.group, sums[1]);
+  rstd = rsqrtf(fmaf(s[0], a.inv_c, a.eps));
+}
+template <typename P, int VEC, int V>
+__device__ __forceinline__ void norm_params(const NormArgs& a, int lane, float (&w)[V][VEC], float (&b)[V][VEC]) {
 #pragma unroll
   for (int v = 0; v < V; ++v) {
-    const int c = (lane + v * group) * VEC;
-    if (c >= a.C) continue;
-    float w[VEC], b[VEC];
+    const int c = (lane + v * a.group) * VEC;
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) { w[e] = 1.f; b[e] = 0.f; }
-    if (a.weight) load_params<P, VEC>(static_cast<const P*>(a.weight) + c, w);
-    if (a.bias) load_params<P, VEC>(static_cast<const P*>(a.bias) + c, b);
-#pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
-      if (row0 + r >= a.rows) continue;
-      float y[VEC];
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) y[e] = fmaf(x[r][v][e] * rstd[r], w[e], b[e]);
-      store_elems<T, VEC>(static_cast<T*>(a.Y) + (row0 + r) * a.sy + c, y);
-    }
+    for (int e = 0; e < VEC; ++e) { w[v][e] = 1.f; b[v][e] = 0.f; }
+    if (a.weight && c < a.C) load_params<P, VEC>(static_cast<const P*>(a.weight) + c, w[v]);
+    if (a.bias && c < a.C) load_params<P, VEC>(static_cast<const P*>(a.bias) + c, b[v]);
   }
 }
-
-// Rows from blockIdx.x * groups on, every gridDim.x * groups-th: a thread has the same columns in all of them.
-template <typename T, typename P, int VEC, int V>
-__global__ void __launch_bounds__(NORM_THREADS) norm_backward_kernel(const NormArgs a) {
-  extern __shared__ float cols[];                          // [2][C], for the sums over the block's groups
-  __shared__ float sums[2][32][2];
-  const int group = a.group, lane = threadIdx.x & (group - 1), groups = blockDim.x >> a.shift;
-  const T *X = static_cast<const T*>(a.X), *dY = static_cast<const T*>(a.dY);
-  float dw[V][VEC], db[V][VEC], w[V][VEC];
+// The gradients of a row (x and dy of it; dy becomes dx), and its part of dw and db.
+template <int VEC, int V, bool FULL>
+__device__ __forceinline__ void norm_row_backward(const NormArgs& a, int lane, float mean, float rstd, float (&x)[V][VEC], float (&dy)[V][VEC],
+                                                  const float (&w)[V][VEC], float (&dw)[V][VEC], float (&db)[V][VEC], float (*sums)[32]) {
+  constexpr int STEP = VEC > 1 ? 2 : 1;
+  Pair t0 = both(0.f), t1 = both(0.f);
 #pragma unroll
   for (int v = 0; v < V; ++v) {
-    const int c = (lane + v * group) * VEC;
+    if (!FULL && (lane + v * a.group) * VEC >= a.C) continue;
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) { dw[v][e] = db[v][e] = 0.f; w[v][e] = 1.f; }
-    if (a.weight && c < a.C) load_params<P, VEC>(static_cast<const P*>(a.weight) + c, w[v]);
-  }
-  int turn = 0;
-  for (long base = (long)blockIdx.x * groups; base < a.rows; base += (long)gridDim.x * groups, turn ^= 1) {
-    const long row = base + (threadIdx.x >> a.shift);
-    const bool in = row < a.rows;
-    float x[V][VEC], dy[V][VEC];
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const int c = (lane + v * group) * VEC;
-      if (in && c < a.C) {
-        load_elems<T, VEC>(X + row * a.sx + c, x[v]);
-        load_elems<T, VEC>(dY + row * a.sy + c, dy[v]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) x[v][e] = dy[v][e] = 0.f;
-      }
-    }
-    const float mean = in ? __ldg(a.mean + row) : 0.f, rstd = in ? __ldg(a.rstd + row) : 0.f;
-    float s[2] = {0.f, 0.f};
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      if (!in || (lane + v * group) * VEC >= a.C) continue;
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        x[v][e] = (x[v][e] - mean) * rstd;
-        dw[v][e] = fmaf(dy[v][e], x[v][e], dw[v][e]);
-        db[v][e] += dy[v][e];
-        dy[v][e] *= w[v][e];
-        s[0] += dy[v][e];
-        s[1] = fmaf(dy[v][e], x[v][e], s[1]);
-      }
-    }
-    group_sum<2>(s, group, sums[turn]);
-    const float m0 = s[0] * a.inv_c, m1 = s[1] * a.inv_c;
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const int c = (lane + v * group) * VEC;
-      if (!in || c >= a.C) continue;
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) dy[v][e] = rstd * (dy[v][e] - m0 - x[v][e] * m1);
-      store_elems<T, VEC>(static_cast<T*>(a.dX) + row * a.sdx + c, dy[v]);
+    for (int e = 0; e < VEC; e += STEP) {
+      // (a row that is not there is zeros, with a mean and rstd of zero)
+      const Pair h = mul<VEC>(add<VEC>(Pair::of(x[v], e), both(-mean)), both(rstd)), d = Pair::of(dy[v], e);
+      fma<VEC>(d, h, Pair::of(dw[v], e)).to(dw[v], e);
+      add<VEC>(d, Pair::of(db[v], e)).to(db[v], e);
+      const Pair g = mul<VEC>(d, Pair::of(w[v], e));
+      t0 = add<VEC>(t0, g);
+      t1 = fma<VEC>(g, h, t1);
+      h.to(x[v], e);
+      g.to(dy[v], e);
     }
   }
-  if (!a.part) return;
-  // The groups of a warp add up by shuffles, the warps (or the groups of several warps) one behind the other.
-  const int width = min(group, 32), team = threadIdx.x / max(group, 32), teams = blockDim.x / max(group, 32);
+  float s[2] = {VEC == 1 ? t0.v.x : t0.v.x + t0.v.y, VEC == 1 ? t1.v.x : t1.v.x + t1.v.y};
+  group_sum<2>(s, a.group, sums);
+  const Pair m0 = both(-s[0] * a.inv_c), m1 = both(-s[1] * a.inv_c), r = both(rstd);
+#pragma unroll
+  for (int v = 0; v < V; ++v)
+#pragma unroll
+    for (int e = 0; e < VEC; e += STEP) mul<VEC>(r, fma<VEC>(Pair::of(x[v], e), m1, add<VEC>(Pair::of(dy[v], e), m0))).to(dy[v], e);
+}
+// The block's sums of dw and db, over its groups: those of a warp by shuffles, the warps' (or the groups' of several warps) side by side in shared memory, then
+// column by column in order.  cols: 2 C floats for each team of a warp, or of a group of several.
+template <int VEC, int V>
+__device__ __forceinline__ void norm_block_sums(const NormArgs& a, int lane, float (&dw)[V][VEC], float (&db)[V][VEC], float* cols) {
+  const int width = min(a.group, 32), team = threadIdx.x / max(a.group, 32), teams = blockDim.x / max(a.group, 32);
   for (int o = width; o < 32; o <<= 1)
 #pragma unroll
     for (int v = 0; v < V; ++v)
@@ -245,29 +218,283 @@ __global__ void __launch_bounds__(NORM_THREADS) norm_backward_kernel(const NormA
         dw[v][e] += __shfl_xor_sync(0xffffffffu, dw[v][e], o);
         db[v][e] += __shfl_xor_sync(0xffffffffu, db[v][e], o);
       }
-  const bool first = (threadIdx.x & 31) < width;
-  for (int t = 0; t < teams; ++t) {
-    if (t == team && first)
+  __syncthreads();                                         // (the memory held rows before)
+  if ((threadIdx.x & 31) < width)
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const int c = (lane + v * a.group) * VEC;
+      if (c >= a.C) continue;
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        cols[(size_t)team * 2 * a.C + c + e] = dw[v][e];
+        cols[(size_t)team * 2 * a.C + a.C + c + e] = db[v][e];
+      }
+    }
+  __syncthreads();
+  for (int c = threadIdx.x; c < 2 * a.C; c += blockDim.x) {
+    float s = cols[c];
+    for (int t = 1; t < teams; ++t) s += cols[(size_t)t * 2 * a.C + c];
+    a.part[(size_t)blockIdx.x * 2 * a.C + c] = s;
+  }
+}
+
+// Rows whose pieces are aligned (VEC > 1), fetched STAGES - 1 rows ahead, or read as they come (VEC = 1).  A group's rows: from its number on, every gridDim.x * groups-th.
+template <typename T, typename P, int VEC, int V, int STAGES, bool FULL>
+__global__ void __launch_bounds__(NORM_THREADS) norm_forward_kernel(const NormArgs a) {
+  extern __shared__ uint4 ring[];
+  __shared__ __align__(16) float sums[2][1][32];
+  const int lane = threadIdx.x & (a.group - 1), groups = blockDim.x >> a.shift, apart = a.group * VEC;      // apart: of a thread's vectors
+  const int step = (int)gridDim.x * groups;
+  const uint32_t mine = (uint32_t)__cvta_generic_to_shared(ring + threadIdx.x), slot = blockDim.x * 16;
+  const uint4* own = ring + threadIdx.x;
+  const long row = (long)blockIdx.x * groups + (threadIdx.x >> a.shift);
+  int left = (int)(a.rows - row), ahead = left;              // rows from this one (the next one fetched) on
+  const T *from = static_cast<const T*>(a.X) + row * a.sx + lane * VEC, *at = from;
+  T* to = static_cast<T*>(a.Y) + row * a.sy + lane * VEC;
+  float *mean_at = a.mean ? a.mean + row : nullptr, *rstd_at = a.rstd + row;
+  const long from_step = step * a.sx, to_step = step * a.sy;
+  const auto fetch = [&](int stage) {
+    if (VEC > 1) {
+      if (ahead > 0)
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+          if (FULL || lane * VEC + v * apart < a.C) copy16_async(mine + (uint32_t)(stage * V + v) * slot, from + v * apart);
+      copies_commit();
+      from += from_step;
+      ahead -= step;
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < STAGES - 1; ++i) fetch(i);
+  float w[V][VEC], b[V][VEC];
+  norm_params<P, VEC, V>(a, lane, w, b);
+  // A row each; ALL: every thread of the warp has one (groups of a warp or more are there or not as a whole).
+  const auto work = [&](auto all, int stage) {
+    constexpr bool ALL = decltype(all)::value;
+    float x[V][VEC];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      if ((ALL || left > 0) && (FULL || lane * VEC + v * apart < a.C)) {
+        if (VEC > 1) load_elems<T, VEC>(reinterpret_cast<const T*>(own + (size_t)(stage * V + v) * blockDim.x), x[v]);
+        else load_elems<T, VEC>(at + v * apart, x[v]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) x[v][e] = 0.f;
+      }
+    }
+    fetch((stage + STAGES - 1) % STAGES);
+    float mean, rstd;
+    norm_row<VEC, V, FULL>(a, lane, x, mean, rstd, sums);
+    if (ALL || left > 0) {
+      if (lane == 0 && mean_at) { *mean_at = mean; *rstd_at = rstd; }
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        const int c = (lane + v * group) * VEC;
-        if (c >= a.C) continue;
+        if (!FULL && lane * VEC + v * apart >= a.C) continue;
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-          cols[c + e] = dw[v][e] + (t ? cols[c + e] : 0.f);
-          cols[a.C + c + e] = db[v][e] + (t ? cols[a.C + c + e] : 0.f);
+        for (int e = 0; e < VEC; e += VEC > 1 ? 2 : 1) fma<VEC>(mul<VEC>(Pair::of(x[v], e), both(rstd)), Pair::of(w[v], e), Pair::of(b[v], e)).to(x[v], e);
+        store_elems<T, VEC>(to + v * apart, x[v]);
+      }
+    }
+  };
+  while (__any_sync(0xffffffffu, left > 0)) {
+#pragma unroll
+    for (int stage = 0; stage < STAGES; ++stage) {
+      if (VEC > 1) copies_wait<(STAGES > 1 ? STAGES - 2 : 0)>();
+      if (__all_sync(0xffffffffu, left > 0)) work(std::true_type(), stage);
+      else if (__any_sync(0xffffffffu, left > 0)) work(std::false_type(), stage);
+      else break;
+      left -= step; to += to_step; rstd_at += step;
+      if (mean_at) mean_at += step;
+      if (VEC == 1) at += from_step;
+    }
+  }
+}
+
+template <typename T, typename P, int VEC, int V, int STAGES, bool FULL>
+__global__ void __launch_bounds__(NORM_THREADS) norm_backward_kernel(const NormArgs a) {
+  extern __shared__ uint4 ring[];
+  __shared__ __align__(16) float sums[2][2][32];
+  const int lane = threadIdx.x & (a.group - 1), groups = blockDim.x >> a.shift, apart = a.group * VEC;
+  const int step = (int)gridDim.x * groups;
+  const uint32_t mine = (uint32_t)__cvta_generic_to_shared(ring + threadIdx.x), slot = blockDim.x * 16;
+  const uint4* own = ring + threadIdx.x;
+  const long row = (long)blockIdx.x * groups + (threadIdx.x >> a.shift);
+  int left = (int)(a.rows - row), ahead = left;
+  const T *from = static_cast<const T*>(a.X) + row * a.sx + lane * VEC, *at = from, *from_dy = static_cast<const T*>(a.dY) + row * a.sy + lane * VEC, *at_dy = from_dy;
+  T* to = static_cast<T*>(a.dX) + row * a.sdx + lane * VEC;
+  const float *mean_at = a.mean + row, *rstd_at = a.rstd + row;
+  const long x_step = step * a.sx, dy_step = step * a.sy, to_step = step * a.sdx;
+  const auto fetch = [&](int stage) {
+    if (VEC > 1) {
+      if (ahead > 0)
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+          if (FULL || lane * VEC + v * apart < a.C) {
+            copy16_async(mine + (uint32_t)(stage * 2 * V + 2 * v) * slot, from + v * apart);
+            copy16_async(mine + (uint32_t)(stage * 2 * V + 2 * v + 1) * slot, from_dy + v * apart);
+          }
+      copies_commit();
+      from += x_step; from_dy += dy_step;
+      ahead -= step;
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < STAGES - 1; ++i) fetch(i);
+  float dw[V][VEC], db[V][VEC], w[V][VEC];
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    const int c = lane * VEC + v * apart;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) { dw[v][e] = db[v][e] = 0.f; w[v][e] = 1.f; }
+    if (a.weight && c < a.C) load_params<P, VEC>(static_cast<const P*>(a.weight) + c, w[v]);
+  }
+  float next_mean = left > 0 ? __ldg(mean_at) : 0.f, next_rstd = left > 0 ? __ldg(rstd_at) : 0.f;
+  int turn = 0;
+  const auto work = [&](auto all, int stage, float mean, float rstd) {
+    constexpr bool ALL = decltype(all)::value;
+    float x[V][VEC], dy[V][VEC];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      if ((ALL || left > 0) && (FULL || lane * VEC + v * apart < a.C)) {
+        if (VEC > 1) {
+          load_elems<T, VEC>(reinterpret_cast<const T*>(own + (size_t)(stage * 2 * V + 2 * v) * blockDim.x), x[v]);
+          load_elems<T, VEC>(reinterpret_cast<const T*>(own + (size_t)(stage * 2 * V + 2 * v + 1) * blockDim.x), dy[v]);
+        } else {
+          load_elems<T, VEC>(at + v * apart, x[v]);
+          load_elems<T, VEC>(at_dy + v * apart, dy[v]);
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) x[v][e] = dy[v][e] = 0.f;
+      }
+    }
+    fetch((stage + STAGES - 1) % STAGES);
+    norm_row_backward<VEC, V, FULL>(a, lane, mean, rstd, x, dy, w, dw, db, sums[turn]);
+    if (ALL || left > 0)
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+        if (FULL || lane * VEC + v * apart < a.C) store_elems<T, VEC>(to + v * apart, dy[v]);
+  };
+  while (__any_sync(0xffffffffu, left > 0)) {
+#pragma unroll
+    for (int stage = 0; stage < STAGES; ++stage) {
+      const float mean = next_mean, rstd = next_rstd;
+      next_mean = next_rstd = 0.f;
+      mean_at += step; rstd_at += step;
+      if (left > step) { next_mean = __ldg(mean_at); next_rstd = __ldg(rstd_at); }
+      if (VEC > 1) copies_wait<(STAGES > 1 ? STAGES - 2 : 0)>();
+      if (__all_sync(0xffffffffu, left > 0)) work(std::true_type(), stage, mean, rstd);
+      else if (__any_sync(0xffffffffu, left > 0)) work(std::false_type(), stage, mean, rstd);
+      else break;
+      turn ^= 1;
+      left -= step; to += to_step;
+      if (VEC == 1) { at += x_step; at_dy += dy_step; }
+    }
+  }
+  pdl_trigger();
+  copies_wait<0>();
+  if (a.part) norm_block_sums<VEC, V>(a, lane, dw, db, reinterpret_cast<float*>(ring));
+}
+
+// ---- dense rows that are not aligned: runs of `a.run` rows, whose bytes are a multiple of 16, through shared memory
+
+// The run from `first` on into (or from) shared memory, `count` values; what is left behind the last whole 16 bytes (the last run) one by one.
+template <typename T>
+__device__ __forceinline__ void run_fetch(uint32_t dst, T* at, const T* from, long count) {
+  constexpr int VEC = VEC_OF<T>;
+  const long whole = count / VEC;
+  for (long i = threadIdx.x; i < whole; i += blockDim.x) copy16_async(dst + (uint32_t)i * 16, from + i * VEC);
+  for (long i = whole * VEC + threadIdx.x; i < count; i += blockDim.x) at[i] = from[i];
+}
+template <typename T>
+__device__ __forceinline__ void run_store(T* to, const T* at, long count) {
+  constexpr int VEC = VEC_OF<T>;
+  const long whole = count / VEC;
+  for (long i = threadIdx.x; i < whole; i += blockDim.x) reinterpret_cast<uint4*>(to)[i] = reinterpret_cast<const uint4*>(at)[i];
+  for (long i = whole * VEC + threadIdx.x; i < count; i += blockDim.x) to[i] = at[i];
+}
+
+constexpr int RUN_STAGES = 4;
+
+template <typename T, typename P, int V, bool BACKWARD>
+__global__ void __launch_bounds__(NORM_THREADS, BACKWARD ? 1 : 2) norm_runs_kernel(const NormArgs a) {
+  extern __shared__ uint4 ring[];
+  __shared__ __align__(16) float sums[2][2][32], sum1[2][1][32];
+  const int lane = threadIdx.x & (a.group - 1), groups = blockDim.x >> a.shift, own = threadIdx.x >> a.shift;
+  const long runs = (a.rows + a.run - 1) / a.run;
+  const size_t run_values = (size_t)a.run * a.C, run_pieces = run_values / VEC_OF<T>;
+  const T *X = static_cast<const T*>(a.X), *dY = static_cast<const T*>(a.dY);
+  T* out = static_cast<T*>(BACKWARD ? a.dX : a.Y);
+  constexpr int TENSORS = BACKWARD ? 2 : 1;
+  long ahead = blockIdx.x;
+  const auto fetch = [&](int stage) {
+    if (ahead < runs) {
+      const long first = ahead * a.run, count = min((long)a.run, a.rows - first) * a.C;
+      uint4* at = ring + (size_t)stage * TENSORS * run_pieces;
+      run_fetch<T>((uint32_t)__cvta_generic_to_shared(at), reinterpret_cast<T*>(at), X + first * a.C, count);
+      if (BACKWARD) run_fetch<T>((uint32_t)__cvta_generic_to_shared(at + run_pieces), reinterpret_cast<T*>(at + run_pieces), dY + first * a.C, count);
+    }
+    copies_commit();
+    ahead += gridDim.x;
+  };
+#pragma unroll
+  for (int i = 0; i < RUN_STAGES - 1; ++i) fetch(i);
+  float w[V][1], b[V][1], dw[V][1], db[V][1];
+  norm_params<P, 1, V>(a, lane, w, b);
+#pragma unroll
+  for (int v = 0; v < V; ++v) dw[v][0] = db[v][0] = 0.f;
+  int stage = 0, turn = 0;
+  for (long i = blockIdx.x; i < runs; i += gridDim.x) {
+    copies_wait<RUN_STAGES - 2>();
+    __syncthreads();
+    T *xs = reinterpret_cast<T*>(ring + (size_t)stage * TENSORS * run_pieces), *ds = reinterpret_cast<T*>(ring + ((size_t)stage * TENSORS + 1) * run_pieces);
+    const long first = i * a.run, here = min((long)a.run, a.rows - first);
+    for (int r0 = 0; r0 < a.run; r0 += groups, turn ^= 1) {
+      const int r = r0 + own;
+      const bool in = r < here;
+      float x[V][1], dy[V][1];
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const int c = lane + v * a.group;
+        x[v][0] = in && c < a.C ? to_f(xs[(size_t)r * a.C + c]) : 0.f;
+        if (BACKWARD) dy[v][0] = in && c < a.C ? to_f(ds[(size_t)r * a.C + c]) : 0.f;
+      }
+      if constexpr (BACKWARD) {
+        const float mean = in ? __ldg(a.mean + first + r) : 0.f, rstd = in ? __ldg(a.rstd + first + r) : 0.f;
+        norm_row_backward<1, V, false>(a, lane, mean, rstd, x, dy, w, dw, db, sums[turn]);
+        if (in)
+#pragma unroll
+          for (int v = 0; v < V; ++v)
+            if (lane + v * a.group < a.C) xs[(size_t)r * a.C + lane + v * a.group] = from_f<T>(dy[v][0]);
+      } else {
+        float mean, rstd;
+        norm_row<1, V, false>(a, lane, x, mean, rstd, sum1);
+        if (in) {
+          if (lane == 0 && a.mean) { a.mean[first + r] = mean; a.rstd[first + r] = rstd; }
+#pragma unroll
+          for (int v = 0; v < V; ++v)
+            if (lane + v * a.group < a.C) xs[(size_t)r * a.C + lane + v * a.group] = from_f<T>(fmaf(x[v][0] * rstd, w[v][0], b[v][0]));
         }
       }
+    }
     __syncthreads();
+    run_store<T>(out + first * a.C, xs, here * a.C);
+    // (the stage before this one was written out before the barrier above: its memory takes the next run)
+    fetch(stage == 0 ? RUN_STAGES - 1 : stage - 1);
+    stage = stage == RUN_STAGES - 1 ? 0 : stage + 1;
   }
-  for (int c = threadIdx.x; c < 2 * a.C; c += blockDim.x) a.part[(size_t)blockIdx.x * 2 * a.C + c] = cols[c];
+  if constexpr (BACKWARD) {
+    pdl_trigger();
+    copies_wait<0>();
+    if (a.part) norm_block_sums<1, V>(a, lane, dw, db, reinterpret_cast<float*>(ring));
+  }
 }
 
 // ---- rows of any length, read from memory (or L2) for every sum; a block takes a row
 
 template <typename T, typename P>
 __global__ void __launch_bounds__(1024) norm_forward_wide_kernel(const NormArgs a) {
-  __shared__ float sums[2][32][1];
+  __shared__ __align__(16) float sums[2][1][32];
   for (long row = blockIdx.x; row < a.rows; row += gridDim.x) {
     const T* x = static_cast<const T*>(a.X) + row * a.sx;
     float s[1] = {0.f};
@@ -287,7 +514,7 @@ __global__ void __launch_bounds__(1024) norm_forward_wide_kernel(const NormArgs 
 }
 template <typename T, typename P>
 __global__ void __launch_bounds__(1024) norm_backward_wide_kernel(const NormArgs a) {
-  __shared__ float sums[2][32][2];
+  __shared__ __align__(16) float sums[2][2][32];
   int turn = 0;
   for (long row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
     const T *x = static_cast<const T*>(a.X) + row * a.sx, *dy = static_cast<const T*>(a.dY) + row * a.sy;
@@ -346,18 +573,17 @@ __global__ void __launch_bounds__(1024) norm_sums_kernel(const float* part, long
 inline int pow2_at_least(long n) { int p = 1; while (p < n) p *= 2; return p; }
 inline bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 
-// Vectors a thread for which there is a kernel: at least `v`, or 0.
-int vectors(long v, bool forward, bool vec, int es) {
-  if (v <= 4) return v <= 2 || forward || es == 4 || !vec ? (int)v : 0;      // (backward, 16-bit: five times 16 floats a thread fit, not 32)
-  if (vec) return forward && v <= 8 ? 8 : 0;
+// Vectors a thread for which there is a kernel: at least `v`, or 0.  (Sixteen values: five times as many floats fit a thread's registers.)
+int vectors(long v, bool vec, int es) {
+  if (vec) return v <= (es == 4 ? 4 : 2) ? (int)v : 0;
   return v <= 8 ? (int)v : v <= 12 ? 12 : v <= 16 ? 16 : 0;
 }
 // Threads a row and vectors a thread: as few idle ones as possible, then rather many vectors a thread, but eight threads that read one line where the row has
 // them.
-void pick_group(long nv, bool forward, int es, NormPlan* p) {
+void pick_group(long nv, int es, NormPlan* p) {
   long best = -1;
   for (int g = 1; g <= NORM_THREADS; g *= 2) {
-    const int v = vectors((nv + g - 1) / g, forward, p->vec, es);
+    const int v = vectors((nv + g - 1) / g, p->vec, es);
     if (v == 0) continue;
     const long slots = (long)v * g;
     if (best < 0 || (g <= 8 ? slots <= best : slots < best)) { best = slots; p->group = g; p->V = v; }
@@ -374,33 +600,45 @@ bool vec_fits(const xconv_norm_desc* d, F&& strides_and_pointers) {
 
 NormArgs args_of(const xconv_norm_desc* d, const NormPlan& p) {
   NormArgs a = {};
-  a.rows = d->rows; a.C = d->C; a.sx = d->x_stride; a.sy = d->y_stride; a.sdx = d->dx_stride; a.eps = d->eps; a.inv_c = 1.f / (float)d->C; a.group = p.group;
+  a.rows = d->rows; a.C = d->C; a.sx = d->x_stride; a.sy = d->y_stride; a.sdx = d->dx_stride; a.eps = d->eps; a.inv_c = 1.f / (float)d->C; a.group = p.group; a.run = p.run;
   while ((1 << a.shift) < p.group) ++a.shift;
   return a;
 }
 
+template <typename K>
+cudaError_t norm_launch(K kernel, const NormPlan& p, const NormArgs& a, cudaStream_t st) {
+  if (p.smem > 40 * 1024) {
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, p.smem);
+    if (e != cudaSuccess) return e;
+  }
+  kernel<<<dim3((unsigned)p.blocks), dim3(p.threads), p.smem, st>>>(a);
+  return cudaGetLastError();
+}
+// Vectors a thread fetches ahead: as many as the plan's shared memory is made for (plan_ring).
+constexpr int norm_stages(int V, int VEC, bool backward) { return VEC == 1 ? 1 : backward ? (V == 1 ? 6 : V == 2 ? 4 : 3) : V == 1 ? 8 : V == 2 ? 6 : 4; }
+
 template <typename T, typename P, int VEC>
 cudaError_t forward_of(const NormPlan& p, const NormArgs& a, cudaStream_t st) {
-  const dim3 grid((unsigned)p.blocks), block(p.threads);
-#define XC_NORM(N, R) if (p.V == N && p.rows_per == R) { norm_forward_kernel<T, P, VEC, N, R><<<grid, block, 0, st>>>(a); return cudaGetLastError(); }
-  XC_NORM(1, 1) XC_NORM(1, 4) XC_NORM(2, 1) XC_NORM(2, 2) XC_NORM(3, 1) XC_NORM(4, 1) XC_NORM(8, 1)
-  if constexpr (VEC == 1) { XC_NORM(5, 1) XC_NORM(6, 1) XC_NORM(7, 1) XC_NORM(12, 1) XC_NORM(16, 1) }
+  if constexpr (VEC == 1) {
+#define XC_NORM(N) if (p.V == N && p.run) return norm_launch(norm_runs_kernel<T, P, N, false>, p, a, st);
+    XC_NORM(1) XC_NORM(2) XC_NORM(3) XC_NORM(4) XC_NORM(5) XC_NORM(6) XC_NORM(7) XC_NORM(8) XC_NORM(12) XC_NORM(16)
+#undef XC_NORM
+  }
+#define XC_NORM(N) if (p.V == N) return p.full ? norm_launch(norm_forward_kernel<T, P, VEC, N, norm_stages(N, VEC, false), (VEC > 1)>, p, a, st) : norm_launch(norm_forward_kernel<T, P, VEC, N, norm_stages(N, VEC, false), false>, p, a, st);
+  XC_NORM(1) XC_NORM(2)
+  if constexpr (VEC <= 4) { XC_NORM(3) XC_NORM(4) }
+  if constexpr (VEC == 1) { XC_NORM(5) XC_NORM(6) XC_NORM(7) XC_NORM(8) XC_NORM(12) XC_NORM(16) }
 #undef XC_NORM
   return cudaErrorInvalidValue;
 }
 template <typename T, typename P, int VEC>
 cudaError_t backward_of(const NormPlan& p, const NormArgs& a, cudaStream_t st) {
-  const dim3 grid((unsigned)p.blocks), block(p.threads);
-  const size_t smem = a.part ? 2 * sizeof(float) * (size_t)a.C : 0;
-#define XC_NORM(N) \
-  if (p.V == N) { \
-    if (smem > 40 * 1024) { \
-      const cudaError_t e = cudaFuncSetAttribute(norm_backward_kernel<T, P, VEC, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem); \
-      if (e != cudaSuccess) return e; \
-    } \
-    norm_backward_kernel<T, P, VEC, N><<<grid, block, smem, st>>>(a); \
-    return cudaGetLastError(); \
+  if constexpr (VEC == 1) {
+#define XC_NORM(N) if (p.V == N && p.run) return norm_launch(norm_runs_kernel<T, P, N, true>, p, a, st);
+    XC_NORM(1) XC_NORM(2) XC_NORM(3) XC_NORM(4) XC_NORM(5) XC_NORM(6) XC_NORM(7) XC_NORM(8) XC_NORM(12) XC_NORM(16)
+#undef XC_NORM
   }
+#define XC_NORM(N) if (p.V == N) return p.full ? norm_launch(norm_backward_kernel<T, P, VEC, N, norm_stages(N, VEC, true), (VEC > 1)>, p, a, st) : norm_launch(norm_backward_kernel<T, P, VEC, N, norm_stages(N, VEC, true), false>, p, a, st);
   XC_NORM(1) XC_NORM(2)
   if constexpr (VEC <= 4) { XC_NORM(3) XC_NORM(4) }
   if constexpr (VEC == 1) { XC_NORM(5) XC_NORM(6) XC_NORM(7) XC_NORM(8) XC_NORM(12) XC_NORM(16) }
@@ -420,50 +658,62 @@ constexpr long WIDE_ROWS = 64;                               // rows that a bloc
 
 }  // namespace
 
-NormPlan plan_norm_forward(const xconv_norm_desc* d, const void* X, const void* weight, const void* bias, const void* Y) {
-  NormPlan p = {};
-  p.vec = vec_fits(d, [&](int vec) {
-    return d->x_stride % vec == 0 && d->y_stride % vec == 0 && aligned(X, 16) && aligned(Y, 16) && aligned(weight, 16) && aligned(bias, 16); });
-  const long nv = p.vec ? d->C / (d->dtype == XCONV_F32 ? 4 : 8) : d->C;
-  const int es = d->dtype == XCONV_F32 ? 4 : 2;
-  pick_group(nv, true, es, &p);
-  if (!p.wide && d->rows * p.group < NORM_SMS * 256L) {      // few rows: a thread has little to do, and more of them do it
-    p.group = std::min(NORM_THREADS, pow2_at_least(nv));
-    p.V = vectors((nv + p.group - 1) / p.group, true, p.vec, es);
-  }
-  p.threads = p.wide ? 1024 : std::max(p.group, 256);
-  p.rows_per = 1;
-  const long groups = p.threads / p.group;
-  if (!p.wide && d->rows >= NORM_SMS * 8 * groups) p.rows_per = p.V == 1 ? 4 : p.V == 2 ? 2 : 1;
-  p.blocks = p.wide ? std::min<long>(d->rows, 8 * NORM_SMS) : (d->rows + groups * p.rows_per - 1) / (groups * p.rows_per);
-  return p;
-}
-
-// Blocks of the backward pass (each leaves a partial sum): as many as the SMs hold at once.
-static NormPlan plan_backward(const xconv_norm_desc* d, bool vec) {
+// What the threads and blocks are: `vec` by pieces of 16 bytes; `dense` rows without gaps from a 16-byte boundary on, which go by runs where they are not `vec`.
+static NormPlan plan(const xconv_norm_desc* d, bool vec, bool dense, bool backward) {
   NormPlan p = {};
   p.vec = vec;
-  const long nv = vec ? d->C / (d->dtype == XCONV_F32 ? 4 : 8) : d->C;
-  pick_group(nv, false, d->dtype == XCONV_F32 ? 4 : 2, &p);
-  p.threads = p.wide ? 1024 : NORM_THREADS;
-  const long groups = p.threads / p.group;
-  p.blocks = std::min<long>((d->rows + groups - 1) / groups, NORM_SMS * (1024 / p.threads));
+  const int es = d->dtype == XCONV_F32 ? 4 : 2, tensors = backward ? 2 : 1;
+  const long nv = vec ? d->C / (16 / es) : d->C;
+  pick_group(nv, es, &p);
   if (p.wide) {
-    const long chunks = std::min<long>((d->rows + WIDE_ROWS - 1) / WIDE_ROWS, 512);
-    p.parts = chunks;
-    p.blocks = std::min<long>(d->rows, 2 * NORM_SMS);
-  } else {
-    p.parts = p.blocks;
+    p.threads = 1024;
+    p.parts = std::min<long>((d->rows + WIDE_ROWS - 1) / WIDE_ROWS, 512);
+    p.blocks = std::min<long>(d->rows, (backward ? 2 : 8) * NORM_SMS);
+    return p;
   }
+  if (!backward && d->rows * p.group < NORM_SMS * 256L) {    // few rows: a thread has little to do, and more of them do it
+    p.group = std::min(NORM_THREADS, pow2_at_least(nv));
+    p.V = vectors((nv + p.group - 1) / p.group, vec, es);
+  }
+  p.full = vec && (long)p.V * p.group == nv;
+  // A block's threads: fewer where its rows would not reach all SMs.
+  p.threads = NORM_THREADS;
+  while (p.threads > std::max(p.group, 128) && d->rows * p.group < (long)NORM_SMS * p.threads) p.threads /= 2;
+  const long groups = p.threads / p.group;
+  const int resident = vec || backward ? 1 : 2;              // of 512 threads: 128 or 64 registers each
+  p.blocks = std::min<long>((d->rows + groups - 1) / groups, (long)NORM_SMS * resident * (NORM_THREADS / p.threads));
+  const size_t stages = norm_stages(p.V, vec ? 2 : 1, backward);
+  if (!vec && dense) p.threads = std::max(p.group, std::min(p.threads, 256));
+  if (vec) p.smem = (int)(stages * p.V * tensors * p.threads * 16);
+  else if (dense) {
+    const long groups = p.threads / p.group, run = std::max<long>(groups, 8);              // (8 rows of any type are a multiple of 16 bytes)
+    const size_t bytes = RUN_STAGES * (size_t)tensors * run * d->C * es;
+    if (bytes <= 200u * 1024) {
+      p.run = (int)run;
+      p.smem = (int)bytes;
+      p.blocks = std::min<long>((d->rows + run - 1) / run, (long)NORM_SMS * std::max<long>(1, std::min<long>(resident * (NORM_THREADS / p.threads), 220 * 1024 / ((long)bytes + 2048))));
+    }
+  }
+  if (backward) p.smem = std::max(p.smem, (int)(p.threads / std::max(p.group, 32) * 2 * sizeof(float)) * d->C);
+  p.parts = p.blocks;
   return p;
 }
-NormPlan plan_norm_backward(const xconv_norm_desc* d, const void* dY, const void* X, const void* weight, const void* dX) {
-  return plan_backward(d, vec_fits(d, [&](int vec) {
-    return d->x_stride % vec == 0 && d->y_stride % vec == 0 && d->dx_stride % vec == 0 && aligned(X, 16) && aligned(dY, 16) && aligned(dX, 16) && aligned(weight, 16); }));
+static bool is_dense(const xconv_norm_desc* d, int64_t s0, int64_t s1, int64_t s2) { return s0 == d->C && s1 == d->C && s2 == d->C; }
+
+NormPlan plan_norm_forward(const xconv_norm_desc* d, const void* X, const void* weight, const void* bias, const void* Y) {
+  const bool at16 = aligned(X, 16) && aligned(Y, 16);
+  const bool vec = at16 && vec_fits(d, [&](int n) { return d->x_stride % n == 0 && d->y_stride % n == 0 && aligned(weight, 16) && aligned(bias, 16); });
+  return plan(d, vec, at16 && is_dense(d, d->x_stride, d->y_stride, d->C), false);
 }
-long norm_backward_parts(const xconv_norm_desc* d) {
-  const long a = plan_backward(d, false).parts;
-  return vec_fits(d, [](int) { return true; }) ? std::max(a, plan_backward(d, true).parts) : a;
+
+NormPlan plan_norm_backward(const xconv_norm_desc* d, const void* dY, const void* X, const void* weight, const void* dX) {
+  const bool at16 = aligned(X, 16) && aligned(dY, 16) && aligned(dX, 16);
+  const bool vec = at16 && vec_fits(d, [&](int n) { return d->x_stride % n == 0 && d->y_stride % n == 0 && d->dx_stride % n == 0 && aligned(weight, 16); });
+  return plan(d, vec, at16 && is_dense(d, d->x_stride, d->y_stride, d->dx_stride), true);
+}
+long norm_backward_parts(const xconv_norm_desc* d) {         // (of any pointers and strides)
+  long most = std::max(plan(d, false, false, true).parts, plan(d, false, true, true).parts);
+  return vec_fits(d, [](int) { return true; }) ? std::max(most, plan(d, true, false, true).parts) : most;
 }
 
 cudaError_t launch_norm_forward(const xconv_norm_desc* d, const NormPlan& p, const void* X, const void* weight, const void* bias, void* Y, float* mean, float* rstd,
@@ -473,7 +723,7 @@ cudaError_t launch_norm_forward(const xconv_norm_desc* d, const NormPlan& p, con
   return with_types(d, [&](auto t, auto w) {
     using T = decltype(t); using P = decltype(w);
     if (p.wide) { norm_forward_wide_kernel<T, P><<<(unsigned)p.blocks, 1024, 0, st>>>(a); return cudaGetLastError(); }
-    return p.vec ? forward_of<T, P, vec_of<T>()>(p, a, st) : forward_of<T, P, 1>(p, a, st);
+    return p.vec ? forward_of<T, P, VEC_OF<T>>(p, a, st) : forward_of<T, P, 1>(p, a, st);
   });
 }
 cudaError_t launch_norm_backward(const xconv_norm_desc* d, const NormPlan& p, const void* dY, const void* X, const float* mean, const float* rstd, const void* weight,
@@ -490,7 +740,7 @@ cudaError_t launch_norm_backward(const xconv_norm_desc* d, const NormPlan& p, co
       norm_columns_wide_kernel<T><<<dim3((unsigned)((d->C + 255) / 256), (unsigned)p.parts), 256, 0, st>>>(a, rows_per);
       return cudaGetLastError();
     }
-    return p.vec ? backward_of<T, P, vec_of<T>()>(p, a, st) : backward_of<T, P, 1>(p, a, st);
+    return p.vec ? backward_of<T, P, VEC_OF<T>>(p, a, st) : backward_of<T, P, 1>(p, a, st);
   });
 }
 cudaError_t launch_norm_sums(const xconv_norm_desc* d, const float* part, long parts, float* dweight, float* dbias, cudaStream_t st) {

@@ -9,9 +9,11 @@ namespace xconv {
 
 struct NormPlan {
   bool vec;              // 16-byte accesses
+  bool full;             // every thread of a row has all its vectors
   bool wide;             // a row does not fit the registers of a block
   int V, group, threads; // vectors (or elements) a thread, threads a row, threads a block
-  int rows_per;          // rows a thread holds at once (forward)
+  int run;               // rows of a run (dense rows that are not aligned), or 0
+  int smem;
   long blocks;
   long parts;            // partial sums of dweight and dbias (backward)
 };
