@@ -155,7 +155,8 @@ def lib() -> ctypes.CDLL:
 # takes everything, and raises every error.
 _native = None
 _NATIVE_CALLS = ("xconv_workspace_bytes", "xconv_forward", "xconv_sketch", "xconv_wgrad", "xconv_dgrad", "xconv_sketch_seeded", "xconv_wgrad_seeded",
-                 "xconv_backprobe", "xconv_contract")
+                 "xconv_backprobe", "xconv_contract", "xconv_layernorm_workspace_bytes", "xconv_layernorm_forward", "xconv_layernorm_backward",
+                 "xconv_update_workspace_bytes", "xconv_orthogonalize", "xconv_muon_step")
 
 
 class _Declines:
@@ -701,6 +702,9 @@ def xconv_layernorm(X: torch.Tensor, weight: torch.Tensor | None = None, bias: t
     """Layer norm over the channels: (Y, mean, rstd).  X: (B, C, H, W) or (B, C, D, H, W) channels-last, normalised pixel by pixel over C, or (..., C) with up to three
     dimensions, normalised over the last.  Views of some of the channels of such a tensor are taken as they are.  weight, bias: C values in X's dtype or
     float32 (1 and 0 where None).  Y is dense in X's dtype and format; mean and rstd are float32, (B, [D,] H, W) or (...)."""
+    out = (_native or _load_native()).layernorm(X, weight, bias, eps)
+    if out is not None:
+        return out
     if _elsewhere(X):
         with _on_device(X):
             return xconv_layernorm(X, weight, bias, eps)
@@ -726,6 +730,9 @@ def _dense_like(t: torch.Tensor) -> torch.Tensor:
 def xconv_layernorm_backward(dY: torch.Tensor, X: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor, weight: torch.Tensor | None = None):
     """Gradients of xconv_layernorm: (dX, dweight, dbias), dX dense in X's dtype and format, dweight and dbias float32 (the same bits every time).  mean and rstd
     are the forward call's, weight what it got.  dweight and dbias are what a weight and a bias would get where the layer has none."""
+    out = (_native or _load_native()).layernorm_backward(dY, X, mean, rstd, weight)
+    if out is not None:
+        return out
     if _elsewhere(X):
         with _on_device(X):
             return xconv_layernorm_backward(dY, X, mean, rstd, weight)
@@ -782,6 +789,9 @@ def xconv_orthogonalize(G, steps: int = 5, coefficients=NEWTON_SCHULZ, eps: floa
     """The gradients in G orthogonalised by Newton-Schulz products (include/xconv.h has the formulas), in G's dtype and layout.  G: a matrix, a batch of matrices
     (3-d), the channels-last weights of a convolution (4-d, 5-d: a row per output channel) -- or a list of such tensors, which are worked on together and
     come back as a list."""
+    out = (_native or _load_native()).orthogonalize(G, steps, coefficients, eps)
+    if out is not None:
+        return out
     many = isinstance(G, (list, tuple))
     tensors = list(G) if many else [G]
     if not tensors:
@@ -808,7 +818,8 @@ def xconv_muon_step(W, dW, M, lr: float, momentum: float = 0.95, nesterov: bool 
     """One step of the Muon optimiser, in place: the momenta M (float32) take in the gradients dW, the weights W (any of the library's dtypes) move against the
     orthogonalised momenta (include/xconv.h has the formulas).  W, dW, M: tensors of one shape and layout as xconv_orthogonalize takes them, or lists of them: a
     whole network's weights in one call take little longer than the largest of them.  Returns W."""
-    many = isinstance(W, (list, tuple))
+    if (_native or _load_native()).muon_step(W, dW, M, lr, momentum, nesterov, weight_decay, steps, coefficients, eps, _ADJUST.get(adjust)) is not None:
+        return W
     Ws, dWs, Ms = (list(t) if isinstance(t, (list, tuple)) else [t] for t in (W, dW, M))
     if not len(Ws) == len(dWs) == len(Ms):
         raise ValueError("W, dW and M must have the same length")

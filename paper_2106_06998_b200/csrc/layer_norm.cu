@@ -76,6 +76,10 @@ __device__ __forceinline__ void store_elems(T* p, const float (&f)[VEC]) {
 __device__ __forceinline__ void copy16_async(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
+// ... or 16 bytes of zeros.
+__device__ __forceinline__ void copy16_async_if(uint32_t dst, const void* src, bool in) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(in ? 16 : 0) : "memory");
+}
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
@@ -90,30 +94,29 @@ __device__ __forceinline__ void load_params(const P* p, float (&f)[VEC]) {
   }
 }
 
-// Sums over the `group` threads of a row, the same in each of them: within a warp by shuffles, across warps through shared memory (a buffer that
-// no one else uses before the group's next sum but one) and a barrier of the group's own: other rows of the block are elsewhere.
+// Sums over the `group` threads of a row, the same in each of them: within a warp by shuffles, across warps through shared memory (a buffer of
+// blockDim.x / 32 entries that no one else uses before the next barrier but one).  All threads of the block take part.
 template <int N>
-__device__ __forceinline__ void group_sum(float (&v)[N], int group, float (*buf)[32]) {
+__device__ __forceinline__ void group_sum(float (&v)[N], int group, float (*buf)[N]) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1)
     if (o < group)
 #pragma unroll
       for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
   if (group <= 32) return;
-  const int warp = threadIdx.x >> 5, per = group >> 5, first = warp & -per;
+  const int warp = threadIdx.x >> 5, per = group >> 5;
   if ((threadIdx.x & 31) == 0)
 #pragma unroll
-    for (int i = 0; i < N; ++i) buf[i][warp] = v[i];
-  asm volatile("bar.sync %0, %1;" ::"r"(1 + first / per), "r"(group) : "memory");      // (at most eight groups of several warps)
+    for (int i = 0; i < N; ++i) buf[warp][i] = v[i];
+  __syncthreads();
+  // (each warp adds the `per` sums by shuffles too: 32 of them at most)
+  const int lane = threadIdx.x & 31, first = warp / per * per;
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    float s = 0.f;
-    for (int k = 0; k < per; k += 2) {
-      const float2 f = *reinterpret_cast<const float2*>(&buf[i][first + k]);
-      s += f.x + f.y;
-    }
-    v[i] = s;
-  }
+  for (int i = 0; i < N; ++i) v[i] = lane < per ? buf[first + lane][i] : 0.f;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
 }
 
 struct NormArgs {
@@ -137,9 +140,12 @@ template <int VEC> __device__ __forceinline__ Pair mul(Pair a, Pair b) { return 
 template <int VEC> __device__ __forceinline__ Pair fma(Pair a, Pair b, Pair c) { return {VEC > 1 ? __ffma2_rn(a.v, b.v, c.v) : make_float2(fmaf(a.v.x, b.v.x, c.v.x), 0.f)}; }
 __device__ __forceinline__ Pair both(float x) { return {make_float2(x, x)}; }
 
+// Whether every thread of a row has a v-th vector: V is the least number of vectors that reaches all of the row (see `vectors`).
+template <int V> __device__ __forceinline__ constexpr bool all_have(int v) { return v < (V <= 8 ? V - 1 : V == 12 ? 8 : 12); }
+
 // A row's values less their mean in x, and y's factor.  FULL: every thread of the row has V whole vectors.
 template <int VEC, int V, bool FULL>
-__device__ __forceinline__ void norm_row(const NormArgs& a, int lane, float (&x)[V][VEC], float& mean, float& rstd, float (*sums)[1][32]) {
+__device__ __forceinline__ void norm_row(const NormArgs& a, int lane, float (&x)[V][VEC], float& mean, float& rstd, float (*sums)[32][1]) {
   constexpr int STEP = VEC > 1 ? 2 : 1;
   Pair t = both(0.f);
 #pragma unroll
@@ -153,7 +159,7 @@ __device__ __forceinline__ void norm_row(const NormArgs& a, int lane, float (&x)
   t = both(0.f);
 #pragma unroll
   for (int v = 0; v < V; ++v)
-    if (FULL || (lane + v * a.group) * VEC < a.C)
+    if (FULL || all_have<V>(v) || (lane + v * a.group) * VEC < a.C)
 #pragma unroll
       for (int e = 0; e < VEC; e += STEP) {
         const Pair d = add<VEC>(Pair::of(x[v], e), both(-mean));
@@ -178,12 +184,12 @@ __device__ __forceinline__ void norm_params(const NormArgs& a, int lane, float (
 // The gradients of a row (x and dy of it; dy becomes dx), and its part of dw and db.
 template <int VEC, int V, bool FULL>
 __device__ __forceinline__ void norm_row_backward(const NormArgs& a, int lane, float mean, float rstd, float (&x)[V][VEC], float (&dy)[V][VEC],
-                                                  const float (&w)[V][VEC], float (&dw)[V][VEC], float (&db)[V][VEC], float (*sums)[32]) {
+                                                  const float (&w)[V][VEC], float (&dw)[V][VEC], float (&db)[V][VEC], float (*sums)[2]) {
   constexpr int STEP = VEC > 1 ? 2 : 1;
   Pair t0 = both(0.f), t1 = both(0.f);
 #pragma unroll
   for (int v = 0; v < V; ++v) {
-    if (!FULL && (lane + v * a.group) * VEC >= a.C) continue;
+    if (!FULL && !all_have<V>(v) && (lane + v * a.group) * VEC >= a.C) continue;
 #pragma unroll
     for (int e = 0; e < VEC; e += STEP) {
       // (a row that is not there is zeros, with a mean and rstd of zero)
@@ -242,23 +248,24 @@ __device__ __forceinline__ void norm_block_sums(const NormArgs& a, int lane, flo
 template <typename T, typename P, int VEC, int V, int STAGES, bool FULL>
 __global__ void __launch_bounds__(NORM_THREADS) norm_forward_kernel(const NormArgs a) {
   extern __shared__ uint4 ring[];
-  __shared__ __align__(16) float sums[2][1][32];
+  __shared__ float sums[2][32][1];
   const int lane = threadIdx.x & (a.group - 1), groups = blockDim.x >> a.shift, apart = a.group * VEC;      // apart: of a thread's vectors
   const int step = (int)gridDim.x * groups;
   const uint32_t mine = (uint32_t)__cvta_generic_to_shared(ring + threadIdx.x), slot = blockDim.x * 16;
   const uint4* own = ring + threadIdx.x;
-  const long row = (long)blockIdx.x * groups + (threadIdx.x >> a.shift);
+  long row = (long)blockIdx.x * groups + (threadIdx.x >> a.shift);
   int left = (int)(a.rows - row), ahead = left;              // rows from this one (the next one fetched) on
   const T *from = static_cast<const T*>(a.X) + row * a.sx + lane * VEC, *at = from;
   T* to = static_cast<T*>(a.Y) + row * a.sy + lane * VEC;
-  float *mean_at = a.mean ? a.mean + row : nullptr, *rstd_at = a.rstd + row;
   const long from_step = step * a.sx, to_step = step * a.sy;
   const auto fetch = [&](int stage) {
     if (VEC > 1) {
-      if (ahead > 0)
+      // (what is not there is fetched as zeros: the rows' arithmetic asks for nothing)
 #pragma unroll
-        for (int v = 0; v < V; ++v)
-          if (FULL || lane * VEC + v * apart < a.C) copy16_async(mine + (uint32_t)(stage * V + v) * slot, from + v * apart);
+      for (int v = 0; v < V; ++v) {
+        const bool in = ahead > 0 && (FULL || all_have<V>(v) || lane * VEC + v * apart < a.C);
+        copy16_async_if(mine + (uint32_t)(stage * V + v) * slot, in ? from + v * apart : static_cast<const T*>(a.X), in);
+      }
       copies_commit();
       from += from_step;
       ahead -= step;
@@ -268,43 +275,38 @@ __global__ void __launch_bounds__(NORM_THREADS) norm_forward_kernel(const NormAr
   for (int i = 0; i < STAGES - 1; ++i) fetch(i);
   float w[V][VEC], b[V][VEC];
   norm_params<P, VEC, V>(a, lane, w, b);
-  // A row each; ALL: every thread of the warp has one (groups of a warp or more are there or not as a whole).
-  const auto work = [&](auto all, int stage) {
-    constexpr bool ALL = decltype(all)::value;
-    float x[V][VEC];
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      if ((ALL || left > 0) && (FULL || lane * VEC + v * apart < a.C)) {
-        if (VEC > 1) load_elems<T, VEC>(reinterpret_cast<const T*>(own + (size_t)(stage * V + v) * blockDim.x), x[v]);
-        else load_elems<T, VEC>(at + v * apart, x[v]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) x[v][e] = 0.f;
-      }
-    }
-    fetch((stage + STAGES - 1) % STAGES);
-    float mean, rstd;
-    norm_row<VEC, V, FULL>(a, lane, x, mean, rstd, sums);
-    if (ALL || left > 0) {
-      if (lane == 0 && mean_at) { *mean_at = mean; *rstd_at = rstd; }
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        if (!FULL && lane * VEC + v * apart >= a.C) continue;
-#pragma unroll
-        for (int e = 0; e < VEC; e += VEC > 1 ? 2 : 1) fma<VEC>(mul<VEC>(Pair::of(x[v], e), both(rstd)), Pair::of(w[v], e), Pair::of(b[v], e)).to(x[v], e);
-        store_elems<T, VEC>(to + v * apart, x[v]);
-      }
-    }
-  };
-  while (__any_sync(0xffffffffu, left > 0)) {
+  int blocks_left = (int)(a.rows - (long)blockIdx.x * groups);     // (the same in all threads of the block)
+  while (blocks_left > 0) {
 #pragma unroll
     for (int stage = 0; stage < STAGES; ++stage) {
+      if (blocks_left <= 0) break;
       if (VEC > 1) copies_wait<(STAGES > 1 ? STAGES - 2 : 0)>();
-      if (__all_sync(0xffffffffu, left > 0)) work(std::true_type(), stage);
-      else if (__any_sync(0xffffffffu, left > 0)) work(std::false_type(), stage);
-      else break;
-      left -= step; to += to_step; rstd_at += step;
-      if (mean_at) mean_at += step;
+      float x[V][VEC];
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        if (VEC > 1) {
+          load_elems<T, VEC>(reinterpret_cast<const T*>(own + (size_t)(stage * V + v) * blockDim.x), x[v]);
+        } else if (left > 0 && (all_have<V>(v) || lane * VEC + v * apart < a.C)) {
+          load_elems<T, VEC>(at + v * apart, x[v]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) x[v][e] = 0.f;
+        }
+      }
+      fetch((stage + STAGES - 1) % STAGES);
+      float mean, rstd;
+      norm_row<VEC, V, FULL>(a, lane, x, mean, rstd, sums);
+      if (left > 0) {
+        if (lane == 0 && a.mean) { a.mean[row] = mean; a.rstd[row] = rstd; }
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          if (!FULL && !all_have<V>(v) && lane * VEC + v * apart >= a.C) continue;
+#pragma unroll
+          for (int e = 0; e < VEC; e += VEC > 1 ? 2 : 1) fma<VEC>(mul<VEC>(Pair::of(x[v], e), both(rstd)), Pair::of(w[v], e), Pair::of(b[v], e)).to(x[v], e);
+          store_elems<T, VEC>(to + v * apart, x[v]);
+        }
+      }
+      row += step; left -= step; blocks_left -= step; to += to_step;
       if (VEC == 1) at += from_step;
     }
   }
@@ -313,23 +315,22 @@ __global__ void __launch_bounds__(NORM_THREADS) norm_forward_kernel(const NormAr
 template <typename T, typename P, int VEC, int V, int STAGES, bool FULL>
 __global__ void __launch_bounds__(NORM_THREADS) norm_backward_kernel(const NormArgs a) {
   extern __shared__ uint4 ring[];
-  __shared__ __align__(16) float sums[2][2][32];
+  __shared__ float sums[2][32][2];
   const int lane = threadIdx.x & (a.group - 1), groups = blockDim.x >> a.shift, apart = a.group * VEC;
   const int step = (int)gridDim.x * groups;
   const uint32_t mine = (uint32_t)__cvta_generic_to_shared(ring + threadIdx.x), slot = blockDim.x * 16;
   const uint4* own = ring + threadIdx.x;
-  const long row = (long)blockIdx.x * groups + (threadIdx.x >> a.shift);
+  long row = (long)blockIdx.x * groups + (threadIdx.x >> a.shift);
   int left = (int)(a.rows - row), ahead = left;
   const T *from = static_cast<const T*>(a.X) + row * a.sx + lane * VEC, *at = from, *from_dy = static_cast<const T*>(a.dY) + row * a.sy + lane * VEC, *at_dy = from_dy;
   T* to = static_cast<T*>(a.dX) + row * a.sdx + lane * VEC;
-  const float *mean_at = a.mean + row, *rstd_at = a.rstd + row;
   const long x_step = step * a.sx, dy_step = step * a.sy, to_step = step * a.sdx;
   const auto fetch = [&](int stage) {
     if (VEC > 1) {
       if (ahead > 0)
 #pragma unroll
         for (int v = 0; v < V; ++v)
-          if (FULL || lane * VEC + v * apart < a.C) {
+          if (FULL || all_have<V>(v) || lane * VEC + v * apart < a.C) {
             copy16_async(mine + (uint32_t)(stage * 2 * V + 2 * v) * slot, from + v * apart);
             copy16_async(mine + (uint32_t)(stage * 2 * V + 2 * v + 1) * slot, from_dy + v * apart);
           }
@@ -348,51 +349,45 @@ __global__ void __launch_bounds__(NORM_THREADS) norm_backward_kernel(const NormA
     for (int e = 0; e < VEC; ++e) { dw[v][e] = db[v][e] = 0.f; w[v][e] = 1.f; }
     if (a.weight && c < a.C) load_params<P, VEC>(static_cast<const P*>(a.weight) + c, w[v]);
   }
-  float next_mean = left > 0 ? __ldg(mean_at) : 0.f, next_rstd = left > 0 ? __ldg(rstd_at) : 0.f;
+  float next_mean = left > 0 ? __ldg(a.mean + row) : 0.f, next_rstd = left > 0 ? __ldg(a.rstd + row) : 0.f;
+  int blocks_left = (int)(a.rows - (long)blockIdx.x * groups);
   int turn = 0;
-  const auto work = [&](auto all, int stage, float mean, float rstd) {
-    constexpr bool ALL = decltype(all)::value;
-    float x[V][VEC], dy[V][VEC];
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      if ((ALL || left > 0) && (FULL || lane * VEC + v * apart < a.C)) {
-        if (VEC > 1) {
-          load_elems<T, VEC>(reinterpret_cast<const T*>(own + (size_t)(stage * 2 * V + 2 * v) * blockDim.x), x[v]);
-          load_elems<T, VEC>(reinterpret_cast<const T*>(own + (size_t)(stage * 2 * V + 2 * v + 1) * blockDim.x), dy[v]);
-        } else {
-          load_elems<T, VEC>(at + v * apart, x[v]);
-          load_elems<T, VEC>(at_dy + v * apart, dy[v]);
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) x[v][e] = dy[v][e] = 0.f;
-      }
-    }
-    fetch((stage + STAGES - 1) % STAGES);
-    norm_row_backward<VEC, V, FULL>(a, lane, mean, rstd, x, dy, w, dw, db, sums[turn]);
-    if (ALL || left > 0)
-#pragma unroll
-      for (int v = 0; v < V; ++v)
-        if (FULL || lane * VEC + v * apart < a.C) store_elems<T, VEC>(to + v * apart, dy[v]);
-  };
-  while (__any_sync(0xffffffffu, left > 0)) {
+  while (blocks_left > 0) {
 #pragma unroll
     for (int stage = 0; stage < STAGES; ++stage) {
+      if (blocks_left <= 0) break;
       const float mean = next_mean, rstd = next_rstd;
       next_mean = next_rstd = 0.f;
-      mean_at += step; rstd_at += step;
-      if (left > step) { next_mean = __ldg(mean_at); next_rstd = __ldg(rstd_at); }
+      if (left > step) { next_mean = __ldg(a.mean + row + step); next_rstd = __ldg(a.rstd + row + step); }
       if (VEC > 1) copies_wait<(STAGES > 1 ? STAGES - 2 : 0)>();
-      if (__all_sync(0xffffffffu, left > 0)) work(std::true_type(), stage, mean, rstd);
-      else if (__any_sync(0xffffffffu, left > 0)) work(std::false_type(), stage, mean, rstd);
-      else break;
+      float x[V][VEC], dy[V][VEC];
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        if (left > 0 && (FULL || all_have<V>(v) || lane * VEC + v * apart < a.C)) {
+          if (VEC > 1) {
+            load_elems<T, VEC>(reinterpret_cast<const T*>(own + (size_t)(stage * 2 * V + 2 * v) * blockDim.x), x[v]);
+            load_elems<T, VEC>(reinterpret_cast<const T*>(own + (size_t)(stage * 2 * V + 2 * v + 1) * blockDim.x), dy[v]);
+          } else {
+            load_elems<T, VEC>(at + v * apart, x[v]);
+            load_elems<T, VEC>(at_dy + v * apart, dy[v]);
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) x[v][e] = dy[v][e] = 0.f;
+        }
+      }
+      fetch((stage + STAGES - 1) % STAGES);
+      norm_row_backward<VEC, V, FULL>(a, lane, mean, rstd, x, dy, w, dw, db, sums[turn]);
       turn ^= 1;
-      left -= step; to += to_step;
+      if (left > 0)
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+          if (FULL || all_have<V>(v) || lane * VEC + v * apart < a.C) store_elems<T, VEC>(to + v * apart, dy[v]);
+      row += step; left -= step; blocks_left -= step; to += to_step;
       if (VEC == 1) { at += x_step; at_dy += dy_step; }
     }
   }
   pdl_trigger();
-  copies_wait<0>();
   if (a.part) norm_block_sums<VEC, V>(a, lane, dw, db, reinterpret_cast<float*>(ring));
 }
 
@@ -419,7 +414,7 @@ constexpr int RUN_STAGES = 4;
 template <typename T, typename P, int V, bool BACKWARD>
 __global__ void __launch_bounds__(NORM_THREADS, BACKWARD ? 1 : 2) norm_runs_kernel(const NormArgs a) {
   extern __shared__ uint4 ring[];
-  __shared__ __align__(16) float sums[2][2][32], sum1[2][1][32];
+  __shared__ float sums[2][32][2], sum1[2][32][1];
   const int lane = threadIdx.x & (a.group - 1), groups = blockDim.x >> a.shift, own = threadIdx.x >> a.shift;
   const long runs = (a.rows + a.run - 1) / a.run;
   const size_t run_values = (size_t)a.run * a.C, run_pieces = run_values / VEC_OF<T>;
@@ -456,8 +451,8 @@ __global__ void __launch_bounds__(NORM_THREADS, BACKWARD ? 1 : 2) norm_runs_kern
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         const int c = lane + v * a.group;
-        x[v][0] = in && c < a.C ? to_f(xs[(size_t)r * a.C + c]) : 0.f;
-        if (BACKWARD) dy[v][0] = in && c < a.C ? to_f(ds[(size_t)r * a.C + c]) : 0.f;
+        x[v][0] = in && (all_have<V>(v) || c < a.C) ? to_f(xs[r * a.C + c]) : 0.f;
+        if (BACKWARD) dy[v][0] = in && (all_have<V>(v) || c < a.C) ? to_f(ds[r * a.C + c]) : 0.f;
       }
       if constexpr (BACKWARD) {
         const float mean = in ? __ldg(a.mean + first + r) : 0.f, rstd = in ? __ldg(a.rstd + first + r) : 0.f;
@@ -465,7 +460,7 @@ __global__ void __launch_bounds__(NORM_THREADS, BACKWARD ? 1 : 2) norm_runs_kern
         if (in)
 #pragma unroll
           for (int v = 0; v < V; ++v)
-            if (lane + v * a.group < a.C) xs[(size_t)r * a.C + lane + v * a.group] = from_f<T>(dy[v][0]);
+            if (all_have<V>(v) || lane + v * a.group < a.C) xs[r * a.C + lane + v * a.group] = from_f<T>(dy[v][0]);
       } else {
         float mean, rstd;
         norm_row<1, V, false>(a, lane, x, mean, rstd, sum1);
@@ -473,7 +468,7 @@ __global__ void __launch_bounds__(NORM_THREADS, BACKWARD ? 1 : 2) norm_runs_kern
           if (lane == 0 && a.mean) { a.mean[first + r] = mean; a.rstd[first + r] = rstd; }
 #pragma unroll
           for (int v = 0; v < V; ++v)
-            if (lane + v * a.group < a.C) xs[(size_t)r * a.C + lane + v * a.group] = from_f<T>(fmaf(x[v][0] * rstd, w[v][0], b[v][0]));
+            if (all_have<V>(v) || lane + v * a.group < a.C) xs[r * a.C + lane + v * a.group] = from_f<T>(fmaf(x[v][0] * rstd, w[v][0], b[v][0]));
         }
       }
     }
@@ -494,7 +489,7 @@ __global__ void __launch_bounds__(NORM_THREADS, BACKWARD ? 1 : 2) norm_runs_kern
 
 template <typename T, typename P>
 __global__ void __launch_bounds__(1024) norm_forward_wide_kernel(const NormArgs a) {
-  __shared__ __align__(16) float sums[2][1][32];
+  __shared__ float sums[2][32][1];
   for (long row = blockIdx.x; row < a.rows; row += gridDim.x) {
     const T* x = static_cast<const T*>(a.X) + row * a.sx;
     float s[1] = {0.f};
@@ -514,7 +509,7 @@ __global__ void __launch_bounds__(1024) norm_forward_wide_kernel(const NormArgs 
 }
 template <typename T, typename P>
 __global__ void __launch_bounds__(1024) norm_backward_wide_kernel(const NormArgs a) {
-  __shared__ __align__(16) float sums[2][2][32];
+  __shared__ float sums[2][32][2];
   int turn = 0;
   for (long row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
     const T *x = static_cast<const T*>(a.X) + row * a.sx, *dy = static_cast<const T*>(a.dY) + row * a.sy;

@@ -33,6 +33,12 @@ struct Library {
   decltype(&xconv_wgrad_seeded) wgrad_seeded;
   decltype(&xconv_backprobe) backprobe;
   decltype(&xconv_contract) contract;
+  decltype(&xconv_layernorm_workspace_bytes) norm_workspace_bytes;
+  decltype(&xconv_layernorm_forward) norm_forward;
+  decltype(&xconv_layernorm_backward) norm_backward;
+  decltype(&xconv_update_workspace_bytes) update_workspace_bytes;
+  decltype(&xconv_orthogonalize) orthogonalize;
+  decltype(&xconv_muon_step) muon_step;
 } lib{};
 PyObject *raise_for_status = nullptr, *workspace = nullptr;
 
@@ -315,6 +321,194 @@ PyObject* contract(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   XM_END
 }
 
+// ---- around the layers
+
+bool raise(xconv_status s, const char* name) {
+  if (s == XCONV_OK) return true;
+  PyObject* r = PyObject_CallFunction(raise_for_status, "is", (int)s, name);
+  Py_XDECREF(r);
+  if (!PyErr_Occurred()) PyErr_SetString(PyExc_RuntimeError, name);
+  return false;
+}
+bool on_current_device(const at::Tensor& t) { return t.device().index() == c10::cuda::current_device(); }
+
+// A dense tensor of the library's layout: matrices and tokens (1-d to 3-d) row-major, images and volumes channels-last.
+const at::Tensor* dense(PyObject* o) {
+  const at::Tensor* t = plain(o);
+  if (!t || t->dim() < 1 || t->dim() > 5 || t->numel() == 0 || dtype_code(*t) < 0 || !on_current_device(*t)) return nullptr;
+  const auto fmt = t->dim() == 4 ? at::MemoryFormat::ChannelsLast : t->dim() == 5 ? at::MemoryFormat::ChannelsLast3d : at::MemoryFormat::Contiguous;
+  return t->is_contiguous(fmt) ? t : nullptr;
+}
+at::Tensor dense_like(const at::Tensor& t) {
+  const auto fmt = t.dim() == 4 ? at::MemoryFormat::ChannelsLast : t.dim() == 5 ? at::MemoryFormat::ChannelsLast3d : at::MemoryFormat::Contiguous;
+  return at::empty(t.sizes(), t.options().requires_grad(false), fmt);
+}
+// The rows of a dense tensor: their shape, and the number of values in each.
+int64_t rows_of(const at::Tensor& t, std::vector<int64_t>* shape) {
+  const int c = t.dim() >= 4 ? 1 : (int)t.dim() - 1;
+  for (int i = 0; i < t.dim(); ++i)
+    if (i != c) shape->push_back(t.size(i));
+  return t.size(c);
+}
+// A vector of C parameters in X's type or float (code: of both), or None.
+bool param_of(PyObject* o, const at::Tensor& X, int64_t C, const at::Tensor** p, int* code) {
+  *p = nullptr;
+  if (o == Py_None) return true;
+  const at::Tensor* t = plain(o);
+  if (!t || t->dim() != 1 || t->size(0) != C || !t->is_contiguous() || t->device() != X.device()) return false;
+  const int c = dtype_code(*t);
+  if (c < 0 || (c != XCONV_F32 && c != dtype_code(X)) || (*code >= 0 && *code != c)) return false;
+  *code = c;
+  *p = t;
+  return true;
+}
+xconv_norm_desc norm_desc(const at::Tensor& X, int64_t C, int code, float eps) {
+  xconv_norm_desc d;
+  std::memset(&d, 0, sizeof d);
+  d.rows = X.numel() / C; d.C = (int32_t)C; d.dtype = dtype_code(X); d.param_dtype = code < 0 ? XCONV_F32 : code; d.eps = eps;
+  d.x_stride = d.y_stride = d.dx_stride = C;
+  return d;
+}
+void* address(const at::Tensor* t) { return t ? t->data_ptr() : nullptr; }
+
+// layernorm(X, weight, bias, eps) -> (Y, mean, rstd)
+PyObject* layernorm(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  XM_BEGIN(4)
+  const at::Tensor* X = dense(a[0]);
+  if (!X || !PyFloat_CheckExact(a[3])) Py_RETURN_NONE;
+  std::vector<int64_t> shape;
+  const int64_t C = rows_of(*X, &shape);
+  const at::Tensor *w, *b;
+  int code = -1;
+  if (C > INT32_MAX || !param_of(a[1], *X, C, &w, &code) || !param_of(a[2], *X, C, &b, &code)) Py_RETURN_NONE;
+  const xconv_norm_desc d = norm_desc(*X, C, code, (float)PyFloat_AS_DOUBLE(a[3]));
+  const auto opt = X->options().dtype(at::kFloat).requires_grad(false);
+  const at::Tensor Y = dense_like(*X), mean = at::empty(shape, opt), rstd = at::empty(shape, opt);
+  const cudaStream_t stream = c10::cuda::getCurrentCUDAStream().stream();
+  const xconv_status s = lib.norm_forward(&d, X->data_ptr(), address(w), address(b), Y.data_ptr(), (float*)mean.data_ptr(), (float*)rstd.data_ptr(), stream);
+  if (!raise(s, "xconv_layernorm_forward")) return nullptr;
+  return Py_BuildValue("(NNN)", THPVariable_Wrap(Y), THPVariable_Wrap(mean), THPVariable_Wrap(rstd));
+  XM_END
+}
+
+// layernorm_backward(dY, X, mean, rstd, weight) -> (dX, dweight, dbias)
+PyObject* layernorm_backward(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  XM_BEGIN(5)
+  const at::Tensor *dY = dense(a[0]), *X = dense(a[1]), *mean = plain(a[2]), *rstd = plain(a[3]);
+  if (!dY || !X || !mean || !rstd || dY->sizes() != X->sizes() || dY->scalar_type() != X->scalar_type() || dY->device() != X->device()) Py_RETURN_NONE;
+  std::vector<int64_t> shape;
+  const int64_t C = rows_of(*X, &shape);
+  for (const at::Tensor* t : {mean, rstd})
+    if (t->scalar_type() != at::kFloat || t->sizes() != at::IntArrayRef(shape) || !t->is_contiguous() || t->device() != X->device()) Py_RETURN_NONE;
+  const at::Tensor* w;
+  int code = -1;
+  if (C > INT32_MAX || !param_of(a[4], *X, C, &w, &code)) Py_RETURN_NONE;
+  const xconv_norm_desc d = norm_desc(*X, C, code, 0.f);
+  const auto opt = X->options().dtype(at::kFloat).requires_grad(false);
+  const at::Tensor dX = dense_like(*X), dw = at::empty({C}, opt), db = at::empty({C}, opt);
+  const cudaStream_t stream = c10::cuda::getCurrentCUDAStream().stream();
+  const at::Tensor ws = scratch(lib.norm_workspace_bytes(&d), *X, stream);
+  const xconv_status s = lib.norm_backward(&d, dY->data_ptr(), X->data_ptr(), (const float*)mean->data_ptr(), (const float*)rstd->data_ptr(), address(w), dX.data_ptr(),
+                                           (float*)dw.data_ptr(), (float*)db.data_ptr(), ws.data_ptr(), (size_t)ws.numel(), stream);
+  if (!raise(s, "xconv_layernorm_backward")) return nullptr;
+  return Py_BuildValue("(NNN)", THPVariable_Wrap(dX), THPVariable_Wrap(dw), THPVariable_Wrap(db));
+  XM_END
+}
+
+// The matrices that a dense tensor of weights holds: two or three dimensions, or a convolution's.
+bool matrices_of(const at::Tensor& t, xconv_matrices* m) {
+  const int64_t dim = t.dim(), rows = dim == 3 ? t.size(1) : t.size(0), batch = dim == 3 ? t.size(0) : 1;
+  if (dim < 2) return false;
+  const int64_t cols = t.numel() / (rows * batch);
+  if (rows > INT32_MAX || cols > INT32_MAX || batch > INT32_MAX) return false;
+  std::memset(m, 0, sizeof *m);
+  m->rows = (int32_t)rows; m->cols = (int32_t)cols; m->batch = (int32_t)batch;
+  return true;
+}
+bool number(PyObject* o, float* v) {
+  if (!PyFloat_CheckExact(o)) return false;
+  *v = (float)PyFloat_AS_DOUBLE(o);
+  return true;
+}
+// steps, coefficients (three floats in a tuple), eps
+bool steps_of(PyObject* steps, PyObject* coefficients, PyObject* eps, xconv_update_desc* d) {
+  std::memset(d, 0, sizeof *d);
+  return small_int(steps, &d->steps) && PyTuple_CheckExact(coefficients) && PyTuple_GET_SIZE(coefficients) == 3 && number(PyTuple_GET_ITEM(coefficients, 0), &d->a) &&
+         number(PyTuple_GET_ITEM(coefficients, 1), &d->b) && number(PyTuple_GET_ITEM(coefficients, 2), &d->c) && number(eps, &d->eps);
+}
+// The items of a list, or the one tensor that is given in its place.
+struct Several {
+  PyObject* list;
+  PyObject* one;
+  explicit Several(PyObject* o) : list(PyList_CheckExact(o) ? o : nullptr), one(o) {}
+  Py_ssize_t size() const { return list ? PyList_GET_SIZE(list) : 1; }
+  PyObject* operator[](Py_ssize_t i) const { return list ? PyList_GET_ITEM(list, i) : one; }
+};
+xconv_status update(decltype(&xconv_orthogonalize) call, const xconv_update_desc& d, const std::vector<xconv_matrices>& items, const at::Tensor& like) {
+  const cudaStream_t stream = c10::cuda::getCurrentCUDAStream().stream();
+  const at::Tensor ws = scratch(lib.update_workspace_bytes(items.data(), (int)items.size()), like, stream);
+  void* p = ws.data_ptr();
+  const size_t bytes = (size_t)ws.numel();
+  xconv_status s;
+  Py_BEGIN_ALLOW_THREADS
+  s = call(&d, items.data(), (int)items.size(), p, bytes, stream);
+  Py_END_ALLOW_THREADS
+  return s;
+}
+
+// orthogonalize(G or list, steps, coefficients, eps) -> O or list
+PyObject* orthogonalize(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  XM_BEGIN(4)
+  xconv_update_desc d;
+  const Several G(a[0]);
+  if (G.size() == 0 || !steps_of(a[1], a[2], a[3], &d)) Py_RETURN_NONE;
+  std::vector<xconv_matrices> items((size_t)G.size());
+  std::vector<const at::Tensor*> in;
+  for (Py_ssize_t i = 0; i < G.size(); ++i) {
+    const at::Tensor* g = dense(G[i]);
+    if (!g || !matrices_of(*g, &items[i])) Py_RETURN_NONE;
+    in.push_back(g);
+  }
+  std::vector<at::Tensor> out;
+  for (size_t i = 0; i < in.size(); ++i) {
+    out.push_back(dense_like(*in[i]));
+    items[i].G = in[i]->data_ptr(); items[i].O = out[i].data_ptr();
+    items[i].g_dtype = items[i].o_dtype = dtype_code(*in[i]);
+  }
+  if (!raise(update(lib.orthogonalize, d, items, out[0]), "xconv_orthogonalize")) return nullptr;
+  if (!G.list) return THPVariable_Wrap(out[0]);
+  THPObjectPtr list(PyList_New((Py_ssize_t)out.size()));
+  if (!list) return nullptr;
+  for (size_t i = 0; i < out.size(); ++i) PyList_SET_ITEM(list.get(), (Py_ssize_t)i, THPVariable_Wrap(out[i]));
+  return list.release();
+  XM_END
+}
+
+// muon_step(W, dW, M (or lists), lr, momentum, nesterov, weight_decay, steps, coefficients, eps, adjust) -> True
+PyObject* muon_step(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  XM_BEGIN(11)
+  xconv_update_desc d;
+  int32_t adjust;
+  const Several W(a[0]), G(a[1]), M(a[2]);
+  if (W.size() == 0 || W.size() != G.size() || W.size() != M.size() || !steps_of(a[7], a[8], a[9], &d) || !number(a[3], &d.lr) || !number(a[4], &d.momentum) ||
+      !PyBool_Check(a[5]) || !number(a[6], &d.weight_decay) || !PyLong_CheckExact(a[10]))
+    Py_RETURN_NONE;
+  adjust = (int32_t)PyLong_AsLong(a[10]);
+  d.nesterov = a[5] == Py_True; d.adjust = adjust;
+  std::vector<xconv_matrices> items((size_t)W.size());
+  const at::Tensor* like = nullptr;
+  for (Py_ssize_t i = 0; i < W.size(); ++i) {
+    const at::Tensor *w = dense(W[i]), *g = dense(G[i]), *m = dense(M[i]);
+    if (!w || !g || !m || g->sizes() != w->sizes() || m->sizes() != w->sizes() || m->scalar_type() != at::kFloat || !matrices_of(*w, &items[i])) Py_RETURN_NONE;
+    items[i].G = g->data_ptr(); items[i].M = (float*)m->data_ptr(); items[i].O = w->data_ptr();
+    items[i].g_dtype = dtype_code(*g); items[i].o_dtype = dtype_code(*w);
+    like = w;
+  }
+  if (!raise(update(lib.muon_step, d, items, *like), "xconv_muon_step")) return nullptr;
+  Py_RETURN_TRUE;
+  XM_END
+}
+
 // use_library(address of each entry point in the order of Library, raise(status, name), workspace(bytes, device))
 PyObject* use_library(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   constexpr Py_ssize_t N = sizeof(Library) / sizeof(void*);
@@ -335,6 +529,7 @@ PyObject* use_library(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
 PyMethodDef methods[] = {
 #define XM_FAST(F) {#F, (PyCFunction)(void (*)(void))F, METH_FASTCALL, nullptr}
     XM_FAST(forward), XM_FAST(sketch), XM_FAST(sketch_seeded), XM_FAST(wgrad), XM_FAST(wgrad_seeded), XM_FAST(dgrad), XM_FAST(backprobe), XM_FAST(contract),
+    XM_FAST(layernorm), XM_FAST(layernorm_backward), XM_FAST(orthogonalize), XM_FAST(muon_step),
     XM_FAST(use_library), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
