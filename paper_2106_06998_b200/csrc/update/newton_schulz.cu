@@ -52,8 +52,8 @@ struct NsArgs {
   unsigned *status, tag;
   float a, b, c, momentum, keep;
   double eps;
-  int muon, nesterov, which;   // which: the buffer that X is in
-  int cs;                      // pairs of CTAs a tile
+  int muon, nesterov, which;   // which: the buffer that X is in (ns_small_kernel: the number of steps)
+  int cs;                      // pairs of CTAs a tile (ns_small_kernel: CTAs a matrix)
 };
 
 __device__ __forceinline__ float load_as_float(const void* p, int dtype, size_t i) {
@@ -160,6 +160,20 @@ __global__ void __launch_bounds__(256) ns_squares_kernel(const __grid_constant__
   }
 }
 
+// Values times 2^13 / norm: a float in [0.5, 1) and a power of two that is applied in halves, so that neither the factor nor a product leaves the floats' range.
+struct NsScale {
+  float f, s1, s2;
+  __device__ __forceinline__ NsScale(double squares, double eps) {
+    const double norm = sqrt(squares);
+    int ex = 0;
+    f = (float)frexp((double)NS_SCALE / (norm < eps ? eps : norm), &ex);
+    const int e1 = min(126, max(-126, ex / 2)), e2 = min(126, max(-126, ex - e1));
+    s1 = __int_as_float((e1 + 127) << 23);
+    s2 = __int_as_float((e2 + 127) << 23);
+  }
+  __device__ __forceinline__ float operator()(float x) const { return x * s1 * f * s2; }
+};
+
 // ---- X0 in blocks: a block of threads per block of 128 x 64 values
 
 __global__ void __launch_bounds__(256) ns_blocks_kernel(const __grid_constant__ NsArgs p) {
@@ -196,18 +210,13 @@ __global__ void __launch_bounds__(256) ns_blocks_kernel(const __grid_constant__ 
   __syncthreads();
   s = sums[0];
   for (int w = 1; w < 8; ++w) s += sums[w];
-  // 2^13 / norm as a float in [0.5, 1) and a power of two that is applied in halves: neither the factor nor a product leaves the floats' range
-  const double norm = sqrt(s);
-  int ex = 0;
-  const float f = (float)frexp((double)NS_SCALE / (norm < p.eps ? p.eps : norm), &ex);
-  const int e1 = min(126, max(-126, ex / 2)), e2 = min(126, max(-126, ex - e1));
-  const float s1 = __int_as_float((e1 + 127) << 23), s2 = __int_as_float((e2 + 127) << 23);
+  const NsScale f(s, p.eps);
   char* out = p.blocks + ((size_t)e.x0 + (size_t)mat * per + at) * NS_BLOCK;
   for (int i = tid; i < NS_ROWS * 8; i += 256) {
     const int r = i & (NS_ROWS - 1), q = i / NS_ROWS;
     float v[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = tile[r][q * 8 + j] * s1 * f * s2;
+    for (int j = 0; j < 8; ++j) v[j] = f(tile[r][q * 8 + j]);
     uint4 hi, lo;
     parts8(v, hi, lo);
     *reinterpret_cast<uint4*>(out + piece_at(r, q)) = hi;
@@ -658,6 +667,361 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_product_kernel(const __grid_
   if (warp == 1) pair_dealloc(tmem);
 }
 
+// ---- matrices whose smaller side is at most 128, in one kernel: a cluster of up to eight CTAs a matrix, X in their shared memory
+
+// Small matrices are bound by latencies: 17 kernels of 7 to 9 us each, of which the products take one.  Here a CTA holds up to three blocks of 64 columns of X for all steps.  A
+// step: the products of the CTA's own columns, summed over the cluster through the SMs' network (each CTA sums some columns and gives them to the others), then A A
+// and B X in every CTA by itself.  Three chains of MMAs with a wait behind each; twelve in all where the cluster is one CTA.
+constexpr int SMALL_THREADS = 512, SMALL_COLUMN_BLOCKS = 3;
+constexpr uint32_t SMALL_X = 0, SMALL_A = SMALL_COLUMN_BLOCKS * NS_OPERAND, SMALL_E = SMALL_A + 2 * NS_OPERAND, SMALL_BYTES = SMALL_E + 2 * NS_OPERAND;
+constexpr int SMALL_CLUSTER = 8;
+
+__device__ __forceinline__ void st_cluster_v4(uint32_t addr, uint32_t rank, uint4 v) {
+  asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %0, %1;\n\tst.shared::cluster.v4.b32 [a], {%2, %3, %4, %5};\n\t}"
+               ::"r"(addr), "r"(rank), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ void st_cluster_f64(uint32_t addr, uint32_t rank, double v) {
+  asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %0, %1;\n\tst.shared::cluster.f64 [a], %2;\n\t}" ::"r"(addr), "r"(rank), "d"(v) : "memory");
+}
+__device__ __forceinline__ void st_shared_v4(uint32_t addr, uint4 v) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async;" ::: "memory"); }
+
+// A chain of a product: two steps of 16 terms (or one), the small products first, into columns `d` of the tensor memory.
+__device__ __forceinline__ void small_chain(uint32_t d, uint32_t a, uint32_t a_hi, uint32_t a_step, uint32_t b, uint32_t b_hi, uint32_t b_step, uint32_t idesc, int steps) {
+  constexpr uint32_t L = NS_PART >> 4;
+  for (int t = 0; t < steps; ++t) umma_warp(d, a + L + t * a_step, a_hi, b + t * b_step, b_hi, idesc, t > 0);
+  for (int t = 0; t < steps; ++t) umma_warp(d, a + t * a_step, a_hi, b + L + t * b_step, b_hi, idesc, 1u);
+  for (int t = 0; t < steps; ++t) umma_warp(d, a + t * a_step, a_hi, b + t * b_step, b_hi, idesc, 1u);
+}
+
+struct SmallWait {             // for the MMAs that were issued last, by all threads
+  uint64_t* bar;
+  uint32_t parity;
+  unsigned *status, tag;
+  __device__ __forceinline__ void operator()() {
+    mbar_wait_warp(bar, parity, status, tag);
+    parity ^= 1u;
+    tc_fence_after();
+  }
+};
+
+// C columns of the chains' sums: COLS columns a thread from `from` on, chains `pitch` columns apart.
+template <int COLS>
+__device__ __forceinline__ void small_sums(float (&sum)[COLS], uint32_t from, int chains, uint32_t pitch) {
+  for (int c = 0; c < chains; ++c) {
+    uint32_t x[COLS / 16][16];
+#pragma unroll
+    for (int q = 0; q < COLS / 16; ++q) tmem_ld16_issue(from + c * pitch + q * 16, x[q]);
+#pragma unroll
+    for (int q = 0; q < COLS / 16; ++q) {
+      tmem_ld_wait(x[q]);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sum[q * 16 + i] += __uint_as_float(x[q][i]);
+    }
+  }
+}
+
+// N: columns of A that are worked on (n rounded up to 64 or 128).
+template <int N>
+__device__ __forceinline__ void small_steps(const NsArgs& p, const NsEntry& e, int mat, uint32_t smem, uint32_t tmem, SmallWait wait, int blocks, int cb0, int rank) {
+  constexpr int COLS = N / 4, CAP = 512 / N;                 // a thread's columns of A; chains that the tensor memory holds at once
+  constexpr uint32_t ALONG = (128u >> 4) << 16, ALONG_HI = (1024u >> 4) | (1u << 14), ALONG_STEP = 256u >> 4;
+  constexpr uint32_t ACROSS = (1024u >> 4) << 16, ACROSS_HI = (128u >> 4) | (1u << 14), ACROSS_STEP = 2048u >> 4;
+  constexpr uint32_t ID = (1u << 4) | ((uint32_t)(TILE_M >> 4) << 24), ID_A = ID | ((uint32_t)(N >> 3) << 17), ID_X = ID | (1u << 16) | ((uint32_t)(64 >> 3) << 17);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quadrant = warp & 3, part = warp >> 2, row = quadrant * 32 + lane;
+  const uint32_t lanes = (uint32_t)(quadrant * 32) << 16, base = smem & 0x3FFFFu;
+  const int k_steps = (e.n + 15) / 16, k_chains = (k_steps + 1) / 2;
+  for (int step = 0; step < p.which; ++step) {
+    float sum[COLS];
+#pragma unroll
+    for (int i = 0; i < COLS; ++i) sum[i] = 0.f;
+    // the products of the CTA's own columns
+    for (int c0 = 0; c0 < 2 * blocks; c0 += CAP) {
+      const int chains = min(CAP, 2 * blocks - c0);
+      if (warp == 0) {
+        for (int c = 0; c < chains; ++c) {
+          const uint32_t x = ALONG | ((base + SMALL_X + (uint32_t)((c0 + c) >> 1) * NS_OPERAND + (uint32_t)((c0 + c) & 1) * 512u) >> 4);
+          small_chain(tmem + c * N, x, ALONG_HI, ALONG_STEP, x, ALONG_HI, ALONG_STEP, ID_A, 2);
+        }
+        umma_commit_warp(wait.bar);
+      }
+      wait();
+      small_sums<COLS>(sum, tmem + lanes + part * COLS, chains, N);
+      tc_fence_before();
+      __syncthreads();
+      tc_fence_after();
+    }
+    if (p.cs > 1) {
+      // Their sum over the cluster: this CTA adds N / cs columns, and gives them to all.
+#pragma unroll
+      for (int q = 0; q < COLS / 4; ++q)
+        asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(smem + SMALL_E + (uint32_t)(((part * (COLS / 4) + q) * 128 + row) * 16)), "f"(sum[4 * q]),
+                     "f"(sum[4 * q + 1]), "f"(sum[4 * q + 2]), "f"(sum[4 * q + 3]) : "memory");
+      cluster_sync();
+      const int groups = N / 8 / p.cs;                       // of eight columns
+      for (int x = threadIdx.x; x < 128 * groups; x += SMALL_THREADS) {
+        const int r = x & 127, q8 = rank * groups + (x >> 7);
+        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if ((r & ~31) < e.n) {
+          float4 f[SMALL_CLUSTER], g[SMALL_CLUSTER];
+#pragma unroll
+          for (int c = 0; c < SMALL_CLUSTER; ++c)
+            if (c < p.cs) {
+              f[c] = ld_cluster_f4(smem + SMALL_E + (uint32_t)((2 * q8 * 128 + r) * 16), c);
+              g[c] = ld_cluster_f4(smem + SMALL_E + (uint32_t)(((2 * q8 + 1) * 128 + r) * 16), c);
+            }
+#pragma unroll
+          for (int c = 0; c < SMALL_CLUSTER; ++c)
+            if (c < p.cs) {
+              v[0] += f[c].x; v[1] += f[c].y; v[2] += f[c].z; v[3] += f[c].w;
+              v[4] += g[c].x; v[5] += g[c].y; v[6] += g[c].z; v[7] += g[c].w;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] *= NS_UNSCALE;
+        uint4 hi, lo;
+        parts8(v, hi, lo);
+        const uint32_t at = smem + SMALL_A + (uint32_t)(q8 >> 3) * NS_OPERAND + piece_at(r, q8 & 7);
+        if (step == 0 || (r & ~31) < e.n)                    // (rows of zeros stay zeros)
+#pragma unroll
+          for (int c = 0; c < SMALL_CLUSTER; ++c)
+            if (c < p.cs) {
+              st_cluster_v4(at, c, hi);
+              st_cluster_v4(at + NS_PART, c, lo);
+            }
+      }
+      fence_async();
+      cluster_sync();
+      fence_async();
+    } else {
+#pragma unroll
+      for (int q = 0; q < COLS / 8; ++q) {
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = sum[q * 8 + i] * NS_UNSCALE;
+        uint4 hi, lo;
+        parts8(v, hi, lo);
+        const int q8 = part * (COLS / 8) + q;
+        const uint32_t at = smem + SMALL_A + (uint32_t)(q8 >> 3) * NS_OPERAND + piece_at(row, q8 & 7);
+        st_shared_v4(at, hi);
+        st_shared_v4(at + NS_PART, lo);
+      }
+      fence_async();
+      __syncthreads();
+    }
+    // A A, and B in A's place
+    if (warp == 0) {
+      tc_fence_after();
+      for (int c = 0; c < k_chains; ++c) {
+        const uint32_t x = ALONG | ((base + SMALL_A + (uint32_t)(c >> 1) * NS_OPERAND + (uint32_t)(c & 1) * 512u) >> 4);
+        small_chain(tmem + c * N, x, ALONG_HI, ALONG_STEP, x, ALONG_HI, ALONG_STEP, ID_A, min(2, k_steps - 2 * c));
+      }
+      umma_commit_warp(wait.bar);
+    }
+    wait();
+#pragma unroll
+    for (int i = 0; i < COLS; ++i) sum[i] = 0.f;
+    small_sums<COLS>(sum, tmem + lanes + part * COLS, k_chains, N);
+#pragma unroll
+    for (int q = 0; q < COLS / 8; ++q) {
+      const int q8 = part * (COLS / 8) + q;
+      const uint32_t at = smem + SMALL_A + (uint32_t)(q8 >> 3) * NS_OPERAND + piece_at(row, q8 & 7);
+      const uint4 ah = ld_shared_v4(at), al = ld_shared_v4(at + NS_PART);
+      const uint32_t h[4] = {ah.x, ah.y, ah.z, ah.w}, l[4] = {al.x, al.y, al.z, al.w};
+      const int d = row < e.n ? row - q8 * 8 : -1;
+      float v[8];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&h[k])), y = __half22float2(*reinterpret_cast<const __half2*>(&l[k]));
+        v[2 * k] = fmaf(p.c * NS_UNSCALE, sum[q * 8 + 2 * k], p.b * (x.x + y.x)) + (d == 2 * k ? p.a * NS_SCALE : 0.f);
+        v[2 * k + 1] = fmaf(p.c * NS_UNSCALE, sum[q * 8 + 2 * k + 1], p.b * (x.y + y.y)) + (d == 2 * k + 1 ? p.a * NS_SCALE : 0.f);
+      }
+      uint4 hi, lo;
+      parts8(v, hi, lo);
+      st_shared_v4(at, hi);
+      st_shared_v4(at + NS_PART, lo);
+    }
+    fence_async();
+    tc_fence_before();
+    __syncthreads();
+    // B X, block by block of X's columns, two at a time
+    const bool last = step + 1 == p.which;
+    for (int b0 = 0; b0 < blocks; b0 += 2) {
+      const int here = min(2, blocks - b0);
+      if (warp == 0) {
+        tc_fence_after();
+        for (int b = 0; b < here; ++b)
+          for (int c = 0; c < k_chains; ++c)
+            small_chain(tmem + (b * 4 + c) * 64, ALONG | ((base + SMALL_A + (uint32_t)(c >> 1) * NS_OPERAND + (uint32_t)(c & 1) * 512u) >> 4), ALONG_HI, ALONG_STEP,
+                        ACROSS | ((base + SMALL_X + (uint32_t)(b0 + b) * NS_OPERAND + (uint32_t)c * 4096u) >> 4), ACROSS_HI, ACROSS_STEP, ID_X, min(2, k_steps - 2 * c));
+        umma_commit_warp(wait.bar);
+      }
+      wait();
+      for (int b = 0; b < here; ++b) {
+        float x[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = 0.f;
+        small_sums<16>(x, tmem + lanes + b * 256 + part * 16, k_chains, 64);
+        if (!last) {
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = x[q * 8 + i] * NS_UNSCALE;
+            uint4 hi, lo;
+            parts8(v, hi, lo);
+            const uint32_t at = smem + SMALL_X + (uint32_t)(b0 + b) * NS_OPERAND + piece_at(row, part * 2 + q);
+            st_shared_v4(at, hi);
+            st_shared_v4(at + NS_PART, lo);
+          }
+        } else if (row < e.n) {
+          const size_t at = (size_t)mat * e.n * e.m;
+          const long c0 = (long)(cb0 + b0 + b) * NS_COLS + part * 16;
+          if (e.rows > e.cols) {
+#pragma unroll
+            for (int k = 0; k < 16; ++k)
+              if (c0 + k < e.m) ns_finish(p, e, at + (size_t)(c0 + k) * e.n + row, x[k]);
+          } else {
+#pragma unroll
+            for (int k = 0; k < 16; k += 4) ns_finish4(p, e, at + (size_t)row * e.m + c0 + k, e.m - c0 - k, make_float4(x[k], x[k + 1], x[k + 2], x[k + 3]));
+          }
+        }
+      }
+      if (!last) fence_async();
+      tc_fence_before();
+      __syncthreads();
+    }
+    if (warp == 0) tc_fence_after();
+  }
+}
+
+__global__ void __launch_bounds__(SMALL_THREADS, 1) ns_small_kernel(const __grid_constant__ NsArgs p) {
+  extern __shared__ uint8_t raw[];
+  __shared__ uint64_t done;
+  __shared__ uint32_t tmem_slot;
+  __shared__ double warp_sums[SMALL_THREADS / 32], cta_sums[SMALL_CLUSTER];
+  const uint32_t smem = (smem_u32(raw) + 1023u) & ~1023u;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = p.cs > 1 ? (int)cluster_rank() : 0, unit = (int)blockIdx.x / p.cs;
+  if (threadIdx.x == 0) {
+    mbar_init(&done, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 0) tmem_alloc_then_trigger(&tmem_slot, 512);
+  int k = 0;
+  while (k + 1 < p.t.entries && unit >= p.t.e[k + 1].sym0) ++k;
+  const NsEntry& e = p.t.e[k];
+  const int mat = unit - e.sym0, kt = x_cols(e), per = (kt + p.cs - 1) / p.cs, cb0 = rank * per, blocks = max(0, min(per, kt - cb0));
+  const bool tall = e.rows > e.cols;
+  pdl_wait();
+  if (blockIdx.x == 0 && threadIdx.x == 0) reinterpret_cast<volatile unsigned*>(p.status)[1] = p.tag;
+  // U of the CTA's columns, two pieces of eight columns a block and thread; a tall matrix's rows are X's columns
+  const size_t base = (size_t)mat * e.n * e.m;
+  float u[SMALL_COLUMN_BLOCKS * 2][8];
+  double s = 0.0;
+#pragma unroll
+  for (int i = 0; i < SMALL_COLUMN_BLOCKS * 2; ++i) {
+    const int piece = (i & 1) * SMALL_THREADS + threadIdx.x, r = tall ? piece & 127 : piece >> 3, q = tall ? piece >> 7 : piece & 7;
+    const long c0 = (long)(cb0 + (i >> 1)) * NS_COLS + q * 8;
+    const bool in = (i >> 1) < blocks && r < e.n;
+    float m[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const bool here = in && c0 + j < e.m;
+      const size_t at = base + (tall ? (size_t)(c0 + j) * e.n + r : (size_t)r * e.m + c0 + j);
+      u[i][j] = here ? load_as_float(e.g, e.g_dtype, at) : 0.f;
+      m[j] = here && p.muon ? e.mom[at] : 0.f;
+    }
+    if (p.muon)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const bool here = in && c0 + j < e.m;
+        const size_t at = base + (tall ? (size_t)(c0 + j) * e.n + r : (size_t)r * e.m + c0 + j);
+        m[j] = fmaf(1.f - p.momentum, u[i][j] - m[j], m[j]);
+        if (here) e.mom[at] = m[j];
+        u[i][j] = update_of(u[i][j], m[j], p.momentum, p.nesterov);
+      }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s += (double)u[i][j] * u[i][j];
+  }
+  // the norm, over the cluster in fixed order
+  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  if (lane == 0) warp_sums[warp] = s;
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (p.cs > 1) {
+    cluster_sync();                                          // (the others have begun)
+    if (threadIdx.x < p.cs) {
+      s = 0.0;
+      for (int w = 0; w < SMALL_THREADS / 32; ++w) s += warp_sums[w];
+      st_cluster_f64(smem_u32(&cta_sums[rank]), threadIdx.x, s);
+    }
+    __syncwarp();
+    cluster_sync();
+    s = 0.0;
+    for (int c = 0; c < p.cs; ++c) s += cta_sums[c];
+  } else {
+    s = 0.0;
+    for (int w = 0; w < SMALL_THREADS / 32; ++w) s += warp_sums[w];
+  }
+  const NsScale f(s, p.eps);
+#pragma unroll
+  for (int i = 0; i < SMALL_COLUMN_BLOCKS * 2; ++i) {
+    const int piece = (i & 1) * SMALL_THREADS + threadIdx.x, r = tall ? piece & 127 : piece >> 3, q = tall ? piece >> 7 : piece & 7;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) u[i][j] = f(u[i][j]);
+    uint4 hi, lo;
+    parts8(u[i], hi, lo);
+    const uint32_t at = smem + SMALL_X + (uint32_t)(i >> 1) * NS_OPERAND + piece_at(r, q);
+    st_shared_v4(at, hi);
+    st_shared_v4(at + NS_PART, lo);
+  }
+  fence_async();
+  __syncthreads();
+  const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&tmem_slot);
+  const SmallWait wait = {&done, 0u, p.status, p.tag};
+  if (e.n <= 64) small_steps<64>(p, e, mat, smem, tmem, wait, blocks, cb0, rank);
+  else small_steps<128>(p, e, mat, smem, tmem, wait, blocks, cb0, rank);
+  tc_fence_before();
+  __syncthreads();
+  if (p.cs > 1) cluster_sync_relaxed();                      // (no CTA ends while the others read its sums)
+  if (warp == 0) tmem_dealloc(tmem, 512);
+}
+
+// Whether all matrices are small ones.
+bool all_small(const NsTable& t) {
+  for (int k = 0; k < t.entries; ++k)
+    if (t.e[k].n > NS_ROWS || x_cols(t.e[k]) > SMALL_COLUMN_BLOCKS * SMALL_CLUSTER) return false;
+  return true;
+}
+
+cudaError_t launch_small(NsArgs& p, int matrices, cudaStream_t st) {
+  constexpr size_t smem = SMALL_BYTES + 1024;
+  int kt = 1;
+  for (int k = 0; k < p.t.entries; ++k) kt = std::max(kt, x_cols(p.t.e[k]));
+  p.cs = 1;
+  while (p.cs * SMALL_COLUMN_BLOCKS < kt) p.cs *= 2;
+  const cudaError_t e = cudaFuncSetAttribute(ns_small_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(matrices * p.cs));
+  cfg.blockDim = dim3(SMALL_THREADS);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)p.cs;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = p.cs > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, ns_small_kernel, p);
+}
+
 template <int MODE>
 cudaError_t launch_product(NsArgs& p, cudaStream_t st) {
   constexpr bool SYM = MODE == NS_GRAM || MODE == NS_SQUARE;
@@ -725,7 +1089,7 @@ void ns_add(NsTable* t, NsEntry e) {
   t->e[t->entries++] = e;
 }
 
-size_t ns_bytes(const NsTable& t) { return sums_bytes(t) + t.ws_blocks * NS_BLOCK; }
+size_t ns_bytes(const NsTable& t) { return all_small(t) ? 0 : sums_bytes(t) + t.ws_blocks * NS_BLOCK; }
 
 cudaError_t launch_newton_schulz(const NsTable& t, const NsOptions& o, void* ws, unsigned tag, cudaStream_t st, int* launches) {
   NsArgs p = {};
@@ -735,6 +1099,16 @@ cudaError_t launch_newton_schulz(const NsTable& t, const NsOptions& o, void* ws,
   p.sums = reinterpret_cast<double*>(static_cast<char*>(ws) + NS_HEADER);
   p.blocks = static_cast<char*>(ws) + NS_HEADER + sums_bytes(t);
   p.a = o.a; p.b = o.b; p.c = o.c; p.eps = o.eps; p.momentum = o.momentum; p.keep = o.keep; p.muon = o.muon; p.nesterov = o.nesterov;
+  if (all_small(t)) {
+    int matrices = 0;
+    for (int k = 0; k < t.entries; ++k) {
+      p.t.e[k].sym0 = matrices;
+      matrices += t.e[k].count;
+    }
+    p.which = o.steps;
+    ++*launches;
+    return launch_small(p, matrices, st);
+  }
   if (!map_blocks(&p.whole, &p.across, p.blocks, t.ws_blocks)) return cudaErrorInvalidValue;
   cudaError_t e = launch_pdl(ns_squares_kernel, dim3((unsigned)t.chunks), dim3(256), 0, st, p);
   if (e != cudaSuccess) return e;
