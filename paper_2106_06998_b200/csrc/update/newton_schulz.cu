@@ -673,8 +673,14 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_product_kernel(const __grid_
 // step: the products of the CTA's own columns, summed over the cluster through the SMs' network (each CTA sums some columns and gives them to the others), then A A
 // and B X in every CTA by itself.  Three chains of MMAs with a wait behind each; twelve in all where the cluster is one CTA.
 constexpr int SMALL_THREADS = 512, SMALL_COLUMN_BLOCKS = 3;
+constexpr int SMALL_ISSUERS = 4;                         // warps that issue MMAs, chains in turn: one warp takes some 80 clocks an MMA
+// X: 128 rows of 192 values, a part behind the other; as in a block, eight rows' pieces lie side by side, with 24 pieces a row.
+constexpr int SMALL_X_PIECES = SMALL_COLUMN_BLOCKS * 8;
+constexpr uint32_t SMALL_X_GROUP = SMALL_X_PIECES * 128, SMALL_X_PART = 16 * SMALL_X_GROUP;
+__device__ __forceinline__ uint32_t small_x_at(int row, int piece) { return (uint32_t)(row >> 3) * SMALL_X_GROUP + (uint32_t)(piece * 128 + (row & 7) * 16); }
 constexpr uint32_t SMALL_X = 0, SMALL_A = SMALL_COLUMN_BLOCKS * NS_OPERAND, SMALL_E = SMALL_A + 2 * NS_OPERAND, SMALL_BYTES = SMALL_E + 2 * NS_OPERAND;
 constexpr int SMALL_CLUSTER = 8;
+static_assert(SMALL_COLUMN_BLOCKS * 2 * SMALL_THREADS * 32 <= SMALL_BYTES - SMALL_A, "rows of U");
 
 __device__ __forceinline__ void st_cluster_v4(uint32_t addr, uint32_t rank, uint4 v) {
   asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %0, %1;\n\tst.shared::cluster.v4.b32 [a], {%2, %3, %4, %5};\n\t}"
@@ -688,12 +694,16 @@ __device__ __forceinline__ void st_shared_v4(uint32_t addr, uint4 v) {
 }
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async;" ::: "memory"); }
 
-// A chain of a product: two steps of 16 terms (or one), the small products first, into columns `d` of the tensor memory.
-__device__ __forceinline__ void small_chain(uint32_t d, uint32_t a, uint32_t a_hi, uint32_t a_step, uint32_t b, uint32_t b_hi, uint32_t b_step, uint32_t idesc, int steps) {
-  constexpr uint32_t L = NS_PART >> 4;
-  for (int t = 0; t < steps; ++t) umma_warp(d, a + L + t * a_step, a_hi, b + t * b_step, b_hi, idesc, t > 0);
-  for (int t = 0; t < steps; ++t) umma_warp(d, a + t * a_step, a_hi, b + L + t * b_step, b_hi, idesc, 1u);
-  for (int t = 0; t < steps; ++t) umma_warp(d, a + t * a_step, a_hi, b + t * b_step, b_hi, idesc, 1u);
+// An operand of the MMAs: its descriptor's halves, and what leads on to the next step of 16 terms and to the second part.
+struct SmallOperand { uint32_t lo, hi, step, part; };
+// A chain of a product: two steps of 16 terms, the small products first, into columns `d` of the tensor memory.
+__device__ __forceinline__ void small_chain(uint32_t d, const SmallOperand& a, const SmallOperand& b, uint32_t idesc) {
+  umma_warp(d, a.lo + a.part, a.hi, b.lo, b.hi, idesc, 0u);
+  umma_warp(d, a.lo + a.part + a.step, a.hi, b.lo + b.step, b.hi, idesc, 1u);
+  umma_warp(d, a.lo, a.hi, b.lo + b.part, b.hi, idesc, 1u);
+  umma_warp(d, a.lo + a.step, a.hi, b.lo + b.part + b.step, b.hi, idesc, 1u);
+  umma_warp(d, a.lo, a.hi, b.lo, b.hi, idesc, 1u);
+  umma_warp(d, a.lo + a.step, a.hi, b.lo + b.step, b.hi, idesc, 1u);
 }
 
 struct SmallWait {             // for the MMAs that were issued last, by all threads
@@ -707,18 +717,25 @@ struct SmallWait {             // for the MMAs that were issued last, by all thr
   }
 };
 
-// C columns of the chains' sums: COLS columns a thread from `from` on, chains `pitch` columns apart.
-template <int COLS>
-__device__ __forceinline__ void small_sums(float (&sum)[COLS], uint32_t from, int chains, uint32_t pitch) {
-  for (int c = 0; c < chains; ++c) {
-    uint32_t x[COLS / 16][16];
+// GROUPS groups of 16 columns of the chains' sums from `from` on, chains `pitch` columns apart; two chains are loaded at once.
+template <int GROUPS>
+__device__ __forceinline__ void small_sums(float (&sum)[GROUPS * 16], uint32_t from, int chains, uint32_t pitch) {
+#pragma unroll 1
+  for (int c = 0; c < chains; c += 2) {
+    const bool two = c + 1 < chains;
 #pragma unroll
-    for (int q = 0; q < COLS / 16; ++q) tmem_ld16_issue(from + c * pitch + q * 16, x[q]);
+    for (int q = 0; q < GROUPS; ++q) {
+      uint32_t x[16], y[16];
+      tmem_ld16_issue(from + c * pitch + q * 16, x);
+      if (two) tmem_ld16_issue(from + (c + 1) * pitch + q * 16, y);
+      tmem_ld_wait(x);
 #pragma unroll
-    for (int q = 0; q < COLS / 16; ++q) {
-      tmem_ld_wait(x[q]);
+      for (int i = 0; i < 16; ++i) sum[q * 16 + i] += __uint_as_float(x[i]);
+      if (two) {
+        tmem_ld_wait(y);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) sum[q * 16 + i] += __uint_as_float(x[q][i]);
+        for (int i = 0; i < 16; ++i) sum[q * 16 + i] += __uint_as_float(y[i]);
+      }
     }
   }
 }
@@ -727,12 +744,23 @@ __device__ __forceinline__ void small_sums(float (&sum)[COLS], uint32_t from, in
 template <int N>
 __device__ __forceinline__ void small_steps(const NsArgs& p, const NsEntry& e, int mat, uint32_t smem, uint32_t tmem, SmallWait wait, int blocks, int cb0, int rank) {
   constexpr int COLS = N / 4, CAP = 512 / N;                 // a thread's columns of A; chains that the tensor memory holds at once
-  constexpr uint32_t ALONG = (128u >> 4) << 16, ALONG_HI = (1024u >> 4) | (1u << 14), ALONG_STEP = 256u >> 4;
-  constexpr uint32_t ACROSS = (1024u >> 4) << 16, ACROSS_HI = (128u >> 4) | (1u << 14), ACROSS_STEP = 2048u >> 4;
-  constexpr uint32_t ID = (1u << 4) | ((uint32_t)(TILE_M >> 4) << 24), ID_A = ID | ((uint32_t)(N >> 3) << 17), ID_X = ID | (1u << 16) | ((uint32_t)(64 >> 3) << 17);
+  constexpr uint32_t ID = (1u << 4) | ((uint32_t)(TILE_M >> 4) << 24), ID_A = ID | ((uint32_t)(N >> 3) << 17);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quadrant = warp & 3, part = warp >> 2, row = quadrant * 32 + lane;
   const uint32_t lanes = (uint32_t)(quadrant * 32) << 16, base = smem & 0x3FFFFu;
-  const int k_steps = (e.n + 15) / 16, k_chains = (k_steps + 1) / 2;
+  const int k_chains = (e.n + 31) / 32;
+  // The operands of chain c: rows of X or A along the result, terms 32 c on; rows of X along the sum.
+  const auto x_along = [&](int c) {
+    return SmallOperand{((128u >> 4) << 16) | ((base + SMALL_X + (uint32_t)c * 512u) >> 4), (SMALL_X_GROUP >> 4) | (1u << 14), 256u >> 4, SMALL_X_PART >> 4};
+  };
+  const auto a_along = [&](int c) {
+    return SmallOperand{((128u >> 4) << 16) | ((base + SMALL_A + (uint32_t)(c >> 1) * NS_OPERAND + (uint32_t)(c & 1) * 512u) >> 4), (1024u >> 4) | (1u << 14), 256u >> 4,
+                        NS_PART >> 4};
+  };
+  const auto x_across = [&](int c, int block) {
+    return SmallOperand{((SMALL_X_GROUP >> 4) << 16) | ((base + SMALL_X + (uint32_t)c * 4u * SMALL_X_GROUP + (uint32_t)block * 1024u) >> 4), (128u >> 4) | (1u << 14), 2u * SMALL_X_GROUP >> 4,
+                        SMALL_X_PART >> 4};
+  };
+#pragma unroll 1
   for (int step = 0; step < p.which; ++step) {
     float sum[COLS];
 #pragma unroll
@@ -740,15 +768,15 @@ __device__ __forceinline__ void small_steps(const NsArgs& p, const NsEntry& e, i
     // the products of the CTA's own columns
     for (int c0 = 0; c0 < 2 * blocks; c0 += CAP) {
       const int chains = min(CAP, 2 * blocks - c0);
-      if (warp == 0) {
-        for (int c = 0; c < chains; ++c) {
-          const uint32_t x = ALONG | ((base + SMALL_X + (uint32_t)((c0 + c) >> 1) * NS_OPERAND + (uint32_t)((c0 + c) & 1) * 512u) >> 4);
-          small_chain(tmem + c * N, x, ALONG_HI, ALONG_STEP, x, ALONG_HI, ALONG_STEP, ID_A, 2);
+      if (warp < SMALL_ISSUERS) {
+        for (int c = warp; c < chains; c += SMALL_ISSUERS) {
+          const SmallOperand x = x_along(c0 + c);
+          small_chain(tmem + c * N, x, x, ID_A);
         }
         umma_commit_warp(wait.bar);
       }
       wait();
-      small_sums<COLS>(sum, tmem + lanes + part * COLS, chains, N);
+      small_sums<COLS / 16>(sum, tmem + lanes + part * COLS, chains, N);
       tc_fence_before();
       __syncthreads();
       tc_fence_after();
@@ -765,19 +793,21 @@ __device__ __forceinline__ void small_steps(const NsArgs& p, const NsEntry& e, i
         const int r = x & 127, q8 = rank * groups + (x >> 7);
         float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         if ((r & ~31) < e.n) {
-          float4 f[SMALL_CLUSTER], g[SMALL_CLUSTER];
+          for (int c0 = 0; c0 < p.cs; c0 += 4) {
+            float4 f[4], g[4];
 #pragma unroll
-          for (int c = 0; c < SMALL_CLUSTER; ++c)
-            if (c < p.cs) {
-              f[c] = ld_cluster_f4(smem + SMALL_E + (uint32_t)((2 * q8 * 128 + r) * 16), c);
-              g[c] = ld_cluster_f4(smem + SMALL_E + (uint32_t)(((2 * q8 + 1) * 128 + r) * 16), c);
-            }
+            for (int c = 0; c < 4; ++c)
+              if (c0 + c < p.cs) {
+                f[c] = ld_cluster_f4(smem + SMALL_E + (uint32_t)((2 * q8 * 128 + r) * 16), c0 + c);
+                g[c] = ld_cluster_f4(smem + SMALL_E + (uint32_t)(((2 * q8 + 1) * 128 + r) * 16), c0 + c);
+              }
 #pragma unroll
-          for (int c = 0; c < SMALL_CLUSTER; ++c)
-            if (c < p.cs) {
-              v[0] += f[c].x; v[1] += f[c].y; v[2] += f[c].z; v[3] += f[c].w;
-              v[4] += g[c].x; v[5] += g[c].y; v[6] += g[c].z; v[7] += g[c].w;
-            }
+            for (int c = 0; c < 4; ++c)
+              if (c0 + c < p.cs) {
+                v[0] += f[c].x; v[1] += f[c].y; v[2] += f[c].z; v[3] += f[c].w;
+                v[4] += g[c].x; v[5] += g[c].y; v[6] += g[c].z; v[7] += g[c].w;
+              }
+          }
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] *= NS_UNSCALE;
@@ -808,22 +838,22 @@ __device__ __forceinline__ void small_steps(const NsArgs& p, const NsEntry& e, i
         st_shared_v4(at, hi);
         st_shared_v4(at + NS_PART, lo);
       }
-      fence_async();
+      fence_async_smem();
       __syncthreads();
     }
     // A A, and B in A's place
-    if (warp == 0) {
+    if (warp < SMALL_ISSUERS) {
       tc_fence_after();
-      for (int c = 0; c < k_chains; ++c) {
-        const uint32_t x = ALONG | ((base + SMALL_A + (uint32_t)(c >> 1) * NS_OPERAND + (uint32_t)(c & 1) * 512u) >> 4);
-        small_chain(tmem + c * N, x, ALONG_HI, ALONG_STEP, x, ALONG_HI, ALONG_STEP, ID_A, min(2, k_steps - 2 * c));
+      for (int c = warp; c < k_chains; c += SMALL_ISSUERS) {
+        const SmallOperand x = a_along(c);
+        small_chain(tmem + c * N, x, x, ID_A);
       }
       umma_commit_warp(wait.bar);
     }
     wait();
 #pragma unroll
     for (int i = 0; i < COLS; ++i) sum[i] = 0.f;
-    small_sums<COLS>(sum, tmem + lanes + part * COLS, k_chains, N);
+    small_sums<COLS / 16>(sum, tmem + lanes + part * COLS, k_chains, N);
 #pragma unroll
     for (int q = 0; q < COLS / 8; ++q) {
       const int q8 = part * (COLS / 8) + q;
@@ -843,27 +873,31 @@ __device__ __forceinline__ void small_steps(const NsArgs& p, const NsEntry& e, i
       st_shared_v4(at, hi);
       st_shared_v4(at + NS_PART, lo);
     }
-    fence_async();
+    fence_async_smem();
     tc_fence_before();
     __syncthreads();
-    // B X, block by block of X's columns, two at a time
+    // B X: as many of the CTA's blocks of columns at once as the tensor memory holds the chains of
     const bool last = step + 1 == p.which;
-    for (int b0 = 0; b0 < blocks; b0 += 2) {
-      const int here = min(2, blocks - b0);
-      if (warp == 0) {
+    const auto result = [&](int r, int four, uint32_t pitch) { return smem + SMALL_E + (uint32_t)r * pitch * 4u + (uint32_t)((four ^ (r & 7)) << 4); };
+    const int at_once = k_chains <= 2 ? SMALL_COLUMN_BLOCKS : 2;
+#pragma unroll 1
+    for (int b0 = 0; b0 < blocks; b0 += at_once) {
+      const int here = min(at_once, blocks - b0);
+      const uint32_t pitch = (uint32_t)here * 64u;
+      if (warp < SMALL_ISSUERS) {
         tc_fence_after();
-        for (int b = 0; b < here; ++b)
-          for (int c = 0; c < k_chains; ++c)
-            small_chain(tmem + (b * 4 + c) * 64, ALONG | ((base + SMALL_A + (uint32_t)(c >> 1) * NS_OPERAND + (uint32_t)(c & 1) * 512u) >> 4), ALONG_HI, ALONG_STEP,
-                        ACROSS | ((base + SMALL_X + (uint32_t)(b0 + b) * NS_OPERAND + (uint32_t)c * 4096u) >> 4), ACROSS_HI, ACROSS_STEP, ID_X, min(2, k_steps - 2 * c));
+        const uint32_t id_x = ID | (1u << 16) | ((pitch >> 3) << 17);
+        for (int c = warp; c < k_chains; c += SMALL_ISSUERS) small_chain(tmem + c * pitch, a_along(c), x_across(c, b0), id_x);
         umma_commit_warp(wait.bar);
       }
       wait();
+#pragma unroll 1
       for (int b = 0; b < here; ++b) {
         float x[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) x[i] = 0.f;
-        small_sums<16>(x, tmem + lanes + b * 256 + part * 16, k_chains, 64);
+        small_sums<1>(x, tmem + lanes + b * 64 + part * 16, k_chains, pitch);
+        const int c8 = (b0 + b) * 8 + part * 2;              // of the CTA's pieces of eight columns
         if (!last) {
 #pragma unroll
           for (int q = 0; q < 2; ++q) {
@@ -872,29 +906,101 @@ __device__ __forceinline__ void small_steps(const NsArgs& p, const NsEntry& e, i
             for (int i = 0; i < 8; ++i) v[i] = x[q * 8 + i] * NS_UNSCALE;
             uint4 hi, lo;
             parts8(v, hi, lo);
-            const uint32_t at = smem + SMALL_X + (uint32_t)(b0 + b) * NS_OPERAND + piece_at(row, part * 2 + q);
+            const uint32_t at = smem + SMALL_X + small_x_at(row, c8 + q);
             st_shared_v4(at, hi);
-            st_shared_v4(at + NS_PART, lo);
+            st_shared_v4(at + SMALL_X_PART, lo);
           }
-        } else if (row < e.n) {
-          const size_t at = (size_t)mat * e.n * e.m;
-          const long c0 = (long)(cb0 + b0 + b) * NS_COLS + part * 16;
-          if (e.rows > e.cols) {
+        } else if (row < e.n) {                              // (128 rows of 128 columns, or 64 of 192: where the cluster's sums were)
 #pragma unroll
-            for (int k = 0; k < 16; ++k)
-              if (c0 + k < e.m) ns_finish(p, e, at + (size_t)(c0 + k) * e.n + row, x[k]);
-          } else {
-#pragma unroll
-            for (int k = 0; k < 16; k += 4) ns_finish4(p, e, at + (size_t)row * e.m + c0 + k, e.m - c0 - k, make_float4(x[k], x[k + 1], x[k + 2], x[k + 3]));
-          }
+          for (int k = 0; k < 4; ++k)
+            asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(result(row, b * 16 + part * 4 + k, pitch)), "f"(x[4 * k]), "f"(x[4 * k + 1]), "f"(x[4 * k + 2]),
+                         "f"(x[4 * k + 3]) : "memory");
         }
       }
-      if (!last) fence_async();
       tc_fence_before();
+      if (!last) fence_async_smem();
       __syncthreads();
+      if (last) {
+        // The result leaves in whole lines.
+        const size_t at = (size_t)mat * e.n * e.m;
+        const long col0 = (long)(cb0 + b0) * NS_COLS;
+        const int width = (int)min((long)pitch, e.m - col0);
+        if (e.rows > e.cols) {
+#pragma unroll 1
+          for (int i = threadIdx.x; i < 128 * width; i += SMALL_THREADS) {
+            const int r = i & 127, c = i >> 7;
+            if (r >= e.n) continue;
+            float v;
+            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(result(r, c >> 2, pitch) + (uint32_t)(c & 3) * 4));
+            ns_finish(p, e, at + (size_t)(col0 + c) * e.n + r, v);
+          }
+        } else {
+          const int fours = (width + 3) / 4;
+#pragma unroll 1
+          for (int i = threadIdx.x; i < e.n * fours; i += SMALL_THREADS) {
+            const int r = i / fours, c4 = i - r * fours;
+            ns_finish4(p, e, at + (size_t)r * e.m + col0 + c4 * 4, e.m - col0 - c4 * 4, ld_shared_f4(result(r, c4, pitch)));
+          }
+        }
+        __syncthreads();
+      }
     }
-    if (warp == 0) tc_fence_after();
+    if (warp < SMALL_ISSUERS) tc_fence_after();
   }
+}
+
+// Pieces 4 i + q0 of row r of the CTA's columns of U, as floats where the thread finds them again; the momenta take in the gradients on the way.  Returns the sum of
+// their squares.
+template <typename G>
+__device__ __forceinline__ double small_load(const NsArgs& p, const NsEntry& e, size_t base, int r, int q0, int cb0, int blocks, uint32_t to) {
+  const G* g = static_cast<const G*>(e.g) + base;
+  float* mom = p.muon ? e.mom + base : nullptr;
+  const bool tall = e.rows > e.cols, vec = !tall && e.m % 8 == 0;
+  double s = 0.0;
+#pragma unroll 2
+  for (int i = 0; i < 2 * blocks; ++i) {
+    const long c0 = (long)cb0 * NS_COLS + (i * 4 + q0) * 8;
+    const int left = r < e.n ? (int)min(8L, e.m - c0) : 0;   // (columns that are there)
+    const size_t at = tall ? (size_t)c0 * e.n + r : (size_t)r * e.m + c0, apart = tall ? e.n : 1;
+    float u[8], m[8];
+    if (vec) {
+      const float4 z = make_float4(0.f, 0.f, 0.f, 0.f), a = left > 0 ? ld4(g + at) : z, b = left > 0 ? ld4(g + at + 4) : z;
+      u[0] = a.x; u[1] = a.y; u[2] = a.z; u[3] = a.w; u[4] = b.x; u[5] = b.y; u[6] = b.z; u[7] = b.w;
+      if (mom) {
+        const float4 c = left > 0 ? ld4(mom + at) : z, d = left > 0 ? ld4(mom + at + 4) : z;
+        m[0] = c.x; m[1] = c.y; m[2] = c.z; m[3] = c.w; m[4] = d.x; m[5] = d.y; m[6] = d.z; m[7] = d.w;
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        u[j] = j < left ? to_f(g[at + j * apart]) : 0.f;
+        if (mom) m[j] = j < left ? mom[at + j * apart] : 0.f;
+      }
+    }
+    if (mom) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        m[j] = fmaf(1.f - p.momentum, u[j] - m[j], m[j]);
+        u[j] = update_of(u[j], m[j], p.momentum, p.nesterov);
+      }
+      if (vec) {
+        if (left > 0) {
+          st4(mom + at, make_float4(m[0], m[1], m[2], m[3]));
+          st4(mom + at + 4, make_float4(m[4], m[5], m[6], m[7]));
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (j < left) mom[at + j * apart] = m[j];
+      }
+    }
+    const uint32_t own = to + (uint32_t)(i * 2 * SMALL_THREADS + threadIdx.x) * 16;
+    st_shared_v4(own, make_uint4(__float_as_uint(u[0]), __float_as_uint(u[1]), __float_as_uint(u[2]), __float_as_uint(u[3])));
+    st_shared_v4(own + SMALL_THREADS * 16, make_uint4(__float_as_uint(u[4]), __float_as_uint(u[5]), __float_as_uint(u[6]), __float_as_uint(u[7])));
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s += (double)u[j] * u[j];
+  }
+  return s;
 }
 
 __global__ void __launch_bounds__(SMALL_THREADS, 1) ns_small_kernel(const __grid_constant__ NsArgs p) {
@@ -906,7 +1012,7 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ns_small_kernel(const __grid
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = p.cs > 1 ? (int)cluster_rank() : 0, unit = (int)blockIdx.x / p.cs;
   if (threadIdx.x == 0) {
-    mbar_init(&done, 1);
+    mbar_init(&done, SMALL_ISSUERS);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 0) tmem_alloc_then_trigger(&tmem_slot, 512);
@@ -914,38 +1020,15 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ns_small_kernel(const __grid
   while (k + 1 < p.t.entries && unit >= p.t.e[k + 1].sym0) ++k;
   const NsEntry& e = p.t.e[k];
   const int mat = unit - e.sym0, kt = x_cols(e), per = (kt + p.cs - 1) / p.cs, cb0 = rank * per, blocks = max(0, min(per, kt - cb0));
-  const bool tall = e.rows > e.cols;
   pdl_wait();
   if (blockIdx.x == 0 && threadIdx.x == 0) reinterpret_cast<volatile unsigned*>(p.status)[1] = p.tag;
-  // U of the CTA's columns, two pieces of eight columns a block and thread; a tall matrix's rows are X's columns
+  // U of the CTA's columns, two pieces of eight columns a block and thread (neighbouring threads have neighbouring rows); a tall matrix's rows are X's columns
   const size_t base = (size_t)mat * e.n * e.m;
-  float u[SMALL_COLUMN_BLOCKS * 2][8];
-  double s = 0.0;
-#pragma unroll
-  for (int i = 0; i < SMALL_COLUMN_BLOCKS * 2; ++i) {
-    const int piece = (i & 1) * SMALL_THREADS + threadIdx.x, r = tall ? piece & 127 : piece >> 3, q = tall ? piece >> 7 : piece & 7;
-    const long c0 = (long)(cb0 + (i >> 1)) * NS_COLS + q * 8;
-    const bool in = (i >> 1) < blocks && r < e.n;
-    float m[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const bool here = in && c0 + j < e.m;
-      const size_t at = base + (tall ? (size_t)(c0 + j) * e.n + r : (size_t)r * e.m + c0 + j);
-      u[i][j] = here ? load_as_float(e.g, e.g_dtype, at) : 0.f;
-      m[j] = here && p.muon ? e.mom[at] : 0.f;
-    }
-    if (p.muon)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const bool here = in && c0 + j < e.m;
-        const size_t at = base + (tall ? (size_t)(c0 + j) * e.n + r : (size_t)r * e.m + c0 + j);
-        m[j] = fmaf(1.f - p.momentum, u[i][j] - m[j], m[j]);
-        if (here) e.mom[at] = m[j];
-        u[i][j] = update_of(u[i][j], m[j], p.momentum, p.nesterov);
-      }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) s += (double)u[i][j] * u[i][j];
-  }
+  const int r = threadIdx.x & 127, q0 = threadIdx.x >> 7;
+  const uint32_t staged = smem + SMALL_A;                    // (a thread's own values)
+  double s = e.g_dtype == XCONV_F32    ? small_load<float>(p, e, base, r, q0, cb0, blocks, staged)
+             : e.g_dtype == XCONV_BF16 ? small_load<bf16>(p, e, base, r, q0, cb0, blocks, staged)
+                                       : small_load<f16>(p, e, base, r, q0, cb0, blocks, staged);
   // the norm, over the cluster in fixed order
   for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
   if (lane == 0) warp_sums[warp] = s;
@@ -968,18 +1051,17 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ns_small_kernel(const __grid
     for (int w = 0; w < SMALL_THREADS / 32; ++w) s += warp_sums[w];
   }
   const NsScale f(s, p.eps);
-#pragma unroll
-  for (int i = 0; i < SMALL_COLUMN_BLOCKS * 2; ++i) {
-    const int piece = (i & 1) * SMALL_THREADS + threadIdx.x, r = tall ? piece & 127 : piece >> 3, q = tall ? piece >> 7 : piece & 7;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) u[i][j] = f(u[i][j]);
+  for (int i = 0; i < 2 * blocks; ++i) {
+    const uint32_t own = staged + (uint32_t)(i * 2 * SMALL_THREADS + threadIdx.x) * 16;
+    const float4 a = ld_shared_f4(own), b = ld_shared_f4(own + SMALL_THREADS * 16);
+    const float v[8] = {f(a.x), f(a.y), f(a.z), f(a.w), f(b.x), f(b.y), f(b.z), f(b.w)};
     uint4 hi, lo;
-    parts8(u[i], hi, lo);
-    const uint32_t at = smem + SMALL_X + (uint32_t)(i >> 1) * NS_OPERAND + piece_at(r, q);
+    parts8(v, hi, lo);
+    const uint32_t at = smem + SMALL_X + small_x_at(r, i * 4 + q0);
     st_shared_v4(at, hi);
-    st_shared_v4(at + NS_PART, lo);
+    st_shared_v4(at + SMALL_X_PART, lo);
   }
-  fence_async();
+  fence_async_smem();
   __syncthreads();
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&tmem_slot);
   const SmallWait wait = {&done, 0u, p.status, p.tag};
