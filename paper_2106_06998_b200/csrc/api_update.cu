@@ -103,7 +103,11 @@ template <class F>
 xconv_status for_tables(const xconv_update_desc* d, const xconv_matrices* items, int count, bool muon, F&& f) {
   static thread_local NsTable t;
   t = NsTable{};
-  for (int k = 0; k < count; ++k) {
+  // The longest sums first: launches share those between their blocks of threads, and end with the short ones.
+  std::vector<int> order((size_t)count);
+  for (int k = 0; k < count; ++k) order[k] = k;
+  std::stable_sort(order.begin(), order.end(), [&](int x, int y) { return std::max(items[x].rows, items[x].cols) > std::max(items[y].rows, items[y].cols); });
+  for (const int k : order) {
     const xconv_matrices& m = items[k];
     const size_t each = ns_blocks_of(m.rows, m.cols), values = (size_t)m.rows * m.cols;
     for (int done = 0; done < m.batch;) {

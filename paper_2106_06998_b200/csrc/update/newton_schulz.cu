@@ -53,19 +53,8 @@ struct NsArgs {
   float a, b, c, momentum, keep;
   double eps;
   int muon, nesterov, which;   // which: the buffer that X is in (ns_small_kernel: the number of steps)
-  int cs;                      // pairs of CTAs a tile (ns_small_kernel: CTAs a matrix)
+  int cs, heavy;               // pairs of CTAs of a cluster, tiles that they share (the first ones; ns_small_kernel: CTAs a matrix)
 };
-
-__device__ __forceinline__ float load_as_float(const void* p, int dtype, size_t i) {
-  if (dtype == XCONV_F32) return static_cast<const float*>(p)[i];
-  if (dtype == XCONV_BF16) return to_f(static_cast<const bf16*>(p)[i]);
-  return to_f(static_cast<const f16*>(p)[i]);
-}
-__device__ __forceinline__ void store_from_float(void* p, int dtype, size_t i, float v) {
-  if (dtype == XCONV_F32) static_cast<float*>(p)[i] = v;
-  else if (dtype == XCONV_BF16) static_cast<bf16*>(p)[i] = from_f<bf16>(v);
-  else static_cast<f16*>(p)[i] = from_f<f16>(v);
-}
 
 __host__ __device__ __forceinline__ int chunks_of(const NsEntry& e) { return (int)(((long)e.n * e.m + NS_CHUNK - 1) / NS_CHUNK); }
 __host__ __device__ __forceinline__ int row_blocks(const NsEntry& e) { return (e.n + NS_ROWS - 1) / NS_ROWS; }
@@ -176,8 +165,36 @@ struct NsScale {
 
 // ---- X0 in blocks: a block of threads per block of 128 x 64 values
 
+// Eight neighbouring values of a row of U (X's columns c0 on), `left` of them there; G: the gradients' type.
+template <typename G>
+__device__ __forceinline__ void ns_load8(const NsArgs& p, const NsEntry& e, size_t base, long row, long c0, int left, float (&u)[8]) {
+  const G* g = static_cast<const G*>(e.g) + base;
+  const float* mom = p.muon ? e.mom + base : nullptr;
+  const bool tall = e.rows > e.cols;
+  const size_t at = tall ? (size_t)c0 * e.n + row : (size_t)row * e.m + c0, apart = tall ? e.n : 1;
+  if (!tall && e.m % 8 == 0) {
+    const float4 z = make_float4(0.f, 0.f, 0.f, 0.f), a = left > 0 ? ld4(g + at) : z, b = left > 0 ? ld4(g + at + 4) : z;
+    u[0] = a.x; u[1] = a.y; u[2] = a.z; u[3] = a.w; u[4] = b.x; u[5] = b.y; u[6] = b.z; u[7] = b.w;
+    if (mom && left > 0) {
+      const float4 c = __ldcg(reinterpret_cast<const float4*>(mom + at)), d = __ldcg(reinterpret_cast<const float4*>(mom + at + 4));
+      const float m[8] = {c.x, c.y, c.z, c.w, d.x, d.y, d.z, d.w};
+#pragma unroll
+      for (int j = 0; j < 8; ++j) u[j] = update_of(u[j], m[j], p.momentum, p.nesterov);
+    }
+  } else {
+    float m[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      u[j] = j < left ? to_f(g[at + j * apart]) : 0.f;
+      if (mom) m[j] = j < left ? __ldcg(mom + at + j * apart) : 0.f;
+    }
+    if (mom)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) u[j] = update_of(u[j], m[j], p.momentum, p.nesterov);
+  }
+}
+
 __global__ void __launch_bounds__(256) ns_blocks_kernel(const __grid_constant__ NsArgs p) {
-  __shared__ float tile[NS_ROWS][NS_COLS + 1];
   __shared__ double sums[8];
   int k = 0;
   while (k + 1 < p.t.entries && (int)blockIdx.x >= p.t.e[k + 1].block0) ++k;
@@ -190,37 +207,34 @@ __global__ void __launch_bounds__(256) ns_blocks_kernel(const __grid_constant__ 
   const int chunks = chunks_of(e);
   double s = 0.0;
   for (int i = tid; i < chunks; i += 256) s += __ldcg(p.sums + e.chunk0 + (long)mat * chunks + i);
+  // U of these rows and columns, pieces of eight values: neighbouring threads have neighbouring rows, whose pieces lie side by side
+  const size_t base = (size_t)mat * e.n * e.m;
+  const long row = (long)rb * NS_ROWS + (tid & (NS_ROWS - 1));
+  float u[4][8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const long c0 = (long)cb * NS_COLS + (i * 2 + tid / NS_ROWS) * 8;
+    const int left = row < e.n ? (int)max(0L, min(8L, e.m - c0)) : 0;
+    if (e.g_dtype == XCONV_F32) ns_load8<float>(p, e, base, row, c0, left, u[i]);
+    else if (e.g_dtype == XCONV_BF16) ns_load8<bf16>(p, e, base, row, c0, left, u[i]);
+    else ns_load8<f16>(p, e, base, row, c0, left, u[i]);
+  }
   for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
   if ((tid & 31) == 0) sums[tid >> 5] = s;
-  // U of these rows and columns; a tall matrix's rows are X's columns
-  const size_t base = (size_t)mat * e.n * e.m;
-  const bool tall = e.rows > e.cols;
-#pragma unroll 8
-  for (int i = tid; i < NS_ROWS * NS_COLS; i += 256) {
-    const int r = tall ? i % NS_ROWS : i / NS_COLS, c = tall ? i / NS_ROWS : i % NS_COLS;
-    const long row = (long)rb * NS_ROWS + r, col = (long)cb * NS_COLS + c;
-    float u = 0.f;
-    if (row < e.n && col < e.m) {
-      const size_t j = base + (tall ? (size_t)col * e.n + row : (size_t)row * e.m + col);
-      u = load_as_float(e.g, e.g_dtype, j);
-      if (p.muon) u = update_of(u, __ldcg(e.mom + j), p.momentum, p.nesterov);
-    }
-    tile[r][c] = u;
-  }
   __syncthreads();
   s = sums[0];
   for (int w = 1; w < 8; ++w) s += sums[w];
   const NsScale f(s, p.eps);
   char* out = p.blocks + ((size_t)e.x0 + (size_t)mat * per + at) * NS_BLOCK;
-  for (int i = tid; i < NS_ROWS * 8; i += 256) {
-    const int r = i & (NS_ROWS - 1), q = i / NS_ROWS;
-    float v[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = f(tile[r][q * 8 + j]);
+  for (int i = 0; i < 4; ++i) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) u[i][j] = f(u[i][j]);
     uint4 hi, lo;
-    parts8(v, hi, lo);
-    *reinterpret_cast<uint4*>(out + piece_at(r, q)) = hi;
-    *reinterpret_cast<uint4*>(out + NS_PART + piece_at(r, q)) = lo;
+    parts8(u[i], hi, lo);
+    const uint32_t to = piece_at(tid & (NS_ROWS - 1), i * 2 + tid / NS_ROWS);
+    *reinterpret_cast<uint4*>(out + to) = hi;
+    *reinterpret_cast<uint4*>(out + NS_PART + to) = lo;
   }
 }
 
@@ -311,36 +325,55 @@ __device__ __forceinline__ NsUnit ns_unit(const NsEntry* es, int entries, int u,
   return w;
 }
 
-// An element of the result, from its sum: the orthogonalised matrix's, or the weight that it moves.
-__device__ __forceinline__ void ns_finish(const NsArgs& p, const NsEntry& e, size_t at, float sum) {
-  float o = sum * (NS_UNSCALE * NS_UNSCALE);
-  if (p.muon) o = fmaf(-e.scale, o, p.keep * load_as_float(e.out, e.out_dtype, at));
-  store_from_float(e.out, e.out_dtype, at, o);
+// Elements of the result, from their sums: the orthogonalised matrix's, or the weights that they move.
+__device__ __forceinline__ float ns_result(const NsArgs& p, const NsEntry& e, float sum, float weight) {
+  const float o = sum * (NS_UNSCALE * NS_UNSCALE);
+  return p.muon ? fmaf(-e.scale, o, p.keep * weight) : o;
 }
-template <typename T>
-__device__ __forceinline__ void ns_finish4_of(const NsArgs& p, const NsEntry& e, size_t at, float4 v) {
+// COUNT groups of four neighbouring ones, `apart` elements from each other, of which `left` values are there in each and `groups` groups; the weights are loaded
+// together.
+template <typename T, int COUNT>
+__device__ __forceinline__ void ns_finish4_of(const NsArgs& p, const NsEntry& e, size_t at, size_t apart, long left, int groups, const float (*v)[4]) {
   T* out = static_cast<T*>(e.out) + at;
-  constexpr float S = NS_UNSCALE * NS_UNSCALE;
-  float4 o = make_float4(v.x * S, v.y * S, v.z * S, v.w * S);
-  if (p.muon) {
-    const float4 w = ld4(out);
-    o = make_float4(fmaf(-e.scale, o.x, p.keep * w.x), fmaf(-e.scale, o.y, p.keep * w.y), fmaf(-e.scale, o.z, p.keep * w.z), fmaf(-e.scale, o.w, p.keep * w.w));
-  }
-  st4(out, o);
-}
-// ... and four neighbouring ones of a row, of which `left` are there.
-__device__ __forceinline__ void ns_finish4(const NsArgs& p, const NsEntry& e, size_t at, long left, float4 v) {
+  float4 w[COUNT];
   if (e.m % 4 == 0) {
     if (left <= 0) return;
-    if (e.out_dtype == XCONV_F32) ns_finish4_of<float>(p, e, at, v);
-    else if (e.out_dtype == XCONV_BF16) ns_finish4_of<bf16>(p, e, at, v);
-    else ns_finish4_of<f16>(p, e, at, v);
+    if (p.muon)
+#pragma unroll
+      for (int k = 0; k < COUNT; ++k) w[k] = k < groups ? ld4(out + k * apart) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int k = 0; k < COUNT; ++k)
+      if (k < groups)
+        st4(out + k * apart, make_float4(ns_result(p, e, v[k][0], w[k].x), ns_result(p, e, v[k][1], w[k].y), ns_result(p, e, v[k][2], w[k].z), ns_result(p, e, v[k][3], w[k].w)));
     return;
   }
-  if (left > 0) ns_finish(p, e, at, v.x);
-  if (left > 1) ns_finish(p, e, at + 1, v.y);
-  if (left > 2) ns_finish(p, e, at + 2, v.z);
-  if (left > 3) ns_finish(p, e, at + 3, v.w);
+#pragma unroll
+  for (int k = 0; k < COUNT; ++k) {
+    if (k >= groups) continue;
+    float a[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) a[j] = p.muon && j < left ? to_f(out[k * apart + j]) : 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (j < left) out[k * apart + j] = from_f<T>(ns_result(p, e, v[k][j], a[j]));
+  }
+}
+template <int COUNT>
+__device__ __forceinline__ void ns_finish4(const NsArgs& p, const NsEntry& e, size_t at, size_t apart, long left, int groups, const float (*v)[4]) {
+  if (e.out_dtype == XCONV_F32) ns_finish4_of<float, COUNT>(p, e, at, apart, left, groups, v);
+  else if (e.out_dtype == XCONV_BF16) ns_finish4_of<bf16, COUNT>(p, e, at, apart, left, groups, v);
+  else ns_finish4_of<f16, COUNT>(p, e, at, apart, left, groups, v);
+}
+// Eight elements of a column of a tall matrix's result, a row's length apart.
+template <typename T>
+__device__ __forceinline__ void ns_finish_across_of(const NsArgs& p, const NsEntry& e, size_t at, long left, const float (&v)[8]) {
+  T* out = static_cast<T*>(e.out) + at;
+  float w[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) w[k] = p.muon && k < left ? to_f(out[(size_t)k * e.n]) : 0.f;
+#pragma unroll
+  for (int k = 0; k < 8; ++k)
+    if (k < left) out[(size_t)k * e.n] = from_f<T>(ns_result(p, e, v[k], w[k]));
 }
 
 // N groups of eight neighbouring sums of a row of this CTA's half of a tile, from column 8 * q8 on (within a block's 64 columns).
@@ -389,12 +422,14 @@ __device__ __forceinline__ void ns_emit(const NsArgs& p, const NsEntry& e, const
     for (int g = 0; g < N; ++g) {
       const long c0 = (long)w.J * NS_TILE + (q8 + g) * 8;
       if (e.rows > e.cols) {
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-          if (c0 + k < e.m) ns_finish(p, e, base + (size_t)(c0 + k) * e.n + r, v[g][k]);
+        const size_t at = base + (size_t)c0 * e.n + r;
+        if (e.out_dtype == XCONV_F32) ns_finish_across_of<float>(p, e, at, e.m - c0, v[g]);
+        else if (e.out_dtype == XCONV_BF16) ns_finish_across_of<bf16>(p, e, at, e.m - c0, v[g]);
+        else ns_finish_across_of<f16>(p, e, at, e.m - c0, v[g]);
       } else {
-        ns_finish4(p, e, base + (size_t)r * e.m + c0, e.m - c0, make_float4(v[g][0], v[g][1], v[g][2], v[g][3]));
-        ns_finish4(p, e, base + (size_t)r * e.m + c0 + 4, e.m - c0 - 4, make_float4(v[g][4], v[g][5], v[g][6], v[g][7]));
+        const float f[2][4] = {{v[g][0], v[g][1], v[g][2], v[g][3]}, {v[g][4], v[g][5], v[g][6], v[g][7]}};
+        ns_finish4<1>(p, e, base + (size_t)r * e.m + c0, 0, e.m - c0, 1, &f[0]);
+        ns_finish4<1>(p, e, base + (size_t)r * e.m + c0 + 4, 0, e.m - c0 - 4, 1, &f[1]);
       }
     }
   }
@@ -426,8 +461,8 @@ __device__ __forceinline__ void ns_emit_rows(const NsArgs& p, const NsEntry& e, 
       }
     const long c = c0 + b * 32;
 #pragma unroll
-    for (int u = 0; u < 8; ++u)
-      if (r0 + u < e.n) ns_finish4(p, e, base + (size_t)(r0 + u) * e.m + c, e.m - c, make_float4(v[u][0], v[u][1], v[u][2], v[u][3]));
+    for (int u = 0; u < 8; u += 2)
+      ns_finish4<2>(p, e, base + (size_t)(r0 + u) * e.m + c, e.m, e.m - c, (int)max(0L, min(2L, e.n - r0 - u)), &v[u]);
   }
 }
 
@@ -449,8 +484,11 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_product_kernel(const __grid_
     prefetch_tmap(&p.whole);
     prefetch_tmap(&p.across);
   }
-  const int part = (int)(rank >> 1);                 // of the tile's terms
-  const int units = SYM ? p.t.syms : p.t.prods, per = 2 * p.cs, u0 = (int)blockIdx.x / per, step = (int)gridDim.x / per;
+  // A cluster of one pair takes every so-manyth tile; a larger one shares a tile that is heavy, or each of its pairs has a tile of its own.
+  const int units = SYM ? p.t.syms : p.t.prods, pair = (int)(rank >> 1), cluster = (int)blockIdx.x / (2 * p.cs);
+  const bool shared = p.cs > 1 && cluster < p.heavy;
+  const int split = shared ? p.cs : 1, part = shared ? pair : 0;      // of the tile's terms
+  const int u0 = p.cs == 1 || shared ? cluster : p.heavy + (cluster - p.heavy) * p.cs + pair, step = p.cs == 1 ? (int)gridDim.x / 2 : units;
   for (int i = threadIdx.x; i < entries * (int)(sizeof(NsEntry) / 4); i += NS_THREADS)
     reinterpret_cast<uint32_t*>(es)[i] = reinterpret_cast<const uint32_t*>(p.t.e)[i];
   if (warp == 1) pair_alloc_then_trigger(&tmem_slot);
@@ -459,7 +497,7 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_product_kernel(const __grid_
   __syncthreads();
   if (threadIdx.x == 0) {                            // (while the kernel before still runs)
     int k = 0;
-    first = ns_unit<MODE>(es, entries, u0, k);
+    first = ns_unit<MODE>(es, entries, min(u0, units - 1), k);
   }
   tc_fence_before();
   __syncthreads();
@@ -483,7 +521,7 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_product_kernel(const __grid_
         uint32_t bytes = (uint32_t)min(2, nt - 2 * w.I) * NS_OPERAND;
         if (SYM) bytes += same ? 0u : (uint32_t)min(2, nt - 2 * w.J) * NS_OPERAND;
         else bytes += kt - 4 * w.J > 2 ? 2 * NS_OPERAND : NS_OPERAND;
-        const int s0 = w.stages * part / p.cs, s1 = w.stages * (part + 1) / p.cs;
+        const int s0 = w.stages * part / split, s1 = w.stages * (part + 1) / split;
         for (int s = s0; s < s1; ++s) {
           if (issued >= NS_STAGES && !mbar_wait(&empty[slot], lap ^ 1u, p.status, p.tag)) { ok = false; break; }
           const uint32_t to = smem + slot * NS_STAGE;
@@ -539,7 +577,7 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_product_kernel(const __grid_
       for (int u = u0; u < units && ok; u += step) {
         const NsUnit w = u == u0 ? first : ns_unit<MODE>(es, entries, u, k);
         const bool same = SYM && w.I == w.J;
-        const int s0 = w.stages * part / p.cs, s1 = w.stages * (part + 1) / p.cs;
+        const int s0 = w.stages * part / split, s1 = w.stages * (part + 1) / split;
         for (int s = s0; s < s1 && ok; ++s) {
           if (!mbar_wait_warp(&full[slot], lap, p.status, p.tag)) { ok = false; break; }
           tc_fence_after();
@@ -587,7 +625,7 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_product_kernel(const __grid_
       float sum[64];
 #pragma unroll
       for (int i = 0; i < 64; ++i) sum[i] = 0.f;
-      const int s0 = w.stages * part / p.cs, s1 = w.stages * (part + 1) / p.cs;
+      const int s0 = w.stages * part / split, s1 = w.stages * (part + 1) / split;
       for (int s = s0 * (4 / NS_CHAIN); s < s1 * (4 / NS_CHAIN); ++s) {
         if (!mbar_wait_warp(&acc_full[set], set_lap, p.status, p.tag)) { ok = false; break; }
         tc_fence_after();
@@ -609,9 +647,9 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_product_kernel(const __grid_
         if (++set == NS_SETS) { set = 0; set_lap ^= 1u; }
       }
       if (!ok) break;
-      if (p.cs == 1 && MODE == NS_LAST && es[w.k].rows <= es[w.k].cols) {
+      if (!shared && MODE == NS_LAST && es[w.k].rows <= es[w.k].cols) {
         ns_emit_rows(p, es[w.k], w, (int)half, row, quarter, sum);
-      } else if (p.cs == 1) {
+      } else if (!shared) {
 #pragma unroll
         for (int q = 0; q < 8; q += 2) {
           float v[2][8];
@@ -631,11 +669,11 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_product_kernel(const __grid_
   __syncwarp();
   tc_fence_before();
   // No arrival and no copy of the pair comes behind this.
-  if (p.cs == 1) {
+  if (!shared) {
     cluster_sync_relaxed();
   } else {
     cluster_sync();
-    if (warp >= 2 && u0 < units) {
+    if (warp >= 2) {
       const NsUnit& w = first;
       const NsEntry& e = es[w.k];
       // This CTA's groups of eight columns; neighbouring lanes have neighbouring rows, or, where rows of the result are written, neighbouring columns.
@@ -738,6 +776,54 @@ __device__ __forceinline__ void small_sums(float (&sum)[GROUPS * 16], uint32_t f
       }
     }
   }
+}
+
+// Four columns of row r of the result in shared memory, rows of `pitch` floats.
+__device__ __forceinline__ uint32_t small_result_at(uint32_t from, int r, int four, uint32_t pitch) {
+  return from + (uint32_t)r * pitch * 4u + (uint32_t)((four ^ (r & 7)) << 4);
+}
+// The result's columns from col0 on leave in whole lines.  (A function of its own: its code and registers stay out of the steps'.)
+template <typename T>
+__device__ __forceinline__ void small_write_of(const NsArgs& p, const NsEntry& e, int mat, uint32_t from, uint32_t pitch, long col0) {
+  T* out = static_cast<T*>(e.out) + (size_t)mat * e.n * e.m;
+  const int width = (int)min((long)pitch, e.m - col0);
+  if (e.rows > e.cols) {
+#pragma unroll 4
+    for (int i = threadIdx.x; i < 128 * width; i += SMALL_THREADS) {
+      const int r = i & 127, c = i >> 7;
+      if (r >= e.n) continue;
+      float v;
+      asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(small_result_at(from, r, c >> 2, pitch) + (uint32_t)(c & 3) * 4));
+      T* to = out + (size_t)(col0 + c) * e.n + r;
+      *to = from_f<T>(ns_result(p, e, v, p.muon ? to_f(*to) : 0.f));
+    }
+  } else {
+    const int fours = (width + 3) / 4;
+    const bool vec = e.m % 4 == 0;
+#pragma unroll 2
+    for (int i = threadIdx.x; i < e.n * fours; i += SMALL_THREADS) {
+      const int r = i / fours, c4 = i - r * fours, left = width - c4 * 4;
+      const float4 f = ld_shared_f4(small_result_at(from, r, c4, pitch));
+      T* to = out + (size_t)r * e.m + col0 + c4 * 4;
+      if (vec) {
+        const float4 w = p.muon ? ld4(to) : make_float4(0.f, 0.f, 0.f, 0.f);
+        st4(to, make_float4(ns_result(p, e, f.x, w.x), ns_result(p, e, f.y, w.y), ns_result(p, e, f.z, w.z), ns_result(p, e, f.w, w.w)));
+      } else {
+        const float v[4] = {f.x, f.y, f.z, f.w};
+        float w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = p.muon && j < left ? to_f(to[j]) : 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (j < left) to[j] = from_f<T>(ns_result(p, e, v[j], w[j]));
+      }
+    }
+  }
+}
+__device__ __noinline__ void small_write(const NsArgs& p, const NsEntry& e, int mat, uint32_t from, uint32_t pitch, long col0) {
+  if (e.out_dtype == XCONV_F32) small_write_of<float>(p, e, mat, from, pitch, col0);
+  else if (e.out_dtype == XCONV_BF16) small_write_of<bf16>(p, e, mat, from, pitch, col0);
+  else small_write_of<f16>(p, e, mat, from, pitch, col0);
 }
 
 // N: columns of A that are worked on (n rounded up to 64 or 128).
@@ -878,7 +964,6 @@ __device__ __forceinline__ void small_steps(const NsArgs& p, const NsEntry& e, i
     __syncthreads();
     // B X: as many of the CTA's blocks of columns at once as the tensor memory holds the chains of
     const bool last = step + 1 == p.which;
-    const auto result = [&](int r, int four, uint32_t pitch) { return smem + SMALL_E + (uint32_t)r * pitch * 4u + (uint32_t)((four ^ (r & 7)) << 4); };
     const int at_once = k_chains <= 2 ? SMALL_COLUMN_BLOCKS : 2;
 #pragma unroll 1
     for (int b0 = 0; b0 < blocks; b0 += at_once) {
@@ -913,7 +998,7 @@ __device__ __forceinline__ void small_steps(const NsArgs& p, const NsEntry& e, i
         } else if (row < e.n) {                              // (128 rows of 128 columns, or 64 of 192: where the cluster's sums were)
 #pragma unroll
           for (int k = 0; k < 4; ++k)
-            asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(result(row, b * 16 + part * 4 + k, pitch)), "f"(x[4 * k]), "f"(x[4 * k + 1]), "f"(x[4 * k + 2]),
+            asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(small_result_at(smem + SMALL_E, row, b * 16 + part * 4 + k, pitch)), "f"(x[4 * k]), "f"(x[4 * k + 1]), "f"(x[4 * k + 2]),
                          "f"(x[4 * k + 3]) : "memory");
         }
       }
@@ -921,27 +1006,7 @@ __device__ __forceinline__ void small_steps(const NsArgs& p, const NsEntry& e, i
       if (!last) fence_async_smem();
       __syncthreads();
       if (last) {
-        // The result leaves in whole lines.
-        const size_t at = (size_t)mat * e.n * e.m;
-        const long col0 = (long)(cb0 + b0) * NS_COLS;
-        const int width = (int)min((long)pitch, e.m - col0);
-        if (e.rows > e.cols) {
-#pragma unroll 1
-          for (int i = threadIdx.x; i < 128 * width; i += SMALL_THREADS) {
-            const int r = i & 127, c = i >> 7;
-            if (r >= e.n) continue;
-            float v;
-            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(result(r, c >> 2, pitch) + (uint32_t)(c & 3) * 4));
-            ns_finish(p, e, at + (size_t)(col0 + c) * e.n + r, v);
-          }
-        } else {
-          const int fours = (width + 3) / 4;
-#pragma unroll 1
-          for (int i = threadIdx.x; i < e.n * fours; i += SMALL_THREADS) {
-            const int r = i / fours, c4 = i - r * fours;
-            ns_finish4(p, e, at + (size_t)r * e.m + col0 + c4 * 4, e.m - col0 - c4 * 4, ld_shared_f4(result(r, c4, pitch)));
-          }
-        }
+        small_write(p, e, mat, smem + SMALL_E, pitch, (long)(cb0 + b0) * NS_COLS);
         __syncthreads();
       }
     }
@@ -1104,20 +1169,51 @@ cudaError_t launch_small(NsArgs& p, int matrices, cudaStream_t st) {
   return cudaLaunchKernelEx(&cfg, ns_small_kernel, p);
 }
 
+// How the tiles of a launch go to the pairs of CTAs: by the times that a stage (1800 clocks), a tile's results (3000) and sums that pairs exchange (11000) take.  The
+// entries' tiles are in the order of the table, the longest sums first.
+struct NsSharing { int cs, heavy; };
+template <typename Stages, typename Units>
+NsSharing share(const NsTable& t, int units, Stages&& stages, Units&& units_of) {
+  double all = 0.0;
+  int longest = 1;
+  for (int k = 0; k < t.entries; ++k) {
+    all += (double)units_of(t.e[k]) * stages(t.e[k]);
+    longest = std::max(longest, stages(t.e[k]));
+  }
+  const int pairs = NS_SMS / 2;
+  NsSharing best = {1, 0};
+  double least = 1800.0 * std::max<double>(longest, all / pairs) + 3000.0 * ((units + pairs - 1) / pairs);
+  // (clusters that are on the SMs at once: eight CTAs within a group of 16 to 20 SMs, two or three short of the SMs' number)
+  for (const NsSharing& size : {NsSharing{2, 32}, NsSharing{4, 16}}) {
+    int heavy = 0, first = 1;
+    for (int k = 0; k < t.entries; ++k) {
+      heavy += units_of(t.e[k]);
+      first = std::max(first, stages(t.e[k]));
+      int rest = 0;
+      for (int j = k + 1; j < t.entries; ++j) rest = std::max(rest, stages(t.e[j]));
+      if (heavy + (units - heavy + size.cs - 1) / size.cs > size.heavy) break;
+      const double time = std::max(1800.0 * ((first + size.cs - 1) / size.cs) + 11000.0, rest ? 1800.0 * rest + 3000.0 : 0.0);
+      if (time < least) { least = time; best = {size.cs, heavy}; }
+    }
+  }
+  return best;
+}
+
 template <int MODE>
 cudaError_t launch_product(NsArgs& p, cudaStream_t st) {
   constexpr bool SYM = MODE == NS_GRAM || MODE == NS_SQUARE;
   constexpr size_t smem = NS_STAGES * NS_STAGE + 1024;
   const int units = SYM ? p.t.syms : p.t.prods;
-  // A pair has a stage at least where the longest sum has that many.
-  int stages = 1;
-  for (int k = 0; k < p.t.entries; ++k) stages = std::max(stages, MODE == NS_GRAM ? x_cols(p.t.e[k]) : a_terms(p.t.e[k]));
-  p.cs = 1;
-  while (p.cs < 4 && units * p.cs * 4 <= NS_SMS && p.cs * 2 <= stages) p.cs *= 2;
+  const NsSharing how = share(p.t, units, [](const NsEntry& e) { return MODE == NS_GRAM ? x_cols(e) : a_terms(e); }, [](const NsEntry& e) {
+    const int rows = tiles(row_blocks(e), 2);
+    return e.count * (SYM ? rows * (rows + 1) / 2 : rows * tiles(x_cols(e), 4));
+  });
+  p.cs = how.cs;
+  p.heavy = how.heavy;
   cudaError_t e = cudaFuncSetAttribute(ns_product_kernel<MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(p.cs > 1 ? units * p.cs * 2 : std::min(2 * units, NS_SMS)));
+  cfg.gridDim = dim3((unsigned)(p.cs > 1 ? 2 * p.cs * (p.heavy + (units - p.heavy + p.cs - 1) / p.cs) : std::min(2 * units, NS_SMS)));
   cfg.blockDim = dim3(NS_THREADS);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
