@@ -83,6 +83,23 @@ __device__ __forceinline__ void copy16_async_if(uint32_t dst, const void* src, b
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
+// Two values of 16 bits in a word.
+template <typename T>
+__device__ __forceinline__ float2 unpack2(uint32_t u) {
+  if constexpr (std::is_same<T, bf16>::value) return make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u));
+  else return __half22float2(*reinterpret_cast<const __half2*>(&u));
+}
+template <typename T>
+__device__ __forceinline__ uint32_t pack2(float x, float y) {
+  if constexpr (std::is_same<T, bf16>::value) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(x, y);
+    return *reinterpret_cast<const uint32_t*>(&v);
+  } else {
+    const __half2 v = __floats2half2_rn(x, y);
+    return *reinterpret_cast<const uint32_t*>(&v);
+  }
+}
+
 // VEC parameters (weight, bias): VEC elements of the activations are up to 32 bytes of them.
 template <typename P, int VEC>
 __device__ __forceinline__ void load_params(const P* p, float (&f)[VEC]) {
@@ -144,8 +161,9 @@ __device__ __forceinline__ Pair both(float x) { return {make_float2(x, x)}; }
 template <int V> __device__ __forceinline__ constexpr bool all_have(int v) { return v < (V <= 8 ? V - 1 : V == 12 ? 8 : 12); }
 
 // A row's values less their mean in x, and y's factor.  FULL: every thread of the row has V whole vectors.
-template <int VEC, int V, bool FULL>
-__device__ __forceinline__ void norm_row(const NormArgs& a, int lane, float (&x)[V][VEC], float& mean, float& rstd, float (*sums)[32][1]) {
+struct NormAll { __device__ __forceinline__ constexpr bool operator()(int, int) const { return true; } };
+template <int VEC, int V, bool FULL, class Has = NormAll>
+__device__ __forceinline__ void norm_row(const NormArgs& a, int lane, float (&x)[V][VEC], float& mean, float& rstd, float (*sums)[32][1], Has has = Has()) {
   constexpr int STEP = VEC > 1 ? 2 : 1;
   Pair t = both(0.f);
 #pragma unroll
@@ -162,7 +180,9 @@ __device__ __forceinline__ void norm_row(const NormArgs& a, int lane, float (&x)
     if (FULL || all_have<V>(v) || (lane + v * a.group) * VEC < a.C)
 #pragma unroll
       for (int e = 0; e < VEC; e += STEP) {
-        const Pair d = add<VEC>(Pair::of(x[v], e), both(-mean));
+        Pair d = add<VEC>(Pair::of(x[v], e), both(-mean));
+        if (!has(v, e)) d.v.x = 0.f;
+        if (VEC > 1 && !has(v, e + 1)) d.v.y = 0.f;
         d.to(x[v], e);
         t = fma<VEC>(d, d, t);
       }
@@ -212,10 +232,12 @@ __device__ __forceinline__ void norm_row_backward(const NormArgs& a, int lane, f
     for (int e = 0; e < VEC; e += STEP) mul<VEC>(r, fma<VEC>(Pair::of(x[v], e), m1, add<VEC>(Pair::of(dy[v], e), m0))).to(dy[v], e);
 }
 // The block's sums of dw and db, over its groups: those of a warp by shuffles, the warps' (or the groups' of several warps) side by side in shared memory, then
-// column by column in order.  cols: 2 C floats for each team of a warp, or of a group of several.
-template <int VEC, int V>
-__device__ __forceinline__ void norm_block_sums(const NormArgs& a, int lane, float (&dw)[V][VEC], float (&db)[V][VEC], float* cols) {
-  const int width = min(a.group, 32), team = threadIdx.x / max(a.group, 32), teams = blockDim.x / max(a.group, 32);
+// column by column in order.  cols: 2 C floats for each team of a warp, or of a group of several.  APART: the groups' columns are not the same (`odd` less than a
+// multiple of VEC): every group is a team.
+template <int VEC, int V, bool APART = false>
+__device__ __forceinline__ void norm_block_sums(const NormArgs& a, int lane, float (&dw)[V][VEC], float (&db)[V][VEC], float* cols, int odd = 0) {
+  const int width = APART ? 32 : min(a.group, 32), team = APART ? threadIdx.x >> a.shift : threadIdx.x / max(a.group, 32);
+  const int teams = APART ? blockDim.x >> a.shift : blockDim.x / max(a.group, 32);
   for (int o = width; o < 32; o <<= 1)
 #pragma unroll
     for (int v = 0; v < V; ++v)
@@ -228,10 +250,10 @@ __device__ __forceinline__ void norm_block_sums(const NormArgs& a, int lane, flo
   if ((threadIdx.x & 31) < width)
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const int c = (lane + v * a.group) * VEC;
-      if (c >= a.C) continue;
+      const int c = (lane + v * a.group) * VEC - odd;
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
+        if (c + e < 0 || c + e >= a.C) continue;
         cols[(size_t)team * 2 * a.C + c + e] = dw[v][e];
         cols[(size_t)team * 2 * a.C + a.C + c + e] = db[v][e];
       }
@@ -411,11 +433,14 @@ __device__ __forceinline__ void run_store(T* to, const T* at, long count) {
 
 constexpr int RUN_STAGES = 4;
 
-template <typename T, typename P, int V, bool BACKWARD>
+// W values a word: two of 16 bits.  A row of an odd number of values then begins within a word where its number is odd -- as its group's number is, runs being
+// multiples of eight rows and groups even in number -- and a thread's columns are the same in all its rows: one less than in the even ones.
+template <typename T, typename P, int W, int V, bool BACKWARD>
 __global__ void __launch_bounds__(NORM_THREADS, BACKWARD ? 1 : 2) norm_runs_kernel(const NormArgs a) {
   extern __shared__ uint4 ring[];
-  __shared__ float sums[2][32][2], sum1[2][32][1];
+  __shared__ __align__(16) float sums[2][32][2], sum1[2][32][1];
   const int lane = threadIdx.x & (a.group - 1), groups = blockDim.x >> a.shift, own = threadIdx.x >> a.shift;
+  const int odd = W == 2 ? own & a.C & 1 : 0;              // values of the row before in the row's first word
   const long runs = (a.rows + a.run - 1) / a.run;
   const size_t run_values = (size_t)a.run * a.C, run_pieces = run_values / VEC_OF<T>;
   const T *X = static_cast<const T*>(a.X), *dY = static_cast<const T*>(a.dY);
@@ -434,10 +459,48 @@ __global__ void __launch_bounds__(NORM_THREADS, BACKWARD ? 1 : 2) norm_runs_kern
   };
 #pragma unroll
   for (int i = 0; i < RUN_STAGES - 1; ++i) fetch(i);
-  float w[V][1], b[V][1], dw[V][1], db[V][1];
-  norm_params<P, 1, V>(a, lane, w, b);
+  // Columns of a thread's v-th word, and whether the row has them: all of it but the first word's first value (odd) and the last words.
+  const auto column = [&](int v) { return (lane + v * a.group) * W - odd; };
+  const auto has = [&](int v, int k) {
+    const int c = column(v) + k;
+    return (v > 0 || W == 1 || k > 0 || c >= 0) && (all_have<V>(v) || c < a.C);
+  };
+  float w[V][W], b[V][W], dw[V][W], db[V][W];
 #pragma unroll
-  for (int v = 0; v < V; ++v) dw[v][0] = db[v][0] = 0.f;
+  for (int v = 0; v < V; ++v)
+#pragma unroll
+    for (int k = 0; k < W; ++k) {
+      w[v][k] = a.weight && has(v, k) ? to_f(static_cast<const P*>(a.weight)[column(v) + k]) : 1.f;
+      b[v][k] = a.bias && has(v, k) ? to_f(static_cast<const P*>(a.bias)[column(v) + k]) : 0.f;
+      dw[v][k] = db[v][k] = 0.f;
+    }
+  const auto read = [&](const T* row, bool in, float (&f)[V][W]) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      if constexpr (W == 2) {
+        float2 t = make_float2(0.f, 0.f);
+        if (in && (has(v, 0) || has(v, 1))) t = unpack2<T>(*reinterpret_cast<const uint32_t*>(row + column(v)));
+        f[v][0] = has(v, 0) ? t.x : 0.f;
+        f[v][1] = has(v, 1) ? t.y : 0.f;
+      } else {
+        f[v][0] = in && has(v, 0) ? to_f(row[column(v)]) : 0.f;
+      }
+    }
+  };
+  const auto write = [&](T* row, const float (&f)[V][W]) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      if constexpr (W == 2) {
+        const uint32_t t = pack2<T>(f[v][0], f[v][1]);
+        T* at = row + column(v);
+        if (has(v, 0) && has(v, 1)) *reinterpret_cast<uint32_t*>(at) = t;
+        else if (has(v, 0)) *reinterpret_cast<unsigned short*>(at) = (unsigned short)t;
+        else if (has(v, 1)) *reinterpret_cast<unsigned short*>(at + 1) = (unsigned short)(t >> 16);
+      } else if (has(v, 0)) {
+        row[column(v)] = from_f<T>(f[v][0]);
+      }
+    }
+  };
   int stage = 0, turn = 0;
   for (long i = blockIdx.x; i < runs; i += gridDim.x) {
     copies_wait<RUN_STAGES - 2>();
@@ -447,28 +510,24 @@ __global__ void __launch_bounds__(NORM_THREADS, BACKWARD ? 1 : 2) norm_runs_kern
     for (int r0 = 0; r0 < a.run; r0 += groups, turn ^= 1) {
       const int r = r0 + own;
       const bool in = r < here;
-      float x[V][1], dy[V][1];
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        const int c = lane + v * a.group;
-        x[v][0] = in && (all_have<V>(v) || c < a.C) ? to_f(xs[r * a.C + c]) : 0.f;
-        if (BACKWARD) dy[v][0] = in && (all_have<V>(v) || c < a.C) ? to_f(ds[r * a.C + c]) : 0.f;
-      }
+      float x[V][W];
+      read(xs + r * a.C, in, x);
       if constexpr (BACKWARD) {
+        float dy[V][W];
+        read(ds + r * a.C, in, dy);
         const float mean = in ? __ldg(a.mean + first + r) : 0.f, rstd = in ? __ldg(a.rstd + first + r) : 0.f;
-        norm_row_backward<1, V, false>(a, lane, mean, rstd, x, dy, w, dw, db, sums[turn]);
-        if (in)
-#pragma unroll
-          for (int v = 0; v < V; ++v)
-            if (all_have<V>(v) || lane + v * a.group < a.C) xs[r * a.C + lane + v * a.group] = from_f<T>(dy[v][0]);
+        norm_row_backward<W, V, true>(a, lane, mean, rstd, x, dy, w, dw, db, sums[turn]);
+        if (in) write(xs + r * a.C, dy);
       } else {
         float mean, rstd;
-        norm_row<1, V, false>(a, lane, x, mean, rstd, sum1);
+        norm_row<W, V, true>(a, lane, x, mean, rstd, sum1, has);
         if (in) {
           if (lane == 0 && a.mean) { a.mean[first + r] = mean; a.rstd[first + r] = rstd; }
 #pragma unroll
           for (int v = 0; v < V; ++v)
-            if (all_have<V>(v) || lane + v * a.group < a.C) xs[r * a.C + lane + v * a.group] = from_f<T>(fmaf(x[v][0] * rstd, w[v][0], b[v][0]));
+#pragma unroll
+            for (int k = 0; k < W; k += W) fma<W>(mul<W>(Pair::of(x[v], k), both(rstd)), Pair::of(w[v], k), Pair::of(b[v], k)).to(x[v], k);
+          write(xs + r * a.C, x);
         }
       }
     }
@@ -481,7 +540,7 @@ __global__ void __launch_bounds__(NORM_THREADS, BACKWARD ? 1 : 2) norm_runs_kern
   if constexpr (BACKWARD) {
     pdl_trigger();
     copies_wait<0>();
-    if (a.part) norm_block_sums<1, V>(a, lane, dw, db, reinterpret_cast<float*>(ring));
+    if (a.part) norm_block_sums<W, V, W == 2>(a, lane, dw, db, reinterpret_cast<float*>(ring), odd);
   }
 }
 
@@ -569,7 +628,8 @@ inline int pow2_at_least(long n) { int p = 1; while (p < n) p *= 2; return p; }
 inline bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 
 // Vectors a thread for which there is a kernel: at least `v`, or 0.  (Sixteen values: five times as many floats fit a thread's registers.)
-int vectors(long v, bool vec, int es) {
+int vectors(long v, bool vec, bool words, int es) {
+  if (words) return v <= 8 ? (int)v : 0;
   if (vec) return v <= (es == 4 ? 4 : 2) ? (int)v : 0;
   return v <= 8 ? (int)v : v <= 12 ? 12 : v <= 16 ? 16 : 0;
 }
@@ -578,7 +638,7 @@ int vectors(long v, bool vec, int es) {
 void pick_group(long nv, int es, NormPlan* p) {
   long best = -1;
   for (int g = 1; g <= NORM_THREADS; g *= 2) {
-    const int v = vectors((nv + g - 1) / g, p->vec, es);
+    const int v = vectors((nv + g - 1) / g, p->vec, p->words, es);
     if (v == 0) continue;
     const long slots = (long)v * g;
     if (best < 0 || (g <= 8 ? slots <= best : slots < best)) { best = slots; p->group = g; p->V = v; }
@@ -615,7 +675,12 @@ constexpr int norm_stages(int V, int VEC, bool backward) { return VEC == 1 ? 1 :
 template <typename T, typename P, int VEC>
 cudaError_t forward_of(const NormPlan& p, const NormArgs& a, cudaStream_t st) {
   if constexpr (VEC == 1) {
-#define XC_NORM(N) if (p.V == N && p.run) return norm_launch(norm_runs_kernel<T, P, N, false>, p, a, st);
+if constexpr (sizeof(T) == 2) {
+#define XC_NORM(N) if (p.V == N && p.words) return norm_launch(norm_runs_kernel<T, P, 2, N, false>, p, a, st);
+      XC_NORM(1) XC_NORM(2) XC_NORM(3) XC_NORM(4) XC_NORM(5) XC_NORM(6) XC_NORM(7) XC_NORM(8)
+#undef XC_NORM
+    }
+#define XC_NORM(N) if (p.V == N && p.run) return norm_launch(norm_runs_kernel<T, P, 1, N, false>, p, a, st);
     XC_NORM(1) XC_NORM(2) XC_NORM(3) XC_NORM(4) XC_NORM(5) XC_NORM(6) XC_NORM(7) XC_NORM(8) XC_NORM(12) XC_NORM(16)
 #undef XC_NORM
   }
@@ -629,7 +694,12 @@ cudaError_t forward_of(const NormPlan& p, const NormArgs& a, cudaStream_t st) {
 template <typename T, typename P, int VEC>
 cudaError_t backward_of(const NormPlan& p, const NormArgs& a, cudaStream_t st) {
   if constexpr (VEC == 1) {
-#define XC_NORM(N) if (p.V == N && p.run) return norm_launch(norm_runs_kernel<T, P, N, true>, p, a, st);
+if constexpr (sizeof(T) == 2) {
+#define XC_NORM(N) if (p.V == N && p.words) return norm_launch(norm_runs_kernel<T, P, 2, N, true>, p, a, st);
+      XC_NORM(1) XC_NORM(2) XC_NORM(3) XC_NORM(4) XC_NORM(5) XC_NORM(6) XC_NORM(7) XC_NORM(8)
+#undef XC_NORM
+    }
+#define XC_NORM(N) if (p.V == N && p.run) return norm_launch(norm_runs_kernel<T, P, 1, N, true>, p, a, st);
     XC_NORM(1) XC_NORM(2) XC_NORM(3) XC_NORM(4) XC_NORM(5) XC_NORM(6) XC_NORM(7) XC_NORM(8) XC_NORM(12) XC_NORM(16)
 #undef XC_NORM
   }
@@ -659,16 +729,22 @@ static NormPlan plan(const xconv_norm_desc* d, bool vec, bool dense, bool backwa
   p.vec = vec;
   const int es = d->dtype == XCONV_F32 ? 4 : 2, tensors = backward ? 2 : 1;
   const long nv = vec ? d->C / (16 / es) : d->C;
-  pick_group(nv, es, &p);
+  // (words of two values, where a block has several groups)
+  if (!vec && dense && es == 2) {
+    p.words = true;
+    pick_group(d->C / 2 + 1, es, &p);
+    p.words = !p.wide && p.group <= 128 && RUN_STAGES * (size_t)tensors * std::max(256 / p.group, 8) * d->C * es <= 200u * 1024;
+  }
+  if (!p.words) pick_group(nv, es, &p);
   if (p.wide) {
     p.threads = 1024;
     p.parts = std::min<long>((d->rows + WIDE_ROWS - 1) / WIDE_ROWS, 512);
     p.blocks = std::min<long>(d->rows, (backward ? 2 : 8) * NORM_SMS);
     return p;
   }
-  if (!backward && d->rows * p.group < NORM_SMS * 256L) {    // few rows: a thread has little to do, and more of them do it
+  if (!backward && !p.words && d->rows * p.group < NORM_SMS * 256L) {    // few rows: a thread has little to do, and more of them do it
     p.group = std::min(NORM_THREADS, pow2_at_least(nv));
-    p.V = vectors((nv + p.group - 1) / p.group, vec, es);
+    p.V = vectors((nv + p.group - 1) / p.group, vec, false, es);
   }
   p.full = vec && (long)p.V * p.group == nv;
   // A block's threads: fewer where its rows would not reach all SMs.
@@ -678,7 +754,7 @@ static NormPlan plan(const xconv_norm_desc* d, bool vec, bool dense, bool backwa
   const int resident = vec || backward ? 1 : 2;              // of 512 threads: 128 or 64 registers each
   p.blocks = std::min<long>((d->rows + groups - 1) / groups, (long)NORM_SMS * resident * (NORM_THREADS / p.threads));
   const size_t stages = norm_stages(p.V, vec ? 2 : 1, backward);
-  if (!vec && dense) p.threads = std::max(p.group, std::min(p.threads, 256));
+  if (!vec && dense) p.threads = p.words ? 256 : std::max(p.group, std::min(p.threads, 256));
   if (vec) p.smem = (int)(stages * p.V * tensors * p.threads * 16);
   else if (dense) {
     const long groups = p.threads / p.group, run = std::max<long>(groups, 8);              // (8 rows of any type are a multiple of 16 bytes)
@@ -689,7 +765,7 @@ static NormPlan plan(const xconv_norm_desc* d, bool vec, bool dense, bool backwa
       p.blocks = std::min<long>((d->rows + run - 1) / run, (long)NORM_SMS * std::max<long>(1, std::min<long>(resident * (NORM_THREADS / p.threads), 220 * 1024 / ((long)bytes + 2048))));
     }
   }
-  if (backward) p.smem = std::max(p.smem, (int)(p.threads / std::max(p.group, 32) * 2 * sizeof(float)) * d->C);
+  if (backward) p.smem = std::max(p.smem, (int)(p.threads / (p.words ? p.group : std::max(p.group, 32)) * 2 * sizeof(float)) * d->C);
   p.parts = p.blocks;
   return p;
 }

@@ -12,6 +12,7 @@ struct NormPlan {
   bool full;             // every thread of a row has all its vectors
   bool wide;             // a row does not fit the registers of a block
   int V, group, threads; // vectors (or elements) a thread, threads a row, threads a block
+  bool words;            // runs two values at a time
   int run;               // rows of a run (dense rows that are not aligned), or 0
   int smem;
   long blocks;

@@ -83,7 +83,9 @@ def check_backward(dY, X, mean, rstd, w, dX, dw, db):
 
 
 SHAPES = [(1, 1), (1, 2), (3, 1), (1, 4096), (5, 7), (33, 97), (9, 24), (257, 1000), (64, 2257), (7, 8192), (5, 4100), (3, 8200), (2, 16392), (4, 9001), (2, 40001),
-          (6, 520), (70001, 8), (4099, 96), (2, 3, 5, 7), (3, 64, 9, 5), (2, 130, 6, 6), (1, 24, 3, 5, 7), (2, 17, 4, 3, 2), (4, 9, 40), (12,), (300, 1536)]
+          (6, 520), (70001, 8), (4099, 96), (2, 3, 5, 7), (3, 64, 9, 5), (2, 130, 6, 6), (1, 24, 3, 5, 7), (2, 17, 4, 3, 2), (4, 9, 40), (12,), (300, 1536),
+          # dense rows that do not begin on 16-byte boundaries, enough for runs, a last run that is not whole; odd and even numbers of values
+          (4099, 97), (999, 33), (5003, 7), (3001, 201), (777, 1), (1235, 98), (2001, 2), (601, 2047), (50, 97, 9, 7)]
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
