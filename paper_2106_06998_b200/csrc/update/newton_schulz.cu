@@ -9,8 +9,10 @@
 // values beside small ones.  With operands rounded to bfloat16 the result is off by 1e-2 (normal values) to 0.3 (eight directions above noise), with one float16 part
 // by 1e-3 to 4e-2; with float arithmetic by 1e-7 to 5e-6.  So every operand is two float16 parts here, x 2^13 = h + l (11 + 11 bits and the sign between
 // them; |X| < 2, |A| < 4, |B| < 8: nothing overflows, and what is lost is below 2^-38), and a product is l h + h l + h h on the tensor cores, as exact as one of floats.
-// The tensor cores' accumulator is not rounded to nearest; a chain is 32 terms (four MMAs of the small products, then two of h h), and the
-// chains are added in float registers.
+// The tensor cores' accumulator is not rounded to nearest; a chain of MMAs is 32 terms long (four MMAs of the small products, then two of h h), and the chains are
+// added in float registers.  Error against 64 bits, times that of the same steps in float arithmetic, gradients of 16 x 75 to 1000 x 1000 values: 0.36 to 1.5; chains of 16
+// terms 0.31 to 2, of 64 terms 0.5 to 2.  Where every result is rounded to 16 bits anyway a chain is 128 terms, since the wait for a free set of sums
+// costs 150 clocks a chain (4096 x 4096 bfloat16: 3440 -> 3040 us; 64 terms 3150, 256 terms 2930, whose largest errors pass four times those of float arithmetic).
 //
 // Layout.  X, A and B lie in the scratch memory as blocks of 128 x 64 values, each part 16 KB in the order that the MMA wants in shared memory without a swizzle
 // (eight rows' 16-byte pieces side by side): whatever the matrices' sizes one tensor map describes them all, eight lanes with a row each write whole lines, and the
@@ -21,8 +23,12 @@
 // A pair of CTAs works on a tile of 256 x 256: each brings 128 rows of either operand, 64 terms (64 KB) a stage, and the two tensor cores read both halves of the second
 // one.  The copies' latency bounds smaller tiles: 192 KB of ring, 2800 clocks from a copy to its arrival, 768 clocks of MMAs for the 64 KB of a
 // tile of 128 x 128 by one CTA (measured there: 1250 clocks a stage), 1536 here.  In a CTA a warp copies, one (of the first CTA) issues the MMAs, sixteen add
-// chains and write results.  Where there are fewer tiles than pairs, a cluster of two or four pairs shares the terms of a tile; each then has a part of the tile's
-// columns, and reads the others' sums of them over the SMs' network.
+// chains and write results.  Where there are fewer tiles than pairs, clusters of two or four pairs share the terms of the tiles with the longest
+// sums; each pair then has a part of the tile's columns, and reads the others' sums of them over the SMs' network.
+//
+// What bounds it (B200, 4096 x 4096 bfloat16, five steps, 3.0 to 3.4 ms on different boards): the tensor cores at the clock that the power limit leaves; 4.1 TFLOP of float16
+// products at 1.2 to 1.35 PFLOP/s, cuBLAS's sustained rate on this board being 1.37.  Smaller calls: 15 kernels of 7 us and more, one behind the other, of which a tile's own
+// products are a third (8 x 1000 x 523 float16 350 us, a residual network's 19 convolutions 570 us).
 #include "newton_schulz.h"
 
 #include <algorithm>
@@ -34,7 +40,7 @@ namespace xconv {
 namespace {
 
 constexpr int NS_SMS = 148;
-constexpr int NS_STAGES = 3, NS_SETS = 2, NS_CHAIN = 2;      // NS_CHAIN: steps of 16 terms
+constexpr int NS_STAGES = 3, NS_SETS = 2, NS_CHAIN = 2, NS_LONG = 2;      // NS_CHAIN: steps of 16 terms, NS_LONG: stages
 constexpr uint32_t NS_OPERAND = 32 * 1024, NS_STAGE = 2 * NS_OPERAND, NS_PART = NS_OPERAND / 2;
 constexpr int NS_ADDERS = 16, NS_THREADS = 32 * (2 + NS_ADDERS);
 constexpr int NS_TILE = 256;
@@ -466,7 +472,7 @@ __device__ __forceinline__ void ns_emit_rows(const NsArgs& p, const NsEntry& e, 
   }
 }
 
-template <int MODE>
+template <int MODE, bool LONG>
 __global__ void __launch_bounds__(NS_THREADS, 1) ns_product_kernel(const __grid_constant__ NsArgs p) {
   constexpr bool SYM = MODE == NS_GRAM || MODE == NS_SQUARE;
   extern __shared__ uint8_t raw[];
@@ -588,21 +594,26 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_product_kernel(const __grid_
           const uint32_t a_step = a_across ? ACROSS_STEP : ALONG_STEP, b_step = b_across ? ACROSS_STEP : ALONG_STEP;
           const uint32_t idesc = IDESC | (a_across ? 1u << 15 : 0u) | (b_across ? 1u << 16 : 0u);
           constexpr uint32_t L = NS_PART >> 4;
+          // (chains begin and end within a stage, or with the first and the last of NS_LONG stages)
+          constexpr int STEPS = LONG ? 4 : NS_CHAIN;
+          const bool begins = !LONG || (s - s0) % NS_LONG == 0, ends = !LONG || (s - s0) % NS_LONG == NS_LONG - 1 || s + 1 == s1;
 #pragma unroll
-          for (int c = 0; c < 4; c += NS_CHAIN) {
-            if (used >= NS_SETS && !mbar_wait_warp(&acc_empty[set], set_lap ^ 1u, p.status, p.tag)) { ok = false; break; }
+          for (int c = 0; c < 4; c += STEPS) {
+            if (begins && used >= NS_SETS && !mbar_wait_warp(&acc_empty[set], set_lap ^ 1u, p.status, p.tag)) { ok = false; break; }
             tc_fence_after();
             const uint32_t d = tmem + set * NS_TILE;
 #pragma unroll
-            for (int t = c; t < c + NS_CHAIN; ++t) pair_mma(d, a + L + t * a_step, a_hi, b + t * b_step, b_hi, idesc, t > c);
+            for (int t = c; t < c + STEPS; ++t) pair_mma(d, a + L + t * a_step, a_hi, b + t * b_step, b_hi, idesc, t > c || !begins);
 #pragma unroll
-            for (int t = c; t < c + NS_CHAIN; ++t) pair_mma(d, a + t * a_step, a_hi, b + L + t * b_step, b_hi, idesc, 1u);
+            for (int t = c; t < c + STEPS; ++t) pair_mma(d, a + t * a_step, a_hi, b + L + t * b_step, b_hi, idesc, 1u);
 #pragma unroll
-            for (int t = c; t < c + NS_CHAIN; ++t) pair_mma(d, a + t * a_step, a_hi, b + t * b_step, b_hi, idesc, 1u);
-            if (c + NS_CHAIN == 4) pair_commit(&empty[slot], pair_mask);
-            pair_commit(&acc_full[set], pair_mask);
-            ++used;
-            if (++set == NS_SETS) { set = 0; set_lap ^= 1u; }
+            for (int t = c; t < c + STEPS; ++t) pair_mma(d, a + t * a_step, a_hi, b + t * b_step, b_hi, idesc, 1u);
+            if (c + STEPS == 4) pair_commit(&empty[slot], pair_mask);
+            if (ends) {
+              pair_commit(&acc_full[set], pair_mask);
+              ++used;
+              if (++set == NS_SETS) { set = 0; set_lap ^= 1u; }
+            }
           }
           if (++slot == NS_STAGES) { slot = 0; lap ^= 1u; }
         }
@@ -626,7 +637,8 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_product_kernel(const __grid_
 #pragma unroll
       for (int i = 0; i < 64; ++i) sum[i] = 0.f;
       const int s0 = w.stages * part / split, s1 = w.stages * (part + 1) / split;
-      for (int s = s0 * (4 / NS_CHAIN); s < s1 * (4 / NS_CHAIN); ++s) {
+      const int chains = LONG ? (s1 - s0 + NS_LONG - 1) / NS_LONG : (s1 - s0) * (4 / NS_CHAIN);
+      for (int c = 0; c < chains; ++c) {
         if (!mbar_wait_warp(&acc_full[set], set_lap, p.status, p.tag)) { ok = false; break; }
         tc_fence_after();
         const uint32_t from = tmem + set * NS_TILE + quarter * 64 + ((uint32_t)(quadrant * 32) << 16);
@@ -642,7 +654,11 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_product_kernel(const __grid_
             if (lane == 0) arrive_at(&acc_empty[set], leader);
           }
 #pragma unroll
-          for (int i = 0; i < 16; ++i) { sum[q * 32 + i] += __uint_as_float(x[i]); sum[q * 32 + 16 + i] += __uint_as_float(y[i]); }
+          for (int i = 0; i < 16; i += 2) {
+            const float2 f = __fadd2_rn(make_float2(sum[q * 32 + i], sum[q * 32 + i + 1]), make_float2(__uint_as_float(x[i]), __uint_as_float(x[i + 1])));
+            const float2 g = __fadd2_rn(make_float2(sum[q * 32 + 16 + i], sum[q * 32 + 17 + i]), make_float2(__uint_as_float(y[i]), __uint_as_float(y[i + 1])));
+            sum[q * 32 + i] = f.x; sum[q * 32 + i + 1] = f.y; sum[q * 32 + 16 + i] = g.x; sum[q * 32 + 17 + i] = g.y;
+          }
         }
         if (++set == NS_SETS) { set = 0; set_lap ^= 1u; }
       }
@@ -1199,7 +1215,7 @@ NsSharing share(const NsTable& t, int units, Stages&& stages, Units&& units_of) 
   return best;
 }
 
-template <int MODE>
+template <int MODE, bool LONG>
 cudaError_t launch_product(NsArgs& p, cudaStream_t st) {
   constexpr bool SYM = MODE == NS_GRAM || MODE == NS_SQUARE;
   constexpr size_t smem = NS_STAGES * NS_STAGE + 1024;
@@ -1210,7 +1226,7 @@ cudaError_t launch_product(NsArgs& p, cudaStream_t st) {
   });
   p.cs = how.cs;
   p.heavy = how.heavy;
-  cudaError_t e = cudaFuncSetAttribute(ns_product_kernel<MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  cudaError_t e = cudaFuncSetAttribute(ns_product_kernel<MODE, LONG>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(p.cs > 1 ? 2 * p.cs * (p.heavy + (units - p.heavy + p.cs - 1) / p.cs) : std::min(2 * units, NS_SMS)));
@@ -1225,7 +1241,7 @@ cudaError_t launch_product(NsArgs& p, cudaStream_t st) {
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, ns_product_kernel<MODE>, p);
+  return cudaLaunchKernelEx(&cfg, ns_product_kernel<MODE, LONG>, p);
 }
 
 // The scratch memory's blocks as rows of 256 values of 8 bytes, 16 of them a block and a copy.  (The copy engine fetches a box row by row: long rows.)  And as rows
@@ -1239,6 +1255,21 @@ bool map_blocks(CUtensorMap* whole, CUtensorMap* across, void* blocks, size_t co
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS &&
          fn(across, CU_TENSOR_MAP_DATA_TYPE_INT64, 3, blocks, dims3, strides3, box3, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <bool LONG>
+cudaError_t launch_steps(NsArgs& p, int steps, cudaStream_t st, int* launches) {
+  cudaError_t e;
+  for (int s = 0; s < steps; ++s) {
+    p.which = s & 1;
+    if ((e = launch_product<NS_GRAM, LONG>(p, st)) != cudaSuccess) return e;
+    ++*launches;
+    if ((e = launch_product<NS_SQUARE, LONG>(p, st)) != cudaSuccess) return e;
+    ++*launches;
+    if ((e = s + 1 < steps ? launch_product<NS_APPLY, LONG>(p, st) : launch_product<NS_LAST, LONG>(p, st)) != cudaSuccess) return e;
+    ++*launches;
+  }
+  return cudaSuccess;
 }
 
 size_t sums_bytes(const NsTable& t) { return ((size_t)t.chunks * sizeof(double) + 1023) / 1024 * 1024; }
@@ -1294,16 +1325,9 @@ cudaError_t launch_newton_schulz(const NsTable& t, const NsOptions& o, void* ws,
   e = launch_pdl(ns_blocks_kernel, dim3((unsigned)t.blocks), dim3(256), 0, st, p);
   if (e != cudaSuccess) return e;
   ++*launches;
-  for (int s = 0; s < o.steps; ++s) {
-    p.which = s & 1;
-    if ((e = launch_product<NS_GRAM>(p, st)) != cudaSuccess) return e;
-    ++*launches;
-    if ((e = launch_product<NS_SQUARE>(p, st)) != cudaSuccess) return e;
-    ++*launches;
-    if ((e = s + 1 < o.steps ? launch_product<NS_APPLY>(p, st) : launch_product<NS_LAST>(p, st)) != cudaSuccess) return e;
-    ++*launches;
-  }
-  return cudaSuccess;
+  bool halves = true;                                        // every result is rounded to 16 bits
+  for (int k = 0; k < t.entries; ++k) halves = halves && t.e[k].out_dtype != XCONV_F32;
+  return halves ? launch_steps<true>(p, o.steps, st, launches) : launch_steps<false>(p, o.steps, st, launches);
 }
 
 }  // namespace xconv
