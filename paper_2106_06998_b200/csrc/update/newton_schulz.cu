@@ -1030,6 +1030,165 @@ __device__ __forceinline__ void small_steps(const NsArgs& p, const NsEntry& e, i
   }
 }
 
+// ---- the same with a smaller side of at most 32, by FP32 multiply-adds in the same kernel
+//
+// Their sums are rounded to nearest, where the tensor cores cut them off; with few terms that shows: error against 64 bits, as a share of 1.5 times that of float
+// arithmetic by the library, at worst 1.18 on the tensor cores and 0.58 here (16 x 75; 20 x 60: 1.18 and 0.53; 32 x 64: 1.01 and 0.49; 64 x 64 there: 0.73).  Nothing waits
+// for MMAs either.  Bound by the loads from shared memory, of which a thread shares each among its products.  Measured, five steps, tensor cores and this: 6 x 75 30.7 and
+// 16.4 us, 16 x 384 47 and 31, 32 x 32 24.6 and 22.6, 32 x 192 36.9 and 43.0, 32 x 256 41.0 and 36.9.
+
+constexpr int TINY = 32, TINY_X = SMALL_COLUMN_BLOCKS * 64 + 4, TINY_A = TINY + 4;      // rows; floats of a row of X, of A and B (16 bytes more: eight rows in different banks)
+
+__device__ __forceinline__ float ld_shared_f(uint32_t addr) {
+  float v;
+  asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(addr));
+  return v;
+}
+__device__ __forceinline__ void st_shared_f(uint32_t addr, float v) { asm volatile("st.shared.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory"); }
+__device__ __forceinline__ float ld_cluster_f(uint32_t addr, uint32_t rank) {
+  float v;
+  asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %1, %2;\n\tld.shared::cluster.f32 %0, [a];\n\t}" : "=f"(v) : "r"(addr), "r"(rank));
+  return v;
+}
+// The products of row i with rows j and, with TWO, j + 16 over `fours` groups of four columns (eight lanes read eight rows in a row: different banks).
+template <bool TWO>
+__device__ __forceinline__ float2 tiny_products(uint32_t rows, int pitch, int i, int j, int fours) {
+  float2 s = make_float2(0.f, 0.f), t = s;
+  uint32_t at = rows + (uint32_t)(i * pitch) * 4, to = rows + (uint32_t)(j * pitch) * 4;
+  const uint32_t next = (uint32_t)pitch * 64;
+#pragma unroll 4
+  for (int c = 0; c < fours; ++c, at += 16, to += 16) {
+    const float4 a = ld_shared_f4(at), x = ld_shared_f4(to);
+    s.x = fmaf(a.x, x.x, s.x); t.x = fmaf(a.y, x.y, t.x);
+    s.x = fmaf(a.z, x.z, s.x); t.x = fmaf(a.w, x.w, t.x);
+    if (TWO) {
+      const float4 y = ld_shared_f4(to + next);
+      s.y = fmaf(a.x, y.x, s.y); t.y = fmaf(a.y, y.y, t.y);
+      s.y = fmaf(a.z, y.z, s.y); t.y = fmaf(a.w, y.w, t.y);
+    }
+  }
+  return make_float2(s.x + t.x, s.y + t.y);
+}
+template <typename T>
+__device__ __forceinline__ void tiny_write(const NsArgs& p, const NsEntry& e, int mat, int row, long col, float v) {
+  T* to = static_cast<T*>(e.out) + (size_t)mat * e.n * e.m + (e.rows > e.cols ? (size_t)col * e.n + row : (size_t)row * e.m + col);
+  *to = from_f<T>(ns_result(p, e, v * (NS_SCALE * NS_SCALE), p.muon ? to_f(*to) : 0.f));
+}
+
+// X X^T of 32 rows over groups of four columns, by 4 x 2 products a thread (six 16-byte loads for 32 multiply-adds, which is what bounds it) and a quarter of the
+// columns a warp: the quarters' sums to `to`.
+__device__ __forceinline__ void tiny_gram(uint32_t X, uint32_t to, int fours) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, i = lane >> 2, j = (warp & 3) * 8 + (lane & 3), quarter = warp >> 2;
+  float s[4][2] = {}, t[4][2] = {};
+  const int end = fours * (quarter + 1) >> 2;
+#pragma unroll 2
+  for (int c = fours * quarter >> 2; c < end; ++c) {
+    float4 a[4], b[2];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) a[k] = ld_shared_f4(X + (uint32_t)((i + 8 * k) * TINY_X + c * 4) * 4);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) b[k] = ld_shared_f4(X + (uint32_t)((j + 4 * k) * TINY_X + c * 4) * 4);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int l = 0; l < 2; ++l) {
+        s[k][l] = fmaf(a[k].x, b[l].x, s[k][l]); t[k][l] = fmaf(a[k].y, b[l].y, t[k][l]);
+        s[k][l] = fmaf(a[k].z, b[l].z, s[k][l]); t[k][l] = fmaf(a[k].w, b[l].w, t[k][l]);
+      }
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+#pragma unroll
+    for (int l = 0; l < 2; ++l) st_shared_f(to + (uint32_t)(quarter * TINY * TINY_A + (i + 8 * k) * TINY_A + j + 4 * l) * 4, s[k][l] + t[k][l]);
+}
+
+// X: 32 rows of TINY_X floats at SMALL_X, of which the CTA's columns are there and zeros. N: 16 or 32 rows at most.
+template <int N>
+__device__ __noinline__ void tiny_steps(const NsArgs& p, const NsEntry& e, int mat, uint32_t smem, int blocks, int cb0) {
+  constexpr bool TWO = N > 16;
+  constexpr int COLS = N / 16, ROWS = N / (4 * COLS);       // of B X a thread, the columns 128 / COLS apart
+  const int t = threadIdx.x, i = t >> 4, j = t & 15;
+  const uint32_t X = smem + SMALL_X, A = smem + SMALL_A, B = A + TINY * TINY_A * 4, at = (uint32_t)(i * TINY_A + j) * 4;
+  const int columns = min(blocks * 64, e.m - cb0 * NS_COLS);
+#pragma unroll 1
+  for (int step = 0; step < p.which; ++step) {
+    float2 s = make_float2(0.f, 0.f);
+    if (TWO) {
+      const uint32_t quarters = smem + SMALL_E + 2u * (TINY * TINY_A * 4);
+      tiny_gram(X, quarters, (columns + 3) >> 2);
+      __syncthreads();
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        s.x += ld_shared_f(quarters + at + (uint32_t)(q * TINY * TINY_A) * 4);
+        s.y += ld_shared_f(quarters + at + (uint32_t)(q * TINY * TINY_A) * 4 + 64);
+      }
+    } else if (i < N) s = tiny_products<false>(X, TINY_X, i, j, (columns + 3) >> 2);
+    if (p.cs > 1) {
+      // (two buffers in turn: one is written again two barriers later)
+      const uint32_t sums = smem + SMALL_E + (uint32_t)(step & 1) * (TINY * TINY_A * 4) + at;
+      st_shared_f(sums, s.x);
+      if (TWO) st_shared_f(sums + 64, s.y);
+      cluster_sync();
+      s = make_float2(0.f, 0.f);
+#pragma unroll 4
+      for (int c = 0; c < p.cs; ++c) {
+        s.x += ld_cluster_f(sums, c);
+        if (TWO) s.y += ld_cluster_f(sums + 64, c);
+      }
+    }
+    if (i < N) {
+      st_shared_f(A + at, s.x);
+      if (TWO) st_shared_f(A + at + 64, s.y);
+    }
+    __syncthreads();
+    if (i < N) {
+      const float2 q = tiny_products<TWO>(A, TINY_A, i, j, N / 4);
+      st_shared_f(B + at, fmaf(p.c, q.x, p.b * s.x) + (i == j && i < e.n ? p.a : 0.f));
+      if (TWO) st_shared_f(B + at + 64, fmaf(p.c, q.y, p.b * s.y) + (i == j + 16 && i < e.n ? p.a : 0.f));
+    }
+    const bool last = step + 1 == p.which;
+    // 128 columns at a time: all have read them before one writes.
+#pragma unroll 1
+    for (int c0 = 0; c0 < columns; c0 += 128) {
+      const int c = c0 + t % (128 / COLS), r0 = t / (128 / COLS) * ROWS;
+      const uint32_t col = X + (uint32_t)c * 4;
+      float x[COLS][N];
+#pragma unroll
+      for (int l = 0; l < COLS; ++l)
+#pragma unroll
+        for (int k = 0; k < N; ++k) x[l][k] = c + l * (128 / COLS) < columns ? ld_shared_f(col + (uint32_t)(k * TINY_X + l * (128 / COLS)) * 4) : 0.f;
+      __syncthreads();
+#pragma unroll 1
+      for (int r = r0; r < r0 + ROWS; ++r) {
+        float y[COLS] = {}, z[COLS] = {};
+#pragma unroll
+        for (int k = 0; k < N; k += 4) {
+          const float4 w = ld_shared_f4(B + (uint32_t)(r * TINY_A + k) * 4);
+#pragma unroll
+          for (int l = 0; l < COLS; ++l) {
+            y[l] = fmaf(w.x, x[l][k], y[l]); z[l] = fmaf(w.y, x[l][k + 1], z[l]);
+            y[l] = fmaf(w.z, x[l][k + 2], y[l]); z[l] = fmaf(w.w, x[l][k + 3], z[l]);
+          }
+        }
+#pragma unroll
+        for (int l = 0; l < COLS; ++l) {
+          const int cl = c + l * (128 / COLS);
+          if (cl >= columns) continue;
+          const float v = y[l] + z[l];
+          if (!last) st_shared_f(X + (uint32_t)(r * TINY_X + cl) * 4, v);
+          else if (r < e.n) {
+            const long to = (long)cb0 * NS_COLS + cl;
+            if (e.out_dtype == XCONV_F32) tiny_write<float>(p, e, mat, r, to, v);
+            else if (e.out_dtype == XCONV_BF16) tiny_write<bf16>(p, e, mat, r, to, v);
+            else tiny_write<f16>(p, e, mat, r, to, v);
+          }
+        }
+      }
+    }
+    __syncthreads();
+  }
+}
+
 // Pieces 4 i + q0 of row r of the CTA's columns of U, as floats where the thread finds them again; the momenta take in the gradients on the way.  Returns the sum of
 // their squares.
 template <typename G>
@@ -1135,7 +1294,16 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ns_small_kernel(const __grid
   for (int i = 0; i < 2 * blocks; ++i) {
     const uint32_t own = staged + (uint32_t)(i * 2 * SMALL_THREADS + threadIdx.x) * 16;
     const float4 a = ld_shared_f4(own), b = ld_shared_f4(own + SMALL_THREADS * 16);
-    const float v[8] = {f(a.x), f(a.y), f(a.z), f(a.w), f(b.x), f(b.y), f(b.z), f(b.w)};
+    float v[8] = {f(a.x), f(a.y), f(a.z), f(a.w), f(b.x), f(b.y), f(b.z), f(b.w)};
+    if (e.n <= TINY) {
+      if (r >= TINY) continue;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] *= NS_UNSCALE;
+      const uint32_t at = smem + SMALL_X + (uint32_t)(r * TINY_X + (i * 4 + q0) * 8) * 4;
+      st_shared_v4(at, make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])));
+      st_shared_v4(at + 16, make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])));
+      continue;
+    }
     uint4 hi, lo;
     parts8(v, hi, lo);
     const uint32_t at = smem + SMALL_X + small_x_at(r, i * 4 + q0);
@@ -1146,7 +1314,9 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ns_small_kernel(const __grid
   __syncthreads();
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&tmem_slot);
   const SmallWait wait = {&done, 0u, p.status, p.tag};
-  if (e.n <= 64) small_steps<64>(p, e, mat, smem, tmem, wait, blocks, cb0, rank);
+  if (e.n <= 16) tiny_steps<16>(p, e, mat, smem, blocks, cb0);
+  else if (e.n <= TINY) tiny_steps<TINY>(p, e, mat, smem, blocks, cb0);
+  else if (e.n <= 64) small_steps<64>(p, e, mat, smem, tmem, wait, blocks, cb0, rank);
   else small_steps<128>(p, e, mat, smem, tmem, wait, blocks, cb0, rank);
   tc_fence_before();
   __syncthreads();

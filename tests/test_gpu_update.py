@@ -91,6 +91,21 @@ def test_orthogonalize_of_any_shape(shape, dtype):
         check(O, G)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("shape", [(16, 193), (17, 192), (32, 191), (32, 1535), (1535, 31), (33, 34), (16, 2), (1, 1000), (5, 15, 1537), (32, 32, 3, 3)])
+def test_sides_of_up_to_32(shape, dtype):
+    for kind in ("normal", "few"):
+        G = make(shape, dtype, seed=5, kind=kind)
+        check(xb.xconv_orthogonalize(G), G)
+
+
+def test_small_sides_beside_larger_ones():
+    G = [make(s, seed=k) for k, s in enumerate([(16, 6, 5, 5), (120, 1400), (10, 84), (32, 700), (33, 40), (3, 20, 30)])]
+    for O, again, g in zip(xb.xconv_orthogonalize(G), xb.xconv_orthogonalize(G), G):
+        check(O, g)
+        assert torch.equal(O, again)           # (alone it may be shared among fewer CTAs: sums in another order)
+
+
 @pytest.mark.parametrize("steps", [1, 2, 3, 8])
 def test_any_number_of_steps(steps):
     for shape in ((100, 300), (300, 100), (2, 40, 50)):
