@@ -843,6 +843,8 @@ def xconv_muon_step(W, dW, M, lr: float, momentum: float = 0.95, nesterov: bool 
     a, b, c = coefficients
     desc = UpdateDesc(steps, a, b, c, eps, lr, momentum, weight_decay, 1 if nesterov else 0, _ADJUST[adjust])
     _update(lib().xconv_muon_step, "xconv_muon_step", desc, items, Ws[0].device)
+    # As every in-place operation: a graph that kept one of them for its backward pass says so.
+    torch.autograd.graph.increment_version([t for t in Ws + Ms if not t.is_inference()])
     return W
 
 

@@ -463,17 +463,17 @@ PyObject* orthogonalize(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   const Several G(a[0]);
   if (G.size() == 0 || !steps_of(a[1], a[2], a[3], &d)) Py_RETURN_NONE;
   std::vector<xconv_matrices> items((size_t)G.size());
-  std::vector<const at::Tensor*> in;
+  std::vector<at::Tensor> in;                        // (held: other threads run during the call, and the list is theirs too)
   for (Py_ssize_t i = 0; i < G.size(); ++i) {
     const at::Tensor* g = dense(G[i]);
     if (!g || !matrices_of(*g, &items[i])) Py_RETURN_NONE;
-    in.push_back(g);
+    in.push_back(*g);
   }
   std::vector<at::Tensor> out;
   for (size_t i = 0; i < in.size(); ++i) {
-    out.push_back(dense_like(*in[i]));
-    items[i].G = in[i]->data_ptr(); items[i].O = out[i].data_ptr();
-    items[i].g_dtype = items[i].o_dtype = dtype_code(*in[i]);
+    out.push_back(dense_like(in[i]));
+    items[i].G = in[i].data_ptr(); items[i].O = out[i].data_ptr();
+    items[i].g_dtype = items[i].o_dtype = dtype_code(in[i]);
   }
   if (!raise(update(lib.orthogonalize, d, items, out[0]), "xconv_orthogonalize")) return nullptr;
   if (!G.list) return THPVariable_Wrap(out[0]);
@@ -496,15 +496,18 @@ PyObject* muon_step(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   adjust = (int32_t)PyLong_AsLong(a[10]);
   d.nesterov = a[5] == Py_True; d.adjust = adjust;
   std::vector<xconv_matrices> items((size_t)W.size());
-  const at::Tensor* like = nullptr;
+  std::vector<at::Tensor> written, read;             // (held)
   for (Py_ssize_t i = 0; i < W.size(); ++i) {
     const at::Tensor *w = dense(W[i]), *g = dense(G[i]), *m = dense(M[i]);
     if (!w || !g || !m || g->sizes() != w->sizes() || m->sizes() != w->sizes() || m->scalar_type() != at::kFloat || !matrices_of(*w, &items[i])) Py_RETURN_NONE;
     items[i].G = g->data_ptr(); items[i].M = (float*)m->data_ptr(); items[i].O = w->data_ptr();
     items[i].g_dtype = dtype_code(*g); items[i].o_dtype = dtype_code(*w);
-    like = w;
+    written.push_back(*w); written.push_back(*m); read.push_back(*g);
   }
-  if (!raise(update(lib.muon_step, d, items, *like), "xconv_muon_step")) return nullptr;
+  if (!raise(update(lib.muon_step, d, items, written[0]), "xconv_muon_step")) return nullptr;
+  // As every in-place operation: a graph that kept one of them for its backward pass says so.
+  for (const at::Tensor& t : written)
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
   Py_RETURN_TRUE;
   XM_END
 }

@@ -131,3 +131,23 @@ def test_muon_step(monkeypatch):
         with pytest.raises(xb.XConvError):
             xb.xconv_muon_step(*args, 0.02)
         assert torch.equal(W, before)
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_a_graph_that_keeps_the_weights_notices_the_step(native, monkeypatch):
+    if not native:
+        monkeypatch.setattr(xb, "_native", _PythonPath())
+    W = _make((20, 30), torch.float32, 0).requires_grad_()
+    x = _make((30, 4), torch.float32, 1).requires_grad_()
+    y = (W @ x).sum()
+    before = W._version
+    M = torch.zeros_like(W.detach())
+    xb.xconv_muon_step(W, torch.ones_like(W.detach()), M, 0.02)
+    assert W._version > before and M._version > 0
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
+    with torch.inference_mode():                                    # (tensors without a count)
+        W = torch.ones(20, 30, device="cuda")
+        M = torch.zeros(20, 30, device="cuda")
+        xb.xconv_muon_step(W, torch.ones(20, 30, device="cuda"), M, 0.02)
+        assert W.isfinite().all() and not torch.equal(W, torch.ones_like(W))
