@@ -723,7 +723,8 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_product_kernel(const __grid_
 
 // ---- matrices whose smaller side is at most 128, in one kernel: a cluster of up to eight CTAs a matrix, X in their shared memory
 
-// Small matrices are bound by latencies: 17 kernels of 7 to 9 us each, of which the products take one.  Here a CTA holds up to three blocks of 64 columns of X for all steps.  A
+// Small matrices are bound by latencies: 17 kernels of 7 to 9 us each, of which the products take one (64 x 576, five steps: 136 us; here 55, with the tensor cores
+// idle most of the time).  Here a CTA holds up to three blocks of 64 columns of X for all steps.  A
 // step: the products of the CTA's own columns, summed over the cluster through the SMs' network (each CTA sums some columns and gives them to the others), then A A
 // and B X in every CTA by itself.  Three chains of MMAs with a wait behind each; twelve in all where the cluster is one CTA.
 constexpr int SMALL_THREADS = 512, SMALL_COLUMN_BLOCKS = 3;
@@ -1035,7 +1036,7 @@ __device__ __forceinline__ void small_steps(const NsArgs& p, const NsEntry& e, i
 // Their sums are rounded to nearest, where the tensor cores cut them off; with few terms that shows: error against 64 bits, as a share of 1.5 times that of float
 // arithmetic by the library, at worst 1.18 on the tensor cores and 0.58 here (16 x 75; 20 x 60: 1.18 and 0.53; 32 x 64: 1.01 and 0.49; 64 x 64 there: 0.73).  Nothing waits
 // for MMAs either.  Bound by the loads from shared memory, of which a thread shares each among its products.  Measured, five steps, tensor cores and this: 6 x 75 30.7 and
-// 16.4 us, 16 x 384 47 and 31, 32 x 32 24.6 and 22.6, 32 x 192 36.9 and 43.0, 32 x 256 41.0 and 36.9.
+// 16.4 us, 16 x 384 47 and 31, 32 x 32 24.6 and 22.6, 32 x 192 36.9 and 43.0, 32 x 256 41.0 and 36.9; three layers of 16 x 75 to 32 x 800 (a cluster of eight) 45 and 45.
 
 constexpr int TINY = 32, TINY_X = SMALL_COLUMN_BLOCKS * 64 + 4, TINY_A = TINY + 4;      // rows; floats of a row of X, of A and B (16 bytes more: eight rows in different banks)
 
@@ -1045,11 +1046,7 @@ __device__ __forceinline__ float ld_shared_f(uint32_t addr) {
   return v;
 }
 __device__ __forceinline__ void st_shared_f(uint32_t addr, float v) { asm volatile("st.shared.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory"); }
-__device__ __forceinline__ float ld_cluster_f(uint32_t addr, uint32_t rank) {
-  float v;
-  asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %1, %2;\n\tld.shared::cluster.f32 %0, [a];\n\t}" : "=f"(v) : "r"(addr), "r"(rank));
-  return v;
-}
+__device__ __forceinline__ float4 add4(float4 a, float4 b) { return make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w); }
 // The products of row i with rows j and, with TWO, j + 16 over `fours` groups of four columns (eight lanes read eight rows in a row: different banks).
 template <bool TWO>
 __device__ __forceinline__ float2 tiny_products(uint32_t rows, int pitch, int i, int j, int fours) {
@@ -1112,39 +1109,37 @@ __device__ __noinline__ void tiny_steps(const NsArgs& p, const NsEntry& e, int m
   const int columns = min(blocks * 64, e.m - cb0 * NS_COLS);
 #pragma unroll 1
   for (int step = 0; step < p.which; ++step) {
-    float2 s = make_float2(0.f, 0.f);
-    if (TWO) {
-      const uint32_t quarters = smem + SMALL_E + 2u * (TINY * TINY_A * 4);
-      tiny_gram(X, quarters, (columns + 3) >> 2);
-      __syncthreads();
+    // The CTA's sums, then the cluster's, four neighbouring ones a thread (those sums in two buffers in turn: one is written again two barriers later).
+    const uint32_t parts = smem + SMALL_E + 2u * (TINY * TINY_A * 4), sums = smem + SMALL_E + (uint32_t)(step & 1) * (TINY * TINY_A * 4);
+    const uint32_t at4 = (uint32_t)((t >> 3) * TINY_A + (t & 7) * 4) * 4;
+    const bool adds = t < N * 8 && (TWO || (t & 7) < 4);
+    if (TWO) tiny_gram(X, parts, (columns + 3) >> 2);
+    else if (i < N) st_shared_f(parts + at, tiny_products<false>(X, TINY_X, i, j, (columns + 3) >> 2).x);
+    __syncthreads();
+    if (adds) {
+      float4 v = ld_shared_f4(parts + at4);
+      if (TWO) {
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        s.x += ld_shared_f(quarters + at + (uint32_t)(q * TINY * TINY_A) * 4);
-        s.y += ld_shared_f(quarters + at + (uint32_t)(q * TINY * TINY_A) * 4 + 64);
+        for (int q = 1; q < 4; ++q) v = add4(v, ld_shared_f4(parts + at4 + (uint32_t)(q * TINY * TINY_A) * 4));
       }
-    } else if (i < N) s = tiny_products<false>(X, TINY_X, i, j, (columns + 3) >> 2);
-    if (p.cs > 1) {
-      // (two buffers in turn: one is written again two barriers later)
-      const uint32_t sums = smem + SMALL_E + (uint32_t)(step & 1) * (TINY * TINY_A * 4) + at;
-      st_shared_f(sums, s.x);
-      if (TWO) st_shared_f(sums + 64, s.y);
-      cluster_sync();
-      s = make_float2(0.f, 0.f);
-#pragma unroll 4
-      for (int c = 0; c < p.cs; ++c) {
-        s.x += ld_cluster_f(sums, c);
-        if (TWO) s.y += ld_cluster_f(sums + 64, c);
-      }
+      st_shared_v4((p.cs > 1 ? sums : A) + at4, make_uint4(__float_as_uint(v.x), __float_as_uint(v.y), __float_as_uint(v.z), __float_as_uint(v.w)));
     }
-    if (i < N) {
-      st_shared_f(A + at, s.x);
-      if (TWO) st_shared_f(A + at + 64, s.y);
+    if (p.cs > 1) {
+      cluster_sync();
+      if (adds) {
+        float4 f[SMALL_CLUSTER];
+#pragma unroll
+        for (int c = 0; c < SMALL_CLUSTER; ++c) f[c] = c < p.cs ? ld_cluster_f4(sums + at4, c) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int c = 1; c < SMALL_CLUSTER; ++c) f[0] = add4(f[0], f[c]);
+        st_shared_v4(A + at4, make_uint4(__float_as_uint(f[0].x), __float_as_uint(f[0].y), __float_as_uint(f[0].z), __float_as_uint(f[0].w)));
+      }
     }
     __syncthreads();
     if (i < N) {
       const float2 q = tiny_products<TWO>(A, TINY_A, i, j, N / 4);
-      st_shared_f(B + at, fmaf(p.c, q.x, p.b * s.x) + (i == j && i < e.n ? p.a : 0.f));
-      if (TWO) st_shared_f(B + at + 64, fmaf(p.c, q.y, p.b * s.y) + (i == j + 16 && i < e.n ? p.a : 0.f));
+      st_shared_f(B + at, fmaf(p.c, q.x, p.b * ld_shared_f(A + at)) + (i == j && i < e.n ? p.a : 0.f));
+      if (TWO) st_shared_f(B + at + 64, fmaf(p.c, q.y, p.b * ld_shared_f(A + at + 64)) + (i == j + 16 && i < e.n ? p.a : 0.f));
     }
     const bool last = step + 1 == p.which;
     // 128 columns at a time: all have read them before one writes.
