@@ -350,8 +350,10 @@ xconv_status xconv_layernorm_backward(const xconv_norm_desc* desc, const void* d
  *   `steps` times   A = X X^T,  X = (a I + b A + c A A) X,
  *   orthogonalize(U) = X    (transposed back),
  * that is, the singular vectors of U with every singular value s / max(|U|, eps) mapped `steps` times by s -> a s + b s^3 + c s^5.
- * The products are as exact as products of floats whatever the storage types; what is below 2^-38 in X is lost, which only matters to a matrix whose
- * norm is far below eps.  A matrix with a value that is not finite becomes NaN; the others keep their bits.
+ * The products are about as exact as products of floats (error against 64 bits 0.3 to 1.5 times theirs; where every O of a call has 16 bits the sums are cut off
+ * more coarsely, some 30 times below the rounding to O); what is below 2^-38 in X is lost, which only matters to a matrix whose norm is far below eps.  A matrix
+ * with a value that is not finite becomes NaN; the others keep their bits.  The same call gives the same bits every time; with other items beside it a
+ * matrix may get its sums in another order.
  *
  * xconv_orthogonalize: O = orthogonalize(G).  G [batch][rows][cols] in g_dtype, O in o_dtype; M is ignored, and so is what follows `eps` in the descriptor.
  * xconv_muon_step, in place: with g = G (in g_dtype) and m = M (float)
