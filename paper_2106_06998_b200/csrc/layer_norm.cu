@@ -13,6 +13,11 @@
 // thread its own 16-byte pieces, so that no thread waits for another's.  Dense rows that do not begin on 16-byte boundaries (odd channel counts) are fetched and
 // written as runs of several rows that do, and picked apart in shared memory.  Other rows (some of the channels of a wider tensor, at odd offsets) are read element by
 // element; rows that do not fit the registers of a block are read again for every sum.
+//
+// Measured (B200, copy rate 6.55 TB/s; launches replayed from a graph): forward, 200704 rows of 128 bfloat16 values, 103 MB, 19.0 us = 5.4 TB/s (a sum of two tensors
+// moving as much takes 17.4); backward, 8192 rows of 4096 bfloat16 values, 201 MB, 46 us = 4.4 TB/s, of which the sums of the columns 2; issue slots 52 % busy, one
+// block of 512 threads with 126 registers an SM, whose sums over a row nothing covers (two rows at once: 65 us; a barrier a group instead of the block's: 56).  47250
+// rows of 97 float16 values by runs: forward 10.3, backward 15.3 us (one value at a time 12.0 and 20.0).  One row: 2.6 us, a launch.
 #include "layer_norm.h"
 
 #include <algorithm>
