@@ -253,3 +253,31 @@ def test_rows_behind_the_last_are_left_as_they_were():
         assert L.xconv_layernorm_backward(ctypes.byref(d), dY.data_ptr(), X.data_ptr(), stats[0].data_ptr(), stats[1].data_ptr(), w.data_ptr(), out.data_ptr(),
                                           None, None, None, 0, s) == 0
         check_backward(dY, X, stats[0, :19], stats[1, :19], w, out[:19], *xb.xconv_layernorm_backward(dY, X, stats[0, :19], stats[1, :19], w)[1:])
+
+
+@pytest.mark.parametrize("C", [97, 136])
+def test_offsets_that_pass_32_bits(C):
+    """Rows of zeros (whose gradients are zeros, and add nothing to the columns' sums) before the ones that are looked at."""
+    tail = 2000
+    rows = 2 ** 32 // C + tail + 5
+    X, dY = (torch.zeros((rows, C), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    x, dy, w, b = make((tail, C), torch.bfloat16, torch.float32, seed=C)
+    X[-tail:], dY[-tail:] = x, dy
+    Y, mean, rstd = xb.xconv_layernorm(X, w, b, eps=EPS)
+    check_forward(x, w, b, Y[-tail:], mean[-tail:], rstd[-tail:])
+    assert torch.equal(Y[:-tail].amin(0), b.bfloat16()) and torch.equal(Y[:-tail].amax(0), b.bfloat16()) and not mean[:-tail].any()
+    del Y
+    dX, dw, db = xb.xconv_layernorm_backward(dY, X, mean, rstd, w)
+    check_backward(dy, x, mean[-tail:], rstd[-tail:], w, dX[-tail:], dw, db)
+    assert not dX[:-tail].amax(0).any() and not dX[:-tail].amin(0).any()
+
+
+@pytest.mark.parametrize("at, C", [(4096, 1000), (4097, 97), (64, 20000)])
+def test_strides_whose_offsets_pass_32_bits(at, C):
+    buffer = torch.empty((35, 2 ** 27), dtype=torch.bfloat16, device="cuda")
+    x, dy, w, b = make((35, C), torch.bfloat16, torch.bfloat16, seed=at)
+    X, dY = buffer[:, at:at + C], buffer[:, 2 ** 26 + at:2 ** 26 + at + C]
+    X.copy_(x); dY.copy_(dy)
+    Y, mean, rstd = xb.xconv_layernorm(X, w, b, eps=EPS)
+    check_forward(x, w, b, Y, mean, rstd)
+    check_backward(dy, x, mean, rstd, w, *xb.xconv_layernorm_backward(dY, X, mean, rstd, w))

@@ -166,7 +166,7 @@ def test_a_matrix_that_is_not_finite_is_the_only_one(bad):
 
 
 def test_more_matrices_than_the_scratch_memory_holds_at_once():
-    """300 matrices of 1024 x 1024 go through the kernels 128 at a time; their gradients lie further apart than 2^31 bytes reach... and come back in order."""
+    """600 matrices of 1024 x 1024 go through the kernels some at a time, and come back in order."""
     G = make((600, 1024, 1024), torch.bfloat16, seed=9, scale=1.0)
     O = xb.xconv_orthogonalize(G)
     for i in (0, 1, 127, 128, 255, 256, 599):
