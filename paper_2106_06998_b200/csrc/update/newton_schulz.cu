@@ -94,7 +94,10 @@ template <typename G>
 __device__ __forceinline__ double squares_of(const NsArgs& p, const NsEntry& e, size_t first, size_t last) {
   const G* g = static_cast<const G*>(e.g);
   double s = 0.0;
-  if ((first | last) % 4 == 0) {                             // (every pointer is aligned to 16 bytes)
+  // (The tensors lie on 16-byte boundaries, but not every entry of a table: where a batch is cut it begins at any of the batch's matrices, of any number of values.  The
+  // accesses of four or eight values elsewhere are those of rows of a multiple of four or eight, whose matrices are too.)
+  const auto fours = [](const void* at, size_t each) { return reinterpret_cast<uintptr_t>(at) % (4 * each) == 0; };
+  if ((last - first) % 4 == 0 && fours(g + first, sizeof(G)) && (!p.muon || fours(e.mom + first, sizeof(float)))) {
     constexpr int DEEP = 4;                                  // loads that are under way together
 #pragma unroll
     for (int k0 = 0; k0 < NS_CHUNK / 1024; k0 += DEEP) {
