@@ -665,10 +665,14 @@ NormArgs args_of(const xconv_norm_desc* d, const NormPlan& p) {
   return a;
 }
 
+// Shared memory of a launch at most: 192 KB of ring, 200 KB of runs, 64 KB of columns' sums.
+constexpr int NORM_SMEM_MAX = 200 * 1024;
+
 template <typename K>
 cudaError_t norm_launch(K kernel, const NormPlan& p, const NormArgs& a, cudaStream_t st) {
   if (p.smem > 40 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, p.smem);
+    // (the same for every size, so that no other thread finds it lowered)
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, NORM_SMEM_MAX);
     if (e != cudaSuccess) return e;
   }
   kernel<<<dim3((unsigned)p.blocks), dim3(p.threads), p.smem, st>>>(a);
@@ -738,7 +742,7 @@ static NormPlan plan(const xconv_norm_desc* d, bool vec, bool dense, bool backwa
   if (!vec && dense && es == 2) {
     p.words = true;
     pick_group(d->C / 2 + 1, es, &p);
-    p.words = !p.wide && p.group <= 128 && RUN_STAGES * (size_t)tensors * std::max(256 / p.group, 8) * d->C * es <= 200u * 1024;
+    p.words = !p.wide && p.group <= 128 && RUN_STAGES * (size_t)tensors * std::max(256 / p.group, 8) * d->C * es <= (size_t)NORM_SMEM_MAX;
   }
   if (!p.words) pick_group(nv, es, &p);
   if (p.wide) {
@@ -764,7 +768,7 @@ static NormPlan plan(const xconv_norm_desc* d, bool vec, bool dense, bool backwa
   else if (dense) {
     const long groups = p.threads / p.group, run = std::max<long>(groups, 8);              // (8 rows of any type are a multiple of 16 bytes)
     const size_t bytes = RUN_STAGES * (size_t)tensors * run * d->C * es;
-    if (bytes <= 200u * 1024) {
+    if (bytes <= (size_t)NORM_SMEM_MAX) {
       p.run = (int)run;
       p.smem = (int)bytes;
       p.blocks = std::min<long>((d->rows + run - 1) / run, (long)NORM_SMS * std::max<long>(1, std::min<long>(resident * (NORM_THREADS / p.threads), 220 * 1024 / ((long)bytes + 2048))));

@@ -1,0 +1,52 @@
+"""Layer norm at the limits of what one call may take for granted: other host threads, other calls on its scratch memory, the ends of the floats' range."""
+import ctypes
+import threading
+
+import pytest
+import torch
+
+import __graft_entry__ as entry
+from paper_2106_06998_b200 import binding as xb
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    entry.build()
+    torch.cuda.set_device(0)
+
+
+@pytest.mark.parametrize("backward", [False, True])
+def test_calls_of_different_sizes_from_two_host_threads(backward):
+    """The same kernel with different amounts of shared memory (gradients: 48 and 96 KB; forward: 32 and 64 KB), by the C ABI's calls, which hold no lock of the interpreter's: no thread lowers
+    the kernel's limit under another one's launch."""
+    errors = []
+
+    def job(rows):
+        try:
+            s = torch.cuda.Stream()
+            with torch.cuda.stream(s):
+                X = torch.randn(rows, 64, device="cuda").bfloat16()
+                Y, mean, rstd = torch.empty_like(X), torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+                dX, dw, db = torch.empty_like(X), torch.empty(64, device="cuda"), torch.empty(64, device="cuda")
+                desc = xb.NormDesc(rows, 64, xb.XCONV_BF16, xb.XCONV_F32, 1e-5, 64, 64, 64)
+                ws = torch.empty(xb.lib().xconv_layernorm_workspace_bytes(ctypes.byref(desc)), dtype=torch.uint8, device="cuda")
+                p = [t.data_ptr() for t in (X, Y, mean, rstd, dX, dw, db, ws)]
+                for i in range(4000):
+                    if backward:
+                        r = xb.lib().xconv_layernorm_backward(ctypes.byref(desc), p[0], p[0], p[2], p[3], None, p[4], p[5], p[6], p[7], ws.numel(), s.cuda_stream)
+                    else:
+                        r = xb.lib().xconv_layernorm_forward(ctypes.byref(desc), p[0], None, None, p[1], p[2], p[3], s.cuda_stream)
+                    assert r == 0, (i, r, xb.lib().xconv_last_cuda_error())
+                    if i % 100 == 0:
+                        s.synchronize()
+                s.synchronize()
+        except BaseException as e:
+            errors.append(e)
+
+    torch.cuda.synchronize()
+    threads = [threading.Thread(target=job, args=(rows,)) for rows in (6000, 200000)]
+    [t.start() for t in threads]
+    [t.join() for t in threads]
+    assert not errors, errors
