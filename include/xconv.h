@@ -389,7 +389,7 @@ xconv_status xconv_muon_step(const xconv_update_desc* desc, const xconv_matrices
  * `cuda_stream`).  XCONV_OK, or XCONV_ERR_TIMEOUT if a bounded device-side wait ran out in that call.
  * The header never needs clearing: every call tags it afresh, so a later call on the same `ws`
  * reports its own outcome.  (Only the tensor-core kernels wait on anything; calls served by the
- * FP32-FMA kernels leave the header as it was.) */
+ * FP32-FMA kernels and the layer norm's gradients leave the header as it was.) */
 xconv_status xconv_workspace_status(const void* ws, void* cuda_stream);
 
 /* Self-test of the failure path: one warp waits, with the same bounded wait the pipelined kernels use,

@@ -19,6 +19,9 @@ static xconv_status validate_norm(const xconv_norm_desc* d) {
   if (d->x_stride > most / d->rows || d->y_stride > most / d->rows || d->dx_stride > most / d->rows) return XCONV_ERR_UNSUPPORTED;
   return XCONV_OK;
 }
+// The words at the front of the scratch memory that xconv_workspace_status reads: no kernel of the norm waits on anything, and they stay as they are.
+static const size_t NORM_HEADER = 256;
+
 static inline bool off(const void* p, size_t a) { return p && reinterpret_cast<uintptr_t>(p) % a != 0; }
 static inline size_t size_of(int dtype) { return dtype == XCONV_F32 ? 4 : 2; }
 static xconv_status cuda_status(cudaError_t e) {
@@ -35,7 +38,7 @@ extern "C" {
 
 size_t xconv_layernorm_workspace_bytes(const xconv_norm_desc* desc) {
   if (validate_norm(desc) != XCONV_OK) return 0;
-  return (size_t)norm_backward_parts(desc) * 2 * (size_t)desc->C * sizeof(float);
+  return NORM_HEADER + (size_t)norm_backward_parts(desc) * 2 * (size_t)desc->C * sizeof(float);
 }
 
 xconv_status xconv_layernorm_forward(const xconv_norm_desc* desc, const void* X, const void* weight, const void* bias, void* Y, float* mean, float* rstd,
@@ -63,7 +66,7 @@ xconv_status xconv_layernorm_backward(const xconv_norm_desc* desc, const void* d
   if (sums && off(ws, 16)) return XCONV_ERR_ALIGNMENT;
   const NormPlan p = plan_norm_backward(desc, dY, X, weight, dX);
   const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  float* part = sums ? static_cast<float*>(ws) : nullptr;
+  float* part = sums ? reinterpret_cast<float*>(static_cast<char*>(ws) + NORM_HEADER) : nullptr;
   new_call();
   ++g_launches;
   xconv_status r = cuda_status(launch_norm_backward(desc, p, dY, X, mean, rstd, weight, dX, part, st));

@@ -728,7 +728,8 @@ cudaError_t with_types(const xconv_norm_desc* d, F&& f) {
   return d->param_dtype == XCONV_F32 ? f(f16(), float()) : f(f16(), f16());
 }
 
-constexpr long WIDE_ROWS = 64;                               // rows that a block of norm_columns_wide_kernel adds, at least
+// Rows that a block of norm_columns_wide_kernel adds, at least, and partial sums at most: with the header in front 4 KB of scratch memory a channel.
+constexpr long WIDE_ROWS = 64, WIDE_PARTS = 511;
 
 }  // namespace
 
@@ -747,7 +748,7 @@ static NormPlan plan(const xconv_norm_desc* d, bool vec, bool dense, bool backwa
   if (!p.words) pick_group(nv, es, &p);
   if (p.wide) {
     p.threads = 1024;
-    p.parts = std::min<long>((d->rows + WIDE_ROWS - 1) / WIDE_ROWS, 512);
+    p.parts = std::min<long>((d->rows + WIDE_ROWS - 1) / WIDE_ROWS, WIDE_PARTS);
     p.blocks = std::min<long>(d->rows, (backward ? 2 : 8) * NORM_SMS);
     return p;
   }

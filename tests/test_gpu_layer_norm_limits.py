@@ -50,3 +50,23 @@ def test_calls_of_different_sizes_from_two_host_threads(backward):
     [t.start() for t in threads]
     [t.join() for t in threads]
     assert not errors, errors
+
+
+def test_the_gradients_leave_the_scratch_memorys_header():
+    """Two equal channels: their sums are the same bits, which in the header would read as a wait that ran out."""
+    X = torch.randn(1000, 40, device="cuda")
+    X[:, 1] = X[:, 0]
+    dY = torch.randn(1000, 40, device="cuda")
+    dY[:, 1] = dY[:, 0]
+    _, mean, rstd = xb.xconv_layernorm(X)
+    ws = xb.workspace(1 << 20, X.device)
+    ws.zero_()
+    assert xb.workspace_status(ws) == 0
+    _, dw, db = xb.xconv_layernorm_backward(dY, X, mean, rstd)
+    assert xb.workspace(1, X.device) is ws and dw[0] == dw[1] != 0 and db[0] == db[1] != 0
+    assert xb.workspace_status(ws) == 0
+    # what another call left there stays
+    assert xb.lib().xconv_selftest_wait_limit(ws.data_ptr(), ws.numel(), 5, torch.cuda.current_stream().cuda_stream) == 0
+    left = ws[:256].clone()
+    xb.xconv_layernorm_backward(dY, X, mean, rstd)
+    assert xb.workspace_status(ws) != 0 and torch.equal(ws[:256], left)
