@@ -206,10 +206,10 @@ __device__ __forceinline__ void norm_params(const NormArgs& a, int lane, float (
     if (a.bias && c < a.C) load_params<P, VEC>(static_cast<const P*>(a.bias) + c, b[v]);
   }
 }
-// The gradients of a row (x and dy of it; dy becomes dx), and its part of dw and db.
-template <int VEC, int V, bool FULL>
+// The gradients of a row (x and dy of it; dy becomes dx), and its part of dw and db.  has: which of the thread's values are the row's; x and dy are zeros elsewhere.
+template <int VEC, int V, bool FULL, class Has = NormAll>
 __device__ __forceinline__ void norm_row_backward(const NormArgs& a, int lane, float mean, float rstd, float (&x)[V][VEC], float (&dy)[V][VEC],
-                                                  const float (&w)[V][VEC], float (&dw)[V][VEC], float (&db)[V][VEC], float (*sums)[2]) {
+                                                  const float (&w)[V][VEC], float (&dw)[V][VEC], float (&db)[V][VEC], float (*sums)[2], Has has = Has()) {
   constexpr int STEP = VEC > 1 ? 2 : 1;
   Pair t0 = both(0.f), t1 = both(0.f);
 #pragma unroll
@@ -218,7 +218,11 @@ __device__ __forceinline__ void norm_row_backward(const NormArgs& a, int lane, f
 #pragma unroll
     for (int e = 0; e < VEC; e += STEP) {
       // (a row that is not there is zeros, with a mean and rstd of zero)
-      const Pair h = mul<VEC>(add<VEC>(Pair::of(x[v], e), both(-mean)), both(rstd)), d = Pair::of(dy[v], e);
+      Pair h = mul<VEC>(add<VEC>(Pair::of(x[v], e), both(-mean)), both(rstd));
+      const Pair d = Pair::of(dy[v], e);
+      // (mean * rstd may be beyond the floats where x - mean is not)
+      if (!has(v, e)) h.v.x = 0.f;
+      if (VEC > 1 && !has(v, e + 1)) h.v.y = 0.f;
       fma<VEC>(d, h, Pair::of(dw[v], e)).to(dw[v], e);
       add<VEC>(d, Pair::of(db[v], e)).to(db[v], e);
       const Pair g = mul<VEC>(d, Pair::of(w[v], e));
@@ -521,7 +525,7 @@ __global__ void __launch_bounds__(NORM_THREADS, BACKWARD ? 1 : 2) norm_runs_kern
         float dy[V][W];
         read(ds + r * a.C, in, dy);
         const float mean = in ? __ldg(a.mean + first + r) : 0.f, rstd = in ? __ldg(a.rstd + first + r) : 0.f;
-        norm_row_backward<W, V, true>(a, lane, mean, rstd, x, dy, w, dw, db, sums[turn]);
+        norm_row_backward<W, V, true>(a, lane, mean, rstd, x, dy, w, dw, db, sums[turn], has);
         if (in) write(xs + r * a.C, dy);
       } else {
         float mean, rstd;

@@ -70,3 +70,24 @@ def test_the_gradients_leave_the_scratch_memorys_header():
     left = ws[:256].clone()
     xb.xconv_layernorm_backward(dY, X, mean, rstd)
     assert xb.workspace_status(ws) != 0 and torch.equal(ws[:256], left)
+
+
+@pytest.mark.parametrize("eps,size", [(1e-5, 1.5e36), (1e-12, 1e33)])
+@pytest.mark.parametrize("C", [7, 31, 97, 100, 601])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_gradients_of_large_rows_without_variance_are_finite(dtype, C, eps, size):
+    """mean * rstd is beyond the floats there, (x - mean) * rstd is zero: also in the columns that a thread does not have."""
+    rows = 70
+    X = torch.full((rows, C), size, device="cuda").to(dtype)
+    X[::2] *= -1
+    mean, rstd = X[:, 0].float().contiguous(), torch.full((rows,), eps ** -0.5, device="cuda")
+    assert not (mean * rstd).isfinite().any()
+    dY = torch.randn(rows, C, device="cuda").to(dtype)
+    dX, dw, db = xb.xconv_layernorm_backward(dY, X, mean, rstd)
+    assert dX.isfinite().all() and (dw == 0).all()
+    g = dY.double()
+    want = rstd.double()[:, None] * (g - g.mean(1, keepdim=True))
+    half = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8}[dtype]
+    # sums of up to 601 terms in chains of 150 at most, four operations behind them, one rounding to the type
+    assert ((dX.double() - want).abs() <= half * want.abs() + (1 + half) * 154 * 2.0 ** -24 * rstd[:, None] * (g.abs() + g.abs().mean(1, keepdim=True))).all()
+    assert ((db.double() - g.sum(0)).abs() <= rows * 2.0 ** -24 * g.abs().sum(0)).all()
