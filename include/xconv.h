@@ -336,8 +336,8 @@ typedef struct {
 xconv_status xconv_layernorm_forward(const xconv_norm_desc* desc, const void* X, const void* weight, const void* bias, void* Y, float* mean, float* rstd,
                                      void* cuda_stream);
 
-/* mean and rstd as the forward call left them (desc.eps is ignored).  weight may be NULL (1), dweight and dbias too: what is NULL is not computed, and with both
- * NULL `ws` may be.  ws: xconv_layernorm_workspace_bytes(desc) bytes, 16-byte aligned (0 for an invalid descriptor). */
+/* mean and rstd as the forward call left them (desc.eps does not enter the gradients, but is refused as there).  weight may be NULL (1), dweight and dbias too: what
+ * is NULL is not computed, and with both NULL `ws` may be.  ws: xconv_layernorm_workspace_bytes(desc) bytes, 16-byte aligned (0 for an invalid descriptor). */
 size_t xconv_layernorm_workspace_bytes(const xconv_norm_desc* desc);
 xconv_status xconv_layernorm_backward(const xconv_norm_desc* desc, const void* dY, const void* X, const float* mean, const float* rstd, const void* weight, void* dX,
                                       float* dweight, float* dbias, void* ws, size_t ws_bytes, void* cuda_stream);

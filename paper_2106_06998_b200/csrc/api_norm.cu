@@ -8,15 +8,16 @@
 
 namespace xconv {
 
-static xconv_status validate_norm(const xconv_norm_desc* d) {
+// dx_stride is the gradients' alone.
+static xconv_status validate_norm(const xconv_norm_desc* d, bool gradients) {
   if (!d || d->rows <= 0 || d->C <= 0 || !(d->eps >= 0.f)) return XCONV_ERR_INVALID_ARG;
   if (d->dtype != XCONV_F32 && d->dtype != XCONV_BF16 && d->dtype != XCONV_F16) return XCONV_ERR_INVALID_ARG;
   if (d->param_dtype != XCONV_F32 && d->param_dtype != d->dtype) return XCONV_ERR_INVALID_ARG;
-  if (d->x_stride < 0 || d->y_stride < 0 || d->dx_stride < 0) return XCONV_ERR_INVALID_ARG;
+  if (d->x_stride < 0 || d->y_stride < 0 || (gradients && d->dx_stride < 0)) return XCONV_ERR_INVALID_ARG;
   // 32-bit grids, and 64-bit element offsets with room to spare
   if (d->rows > 2000000000L || d->C > (1 << 30)) return XCONV_ERR_UNSUPPORTED;
   const long most = 1L << 60;
-  if (d->x_stride > most / d->rows || d->y_stride > most / d->rows || d->dx_stride > most / d->rows) return XCONV_ERR_UNSUPPORTED;
+  if (d->x_stride > most / d->rows || d->y_stride > most / d->rows || (gradients && d->dx_stride > most / d->rows)) return XCONV_ERR_UNSUPPORTED;
   return XCONV_OK;
 }
 // The words at the front of the scratch memory that xconv_workspace_status reads: no kernel of the norm waits on anything, and they stay as they are.
@@ -37,13 +38,13 @@ using namespace xconv;
 extern "C" {
 
 size_t xconv_layernorm_workspace_bytes(const xconv_norm_desc* desc) {
-  if (validate_norm(desc) != XCONV_OK) return 0;
+  if (validate_norm(desc, true) != XCONV_OK) return 0;
   return NORM_HEADER + (size_t)norm_backward_parts(desc) * 2 * (size_t)desc->C * sizeof(float);
 }
 
 xconv_status xconv_layernorm_forward(const xconv_norm_desc* desc, const void* X, const void* weight, const void* bias, void* Y, float* mean, float* rstd,
                                      void* cuda_stream) {
-  const xconv_status s = validate_norm(desc);
+  const xconv_status s = validate_norm(desc, false);
   if (s != XCONV_OK) return s;
   if (!X || !Y || !mean != !rstd || desc->y_stride < desc->C) return XCONV_ERR_INVALID_ARG;
   const size_t es = size_of(desc->dtype), ps = size_of(desc->param_dtype);
@@ -56,7 +57,7 @@ xconv_status xconv_layernorm_forward(const xconv_norm_desc* desc, const void* X,
 
 xconv_status xconv_layernorm_backward(const xconv_norm_desc* desc, const void* dY, const void* X, const float* mean, const float* rstd, const void* weight, void* dX,
                                       float* dweight, float* dbias, void* ws, size_t ws_bytes, void* cuda_stream) {
-  const xconv_status s = validate_norm(desc);
+  const xconv_status s = validate_norm(desc, true);
   if (s != XCONV_OK) return s;
   if (!dY || !X || !mean || !rstd || !dX || desc->dx_stride < desc->C) return XCONV_ERR_INVALID_ARG;
   const size_t es = size_of(desc->dtype), ps = size_of(desc->param_dtype);
