@@ -641,6 +641,13 @@ def xconv_dgrad(dY: torch.Tensor, W: torch.Tensor, circular: bool = False) -> to
 
 # ------------------------------------------------------------------ around the layers
 
+def _int32(value: int, what: str) -> int:
+    """`value` as a descriptor's field of 32 bits holds it: ctypes would cut off what does not fit."""
+    if not -2 ** 31 <= value < 2 ** 31:
+        raise ValueError(f"{what} = {value} does not fit 32 bits")
+    return value
+
+
 def _rows(t: torch.Tensor, name: str):
     """(shape of the rows, C, row stride) of a tensor whose last axis -- of images and volumes (4-d, 5-d): whose channel axis -- has neighbouring values, and
     whose rows lie at one distance from each other: dense channels-last or row-major tensors, and views of some of their channels."""
@@ -651,7 +658,7 @@ def _rows(t: torch.Tensor, name: str):
         shape.append(shape.pop(1)); strides.append(strides.pop(1))
     if not 1 <= t.dim() <= 5:
         raise ValueError(f"{name} must have one to five dimensions")
-    C, unit = shape.pop(), strides.pop()
+    C, unit = _int32(shape.pop(), f"{name}: values of a row"), strides.pop()
     if C > 1 and unit != 1:
         raise ValueError(f"{name}: the values of a row must be neighbours (4-d and 5-d tensors in torch.channels_last(_3d) memory format)")
     row, span = None, None
@@ -771,7 +778,7 @@ def _matrices(t: torch.Tensor, name: str):
         cols = t.numel() // rows if rows else 0
     if t.numel() == 0:
         raise ValueError(f"{name} is empty")
-    return rows, cols, batch
+    return tuple(_int32(n, f"{name}: {what}") for n, what in ((rows, "rows"), (cols, "columns"), (batch, "matrices")))
 
 
 def _same_layout(a: torch.Tensor, b: torch.Tensor, names: str):
@@ -792,6 +799,7 @@ def xconv_orthogonalize(G, steps: int = 5, coefficients=NEWTON_SCHULZ, eps: floa
     out = (_native or _load_native()).orthogonalize(G, steps, coefficients, eps)
     if out is not None:
         return out
+    _int32(steps, "steps")
     many = isinstance(G, (list, tuple))
     tensors = list(G) if many else [G]
     if not tensors:
@@ -820,6 +828,7 @@ def xconv_muon_step(W, dW, M, lr: float, momentum: float = 0.95, nesterov: bool 
     whole network's weights in one call take little longer than the largest of them.  Returns W."""
     if (_native or _load_native()).muon_step(W, dW, M, lr, momentum, nesterov, weight_decay, steps, coefficients, eps, _ADJUST.get(adjust)) is not None:
         return W
+    _int32(steps, "steps")
     Ws, dWs, Ms = (list(t) if isinstance(t, (list, tuple)) else [t] for t in (W, dW, M))
     if not len(Ws) == len(dWs) == len(Ms):
         raise ValueError("W, dW and M must have the same length")
