@@ -265,6 +265,9 @@ __device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr, uint32_t rank) { 
                : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr), "r"(rank));
   return v;
 }
+__device__ __forceinline__ void st_cluster_u32(uint32_t addr, uint32_t rank, uint32_t v) {
+  asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %0, %1;\n\tst.shared::cluster.u32 [a], %2;\n\t}" ::"r"(addr), "r"(rank), "r"(v) : "memory");
+}
 __device__ __forceinline__ void arrive_at(uint64_t* bar, uint32_t rank) {      // ... of the same barrier in another CTA of the cluster
   asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %0, %1;\n\tmbarrier.arrive.shared::cluster.b64 _, [a];\n\t}"
                ::"r"(smem_u32(bar)), "r"(rank) : "memory");
@@ -483,12 +486,14 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_product_kernel(const __grid_
   __shared__ NsEntry es[NS_MOST];
   __shared__ NsUnit first;
   __shared__ uint32_t tmem_slot;
+  __shared__ uint32_t lost;                          // whether a wait for the sums of a shared tile ran out, in any CTA of the cluster
   const uint32_t smem = (smem_u32(raw) + 1023u) & ~1023u;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, entries = p.t.entries;
   const uint32_t rank = cluster_rank(), half = rank & 1u, leader = rank & ~1u;
   if (threadIdx.x == 0) {
     for (int i = 0; i < NS_STAGES; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); }
     for (int i = 0; i < NS_SETS; ++i) { mbar_init(&acc_full[i], 1); mbar_init(&acc_empty[i], 2 * NS_ADDERS); }
+    lost = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     prefetch_tmap(&p.whole);
     prefetch_tmap(&p.across);
@@ -684,6 +689,8 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_product_kernel(const __grid_
                        "f"(sum[4 * q + 2]), "f"(sum[4 * q + 3]) : "memory");
       }
     }
+    // (sums that are not there: none of the tile's is written)
+    if (!ok && shared && lane < 2 * p.cs) st_cluster_u32(smem_u32(&lost), (uint32_t)lane, 1u);
   }
   __syncwarp();
   tc_fence_before();
@@ -692,7 +699,7 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_product_kernel(const __grid_
     cluster_sync_relaxed();
   } else {
     cluster_sync();
-    if (warp >= 2) {
+    if (warp >= 2 && *reinterpret_cast<volatile uint32_t*>(&lost) == 0) {
       const NsUnit& w = first;
       const NsEntry& e = es[w.k];
       // This CTA's groups of eight columns; neighbouring lanes have neighbouring rows, or, where rows of the result are written, neighbouring columns.
@@ -764,14 +771,15 @@ __device__ __forceinline__ void small_chain(uint32_t d, const SmallOperand& a, c
   umma_warp(d, a.lo + a.step, a.hi, b.lo + b.step, b.hi, idesc, 1u);
 }
 
-struct SmallWait {             // for the MMAs that were issued last, by all threads
+struct SmallWait {             // for the MMAs that were issued last, by all threads; false where it ran out (the same in all lanes of a warp)
   uint64_t* bar;
   uint32_t parity;
   unsigned *status, tag;
-  __device__ __forceinline__ void operator()() {
-    mbar_wait_warp(bar, parity, status, tag);
+  __device__ __forceinline__ bool operator()() {
+    if (!mbar_wait_warp(bar, parity, status, tag)) return false;
     parity ^= 1u;
     tc_fence_after();
+    return true;
   }
 };
 
@@ -847,8 +855,12 @@ __device__ __noinline__ void small_write(const NsArgs& p, const NsEntry& e, int 
 }
 
 // N: columns of A that are worked on (n rounded up to 64 or 128).
+// Where a wait runs out, its warp leaves what the MMAs read and write alone, the block issues nothing more and writes no result, and the warp waits once more (with
+// the same limit) before the tensor memory is given back.  The CTAs of a cluster learn of it between the two barriers of the next step's sums, and end together: `gone`
+// (a word of shared memory) is written before the first of these barriers and read behind it, so that all of a cluster's threads read the same.
 template <int N>
-__device__ __forceinline__ void small_steps(const NsArgs& p, const NsEntry& e, int mat, uint32_t smem, uint32_t tmem, SmallWait wait, int blocks, int cb0, int rank) {
+__device__ __forceinline__ void small_steps(const NsArgs& p, const NsEntry& e, int mat, uint32_t smem, uint32_t tmem, SmallWait wait, int blocks, int cb0, int rank,
+                                            uint32_t* gone) {
   constexpr int COLS = N / 4, CAP = 512 / N;                 // a thread's columns of A; chains that the tensor memory holds at once
   constexpr uint32_t ID = (1u << 4) | ((uint32_t)(TILE_M >> 4) << 24), ID_A = ID | ((uint32_t)(N >> 3) << 17);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quadrant = warp & 3, part = warp >> 2, row = quadrant * 32 + lane;
@@ -866,13 +878,14 @@ __device__ __forceinline__ void small_steps(const NsArgs& p, const NsEntry& e, i
     return SmallOperand{((SMALL_X_GROUP >> 4) << 16) | ((base + SMALL_X + (uint32_t)c * 4u * SMALL_X_GROUP + (uint32_t)block * 1024u) >> 4), (128u >> 4) | (1u << 14), 2u * SMALL_X_GROUP >> 4,
                         SMALL_X_PART >> 4};
   };
+  bool ok = true, lost = false;                              // the warp's last wait; any of the block's (the same in all its threads)
 #pragma unroll 1
   for (int step = 0; step < p.which; ++step) {
     float sum[COLS];
 #pragma unroll
     for (int i = 0; i < COLS; ++i) sum[i] = 0.f;
     // the products of the CTA's own columns
-    for (int c0 = 0; c0 < 2 * blocks; c0 += CAP) {
+    for (int c0 = 0; c0 < 2 * blocks && !lost; c0 += CAP) {
       const int chains = min(CAP, 2 * blocks - c0);
       if (warp < SMALL_ISSUERS) {
         for (int c = warp; c < chains; c += SMALL_ISSUERS) {
@@ -881,10 +894,10 @@ __device__ __forceinline__ void small_steps(const NsArgs& p, const NsEntry& e, i
         }
         umma_commit_warp(wait.bar);
       }
-      wait();
-      small_sums<COLS / 16>(sum, tmem + lanes + part * COLS, chains, N);
+      ok = wait();
+      if (ok) small_sums<COLS / 16>(sum, tmem + lanes + part * COLS, chains, N);
       tc_fence_before();
-      __syncthreads();
+      lost = __syncthreads_or(!ok);
       tc_fence_after();
     }
     if (p.cs > 1) {
@@ -893,7 +906,9 @@ __device__ __forceinline__ void small_steps(const NsArgs& p, const NsEntry& e, i
       for (int q = 0; q < COLS / 4; ++q)
         asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(smem + SMALL_E + (uint32_t)(((part * (COLS / 4) + q) * 128 + row) * 16)), "f"(sum[4 * q]),
                      "f"(sum[4 * q + 1]), "f"(sum[4 * q + 2]), "f"(sum[4 * q + 3]) : "memory");
+      if (lost && threadIdx.x < p.cs) st_cluster_u32(smem_u32(gone), threadIdx.x, 1u);
       cluster_sync();
+      if (*reinterpret_cast<volatile uint32_t*>(gone) != 0) break;
       const int groups = N / 8 / p.cs;                       // of eight columns
       for (int x = threadIdx.x; x < 128 * groups; x += SMALL_THREADS) {
         const int r = x & 127, q8 = rank * groups + (x >> 7);
@@ -932,6 +947,7 @@ __device__ __forceinline__ void small_steps(const NsArgs& p, const NsEntry& e, i
       cluster_sync();
       fence_async();
     } else {
+      if (lost) break;
 #pragma unroll
       for (int q = 0; q < COLS / 8; ++q) {
         float v[8];
@@ -956,37 +972,39 @@ __device__ __forceinline__ void small_steps(const NsArgs& p, const NsEntry& e, i
       }
       umma_commit_warp(wait.bar);
     }
-    wait();
+    ok = wait();
+    if (ok) {
 #pragma unroll
-    for (int i = 0; i < COLS; ++i) sum[i] = 0.f;
-    small_sums<COLS / 16>(sum, tmem + lanes + part * COLS, k_chains, N);
+      for (int i = 0; i < COLS; ++i) sum[i] = 0.f;
+      small_sums<COLS / 16>(sum, tmem + lanes + part * COLS, k_chains, N);
 #pragma unroll
-    for (int q = 0; q < COLS / 8; ++q) {
-      const int q8 = part * (COLS / 8) + q;
-      const uint32_t at = smem + SMALL_A + (uint32_t)(q8 >> 3) * NS_OPERAND + piece_at(row, q8 & 7);
-      const uint4 ah = ld_shared_v4(at), al = ld_shared_v4(at + NS_PART);
-      const uint32_t h[4] = {ah.x, ah.y, ah.z, ah.w}, l[4] = {al.x, al.y, al.z, al.w};
-      const int d = row < e.n ? row - q8 * 8 : -1;
-      float v[8];
+      for (int q = 0; q < COLS / 8; ++q) {
+        const int q8 = part * (COLS / 8) + q;
+        const uint32_t at = smem + SMALL_A + (uint32_t)(q8 >> 3) * NS_OPERAND + piece_at(row, q8 & 7);
+        const uint4 ah = ld_shared_v4(at), al = ld_shared_v4(at + NS_PART);
+        const uint32_t h[4] = {ah.x, ah.y, ah.z, ah.w}, l[4] = {al.x, al.y, al.z, al.w};
+        const int d = row < e.n ? row - q8 * 8 : -1;
+        float v[8];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&h[k])), y = __half22float2(*reinterpret_cast<const __half2*>(&l[k]));
-        v[2 * k] = fmaf(p.c * NS_UNSCALE, sum[q * 8 + 2 * k], p.b * (x.x + y.x)) + (d == 2 * k ? p.a * NS_SCALE : 0.f);
-        v[2 * k + 1] = fmaf(p.c * NS_UNSCALE, sum[q * 8 + 2 * k + 1], p.b * (x.y + y.y)) + (d == 2 * k + 1 ? p.a * NS_SCALE : 0.f);
+        for (int k = 0; k < 4; ++k) {
+          const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&h[k])), y = __half22float2(*reinterpret_cast<const __half2*>(&l[k]));
+          v[2 * k] = fmaf(p.c * NS_UNSCALE, sum[q * 8 + 2 * k], p.b * (x.x + y.x)) + (d == 2 * k ? p.a * NS_SCALE : 0.f);
+          v[2 * k + 1] = fmaf(p.c * NS_UNSCALE, sum[q * 8 + 2 * k + 1], p.b * (x.y + y.y)) + (d == 2 * k + 1 ? p.a * NS_SCALE : 0.f);
+        }
+        uint4 hi, lo;
+        parts8(v, hi, lo);
+        st_shared_v4(at, hi);
+        st_shared_v4(at + NS_PART, lo);
       }
-      uint4 hi, lo;
-      parts8(v, hi, lo);
-      st_shared_v4(at, hi);
-      st_shared_v4(at + NS_PART, lo);
     }
     fence_async_smem();
     tc_fence_before();
-    __syncthreads();
+    lost = __syncthreads_or(!ok);
     // B X: as many of the CTA's blocks of columns at once as the tensor memory holds the chains of
     const bool last = step + 1 == p.which;
     const int at_once = k_chains <= 2 ? SMALL_COLUMN_BLOCKS : 2;
 #pragma unroll 1
-    for (int b0 = 0; b0 < blocks; b0 += at_once) {
+    for (int b0 = 0; b0 < blocks && !lost; b0 += at_once) {
       const int here = min(at_once, blocks - b0);
       const uint32_t pitch = (uint32_t)here * 64u;
       if (warp < SMALL_ISSUERS) {
@@ -995,9 +1013,9 @@ __device__ __forceinline__ void small_steps(const NsArgs& p, const NsEntry& e, i
         for (int c = warp; c < k_chains; c += SMALL_ISSUERS) small_chain(tmem + c * pitch, a_along(c), x_across(c, b0), id_x);
         umma_commit_warp(wait.bar);
       }
-      wait();
+      ok = wait();
 #pragma unroll 1
-      for (int b = 0; b < here; ++b) {
+      for (int b = 0; ok && b < here; ++b) {
         float x[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) x[i] = 0.f;
@@ -1024,14 +1042,16 @@ __device__ __forceinline__ void small_steps(const NsArgs& p, const NsEntry& e, i
       }
       tc_fence_before();
       if (!last) fence_async_smem();
-      __syncthreads();
-      if (last) {
+      lost = __syncthreads_or(!ok);
+      if (last && !lost) {
         small_write(p, e, mat, smem + SMALL_E, pitch, (long)(cb0 + b0) * NS_COLS);
         __syncthreads();
       }
     }
     if (warp < SMALL_ISSUERS) tc_fence_after();
+    if (lost && p.cs == 1) break;
   }
+  if (!ok) wait();
 }
 
 // ---- the same with a smaller side of at most 32, by FP32 multiply-adds in the same kernel
@@ -1244,13 +1264,14 @@ __device__ __forceinline__ double small_load(const NsArgs& p, const NsEntry& e, 
 __global__ void __launch_bounds__(SMALL_THREADS, 1) ns_small_kernel(const __grid_constant__ NsArgs p) {
   extern __shared__ uint8_t raw[];
   __shared__ uint64_t done;
-  __shared__ uint32_t tmem_slot;
+  __shared__ uint32_t tmem_slot, gone;
   __shared__ double warp_sums[SMALL_THREADS / 32], cta_sums[SMALL_CLUSTER];
   const uint32_t smem = (smem_u32(raw) + 1023u) & ~1023u;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = p.cs > 1 ? (int)cluster_rank() : 0, unit = (int)blockIdx.x / p.cs;
   if (threadIdx.x == 0) {
     mbar_init(&done, SMALL_ISSUERS);
+    gone = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 0) tmem_alloc_then_trigger(&tmem_slot, 512);
@@ -1314,8 +1335,8 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ns_small_kernel(const __grid
   const SmallWait wait = {&done, 0u, p.status, p.tag};
   if (e.n <= 16) tiny_steps<16>(p, e, mat, smem, blocks, cb0);
   else if (e.n <= TINY) tiny_steps<TINY>(p, e, mat, smem, blocks, cb0);
-  else if (e.n <= 64) small_steps<64>(p, e, mat, smem, tmem, wait, blocks, cb0, rank);
-  else small_steps<128>(p, e, mat, smem, tmem, wait, blocks, cb0, rank);
+  else if (e.n <= 64) small_steps<64>(p, e, mat, smem, tmem, wait, blocks, cb0, rank, &gone);
+  else small_steps<128>(p, e, mat, smem, tmem, wait, blocks, cb0, rank, &gone);
   tc_fence_before();
   __syncthreads();
   if (p.cs > 1) cluster_sync_relaxed();                      // (no CTA ends while the others read its sums)
