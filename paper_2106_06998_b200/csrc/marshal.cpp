@@ -370,6 +370,15 @@ xconv_norm_desc norm_desc(const at::Tensor& X, int64_t C, int code, float eps) {
   return d;
 }
 void* address(const at::Tensor* t) { return t ? t->data_ptr() : nullptr; }
+// A call into the library without the interpreter's lock.
+template <class Call>
+xconv_status unlocked(Call&& call) {
+  xconv_status s;
+  Py_BEGIN_ALLOW_THREADS
+  s = call();
+  Py_END_ALLOW_THREADS
+  return s;
+}
 
 // layernorm(X, weight, bias, eps) -> (Y, mean, rstd)
 PyObject* layernorm(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
@@ -385,7 +394,8 @@ PyObject* layernorm(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   const auto opt = X->options().dtype(at::kFloat).requires_grad(false);
   const at::Tensor Y = dense_like(*X), mean = at::empty(shape, opt), rstd = at::empty(shape, opt);
   const cudaStream_t stream = c10::cuda::getCurrentCUDAStream().stream();
-  const xconv_status s = lib.norm_forward(&d, X->data_ptr(), address(w), address(b), Y.data_ptr(), (float*)mean.data_ptr(), (float*)rstd.data_ptr(), stream);
+  const void *x = X->data_ptr(), *wp = address(w), *bp = address(b);
+  const xconv_status s = unlocked([&] { return lib.norm_forward(&d, x, wp, bp, Y.data_ptr(), (float*)mean.data_ptr(), (float*)rstd.data_ptr(), stream); });
   if (!raise(s, "xconv_layernorm_forward")) return nullptr;
   return Py_BuildValue("(NNN)", THPVariable_Wrap(Y), THPVariable_Wrap(mean), THPVariable_Wrap(rstd));
   XM_END
@@ -408,8 +418,10 @@ PyObject* layernorm_backward(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   const at::Tensor dX = dense_like(*X), dw = at::empty({C}, opt), db = at::empty({C}, opt);
   const cudaStream_t stream = c10::cuda::getCurrentCUDAStream().stream();
   const at::Tensor ws = scratch(lib.norm_workspace_bytes(&d), *X, stream);
-  const xconv_status s = lib.norm_backward(&d, dY->data_ptr(), X->data_ptr(), (const float*)mean->data_ptr(), (const float*)rstd->data_ptr(), address(w), dX.data_ptr(),
-                                           (float*)dw.data_ptr(), (float*)db.data_ptr(), ws.data_ptr(), (size_t)ws.numel(), stream);
+  const void *dy = dY->data_ptr(), *x = X->data_ptr(), *wp = address(w);
+  const float *m = (const float*)mean->data_ptr(), *r = (const float*)rstd->data_ptr();
+  const xconv_status s = unlocked([&] {
+    return lib.norm_backward(&d, dy, x, m, r, wp, dX.data_ptr(), (float*)dw.data_ptr(), (float*)db.data_ptr(), ws.data_ptr(), (size_t)ws.numel(), stream); });
   if (!raise(s, "xconv_layernorm_backward")) return nullptr;
   return Py_BuildValue("(NNN)", THPVariable_Wrap(dX), THPVariable_Wrap(dw), THPVariable_Wrap(db));
   XM_END
@@ -447,13 +459,7 @@ struct Several {
 xconv_status update(decltype(&xconv_orthogonalize) call, const xconv_update_desc& d, const std::vector<xconv_matrices>& items, const at::Tensor& like) {
   const cudaStream_t stream = c10::cuda::getCurrentCUDAStream().stream();
   const at::Tensor ws = scratch(lib.update_workspace_bytes(items.data(), (int)items.size()), like, stream);
-  void* p = ws.data_ptr();
-  const size_t bytes = (size_t)ws.numel();
-  xconv_status s;
-  Py_BEGIN_ALLOW_THREADS
-  s = call(&d, items.data(), (int)items.size(), p, bytes, stream);
-  Py_END_ALLOW_THREADS
-  return s;
+  return unlocked([&] { return call(&d, items.data(), (int)items.size(), ws.data_ptr(), (size_t)ws.numel(), stream); });
 }
 
 // orthogonalize(G or list, steps, coefficients, eps) -> O or list
