@@ -103,7 +103,7 @@ template <class F>
 xconv_status for_tables(const xconv_update_desc* d, const xconv_matrices* items, int count, bool muon, F&& f) {
   static thread_local NsTable t;
   t = NsTable{};
-  // The longest sums first: launches share those between their blocks of threads, and end with the short ones.
+  // The longest sides first: launches share the longest sums (those of X X^T, at least) between their blocks of threads, and end with the short ones.
   std::vector<int> order((size_t)count);
   for (int k = 0; k < count; ++k) order[k] = k;
   std::stable_sort(order.begin(), order.end(), [&](int x, int y) { return std::max(items[x].rows, items[x].cols) > std::max(items[y].rows, items[y].cols); });

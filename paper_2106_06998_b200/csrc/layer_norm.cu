@@ -688,7 +688,7 @@ constexpr int norm_stages(int V, int VEC, bool backward) { return VEC == 1 ? 1 :
 template <typename T, typename P, int VEC>
 cudaError_t forward_of(const NormPlan& p, const NormArgs& a, cudaStream_t st) {
   if constexpr (VEC == 1) {
-if constexpr (sizeof(T) == 2) {
+    if constexpr (sizeof(T) == 2) {
 #define XC_NORM(N) if (p.V == N && p.words) return norm_launch(norm_runs_kernel<T, P, 2, N, false>, p, a, st);
       XC_NORM(1) XC_NORM(2) XC_NORM(3) XC_NORM(4) XC_NORM(5) XC_NORM(6) XC_NORM(7) XC_NORM(8)
 #undef XC_NORM
@@ -707,7 +707,7 @@ if constexpr (sizeof(T) == 2) {
 template <typename T, typename P, int VEC>
 cudaError_t backward_of(const NormPlan& p, const NormArgs& a, cudaStream_t st) {
   if constexpr (VEC == 1) {
-if constexpr (sizeof(T) == 2) {
+    if constexpr (sizeof(T) == 2) {
 #define XC_NORM(N) if (p.V == N && p.words) return norm_launch(norm_runs_kernel<T, P, 2, N, true>, p, a, st);
       XC_NORM(1) XC_NORM(2) XC_NORM(3) XC_NORM(4) XC_NORM(5) XC_NORM(6) XC_NORM(7) XC_NORM(8)
 #undef XC_NORM

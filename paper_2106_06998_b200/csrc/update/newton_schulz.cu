@@ -10,9 +10,10 @@
 // by 1e-3 to 4e-2; with float arithmetic by 1e-7 to 5e-6.  So every operand is two float16 parts here, x 2^13 = h + l (11 + 11 bits and the sign between
 // them; |X| < 2, |A| < 4, |B| < 8: nothing overflows, and what is lost is below 2^-38), and a product is l h + h l + h h on the tensor cores, as exact as one of floats.
 // The tensor cores' accumulator is not rounded to nearest; a chain of MMAs is 32 terms long (four MMAs of the small products, then two of h h), and the chains are
-// added in float registers.  Error against 64 bits, times that of the same steps in float arithmetic, gradients of 16 x 75 to 1000 x 1000 values: 0.36 to 1.5; chains of 16
-// terms 0.31 to 2, of 64 terms 0.5 to 2.  Where every result is rounded to 16 bits anyway a chain is 128 terms, since the wait for a free set of sums
-// costs 150 clocks a chain (4096 x 4096 bfloat16: 3440 -> 3040 us; 64 terms 3150, 256 terms 2930, whose largest errors pass four times those of float arithmetic).
+// added in float registers.  Error against 64 bits, times that of the same steps in float arithmetic (root mean square over up to 2000 random matrices): smaller sides of 129 and
+// more 0.25 to 0.9, of 33 to 128 0.2 to 1.95 (33 x 161).  Where every result is rounded to 16 bits anyway a chain is 128 terms, since the wait for a free set of sums
+// costs 150 clocks a chain (4096 x 4096 bfloat16: 3440 -> 3040 us; 64 terms 3150, 256 terms 2930, whose largest errors pass four times those of float arithmetic).  That
+// error is 0.5 to 2.1 times that of float arithmetic (40 x 5000: 2.9), and the rounding of the result 11 (float16, 4096 x 4096, eight directions above noise) to 800 times it.
 //
 // Layout.  X, A and B lie in the scratch memory as blocks of 128 x 64 values, each part 16 KB in the order that the MMA wants in shared memory without a swizzle
 // (eight rows' 16-byte pieces side by side): whatever the matrices' sizes one tensor map describes them all, eight lanes with a row each write whole lines, and the
@@ -1056,9 +1057,9 @@ __device__ __forceinline__ void small_steps(const NsArgs& p, const NsEntry& e, i
 
 // ---- the same with a smaller side of at most 32, by FP32 multiply-adds in the same kernel
 //
-// Their sums are rounded to nearest, where the tensor cores cut them off; with few terms that shows: error against 64 bits, as a share of 1.5 times that of float
-// arithmetic by the library, at worst 1.18 on the tensor cores and 0.58 here (16 x 75; 20 x 60: 1.18 and 0.53; 32 x 64: 1.01 and 0.49; 64 x 64 there: 0.73).  Nothing waits
-// for MMAs either.  Bound by the loads from shared memory, of which a thread shares each among its products.  Measured, five steps, tensor cores and this: 6 x 75 30.7 and
+// Their sums are rounded to nearest, where the tensor cores cut them off; with few terms that shows: error against 64 bits, times that of float arithmetic by
+// the library, root mean square over 200 to 2000 normal matrices, 1.25 on the tensor cores and 0.68 here (16 x 75; 24 x 40: 1.67 and 0.67; 32 x 64: 1.89 and 0.66; 32 x 288: 1.61
+// and 0.47).  Nothing waits for MMAs either.  Bound by the loads from shared memory, of which a thread shares each among its products.  Measured, five steps, tensor cores and this: 6 x 75 30.7 and
 // 16.4 us, 16 x 384 47 and 31, 32 x 32 24.6 and 22.6, 32 x 192 36.9 and 43.0, 32 x 256 41.0 and 36.9; three layers of 16 x 75 to 32 x 800 (a cluster of eight) 45 and 45.
 
 constexpr int TINY = 32, TINY_X = SMALL_COLUMN_BLOCKS * 64 + 4, TINY_A = TINY + 4;      // rows; floats of a row of X, of A and B (16 bytes more: eight rows in different banks)
@@ -1374,8 +1375,13 @@ cudaError_t launch_small(NsArgs& p, int matrices, cudaStream_t st) {
   return cudaLaunchKernelEx(&cfg, ns_small_kernel, p);
 }
 
-// How the tiles of a launch go to the pairs of CTAs: by the times that a stage (1800 clocks), a tile's results (3000) and sums that pairs exchange (11000) take.  The
-// entries' tiles are in the order of the table, the longest sums first.
+// How the tiles of a launch go to the pairs of CTAs: by the times that a stage (1800 clocks), a tile's results (3000) and sums that pairs exchange (11000) take.  Those that
+// are shared are the first of the table, which is in the order of the matrices' larger sides: the longest sums first in X X^T, while in A A and B X, whose sums are as long
+// as the smaller sides, a long sum may stand behind short ones and is then shared with all of those or not at all.
+//
+// Measured, five steps of float matrices, in us: no tile shared, all by two pairs, all by four (where the GPU has so many clusters), and by this rule.  256 x 256 154 155 152 154;
+// 512 x 512 215 187 170 170; 512 x 4608 509 346 265 265; four of them 616 455 378 378; 200 x 8000 701 438 298 303; 1024 x 1024 326 252 270 270; two of them 329 263 329 264;
+// 1024 x 4096 572 409 330 329; 16 of 256 x 256 163 169 299 162; 2048 x 2048 605 (too many tiles) 603; 512 x 4608 beside 40 of 256 x 256 584 (too many) 346.
 struct NsSharing { int cs, heavy; };
 template <typename Stages, typename Units>
 NsSharing share(const NsTable& t, int units, Stages&& stages, Units&& units_of) {
