@@ -351,9 +351,9 @@ xconv_status xconv_layernorm_backward(const xconv_norm_desc* desc, const void* d
  *   orthogonalize(U) = X    (transposed back),
  * that is, the singular vectors of U with every singular value s / max(|U|, eps) mapped `steps` times by s -> a s + b s^3 + c s^5.
  * The products are about as exact as products of floats.  Error against 64 bits, times that of the same steps in float arithmetic, root mean square over many random
- * matrices: up to 0.9 where the smaller side is above 128, up to 2.0 from 33 to 128; up to 32, 0.3 to 1.2 by FP32 multiply-adds, which serve them where no matrix of the
- * part (below) has a smaller side above 128 or a larger one above 1536, and up to 1.9 beside such a one.  (A single matrix of a few values may be off by more: 3e-5 of the result for
- * one of 2000 of 2 x 2.)  Where every O of a part has 16 bits the tensor cores' sums are cut off more coarsely, up to 3 times the error of float arithmetic, 11 times and more below
+ * matrices: up to 0.9 where the smaller side is above 128, up to 2.0 from 33 to 128; up to 32, 0.2 to 1.2 by FP32 multiply-adds, which serve them where no matrix of the
+ * part (below) has a smaller side above 128 or a larger one above 1536, and 0.3 to 2.6 beside such a one or where they are one.  (1 x 1: 2.5e-7 of the value, and 4.5e-7.  A single
+ * matrix of a few values may be off by more: up to 2e-5 and 3e-5 of the result's norm, in millions of 2 x 2.)  Where every O of a part has 16 bits the tensor cores' sums are cut off more coarsely, up to 3 times the error of float arithmetic, 11 times and more below
  * the rounding to float16 and 86 times below that to bfloat16.  What is below 2^-38 in X is lost, which only matters to a matrix whose norm is far below eps.  A matrix with a
  * value that is not finite becomes NaN; the others keep their bits.  The same call gives the same bits every time; with other items beside it a matrix may get its
  * sums in another order, or by the other kind of arithmetic, as said.

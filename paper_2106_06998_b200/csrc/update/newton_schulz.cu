@@ -11,7 +11,7 @@
 // them; |X| < 2, |A| < 4, |B| < 8: nothing overflows, and what is lost is below 2^-38), and a product is l h + h l + h h on the tensor cores, as exact as one of floats.
 // The tensor cores' accumulator is not rounded to nearest; a chain of MMAs is 32 terms long (four MMAs of the small products, then two of h h), and the chains are
 // added in float registers.  Error against 64 bits, times that of the same steps in float arithmetic (root mean square over up to 2000 random matrices): smaller sides of 129 and
-// more 0.25 to 0.9, of 33 to 128 0.2 to 1.95 (33 x 161).  Where every result is rounded to 16 bits anyway a chain is 128 terms, since the wait for a free set of sums
+// more 0.1 to 0.9, of 33 to 128 0.1 to 1.95 (33 x 161), of up to 32 0.3 to 2.6 (4 x 4660).  Where every result is rounded to 16 bits anyway a chain is 128 terms, since the wait for a free set of sums
 // costs 150 clocks a chain (4096 x 4096 bfloat16: 3440 -> 3040 us; 64 terms 3150, 256 terms 2930, whose largest errors pass four times those of float arithmetic).  That
 // error is 0.5 to 2.1 times that of float arithmetic (40 x 5000: 2.9), and the rounding of the result 11 (float16, 4096 x 4096, eight directions above noise) to 800 times it.
 //
