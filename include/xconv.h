@@ -389,11 +389,65 @@ size_t xconv_update_workspace_bytes(const xconv_matrices* items, int count);
 xconv_status xconv_orthogonalize(const xconv_update_desc* desc, const xconv_matrices* items, int count, void* ws, size_t ws_bytes, void* cuda_stream);
 xconv_status xconv_muon_step(const xconv_update_desc* desc, const xconv_matrices* items, int count, void* ws, size_t ws_bytes, void* cuda_stream);
 
+/* The end of one block and the beginning of the next: dropout from a seed, the residual's addition, the root-mean-square norm, and its output in 8 bits.
+ *
+ * Rows as for the layer norm: row i (of `rows`; none is fine) has the values of a pixel's channels or of a token, element (i, c) of a tensor at i * stride + c.  X, residual, H, Y,
+ * dY, dH, dX and dresidual are stored in `dtype`, the weight in `param_dtype` (XCONV_F32, or `dtype`); rstd, scales and dweight are float, and so are all sums.  What is
+ * rounded is rounded once.  Pointers need the alignment of their elements only; where all rows lie on 16-byte boundaries they are read and written 16 bytes at
+ * a time.  Inputs may have a stride below C, outputs not.  Outputs overlap neither inputs nor each other.  Fields that a call does not mention are ignored.
+ *
+ * THE MASK.  drop(x) is 0 where a value is dropped, whatever it was, and x / (1 - p) elsewhere; drop'(g), its gradient, is the same of g.  The mask is drawn from `seed` wherever it
+ * is needed and never stored: a layer keeps the seed between its passes, as Algorithm 1 keeps that of the probes.  Row i has mask row m = i div rows_per_mask: 1 for a mask of single
+ * values, the pixels of a sample for one of whole channels.  Philox-4x32-10 (as above) with counter (b in words 0-1, w, 0), b = m * ceil(C / 8) + c div 8, and the seed as
+ * key makes eight halves of 16 bits, the low half of a word first.  The (c mod 8)-th half of the block of w = 3 is the upper half of a number u of 32 bits, that of w = 4 its lower
+ * half.  The value is dropped iff u < floor(p * 2^32).  seed_add, where it is not NULL, is a device pointer to a number that the kernels add to the seed (modulo 2^64) when they
+ * run: a captured graph draws another mask in every replay if the number is moved on between them.  p = 0: nothing is drawn, and the other fields are ignored.
+ *
+ * THE NORM.  h = drop(X) + residual,   rstd = 1 / sqrt(sum_c h^2 / C + eps),   Y = h * rstd * weight,  from the h that is not rounded.
+ * Gradients, with xh = H * rstd and g = dY * weight:
+ *   dresidual = dH + rstd * (g - xh * sum_c (g * xh) / C),   dX = drop'(dresidual, before its rounding),   dweight[c] = sum_i dY * xh.
+ *
+ * 8 BITS.  q_type other than XCONV_Q_NONE: Y is stored in one byte a value, for every `q_group` neighbouring values of a row (0, or C and more: the row; 32, 64, 128; a row's last group may
+ * be shorter) with a scale = max(their largest magnitude, 2^-100) / M, M = 448 (XCONV_Q_E4M3: four-bit exponent, three-bit mantissa) or 127 (XCONV_Q_INT8):
+ * Y = the nearest to y * (1 / scale), ties to even.  A group with a value that is not finite comes back as NaN.  scales [rows][ceil(C / q_group)], or [rows]. */
+typedef enum { XCONV_Q_NONE = 0, XCONV_Q_E4M3 = 1, XCONV_Q_INT8 = 2 } xconv_qtype;
+typedef struct {
+  int64_t rows;
+  int32_t C;
+  int32_t dtype, param_dtype;
+  float eps;                          /* not negative */
+  int32_t q_type, q_group;
+  int64_t x_stride, r_stride;         /* X and dX; residual and dresidual */
+  int64_t h_stride, dh_stride;        /* H; dH */
+  int64_t y_stride;                   /* Y (of 8 bits too) and dY */
+  double p;                           /* 0 to 1 */
+  unsigned long long seed;
+  const unsigned long long* seed_add;
+  int64_t rows_per_mask;              /* at least 1 */
+} xconv_rows_desc;
+
+/* residual, weight (1), H and rstd may be NULL; scales is NULL without 8 bits. */
+xconv_status xconv_rmsnorm_forward(const xconv_rows_desc* desc, const void* X, const void* residual, const void* weight, void* H, void* Y, float* scales, float* rstd,
+                                   void* cuda_stream);
+
+/* H and rstd as the forward call left them (H = X where nothing was added and nothing dropped).  weight (1), dH (0), dX, dresidual and dweight may be NULL: what is NULL is not computed; not
+ * all three of the last.  Without dropout dX and dresidual are the same values.  ws: xconv_rmsnorm_workspace_bytes(desc) bytes, 16-byte aligned (0 for an invalid descriptor), or NULL with
+ * dweight.  With no rows dweight becomes zeros. */
+size_t xconv_rmsnorm_workspace_bytes(const xconv_rows_desc* desc);
+xconv_status xconv_rmsnorm_backward(const xconv_rows_desc* desc, const void* dY, const void* H, const float* rstd, const void* weight, const void* dH, void* dX, void* dresidual,
+                                    float* dweight, void* ws, size_t ws_bytes, void* cuda_stream);
+
+/* Y = drop(X) + residual (NULL: 0).  Its gradient is the same call on dY, with the residual NULL. */
+xconv_status xconv_dropout(const xconv_rows_desc* desc, const void* X, const void* residual, void* Y, void* cuda_stream);
+
+/* X = Q * scales: what the 8-bit values stand for, in `dtype`.  Q at y_stride, X at x_stride. */
+xconv_status xconv_dequantize(const xconv_rows_desc* desc, const void* Q, const float* scales, void* X, void* cuda_stream);
+
 /* Reads the status the kernels of the last call left in the header of `ws` (synchronises
  * `cuda_stream`).  XCONV_OK, or XCONV_ERR_TIMEOUT if a bounded device-side wait ran out in that call.
  * The header never needs clearing: every call tags it afresh, so a later call on the same `ws`
  * reports its own outcome.  (Only the tensor-core kernels wait on anything; calls served by the
- * FP32-FMA kernels and the layer norm's gradients leave the header as it was.) */
+ * FP32-FMA kernels and the gradients of the norms leave the header as it was.) */
 xconv_status xconv_workspace_status(const void* ws, void* cuda_stream);
 
 /* Self-test of the failure path: one warp waits, with the same bounded wait the pipelined kernels use,

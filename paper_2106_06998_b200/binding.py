@@ -12,7 +12,7 @@ import ctypes
 import os
 import threading
 import warnings
-from ctypes import POINTER, Structure, c_char_p, c_float, c_int, c_int32, c_int64, c_size_t, c_void_p
+from ctypes import POINTER, Structure, c_char_p, c_double, c_float, c_int, c_int32, c_int64, c_size_t, c_void_p
 
 import torch
 
@@ -37,6 +37,7 @@ EXPORTS = ("xconv_workspace_bytes", "xconv_engine_for", "xconv_variants_for", "x
            "xconv_block_sparse_probes_from_seed",
            "xconv_layernorm_workspace_bytes", "xconv_layernorm_forward", "xconv_layernorm_backward",
            "xconv_update_workspace_bytes", "xconv_orthogonalize", "xconv_muon_step",
+           "xconv_rmsnorm_forward", "xconv_rmsnorm_workspace_bytes", "xconv_rmsnorm_backward", "xconv_dropout", "xconv_dequantize",
            "xconv_last_launch_count", "xconv_last_cuda_error", "xconv_status_string")
 
 
@@ -60,6 +61,12 @@ class UpdateDesc(Structure):
 class Matrices(Structure):
     _fields_ = [("G", c_void_p), ("M", c_void_p), ("O", c_void_p), ("rows", c_int32), ("cols", c_int32), ("batch", c_int32),
                 ("g_dtype", c_int32), ("o_dtype", c_int32)]
+
+
+class RowsDesc(Structure):
+    _fields_ = [("rows", c_int64), ("C", c_int32), ("dtype", c_int32), ("param_dtype", c_int32), ("eps", c_float), ("q_type", c_int32), ("q_group", c_int32),
+                ("x_stride", c_int64), ("r_stride", c_int64), ("h_stride", c_int64), ("dh_stride", c_int64), ("y_stride", c_int64),
+                ("p", c_double), ("seed", ctypes.c_ulonglong), ("seed_add", c_void_p), ("rows_per_mask", c_int64)]
 
 
 class XConvError(RuntimeError):
@@ -143,6 +150,12 @@ def lib() -> ctypes.CDLL:
     L.xconv_orthogonalize.restype = c_int
     L.xconv_muon_step.argtypes = L.xconv_orthogonalize.argtypes
     L.xconv_muon_step.restype = c_int
+    R = POINTER(RowsDesc)
+    L.xconv_rmsnorm_forward.argtypes = [R] + [c_void_p] * 8; L.xconv_rmsnorm_forward.restype = c_int
+    L.xconv_rmsnorm_workspace_bytes.argtypes = [R]; L.xconv_rmsnorm_workspace_bytes.restype = c_size_t
+    L.xconv_rmsnorm_backward.argtypes = [R] + [c_void_p] * 9 + [c_size_t, c_void_p]; L.xconv_rmsnorm_backward.restype = c_int
+    L.xconv_dropout.argtypes = [R] + [c_void_p] * 4; L.xconv_dropout.restype = c_int
+    L.xconv_dequantize.argtypes = [R] + [c_void_p] * 4; L.xconv_dequantize.restype = c_int
     L.xconv_workspace_status.argtypes = [c_void_p, c_void_p]; L.xconv_workspace_status.restype = c_int
     L.xconv_last_launch_count.argtypes = []; L.xconv_last_launch_count.restype = c_int
     L.xconv_last_cuda_error.argtypes = []; L.xconv_last_cuda_error.restype = c_int
@@ -157,6 +170,7 @@ _native = None
 _NATIVE_CALLS = ("xconv_workspace_bytes", "xconv_forward", "xconv_sketch", "xconv_wgrad", "xconv_dgrad", "xconv_sketch_seeded", "xconv_wgrad_seeded",
                  "xconv_backprobe", "xconv_contract", "xconv_layernorm_workspace_bytes", "xconv_layernorm_forward", "xconv_layernorm_backward",
                  "xconv_update_workspace_bytes", "xconv_orthogonalize", "xconv_muon_step")
+_NATIVE_ROWS = ("xconv_dropout", "xconv_rmsnorm_forward", "xconv_rmsnorm_workspace_bytes", "xconv_rmsnorm_backward", "xconv_dequantize")
 
 
 class _Declines:
@@ -178,6 +192,7 @@ def _load_native():
         _native = _Declines()
         return _native
     _marshal.use_library(*(ctypes.cast(getattr(L, name), c_void_p).value for name in _NATIVE_CALLS), _check, workspace)
+    _marshal.use_rows(*(ctypes.cast(getattr(L, name), c_void_p).value for name in _NATIVE_ROWS))
     _native = _marshal
     return _marshal
 
@@ -729,9 +744,13 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _dense_like(t: torch.Tensor) -> torch.Tensor:
+def _dense_like(t: torch.Tensor, dtype=None, C: int | None = None) -> torch.Tensor:
+    """An empty tensor of t's shape, or with C channels in the place of its own, in t's dtype or another."""
     fmt = {4: torch.channels_last, 5: torch.channels_last_3d}.get(t.dim(), torch.contiguous_format)
-    return torch.empty(t.shape, dtype=t.dtype, device=t.device, memory_format=fmt)
+    shape = list(t.shape)
+    if C is not None:
+        shape[1 if t.dim() >= 4 else -1] = C
+    return torch.empty(shape, dtype=dtype or t.dtype, device=t.device, memory_format=fmt)
 
 
 def xconv_layernorm_backward(dY: torch.Tensor, X: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor, weight: torch.Tensor | None = None):
@@ -855,6 +874,195 @@ def xconv_muon_step(W, dW, M, lr: float, momentum: float = 0.95, nesterov: bool 
     # As every in-place operation: a graph that kept one of them for its backward pass says so.
     torch.autograd.graph.increment_version([t for t in Ws + Ms if not t.is_inference()])
     return W
+
+
+# ------------------------------------------------------------------ between the blocks
+
+XCONV_Q_NONE, XCONV_Q_E4M3, XCONV_Q_INT8 = 0, 1, 2
+_Q_TYPES = {torch.float8_e4m3fn: XCONV_Q_E4M3, torch.int8: XCONV_Q_INT8}
+
+
+def _some_rows(t: torch.Tensor, name: str):
+    """_rows, of a tensor without rows too."""
+    if t.numel() or not t.is_cuda or not 1 <= t.dim() <= 5:
+        shape, C, row = _rows(t, name)
+    else:
+        shape = list(t.shape)
+        C = shape.pop(1 if t.dim() >= 4 else -1)
+        row = C
+    if C == 0:
+        raise ValueError(f"{name}: rows have no values")
+    return shape, C, row
+
+
+def _like_x(t: torch.Tensor | None, X: torch.Tensor, name: str) -> int:
+    """The row stride of a tensor of X's shape and type (0 where there is none)."""
+    if t is None:
+        return 0
+    if t.shape != X.shape or t.dtype != X.dtype or t.device != X.device:
+        raise ValueError(f"{name} must have the shape, dtype and device of the other tensors")
+    return _some_rows(t, name)[2]
+
+
+def _row_count(shape) -> int:
+    n = 1
+    for s in shape:
+        n *= s
+    return n
+
+
+def _rows_desc(X: torch.Tensor, shape, C: int, code: int = XCONV_F32, **fields) -> RowsDesc:
+    return RowsDesc(rows=_row_count(shape), C=C, dtype=_dtype_code(X.dtype), param_dtype=code, rows_per_mask=1, **fields)
+
+
+def _set_mask(desc: RowsDesc, X: torch.Tensor, shape, p: float, seed, channels: bool):
+    """The descriptor's mask.  Returns what has to live until the call is made."""
+    if not 0.0 <= p <= 1.0:
+        raise ValueError(f"p must be between 0 and 1, got {p}")
+    if p == 0.0:
+        return
+    if seed is None:
+        raise ValueError("dropout needs a seed")
+    desc.p = p
+    if isinstance(seed, torch.Tensor):
+        if not seed.is_cuda or seed.device != X.device or seed.dtype != torch.int64 or seed.numel() != 1:
+            raise ValueError("a seed in device memory must be one int64 on X's device")
+        desc.seed_add = seed.data_ptr()
+    else:
+        desc.seed = int(seed) % 2 ** 64
+    if channels:
+        desc.rows_per_mask = max(1, _row_count(shape[1:]))
+
+
+def xconv_dropout(X: torch.Tensor, p: float, seed, residual: torch.Tensor | None = None, channels: bool = False) -> torch.Tensor:
+    """Dropout whose mask is drawn from a seed and never stored: 0 with probability p, X / (1 - p) elsewhere, plus the residual (X's shape and dtype).  X as for
+    xconv_layernorm.  seed: 64 bits, or an int64 tensor of one value on X's device that is read when the kernel runs (a captured graph draws another mask where
+    that value has been moved on).  channels: whole channels of a sample -- (B, C, ...) images and volumes, (B, T, C) -- share their fate.  The same
+    seed, p, shape and `channels` give the same mask (include/xconv.h has its definition)."""
+    out = (_native or _load_native()).dropout(X, p, seed, residual, channels)
+    if out is not None:
+        return out
+    if _elsewhere(X):
+        with _on_device(X):
+            return xconv_dropout(X, p, seed, residual, channels)
+    shape, C, row = _some_rows(X, "X")
+    desc = _rows_desc(X, shape, C, x_stride=row, r_stride=_like_x(residual, X, "residual"), y_stride=C)
+    _set_mask(desc, X, shape, p, seed, channels)
+    Y = _dense_like(X)
+    if X.numel():
+        _check(lib().xconv_dropout(ctypes.byref(desc), X.data_ptr(), _ptr(residual), Y.data_ptr(), _stream()), "xconv_dropout")
+    return Y
+
+
+def xconv_dropout_backward(dY: torch.Tensor, p: float, seed, channels: bool = False) -> torch.Tensor:
+    """The gradient of xconv_dropout with respect to X: dY / (1 - p) where the value was kept.  (That of the residual is dY itself.)"""
+    return xconv_dropout(dY, p, seed, None, channels)
+
+
+def _rmsnorm(X, weight, residual, eps, p, seed, channels, q_type, qdtype, group):
+    shape, C, row = _some_rows(X, "X")
+    code = _norm_params(C, X, weight=weight)
+    desc = _rows_desc(X, shape, C, code, eps=eps, q_type=q_type, q_group=group, x_stride=row, r_stride=_like_x(residual, X, "residual"), h_stride=C, y_stride=C)
+    _set_mask(desc, X, shape, p, seed, channels)
+    H = _dense_like(X) if residual is not None or p > 0 else None
+    scales = None
+    if q_type:
+        groups = -(-C // group) if 0 < group < C else 1
+        Y, scales = _dense_like(X, qdtype), _dense_like(X, torch.float32, groups)
+    else:
+        Y = _dense_like(X)
+    rstd = torch.empty(shape, dtype=torch.float32, device=X.device)
+    if X.numel():
+        _check(lib().xconv_rmsnorm_forward(ctypes.byref(desc), X.data_ptr(), _ptr(residual), _ptr(weight), _ptr(H), Y.data_ptr(), _ptr(scales), rstd.data_ptr(), _stream()),
+               "xconv_rmsnorm_forward")
+    return Y, scales, X if H is None else H, rstd
+
+
+def xconv_rmsnorm(X: torch.Tensor, weight: torch.Tensor | None = None, residual: torch.Tensor | None = None, eps: float = 1e-6, p: float = 0.0, seed=None, channels: bool = False):
+    """Root-mean-square norm over the channels of H = dropout(X) + residual: (Y, H, rstd), Y = H * rstd * weight.  X as for xconv_layernorm; residual: X's shape and
+    dtype; weight: C values in X's dtype or float32 (1 where None); p, seed, channels as for xconv_dropout (p = 0: none).  Y and H are dense in X's dtype and
+    format, rstd is float32, (B, [D,] H, W) or (...).  H is X itself where nothing is added to it and nothing dropped."""
+    out = (_native or _load_native()).rmsnorm(X, weight, residual, eps, p, seed, channels)
+    if out is not None:
+        return out
+    if _elsewhere(X):
+        with _on_device(X):
+            return xconv_rmsnorm(X, weight, residual, eps, p, seed, channels)
+    Y, _, H, rstd = _rmsnorm(X, weight, residual, eps, p, seed, channels, XCONV_Q_NONE, None, 0)
+    return Y, H, rstd
+
+
+def xconv_rmsnorm_quantized(X: torch.Tensor, weight: torch.Tensor | None = None, residual: torch.Tensor | None = None, eps: float = 1e-6, qdtype=torch.float8_e4m3fn, group: int = 0,
+                            p: float = 0.0, seed=None, channels: bool = False):
+    """xconv_rmsnorm with Y in 8 bits (torch.float8_e4m3fn or torch.int8): (Q, scales, H, rstd), Y = Q * scales.  A scale for every row (group = 0), or for every 32, 64 or
+    128 neighbouring channels.  Q has X's shape and format, scales (float32) the same with a scale in the place of a group's channels."""
+    out = (_native or _load_native()).rmsnorm_quantized(X, weight, residual, eps, qdtype, group, p, seed, channels)
+    if out is not None:
+        return out
+    if _elsewhere(X):
+        with _on_device(X):
+            return xconv_rmsnorm_quantized(X, weight, residual, eps, qdtype, group, p, seed, channels)
+    if qdtype not in _Q_TYPES:
+        raise TypeError(f"8 bits are float8_e4m3fn or int8, got {qdtype}")
+    return _rmsnorm(X, weight, residual, eps, p, seed, channels, _Q_TYPES[qdtype], qdtype, _q_group(group))
+
+
+def _q_group(group: int) -> int:
+    if group < 0:
+        raise ValueError(f"group must not be negative, got {group}")
+    return _int32(group, "group")
+
+
+def xconv_dequantize(Q: torch.Tensor, scales: torch.Tensor, group: int = 0, dtype=torch.bfloat16) -> torch.Tensor:
+    """What 8-bit values stand for, Q * scales, in a dtype that the layers take; Q, scales and group as xconv_rmsnorm_quantized has them."""
+    out = (_native or _load_native()).dequantize(Q, scales, group, dtype)
+    if out is not None:
+        return out
+    if _elsewhere(Q):
+        with _on_device(Q):
+            return xconv_dequantize(Q, scales, group, dtype)
+    if Q.dtype not in _Q_TYPES:
+        raise TypeError(f"8 bits are float8_e4m3fn or int8, got {Q.dtype}")
+    shape, C, row = _some_rows(Q, "Q")
+    group = _q_group(group)
+    groups = -(-C // group) if 0 < group < C else 1
+    want = list(Q.shape)
+    want[1 if Q.dim() >= 4 else -1] = groups
+    if not scales.is_cuda or scales.device != Q.device or scales.dtype != torch.float32 or list(scales.shape) != want or _some_rows(scales, "scales")[2] != groups:
+        raise ValueError(f"scales must be a dense float32 tensor of shape {tuple(want)} in Q's format on Q's device")
+    X = _dense_like(Q, dtype)
+    desc = _rows_desc(X, shape, C, q_type=_Q_TYPES[Q.dtype], q_group=group, x_stride=C, y_stride=row)
+    if Q.numel():
+        _check(lib().xconv_dequantize(ctypes.byref(desc), Q.data_ptr(), scales.data_ptr(), X.data_ptr(), _stream()), "xconv_dequantize")
+    return X
+
+
+def xconv_rmsnorm_backward(dY: torch.Tensor, H: torch.Tensor, rstd: torch.Tensor, weight: torch.Tensor | None = None, dH: torch.Tensor | None = None, p: float = 0.0, seed=None,
+                           channels: bool = False):
+    """Gradients of xconv_rmsnorm: (dX, dresidual, dweight).  H and rstd are the forward call's, weight, p, seed and channels what it got; dH is the gradient that reaches H
+    past the norm (None: none).  dX and dresidual are dense in H's dtype and format -- one tensor, where nothing was dropped -- and dweight is float32 (the same bits every
+    time; what a weight would get where the layer has none)."""
+    out = (_native or _load_native()).rmsnorm_backward(dY, H, rstd, weight, dH, p, seed, channels)
+    if out is not None:
+        return out
+    if _elsewhere(H):
+        with _on_device(H):
+            return xconv_rmsnorm_backward(dY, H, rstd, weight, dH, p, seed, channels)
+    shape, C, row = _some_rows(H, "H")
+    if not rstd.is_cuda or rstd.device != H.device or rstd.dtype != torch.float32 or list(rstd.shape) != shape or not rstd.is_contiguous():
+        raise ValueError(f"rstd must be a contiguous float32 CUDA tensor of shape {tuple(shape)}: the forward call's")
+    code = _norm_params(C, H, weight=weight)
+    desc = _rows_desc(H, shape, C, code, x_stride=C, r_stride=C, h_stride=row, dh_stride=_like_x(dH, H, "dH"), y_stride=_like_x(dY, H, "dY"))
+    _set_mask(desc, H, shape, p, seed, channels)
+    dX = _dense_like(H)
+    dR = _dense_like(H) if p > 0 else None
+    dweight = torch.empty(C, dtype=torch.float32, device=H.device)
+    ws = workspace(lib().xconv_rmsnorm_workspace_bytes(ctypes.byref(desc)), H.device)
+    if not H.numel():
+        return dX, dX if dR is None else dR, dweight.zero_()
+    _check(lib().xconv_rmsnorm_backward(ctypes.byref(desc), dY.data_ptr(), H.data_ptr(), rstd.data_ptr(), _ptr(weight), _ptr(dH), dX.data_ptr(), _ptr(dR),
+                                        dweight.data_ptr(), ws.data_ptr(), ws.numel(), _stream()), "xconv_rmsnorm_backward")
+    return dX, dX if dR is None else dR, dweight
 
 
 def host_arena_bytes(desc: XConvDesc) -> int:

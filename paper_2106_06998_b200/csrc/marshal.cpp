@@ -5,6 +5,7 @@
 // A function returns None for whatever is not the ordinary case (tensors that are not dense CUDA tensors, subclasses, modes that want to see every call, a
 // layout or shape that does not fit, an option that is rarely given): binding.py then goes its own way, which is where every error is raised.
 #include <torch/csrc/Device.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/utils/object_ptr.h>
@@ -40,6 +41,14 @@ struct Library {
   decltype(&xconv_orthogonalize) orthogonalize;
   decltype(&xconv_muon_step) muon_step;
 } lib{};
+// ... and those between the blocks.
+struct RowsLibrary {
+  decltype(&xconv_dropout) dropout;
+  decltype(&xconv_rmsnorm_forward) rms_forward;
+  decltype(&xconv_rmsnorm_workspace_bytes) rms_workspace_bytes;
+  decltype(&xconv_rmsnorm_backward) rms_backward;
+  decltype(&xconv_dequantize) dequantize;
+} rows_lib{};
 PyObject *raise_for_status = nullptr, *workspace = nullptr;
 
 bool watched() {      // modes that are to see the tensor functions of the Python path
@@ -332,12 +341,17 @@ bool raise(xconv_status s, const char* name) {
 }
 bool on_current_device(const at::Tensor& t) { return t.device().index() == c10::cuda::current_device(); }
 
-// A dense tensor of the library's layout: matrices and tokens (1-d to 3-d) row-major, images and volumes channels-last.
-const at::Tensor* dense(PyObject* o) {
+// A dense tensor of the library's layout, of any type: matrices and tokens (1-d to 3-d) row-major, images and volumes channels-last.
+const at::Tensor* dense_of_any(PyObject* o) {
   const at::Tensor* t = plain(o);
-  if (!t || t->dim() < 1 || t->dim() > 5 || t->numel() == 0 || dtype_code(*t) < 0 || !on_current_device(*t)) return nullptr;
+  if (!t || t->dim() < 1 || t->dim() > 5 || t->numel() == 0 || !on_current_device(*t)) return nullptr;
   const auto fmt = t->dim() == 4 ? at::MemoryFormat::ChannelsLast : t->dim() == 5 ? at::MemoryFormat::ChannelsLast3d : at::MemoryFormat::Contiguous;
   return t->is_contiguous(fmt) ? t : nullptr;
+}
+// ... of a type that the layers take.
+const at::Tensor* dense(PyObject* o) {
+  const at::Tensor* t = dense_of_any(o);
+  return t && dtype_code(*t) >= 0 ? t : nullptr;
 }
 at::Tensor dense_like(const at::Tensor& t) {
   const auto fmt = t.dim() == 4 ? at::MemoryFormat::ChannelsLast : t.dim() == 5 ? at::MemoryFormat::ChannelsLast3d : at::MemoryFormat::Contiguous;
@@ -518,6 +532,194 @@ PyObject* muon_step(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   XM_END
 }
 
+// ---- between the blocks
+
+#define XM_BEGIN_ROWS(N) HANDLE_TH_ERRORS if (nargs != (N) || !rows_lib.dropout || watched()) Py_RETURN_NONE;
+
+// A tensor like X, or None.
+bool like_or_none(PyObject* o, const at::Tensor& X, const at::Tensor** t) {
+  *t = nullptr;
+  if (o == Py_None) return true;
+  *t = dense(o);
+  return *t && (*t)->sizes() == X.sizes() && (*t)->scalar_type() == X.scalar_type() && (*t)->device() == X.device();
+}
+xconv_rows_desc rows_desc(const at::Tensor& X, int64_t C, int dtype, int code) {
+  xconv_rows_desc d;
+  std::memset(&d, 0, sizeof d);
+  d.rows = X.numel() / C; d.C = (int32_t)C; d.dtype = dtype; d.param_dtype = code < 0 ? XCONV_F32 : code;
+  d.x_stride = d.r_stride = d.h_stride = d.dh_stride = d.y_stride = C;
+  d.rows_per_mask = 1;
+  return d;
+}
+// p (a float), seed (an integer, where p is not 0), channels
+bool mask_of(PyObject* p, PyObject* seed, PyObject* channels, const std::vector<int64_t>& shape, xconv_rows_desc* d) {
+  if (!PyFloat_CheckExact(p) || !PyBool_Check(channels)) return false;
+  d->p = PyFloat_AS_DOUBLE(p);
+  if (!(d->p >= 0.0 && d->p <= 1.0)) return false;
+  if (d->p == 0.0) return true;
+  if (!PyLong_CheckExact(seed)) return false;
+  d->seed = PyLong_AsUnsignedLongLongMask(seed);
+  if (channels == Py_True)
+    for (size_t i = 1; i < shape.size(); ++i) d->rows_per_mask *= shape[i];
+  return true;
+}
+bool group_of(PyObject* o, int32_t* group) {
+  if (!PyLong_CheckExact(o)) return false;
+  int over = 0;
+  const long v = PyLong_AsLongAndOverflow(o, &over);
+  if (over || v < 0 || v > INT32_MAX) return false;
+  *group = (int32_t)v;
+  return true;
+}
+int64_t groups_of(int64_t C, int32_t group) { return group > 0 && group < C ? (C + group - 1) / group : 1; }
+int q_code(at::ScalarType t) { return t == at::kFloat8_e4m3fn ? XCONV_Q_E4M3 : t == at::kChar ? XCONV_Q_INT8 : XCONV_Q_NONE; }
+at::Tensor dense_like(const at::Tensor& t, at::ScalarType type, int64_t C) {
+  const auto fmt = t.dim() == 4 ? at::MemoryFormat::ChannelsLast : t.dim() == 5 ? at::MemoryFormat::ChannelsLast3d : at::MemoryFormat::Contiguous;
+  std::vector<int64_t> sizes = t.sizes().vec();
+  sizes[t.dim() >= 4 ? 1 : t.dim() - 1] = C;
+  return at::empty(sizes, t.options().dtype(type).requires_grad(false), fmt);
+}
+
+// dropout(X, p, seed, residual, channels) -> Y
+PyObject* dropout(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  XM_BEGIN_ROWS(5)
+  const at::Tensor *X = dense(a[0]), *R;
+  if (!X || !like_or_none(a[3], *X, &R)) Py_RETURN_NONE;
+  std::vector<int64_t> shape;
+  const int64_t C = rows_of(*X, &shape);
+  if (C > INT32_MAX) Py_RETURN_NONE;
+  xconv_rows_desc d = rows_desc(*X, C, dtype_code(*X), -1);
+  if (!mask_of(a[1], a[2], a[4], shape, &d)) Py_RETURN_NONE;
+  const at::Tensor Y = dense_like(*X);
+  const cudaStream_t stream = c10::cuda::getCurrentCUDAStream().stream();
+  const void *x = X->data_ptr(), *r = address(R);
+  const xconv_status s = unlocked([&] { return rows_lib.dropout(&d, x, r, Y.data_ptr(), stream); });
+  if (!raise(s, "xconv_dropout")) return nullptr;
+  return THPVariable_Wrap(Y);
+  XM_END
+}
+
+// The norm of X (a[0]) with weight (a[1]) and residual (a[2]), eps (a[3]); Y of the type `y`, in 8 bits where `group` is not negative.
+struct Normed { at::Tensor Y, scales, H, rstd; xconv_status status = XCONV_OK; bool done = false; };
+Normed norm_rows(PyObject* const* a, PyObject* p, PyObject* seed, PyObject* channels, at::ScalarType y, int32_t group) {
+  Normed n;
+  const at::Tensor *X = dense(a[0]), *R, *w;
+  int code = -1;
+  if (!X || !like_or_none(a[2], *X, &R) || !PyFloat_CheckExact(a[3])) return n;
+  std::vector<int64_t> shape;
+  const int64_t C = rows_of(*X, &shape);
+  if (C > INT32_MAX || !param_of(a[1], *X, C, &w, &code)) return n;
+  xconv_rows_desc d = rows_desc(*X, C, dtype_code(*X), code);
+  d.eps = (float)PyFloat_AS_DOUBLE(a[3]);
+  if (!mask_of(p, seed, channels, shape, &d)) return n;
+  float* scales = nullptr;
+  if (group >= 0) {
+    d.q_type = q_code(y); d.q_group = group;
+    n.scales = dense_like(*X, at::kFloat, groups_of(C, group));
+    scales = (float*)n.scales.data_ptr();
+  }
+  n.Y = dense_like(*X, group >= 0 ? y : X->scalar_type(), C);
+  n.rstd = at::empty(shape, X->options().dtype(at::kFloat).requires_grad(false));
+  const bool sum = R || d.p > 0.0;
+  n.H = sum ? dense_like(*X) : *X;
+  const cudaStream_t stream = c10::cuda::getCurrentCUDAStream().stream();
+  const void *x = X->data_ptr(), *r = address(R), *wp = address(w);
+  void *h = sum ? n.H.data_ptr() : nullptr, *yp = n.Y.data_ptr();
+  float* rstd = (float*)n.rstd.data_ptr();
+  n.status = unlocked([&] { return rows_lib.rms_forward(&d, x, r, wp, h, yp, scales, rstd, stream); });
+  n.done = true;
+  return n;
+}
+
+// rmsnorm(X, weight, residual, eps, p, seed, channels) -> (Y, H, rstd)
+PyObject* rmsnorm(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  XM_BEGIN_ROWS(7)
+  const Normed n = norm_rows(a, a[4], a[5], a[6], at::kFloat, -1);
+  if (!n.done) Py_RETURN_NONE;
+  if (!raise(n.status, "xconv_rmsnorm_forward")) return nullptr;
+  return Py_BuildValue("(NNN)", THPVariable_Wrap(n.Y), THPVariable_Wrap(n.H), THPVariable_Wrap(n.rstd));
+  XM_END
+}
+
+// rmsnorm_quantized(X, weight, residual, eps, qdtype, group, p, seed, channels) -> (Q, scales, H, rstd)
+PyObject* rmsnorm_quantized(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  XM_BEGIN_ROWS(9)
+  int32_t group;
+  if (!THPDtype_Check(a[4]) || !group_of(a[5], &group)) Py_RETURN_NONE;
+  const at::ScalarType type = reinterpret_cast<THPDtype*>(a[4])->scalar_type;
+  if (q_code(type) == XCONV_Q_NONE) Py_RETURN_NONE;
+  const Normed n = norm_rows(a, a[6], a[7], a[8], type, group);
+  if (!n.done) Py_RETURN_NONE;
+  if (!raise(n.status, "xconv_rmsnorm_forward")) return nullptr;
+  return Py_BuildValue("(NNNN)", THPVariable_Wrap(n.Y), THPVariable_Wrap(n.scales), THPVariable_Wrap(n.H), THPVariable_Wrap(n.rstd));
+  XM_END
+}
+
+// rmsnorm_backward(dY, H, rstd, weight, dH, p, seed, channels) -> (dX, dresidual, dweight)
+PyObject* rmsnorm_backward(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  XM_BEGIN_ROWS(8)
+  const at::Tensor *H = dense(a[1]), *dY, *dH, *rstd = plain(a[2]), *w;
+  int code = -1;
+  if (!H || a[0] == Py_None || !like_or_none(a[0], *H, &dY) || !like_or_none(a[4], *H, &dH) || !rstd) Py_RETURN_NONE;
+  std::vector<int64_t> shape;
+  const int64_t C = rows_of(*H, &shape);
+  if (rstd->scalar_type() != at::kFloat || rstd->sizes() != at::IntArrayRef(shape) || !rstd->is_contiguous() || rstd->device() != H->device()) Py_RETURN_NONE;
+  if (C > INT32_MAX || !param_of(a[3], *H, C, &w, &code)) Py_RETURN_NONE;
+  xconv_rows_desc d = rows_desc(*H, C, dtype_code(*H), code);
+  if (!mask_of(a[5], a[6], a[7], shape, &d)) Py_RETURN_NONE;
+  const bool two = d.p > 0.0;
+  const at::Tensor dX = dense_like(*H), dR = two ? dense_like(*H) : dX, dw = at::empty({C}, H->options().dtype(at::kFloat).requires_grad(false));
+  const cudaStream_t stream = c10::cuda::getCurrentCUDAStream().stream();
+  const at::Tensor ws = scratch(rows_lib.rms_workspace_bytes(&d), *H, stream);
+  const void *dy = dY->data_ptr(), *h = H->data_ptr(), *wp = address(w), *dh = address(dH);
+  const float* r = (const float*)rstd->data_ptr();
+  void* dr = two ? dR.data_ptr() : nullptr;
+  const xconv_status s = unlocked([&] {
+    return rows_lib.rms_backward(&d, dy, h, r, wp, dh, dX.data_ptr(), dr, (float*)dw.data_ptr(), ws.data_ptr(), (size_t)ws.numel(), stream); });
+  if (!raise(s, "xconv_rmsnorm_backward")) return nullptr;
+  return Py_BuildValue("(NNN)", THPVariable_Wrap(dX), THPVariable_Wrap(dR), THPVariable_Wrap(dw));
+  XM_END
+}
+
+// dequantize(Q, scales, group, dtype) -> X
+PyObject* dequantize(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  XM_BEGIN_ROWS(4)
+  const at::Tensor *Q = dense_of_any(a[0]), *scales = dense(a[1]);
+  int32_t group;
+  if (!Q || !scales || q_code(Q->scalar_type()) == XCONV_Q_NONE || !group_of(a[2], &group) || !THPDtype_Check(a[3])) Py_RETURN_NONE;
+  const at::ScalarType type = reinterpret_cast<THPDtype*>(a[3])->scalar_type;
+  const int dtype = type == at::kFloat ? XCONV_F32 : type == at::kBFloat16 ? XCONV_BF16 : type == at::kHalf ? XCONV_F16 : -1;
+  std::vector<int64_t> shape;
+  const int64_t C = rows_of(*Q, &shape);
+  if (C > INT32_MAX || dtype < 0) Py_RETURN_NONE;
+  std::vector<int64_t> want = Q->sizes().vec();
+  want[Q->dim() >= 4 ? 1 : Q->dim() - 1] = groups_of(C, group);
+  if (scales->scalar_type() != at::kFloat || scales->sizes() != at::IntArrayRef(want) || scales->device() != Q->device()) Py_RETURN_NONE;
+  xconv_rows_desc d = rows_desc(*Q, C, dtype, -1);
+  d.q_type = q_code(Q->scalar_type()); d.q_group = group;
+  const at::Tensor X = dense_like(*Q, type, C);
+  const cudaStream_t stream = c10::cuda::getCurrentCUDAStream().stream();
+  const void* q = Q->data_ptr();
+  const float* f = (const float*)scales->data_ptr();
+  const xconv_status s = unlocked([&] { return rows_lib.dequantize(&d, q, f, X.data_ptr(), stream); });
+  if (!raise(s, "xconv_dequantize")) return nullptr;
+  return THPVariable_Wrap(X);
+  XM_END
+}
+
+// use_rows(address of each entry point in the order of RowsLibrary)
+PyObject* use_rows(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  constexpr Py_ssize_t N = sizeof(RowsLibrary) / sizeof(void*);
+  if (nargs != N) { PyErr_SetString(PyExc_TypeError, "use_rows takes the entry points"); return nullptr; }
+  void* at[N];
+  for (Py_ssize_t i = 0; i < N; ++i) {
+    at[i] = PyLong_AsVoidPtr(a[i]);
+    if (PyErr_Occurred()) return nullptr;
+  }
+  std::memcpy(&rows_lib, at, sizeof rows_lib);
+  Py_RETURN_NONE;
+}
+
 // use_library(address of each entry point in the order of Library, raise(status, name), workspace(bytes, device))
 PyObject* use_library(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   constexpr Py_ssize_t N = sizeof(Library) / sizeof(void*);
@@ -539,6 +741,7 @@ PyMethodDef methods[] = {
 #define XM_FAST(F) {#F, (PyCFunction)(void (*)(void))F, METH_FASTCALL, nullptr}
     XM_FAST(forward), XM_FAST(sketch), XM_FAST(sketch_seeded), XM_FAST(wgrad), XM_FAST(wgrad_seeded), XM_FAST(dgrad), XM_FAST(backprobe), XM_FAST(contract),
     XM_FAST(layernorm), XM_FAST(layernorm_backward), XM_FAST(orthogonalize), XM_FAST(muon_step),
+    XM_FAST(dropout), XM_FAST(rmsnorm), XM_FAST(rmsnorm_quantized), XM_FAST(rmsnorm_backward), XM_FAST(dequantize), XM_FAST(use_rows),
     XM_FAST(use_library), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
