@@ -6,130 +6,173 @@
 // leave a partial sum a column each, which a second kernel adds in fixed order (no atomics: the same bits every time).
 #include "rows.cuh"
 
-#include <algorithm>
-
 namespace xconv {
 
 namespace {
 
 struct RmsBackArgs {
-  const void *dY, *H, *dH;
+  Rows dY, H, dH, dX, dR;
   const float* rstd;
   Weight w;
-  void *dX, *dR;
   float* part;
-  long rows, sy, sh, sdh, sx, sr;
+  long rows;
   int C, octets, group;
   float inv_c;
   Drop drop;
 };
 
-// V octets a thread; V = 0: rows of any length, read again for the second step; dw is then another kernel's.
-template <typename T, int V, bool VEC>
-__global__ void __launch_bounds__(1024) rms_backward_kernel(const RmsBackArgs a) {
-  extern __shared__ float cols[];                            // C floats a warp, or a block of several
+// xh and g of an octet from what was fetched of h and dy, and its part of dw.
+template <typename T, bool VEC>
+__device__ __forceinline__ void weigh(const RmsBackArgs& a, const T* h, const T* dy, const Fetched<T, VEC>& fh, const Fetched<T, VEC>& fy, int k, bool in, float rstd,
+                                      const float (&w)[8], float (&xh)[8], float (&g)[8], float (&dw)[8]) {
+  values_of<T, VEC>(fh, h, 8 * k, a.C, in, xh);
+  values_of<T, VEC>(fy, dy, 8 * k, a.C, in, g);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    xh[e] *= rstd;
+    dw[e] = fmaf(g[e], xh[e], dw[e]);
+    g[e] *= w[e];
+  }
+}
+// dr, and dx, of an octet.
+template <typename T, bool VEC, int DROP>
+__device__ __forceinline__ void write_out(const RmsBackArgs& a, uint2 key, unsigned long long block, long row, const Fetched<T, VEC>& fd, int k, bool in, float rstd, float mean,
+                                          const float (&xh)[8], const float (&g)[8]) {
+  float d[8];
+  if (a.dH.p) {
+    values_of<T, VEC>(fd, row_of<T>(a.dH, row), 8 * k, a.C, in, d);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) d[e] = fmaf(rstd, fmaf(-xh[e], mean, g[e]), d[e]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) d[e] = rstd * fmaf(-xh[e], mean, g[e]);
+  }
+  if (a.dR.p) store8<T, VEC>(const_cast<T*>(row_of<T>(a.dR, row)), 8 * k, a.C, in, d);
+  if (a.dX.p) {
+    if (DROP) {
+      bool gone[8];
+      mask8(a.drop, key, block + k, gone);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) d[e] = gone[e] ? 0.f : d[e] * a.drop.scale;
+    }
+    store8<T, VEC>(const_cast<T*>(row_of<T>(a.dX, row)), 8 * k, a.C, in, d);
+  }
+}
+
+// ---- rows in registers, V octets a thread; the next row is fetched while this one is worked on
+
+template <typename T, int V, bool VEC, int DROP>
+__global__ void __launch_bounds__(512) rms_backward_kernel(const RmsBackArgs a) {
+  extern __shared__ float cols[];                            // C floats a warp, in a block of several groups
   __shared__ float sums[2][32];
   const int group = a.group, lane = group <= 32 ? threadIdx.x & (group - 1) : threadIdx.x;
   const int groups = group <= 32 ? blockDim.x / group : 1, own = group <= 32 ? threadIdx.x / group : 0;
-  const uint2 key = a.drop.on ? a.drop.key() : make_uint2(0u, 0u);
-  const int steps = V ? V : (a.octets + group - 1) / group;
-  constexpr int HELD = V ? V : 1;
-  float dw[HELD][8];
+  const uint2 key = a.drop.key<DROP>();
+  const long step = (long)gridDim.x * groups;
+  long row = (long)blockIdx.x * groups + own;
+  Fetched<T, VEC> fh[V], fy[V], fd[V];
+  float next_rstd = 0.f;
+  const auto fetch = [&](long next) {
+    const bool in = next < a.rows;
+    next_rstd = in ? __ldg(a.rstd + next) : 0.f;
 #pragma unroll
-  for (int v = 0; v < HELD; ++v)
+    for (int v = 0; v < V; ++v) {
+      const int k = lane + v * group;
+      fetch8<T, VEC>(a.H, row_of<T>(a.H, next), next, 8 * k, a.C, in && k < a.octets, fh[v]);
+      fetch8<T, VEC>(a.dY, row_of<T>(a.dY, next), next, 8 * k, a.C, in && k < a.octets, fy[v]);
+      if (a.dH.p) fetch8<T, VEC>(a.dH, row_of<T>(a.dH, next), next, 8 * k, a.C, in && k < a.octets, fd[v]);
+    }
+  };
+  fetch(row);
+  float dw[V][8], w[V][8];
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) dw[v][e] = 0.f;
+    a.w.load<T, VEC>(8 * min(lane + v * group, a.octets - 1), a.C, w[v]);
+  }
   int turn = 0;
-  for (long row0 = (long)blockIdx.x * groups; row0 < a.rows; row0 += (long)gridDim.x * groups, turn ^= 1) {
-    const long row = row0 + own;
+  for (long row0 = (long)blockIdx.x * groups; row0 < a.rows; row0 += step, row += step, turn ^= 1) {
     const bool in = row < a.rows;
-    const float rstd = in ? __ldg(a.rstd + row) : 0.f;
-    float xh[HELD][8], g[HELD][8], s = 0.f;
-    const auto read = [&](int k, float (&x)[8], float (&y)[8]) {
+    const float rstd = next_rstd;
+    float xh[V][8], g[V][8], s = 0.f;
+    Fetched<T, VEC> d[V];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = y[e] = 0.f;
-      if (!in || k >= a.octets) return;
-      load8<T, VEC>(static_cast<const T*>(a.H) + row * a.sh, 8 * k, a.C, x);
-      load8<T, VEC>(static_cast<const T*>(a.dY) + row * a.sy, 8 * k, a.C, y);
-    };
-    const auto weigh = [&](int k, float (&x)[8], float (&y)[8], float (&d)[8]) {
-      float w[8];
+    for (int v = 0; v < V; ++v) {
+      const int k = lane + v * group;
+      weigh<T, VEC>(a, row_of<T>(a.H, row), row_of<T>(a.dY, row), fh[v], fy[v], k, in && k < a.octets, rstd, w[v], xh[v], g[v], dw[v]);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) w[e] = 0.f;
-      if (k < a.octets) a.w.load<T, VEC>(8 * k, a.C, w);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        x[e] *= rstd;
-        d[e] = fmaf(y[e], x[e], d[e]);
-        y[e] *= w[e];
-      }
-    };
-#pragma unroll
-    for (int v = 0; v < steps; ++v) {
-      const int i = V ? v : 0, k = lane + v * group;
-      read(k, xh[i], g[i]);
-      weigh(k, xh[i], g[i], dw[i]);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) s = fmaf(g[i][e], xh[i][e], s);
+      for (int e = 0; e < 8; ++e) s = fmaf(g[v][e], xh[v][e], s);
+      d[v] = fd[v];
     }
+    fetch(row + step);
     const float mean = row_sum(s, group, sums[turn]) * a.inv_c;
-    const unsigned long long block = (unsigned long long)a.drop.mask_row(row) * a.octets;
+    const unsigned long long block = DROP ? a.drop.first_block(row, a.octets) : 0;
 #pragma unroll
-    for (int v = 0; v < steps; ++v) {
-      const int i = V ? v : 0, k = lane + v * group;
-      if (!in || k >= a.octets) continue;
-      if (!V) {
-        read(k, xh[0], g[0]);
-        weigh(k, xh[0], g[0], dw[0]);
-      }
-      float d[8];
-      if (a.dH) {
-        load8<T, VEC>(static_cast<const T*>(a.dH) + row * a.sdh, 8 * k, a.C, d);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) d[e] = fmaf(rstd, fmaf(-xh[i][e], mean, g[i][e]), d[e]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) d[e] = rstd * fmaf(-xh[i][e], mean, g[i][e]);
-      }
-      if (a.dR) store8<T, VEC>(static_cast<T*>(a.dR) + row * a.sr, 8 * k, a.C, d);
-      if (a.dX) {
-        if (a.drop.on) drop8(a.drop, key, block + k, d);
-        store8<T, VEC>(static_cast<T*>(a.dX) + row * a.sx, 8 * k, a.C, d);
-      }
+    for (int v = 0; v < V; ++v) {
+      const int k = lane + v * group;
+      write_out<T, VEC, DROP>(a, key, block, row, d[v], k, in && k < a.octets, rstd, mean, xh[v], g[v]);
     }
   }
-  if constexpr (V > 0) {
-    if (!a.part) return;
-    // The groups of a warp by shuffles, the warps side by side in shared memory, then column by column in order.
-    for (int o = group; o < 32; o <<= 1)
+  if (!a.part) return;
+  // The groups of a warp by shuffles, the warps side by side in shared memory, then column by column in order.
+  for (int o = group; o < 32; o <<= 1)
 #pragma unroll
-      for (int v = 0; v < HELD; ++v)
+    for (int v = 0; v < V; ++v)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) dw[v][e] += __shfl_xor_sync(0xffffffffu, dw[v][e], o);
-    if (group > 32) {
+      for (int e = 0; e < 8; ++e) dw[v][e] += __shfl_xor_sync(0xffffffffu, dw[v][e], o);
+  const bool several = group <= 32;
+  const int warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  float* to = several ? cols + warp * a.C : a.part + (size_t)blockIdx.x * a.C;
+  if ((threadIdx.x & 31) < group)
 #pragma unroll
-      for (int v = 0; v < HELD; ++v)
+    for (int v = 0; v < V; ++v)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int c = 8 * (lane + v * group) + e;
-          if (c < a.C) a.part[(size_t)blockIdx.x * a.C + c] = dw[v][e];
-        }
-      return;
+      for (int e = 0; e < 8; ++e) {
+        const int c = 8 * (lane + v * group) + e;
+        if (c < a.C) to[c] = dw[v][e];
+      }
+  if (!several) return;
+  __syncthreads();
+  for (int c = threadIdx.x; c < a.C; c += blockDim.x) {
+    float t = cols[c];
+    for (int i = 1; i < warps; ++i) t += cols[i * a.C + c];
+    a.part[(size_t)blockIdx.x * a.C + c] = t;
+  }
+}
+
+// ---- rows of any length, a block each, read again for the second step; dw is another kernel's
+
+template <typename T, bool VEC, int DROP>
+__global__ void __launch_bounds__(1024) rms_backward_wide_kernel(const RmsBackArgs a) {
+  __shared__ float sums[2][32];
+  const uint2 key = a.drop.key<DROP>();
+  const int steps = (a.octets + 1023) / 1024;
+  int turn = 0;
+  for (long row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
+    const float rstd = __ldg(a.rstd + row);
+    float xh[8], g[8], unused[8], s = 0.f;
+    const auto read = [&](int k) {
+      Fetched<T, VEC> fh, fy;
+      fetch8<T, VEC>(a.H, row_of<T>(a.H, row), row, 8 * k, a.C, k < a.octets, fh);
+      fetch8<T, VEC>(a.dY, row_of<T>(a.dY, row), row, 8 * k, a.C, k < a.octets, fy);
+      float w[8];
+      a.w.load<T, VEC>(8 * min(k, a.octets - 1), a.C, w);
+      weigh<T, VEC>(a, row_of<T>(a.H, row), row_of<T>(a.dY, row), fh, fy, k, k < a.octets, rstd, w, xh, g, unused);
+    };
+    for (int v = 0; v < steps; ++v) {
+      read(threadIdx.x + v * 1024);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s = fmaf(g[e], xh[e], s);
     }
-    const int warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-    if ((threadIdx.x & 31) < group)
-#pragma unroll
-      for (int v = 0; v < HELD; ++v)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int c = 8 * (lane + v * group) + e;
-          if (c < a.C) cols[warp * a.C + c] = dw[v][e];
-        }
-    __syncthreads();
-    for (int c = threadIdx.x; c < a.C; c += blockDim.x) {
-      float t = cols[c];
-      for (int i = 1; i < warps; ++i) t += cols[i * a.C + c];
-      a.part[(size_t)blockIdx.x * a.C + c] = t;
+    const float mean = row_sum(s, 1024, sums[turn]) * a.inv_c;
+    const unsigned long long block = DROP ? a.drop.first_block(row, a.octets) : 0;
+    for (int v = 0; v < steps; ++v) {
+      const int k = threadIdx.x + v * 1024;
+      read(k);
+      Fetched<T, VEC> fd;
+      if (a.dH.p) fetch8<T, VEC>(a.dH, row_of<T>(a.dH, row), row, 8 * k, a.C, k < a.octets, fd);
+      write_out<T, VEC, DROP>(a, key, block, row, fd, k, k < a.octets, rstd, mean, xh, g);
     }
   }
 }
@@ -143,7 +186,7 @@ __global__ void __launch_bounds__(256) rms_columns_kernel(const RmsBackArgs a, l
   float dw = 0.f;
 #pragma unroll 4
   for (long row = r0; row < r1; ++row)
-    dw = fmaf(to_f(static_cast<const T*>(a.dY)[row * a.sy + c]), to_f(static_cast<const T*>(a.H)[row * a.sh + c]) * __ldg(a.rstd + row), dw);
+    dw = fmaf(to_f(row_of<T>(a.dY, row)[c]), to_f(row_of<T>(a.H, row)[c]) * __ldg(a.rstd + row), dw);
   a.part[(size_t)blockIdx.y * a.C + c] = dw;
 }
 
@@ -166,18 +209,12 @@ __global__ void __launch_bounds__(1024) rms_sums_kernel(const float* part, int p
 // Rows that a block of rms_columns_kernel adds, at least, and partial sums at most.
 constexpr long WIDE_ROWS = 64, WIDE_PARTS = 512;
 
-struct Plan { int V, group, threads; long blocks, parts; };
+struct Plan { Team team; long blocks, parts; };
 Plan plan_of(const xconv_rows_desc* d) {
   Plan p = {};
-  const long octets = (d->C + 7) / 8;
-  p.V = 1;
-  if (octets <= 32) p.group = pow2_from(octets);
-  else if (octets <= 1024) p.group = (int)((octets + 31) / 32 * 32);
-  else { p.group = 1024; p.V = 0; }
-  p.threads = p.group <= 32 ? 128 : p.group;
-  const long groups = p.group <= 32 ? p.threads / p.group : 1;
-  p.blocks = std::min((d->rows + groups - 1) / groups, (long)ROWS_SMS * std::max(1, 1024 / p.threads));
-  p.parts = p.V ? p.blocks : std::min((d->rows + WIDE_ROWS - 1) / WIDE_ROWS, WIDE_PARTS);
+  p.team = team_of((d->C + 7) / 8);
+  p.blocks = std::min((d->rows + p.team.groups - 1) / p.team.groups, (long)ROWS_SMS * std::max(1, 512 / p.team.threads));
+  p.parts = p.team.V ? p.blocks : std::min((d->rows + WIDE_ROWS - 1) / WIDE_ROWS, WIDE_PARTS);
   return p;
 }
 
@@ -189,23 +226,29 @@ cudaError_t launch_rms_backward(const xconv_rows_desc* d, const void* dY, const 
                                 float* dweight, float* part, cudaStream_t st, int* launches) {
   const Plan p = plan_of(d);
   RmsBackArgs a = {};
-  a.dY = dY; a.H = H; a.dH = dH; a.rstd = rstd; a.w = {weight, d->param_dtype == XCONV_F32}; a.dX = dX; a.dR = dR; a.part = part;
-  a.rows = d->rows; a.sy = d->y_stride; a.sh = d->h_stride; a.sdh = d->dh_stride; a.sx = d->x_stride; a.sr = d->r_stride;
-  a.C = d->C; a.octets = (d->C + 7) / 8; a.group = p.group; a.inv_c = 1.f / (float)d->C;
+  const size_t es = d->dtype == XCONV_F32 ? 4 : 2;
+  a.dY = rows_of(dY, d->rows, d->C, d->y_stride, es); a.H = rows_of(H, d->rows, d->C, d->h_stride, es); a.dH = rows_of(dH, d->rows, d->C, d->dh_stride, es);
+  a.dX = rows_of(dX, d->rows, d->C, d->x_stride, es); a.dR = rows_of(dR, d->rows, d->C, d->r_stride, es);
+  a.rstd = rstd; a.w = {weight, d->param_dtype == XCONV_F32}; a.part = part;
+  a.rows = d->rows; a.C = d->C; a.octets = (d->C + 7) / 8; a.group = p.team.group; a.inv_c = 1.f / (float)d->C;
   a.drop = drop_of(d);
-  const int n = d->dtype == XCONV_F32 ? 4 : 8;
-  const bool vec = d->C % n == 0 && at(dY, 16) && at(H, 16) && at(dH, 16) && at(weight, 16) && at(dX, 16) && at(dR, 16) && d->y_stride % n == 0 && d->h_stride % n == 0 &&
-                   (!dH || d->dh_stride % n == 0) && (!dX || d->x_stride % n == 0) && (!dR || d->r_stride % n == 0);
+  const bool vec = d->C % (16 / es) == 0 && whole(a.dY, 16) && whole(a.H, 16) && whole(a.dH, 16) && whole(a.dX, 16) && whole(a.dR, 16) && at(weight, 16);
   if (d->rows > 0) {
     const cudaError_t e = with_type(d->dtype, [&](auto t) {
       using T = decltype(t);
-      if (p.V || dX || dR) {
-        const auto kernel = vec ? (p.V ? rms_backward_kernel<T, 1, true> : rms_backward_kernel<T, 0, true>) : (p.V ? rms_backward_kernel<T, 1, false> : rms_backward_kernel<T, 0, false>);
-        const size_t smem = p.V && part && p.group <= 32 ? (size_t)(p.threads / 32) * d->C * sizeof(float) : 0;
-        kernel<<<(unsigned)p.blocks, p.threads, smem, st>>>(a);
+      const int V = p.team.V;
+      if (V || dX || dR) {
+        const auto pick = [&](auto v, auto dropped) -> void (*)(const RmsBackArgs) {
+          constexpr bool VEC = decltype(v)::value;
+          constexpr int DROP = decltype(dropped)::value;
+          return V == 0 ? rms_backward_wide_kernel<T, VEC, DROP> : V == 1 ? rms_backward_kernel<T, 1, VEC, DROP> : rms_backward_kernel<T, 2, VEC, DROP>;
+        };
+        const auto kernel = with_kinds(vec, a.dX.p ? a.drop.how : DROP_NONE, pick);
+        const size_t smem = V && part && p.team.group <= 32 ? (size_t)(p.team.threads / 32) * d->C * sizeof(float) : 0;
+        kernel<<<(unsigned)p.blocks, p.team.threads, smem, st>>>(a);
         ++*launches;
       }
-      if (!p.V && part) {
+      if (!V && part) {
         rms_columns_kernel<T><<<dim3((unsigned)((d->C + 255) / 256), (unsigned)p.parts), 256, 0, st>>>(a, (d->rows + p.parts - 1) / p.parts);
         ++*launches;
       }

@@ -6,18 +6,15 @@
 // is rounded once, where it is written).
 #include "rows.cuh"
 
-#include <algorithm>
-
 namespace xconv {
 
 namespace {
 
 struct RmsArgs {
-  const void *X, *R;
+  Rows X, R, H, Y;
   Weight w;
-  void *H, *Y;
   float *scales, *rstd;
-  long rows, sx, sr, sh, sy;
+  long rows;
   int C, octets, group;
   int q, q_group, q_groups;        // 8 bits: the type, values of a scale (0: the row), scales of a row
   float eps, inv_c;
@@ -47,116 +44,177 @@ __device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
 }
 __device__ __forceinline__ uint32_t int8(float v) { return (uint32_t)max(-127, min(127, __float2int_rn(v))) & 0xffu; }
 template <bool VEC>
-__device__ __forceinline__ void store8q(unsigned char* row, int c, int C, const float (&y)[8], float inv, int q) {
+__device__ __forceinline__ void store8q(unsigned char* row, int c, int C, bool in, const float (&y)[8], float inv, int q) {
   uint32_t b[2];
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    const float *v = y + 4 * i;
+    const float* v = y + 4 * i;
     b[i] = q == XCONV_Q_E4M3 ? e4m3x2(v[0] * inv, v[1] * inv) | e4m3x2(v[2] * inv, v[3] * inv) << 16
                              : int8(v[0] * inv) | int8(v[1] * inv) << 8 | int8(v[2] * inv) << 16 | int8(v[3] * inv) << 24;
   }
-  if (VEC) {
-    *reinterpret_cast<uint2*>(row + c) = make_uint2(b[0], b[1]);
+  store8<unsigned char, VEC>(row, c, C, in, b);
+}
+// The scale of this lane's octet, whose largest magnitude is m (of its group of `width` values, which neighbouring lanes hold).
+__device__ __forceinline__ uint32_t group_most(uint32_t m, int width) {
+  for (int o = width >> 4; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+  return m;
+}
+
+// The octet of h from what was fetched of x and r.
+template <typename T, bool VEC, int DROP>
+__device__ __forceinline__ void sum_of(const RmsArgs& a, uint2 key, unsigned long long block, const T* x, const T* r, const Fetched<T, VEC>& fx, const Fetched<T, VEC>& fr, int k, bool in,
+                                       float (&h)[8]) {
+  values_of<T, VEC>(fx, x, 8 * k, a.C, in, h);
+  float f[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) f[e] = 0.f;
+  if (a.R.p) values_of<T, VEC>(fr, r, 8 * k, a.C, in, f);
+  if (DROP) {
+    bool gone[8];
+    mask8(a.drop, key, block + k, gone);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) h[e] = gone[e] ? f[e] : fmaf(h[e], a.drop.scale, f[e]);
   } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (c + e < C) row[c + e] = (unsigned char)(b[e / 4] >> (8 * (e % 4)));
+    for (int e = 0; e < 8; ++e) h[e] += f[e];
   }
 }
 
-// ---- the kernel.  V octets a thread; V = 0: rows of any length, read again for every step.
+// ---- rows in registers, V octets a thread; the next row is fetched while this one is worked on
 
-template <typename T, int V, bool VEC>
-__global__ void __launch_bounds__(1024) rms_forward_kernel(const RmsArgs a) {
+template <typename T, int V, bool VEC, bool Q, int DROP>
+__global__ void __launch_bounds__(512) rms_forward_kernel(const RmsArgs a) {
   __shared__ float sums[2][32];
   __shared__ uint32_t most[2][32];
   const int group = a.group, lane = group <= 32 ? threadIdx.x & (group - 1) : threadIdx.x;
   const int groups = group <= 32 ? blockDim.x / group : 1, own = group <= 32 ? threadIdx.x / group : 0;
-  const uint2 key = a.drop.on ? a.drop.key() : make_uint2(0u, 0u);
-  const int steps = V ? V : (a.octets + group - 1) / group;
-  int turn = 0;
-  for (long row0 = (long)blockIdx.x * groups; row0 < a.rows; row0 += (long)gridDim.x * groups, turn ^= 1) {
-    const long row = row0 + own;
-    const bool in = row < a.rows;
-    const T *x = static_cast<const T*>(a.X) + row * a.sx, *r = static_cast<const T*>(a.R) + row * a.sr;
-    const unsigned long long block = (unsigned long long)a.drop.mask_row(row) * a.octets;
-    const auto sum_of = [&](int k, float (&h)[8]) {
-      if (!in || k >= a.octets) {
+  const uint2 key = a.drop.key<DROP>();
+  const long step = (long)gridDim.x * groups;
+  long row = (long)blockIdx.x * groups + own;
+  Fetched<T, VEC> fx[V], fr[V];
+  const auto fetch = [&](long next) {
+    const bool in = next < a.rows;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) h[e] = 0.f;
-        return;
-      }
-      load8<T, VEC>(x, 8 * k, a.C, h);
-      float f[8];
-      if (a.R) load8<T, VEC>(r, 8 * k, a.C, f);
-      if (a.drop.on) drop8(a.drop, key, block + k, h);
-      if (a.R)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) h[e] += f[e];
-    };
-    float held[V ? V : 1][8], ss = 0.f;
-#pragma unroll
-    for (int v = 0; v < steps; ++v) {
+    for (int v = 0; v < V; ++v) {
       const int k = lane + v * group;
-      float (&h)[8] = held[V ? v : 0];
-      sum_of(k, h);
-      if (a.H && in && k < a.octets) store8<T, VEC>(static_cast<T*>(a.H) + row * a.sh, 8 * k, a.C, h);
+      fetch8<T, VEC>(a.X, row_of<T>(a.X, next), next, 8 * k, a.C, in && k < a.octets, fx[v]);
+      if (a.R.p) fetch8<T, VEC>(a.R, row_of<T>(a.R, next), next, 8 * k, a.C, in && k < a.octets, fr[v]);
+    }
+  };
+  fetch(row);
+  int turn = 0;
+  for (long row0 = (long)blockIdx.x * groups; row0 < a.rows; row0 += step, row += step, turn ^= 1) {
+    const bool in = row < a.rows;
+    const T *x = row_of<T>(a.X, row), *r = row_of<T>(a.R, row);
+    const unsigned long long block = DROP ? a.drop.first_block(row, a.octets) : 0;
+    float h[V][8], ss = 0.f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) ss = fmaf(h[e], h[e], ss);
+    for (int v = 0; v < V; ++v) {
+      const int k = lane + v * group;
+      sum_of<T, VEC, DROP>(a, key, block, x, r, fx[v], fr[v], k, in && k < a.octets, h[v]);
+    }
+    fetch(row + step);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const int k = lane + v * group;
+      if (a.H.p) store8<T, VEC>(const_cast<T*>(row_of<T>(a.H, row)), 8 * k, a.C, in && k < a.octets, h[v]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) ss = fmaf(h[v][e], h[v][e], ss);
     }
     ss = row_sum(ss, group, sums[turn]);
     const float rstd = rsqrtf(fmaf(ss, a.inv_c, a.eps));
     if (in && lane == 0 && a.rstd) a.rstd[row] = rstd;
-    const auto normed = [&](int v, float (&y)[8]) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
       const int k = lane + v * group;
-      if (!V) sum_of(k, held[0]);
       float w[8];
+      a.w.load<T, VEC>(8 * min(k, a.octets - 1), a.C, w);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) w[e] = 0.f;
-      if (k < a.octets) a.w.load<T, VEC>(8 * k, a.C, w);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = held[V ? v : 0][e] * rstd * w[e];
-    };
-    float y[8];
-    if (!a.q) {
-#pragma unroll
-      for (int v = 0; v < steps; ++v) {
-        normed(v, y);
-        const int k = lane + v * group;
-        if (in && k < a.octets) store8<T, VEC>(static_cast<T*>(a.Y) + row * a.sy, 8 * k, a.C, y);
-      }
-      continue;
+      for (int e = 0; e < 8; ++e) h[v][e] *= rstd * w[e];
+      if (!Q) store8<T, VEC>(const_cast<T*>(row_of<T>(a.Y, row)), 8 * k, a.C, in && k < a.octets, h[v]);
     }
-    uint32_t m = 0;
-    if (!a.q_group) {
+    if constexpr (Q) {
+      uint32_t m[V];
 #pragma unroll
-      for (int v = 0; v < steps; ++v) {
-        normed(v, y);
-        m = max(m, magnitude(y));
-        if (V)
+      for (int v = 0; v < V; ++v) m[v] = magnitude(h[v]);
+      if (a.q_group) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) held[V ? v : 0][e] = y[e];
-      }
-      m = row_max(m, group, most[turn]);
-    }
-#pragma unroll
-    for (int v = 0; v < steps; ++v) {
-      const int k = lane + v * group;
-      if (V && !a.q_group) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = held[V ? v : 0][e];
+        for (int v = 0; v < V; ++v) m[v] = group_most(m[v], a.q_group);
       } else {
-        normed(v, y);
+#pragma unroll
+        for (int v = 1; v < V; ++v) m[0] = max(m[0], m[v]);
+        m[0] = row_max(m[0], group, most[turn]);
+#pragma unroll
+        for (int v = 1; v < V; ++v) m[v] = m[0];
       }
-      if (a.q_group) {                                       // (a scale's octets are neighbours in a warp)
-        m = magnitude(y);
-        for (int o = a.q_group >> 4; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const int k = lane + v * group;
+        const bool here = in && k < a.octets;
+        const float scale = q_scale(m[v], a.q);
+        if (here && (a.q_group ? (8 * k) % a.q_group == 0 : k == 0)) a.scales[row * a.q_groups + (a.q_group ? 8 * k / a.q_group : 0)] = scale;
+        store8q<VEC>(const_cast<unsigned char*>(row_of<unsigned char>(a.Y, row)), 8 * k, a.C, here, h[v], 1.f / scale, a.q);
       }
+    }
+  }
+}
+
+// ---- rows of any length, a block each, read again for every step
+
+template <typename T, bool VEC, int DROP>
+__global__ void __launch_bounds__(1024) rms_forward_wide_kernel(const RmsArgs a) {
+  __shared__ float sums[2][32];
+  __shared__ uint32_t most[2][32];
+  const uint2 key = a.drop.key<DROP>();
+  const int steps = (a.octets + 1023) / 1024;
+  int turn = 0;
+  for (long row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
+    const T *x = row_of<T>(a.X, row), *r = row_of<T>(a.R, row);
+    const unsigned long long block = DROP ? a.drop.first_block(row, a.octets) : 0;
+    const auto sum = [&](int k, float (&h)[8]) {
+      Fetched<T, VEC> fx, fr;
+      fetch8<T, VEC>(a.X, x, row, 8 * k, a.C, k < a.octets, fx);
+      if (a.R.p) fetch8<T, VEC>(a.R, r, row, 8 * k, a.C, k < a.octets, fr);
+      sum_of<T, VEC, DROP>(a, key, block, x, r, fx, fr, k, k < a.octets, h);
+    };
+    float ss = 0.f, y[8];
+    for (int v = 0; v < steps; ++v) {
+      const int k = threadIdx.x + v * 1024;
+      sum(k, y);
+      if (a.H.p) store8<T, VEC>(const_cast<T*>(row_of<T>(a.H, row)), 8 * k, a.C, k < a.octets, y);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) ss = fmaf(y[e], y[e], ss);
+    }
+    ss = row_sum(ss, 1024, sums[turn]);
+    const float rstd = rsqrtf(fmaf(ss, a.inv_c, a.eps));
+    if (threadIdx.x == 0 && a.rstd) a.rstd[row] = rstd;
+    const auto normed = [&](int k) {
+      sum(k, y);
+      float w[8];
+      a.w.load<T, VEC>(8 * min(k, a.octets - 1), a.C, w);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] *= rstd * w[e];
+    };
+    uint32_t m = 0;
+    if (a.q && !a.q_group) {
+      for (int v = 0; v < steps; ++v) {
+        normed(threadIdx.x + v * 1024);
+        m = max(m, magnitude(y));
+      }
+      m = row_max(m, 1024, most[turn]);
+    }
+    for (int v = 0; v < steps; ++v) {
+      const int k = threadIdx.x + v * 1024;
+      const bool here = k < a.octets;
+      normed(k);
+      if (!a.q) {
+        store8<T, VEC>(const_cast<T*>(row_of<T>(a.Y, row)), 8 * k, a.C, here, y);
+        continue;
+      }
+      if (a.q_group) m = group_most(magnitude(y), a.q_group);
       const float scale = q_scale(m, a.q);
-      if (!in || k >= a.octets) continue;
-      const bool first = a.q_group ? (8 * k) % a.q_group == 0 : k == 0;
-      if (first) a.scales[row * a.q_groups + (a.q_group ? 8 * k / a.q_group : 0)] = scale;
-      store8q<VEC>(static_cast<unsigned char*>(a.Y) + row * a.sy, 8 * k, a.C, y, 1.f / scale, a.q);
+      if (here && (a.q_group ? (8 * k) % a.q_group == 0 : k == 0)) a.scales[row * a.q_groups + (a.q_group ? 8 * k / a.q_group : 0)] = scale;
+      store8q<VEC>(const_cast<unsigned char*>(row_of<unsigned char>(a.Y, row)), 8 * k, a.C, here, y, 1.f / scale, a.q);
     }
   }
 }
@@ -166,25 +224,28 @@ __global__ void __launch_bounds__(1024) rms_forward_kernel(const RmsArgs a) {
 cudaError_t launch_rms_forward(const xconv_rows_desc* d, const void* X, const void* residual, const void* weight, void* H, void* Y, float* scales, float* rstd,
                                cudaStream_t st) {
   RmsArgs a = {};
-  a.X = X; a.R = residual; a.w = {weight, d->param_dtype == XCONV_F32}; a.H = H; a.Y = Y; a.scales = scales; a.rstd = rstd;
-  a.rows = d->rows; a.sx = d->x_stride; a.sr = d->r_stride; a.sh = d->h_stride; a.sy = d->y_stride;
-  a.C = d->C; a.octets = (d->C + 7) / 8; a.eps = d->eps; a.inv_c = 1.f / (float)d->C;
+  const size_t es = d->dtype == XCONV_F32 ? 4 : 2, ys = d->q_type ? 1 : es;
+  a.X = rows_of(X, d->rows, d->C, d->x_stride, es); a.R = rows_of(residual, d->rows, d->C, d->r_stride, es);
+  a.H = rows_of(H, d->rows, d->C, d->h_stride, es); a.Y = rows_of(Y, d->rows, d->C, d->y_stride, ys);
+  a.w = {weight, d->param_dtype == XCONV_F32}; a.scales = scales; a.rstd = rstd;
+  a.rows = d->rows; a.C = d->C; a.octets = (d->C + 7) / 8; a.eps = d->eps; a.inv_c = 1.f / (float)d->C;
   a.q = d->q_type; a.q_group = d->q_group < d->C ? d->q_group : 0; a.q_groups = a.q_group ? (d->C + a.q_group - 1) / a.q_group : 1;
   a.drop = drop_of(d);
-  const int n = d->dtype == XCONV_F32 ? 4 : 8;             // values of 16 bytes
-  const bool vec = d->C % (a.q ? 8 : n) == 0 && at(X, 16) && at(residual, 16) && at(weight, 16) && at(H, 16) && at(Y, a.q ? 8 : 16) && d->x_stride % n == 0 &&
-                   (!residual || d->r_stride % n == 0) && (!H || d->h_stride % n == 0) && d->y_stride % (a.q ? 8 : n) == 0;
-  int V = 1;
-  if (a.octets <= 32) a.group = pow2_from(a.octets);
-  else if (a.octets <= 1024) a.group = (a.octets + 31) / 32 * 32;
-  else { a.group = 1024; V = 0; }
-  const int threads = a.group <= 32 ? 128 : a.group;
-  const long groups = a.group <= 32 ? threads / a.group : 1;
-  const long blocks = std::min((d->rows + groups - 1) / groups, (long)ROWS_SMS * (2048 / threads));
+  const bool vec = d->C % (a.q ? 8 : 16 / es) == 0 && whole(a.X, 16) && whole(a.R, 16) && whole(a.H, 16) && whole(a.Y, a.q ? 8 : 16) && at(weight, 16);
+  const Team p = team_of(a.octets);
+  a.group = p.group;
+  const long blocks = std::min((d->rows + p.groups - 1) / p.groups, (long)ROWS_SMS * std::max(1, 2048 / p.threads));
   return with_type(d->dtype, [&](auto t) {
     using T = decltype(t);
-    const auto kernel = vec ? (V ? rms_forward_kernel<T, 1, true> : rms_forward_kernel<T, 0, true>) : (V ? rms_forward_kernel<T, 1, false> : rms_forward_kernel<T, 0, false>);
-    kernel<<<(unsigned)blocks, threads, 0, st>>>(a);
+    const auto pick = [&](auto v, auto dropped) -> void (*)(const RmsArgs) {
+      constexpr bool VEC = decltype(v)::value;
+      constexpr int DROP = decltype(dropped)::value;
+      if (p.V == 0) return rms_forward_wide_kernel<T, VEC, DROP>;
+      if (a.q) return p.V == 1 ? rms_forward_kernel<T, 1, VEC, true, DROP> : rms_forward_kernel<T, 2, VEC, true, DROP>;
+      return p.V == 1 ? rms_forward_kernel<T, 1, VEC, false, DROP> : rms_forward_kernel<T, 2, VEC, false, DROP>;
+    };
+    const auto kernel = with_kinds(vec, a.drop.how, pick);
+    kernel<<<(unsigned)blocks, p.threads, 0, st>>>(a);
     return cudaGetLastError();
   });
 }

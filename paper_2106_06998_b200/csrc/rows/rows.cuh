@@ -1,6 +1,7 @@
 // What the kernels on rows share: eight neighbouring values of a row (an octet: what one Philox block decides about) as floats, the mask, sums over a row.
 #pragma once
 
+#include <algorithm>
 #include <type_traits>
 
 #include "../common.cuh"
@@ -10,22 +11,117 @@ namespace xconv {
 
 constexpr int ROWS_SMS = 148;
 
-// ---- octets
+// Division of numbers below 2^31 by one that is known before the launch: the high part of a product with ceil(2^(32 + l) / d) - 2^32, l = ceil(log2 d) (Granlund, Montgomery,
+// "Division by invariant integers using multiplication", PLDI'94).
+struct Divisor {
+  uint32_t d, m, l;
+  __device__ __forceinline__ uint32_t operator()(uint32_t n) const { return (__umulhi(m, n) + n) >> l; }
+};
+inline Divisor divisor(uint32_t d) {
+  uint32_t l = 0;
+  while ((1ull << l) < d) ++l;
+  return {d, (uint32_t)(((1ull << 32) * ((1ull << l) - d)) / d + 1), l};
+}
 
-// VEC: rows and pointers are at 16-byte boundaries, and C is a multiple of 16 bytes' values: accesses of 16 bytes; element by element otherwise.
-// Values from C on are zeros, and are not written.
+// ---- octets in memory
+
+// A tensor's rows.  An octet is read in pieces of 16 bytes (of 8-bit values: 8) at their own boundaries, whatever the octet's alignment: those that hold one of its values,
+// from which it is cut out by shifts -- the same ones for all octets of a row.  (Value by value that takes eight accesses, of lanes that are 16 bytes apart.)  A piece that reaches beyond
+// the tensor's own bytes is read value by value.  VEC: every row begins on such a boundary, and C is a multiple of a piece's values.
+struct Rows {
+  const char* p;                   // null: no such tensor
+  long stride;                     // bytes
+  const char* end;                 // of its own bytes
+  long inner;                      // rows but the first and the last one, where no piece of theirs can reach beyond the tensor's bytes
+};
+
+template <typename T>
+struct Octet {
+  static constexpr int WORDS = 2 * sizeof(T), PIECE = sizeof(T) == 1 ? 2 : 4, PER = 4 * PIECE / sizeof(T);      // words of an octet and of a piece, values of a piece
+};
 template <typename T, bool VEC>
-__device__ __forceinline__ void load8(const T* row, int c, int C, float (&f)[8]) {
-  if constexpr (!VEC) {
+struct Fetched {
+  uint32_t w[Octet<T>::WORDS + (VEC ? 0 : Octet<T>::PIECE)];
+};
+
+template <typename T>
+__device__ __forceinline__ const T* row_of(const Rows& t, long row) { return reinterpret_cast<const T*>(t.p + row * t.stride); }
+// Values between the boundary before a row and the row.
+template <typename T, bool VEC>
+__device__ __forceinline__ int shift_of(const T* row) { return VEC ? 0 : (int)(reinterpret_cast<uintptr_t>(row) % (4 * Octet<T>::PIECE) / sizeof(T)); }
+
+// The octet from value c on (a multiple of 8) of the n-th row, as its pieces lie in memory: pieces that are not needed (`in` false, or from C on) as zeros.
+template <typename T, bool VEC>
+__device__ __forceinline__ void fetch8(const Rows& t, const T* row, long n, int c, int C, bool in, Fetched<T, VEC>& f) {
+  constexpr int PIECE = Octet<T>::PIECE, PER = Octet<T>::PER;
+  const int shift = shift_of<T, VEC>(row);
+  const bool inner = VEC || (unsigned long)(n - 1) < (unsigned long)t.inner;
+  const char* at = reinterpret_cast<const char*>(row + (c - shift));
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] = c + e < C ? to_f(row[c + e]) : 0.f;
-  } else if constexpr (sizeof(T) == 4) {
-    const float4 u = *reinterpret_cast<const float4*>(row + c);
-    const float4 v = c + 4 < C ? *reinterpret_cast<const float4*>(row + c + 4) : make_float4(0.f, 0.f, 0.f, 0.f);
-    f[0] = u.x; f[1] = u.y; f[2] = u.z; f[3] = u.w; f[4] = v.x; f[5] = v.y; f[6] = v.z; f[7] = v.w;
+  for (int i = 0; i < (int)(sizeof(f.w) / (4 * PIECE)); ++i) {
+    const char* q = at + 4 * PIECE * i;
+    uint32_t* w = f.w + PIECE * i;
+    const bool needed = in && c - shift + i * PER < C && (VEC || i * PER < 8 + shift);
+    if (needed && (inner || (q >= t.p && q + 4 * PIECE <= t.end))) {
+      if constexpr (PIECE == 4) {
+        const uint4 u = __ldg(reinterpret_cast<const uint4*>(q));
+        w[0] = u.x; w[1] = u.y; w[2] = u.z; w[3] = u.w;
+      } else {
+        const uint2 u = __ldg(reinterpret_cast<const uint2*>(q));
+        w[0] = u.x; w[1] = u.y;
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < PIECE; ++k) w[k] = 0u;
+      if (!VEC && needed)
+#pragma unroll
+        for (int e = 0; e < PER; ++e) {
+          const char* v = q + e * sizeof(T);
+          if (v < t.p || v >= t.end) continue;
+          if constexpr (sizeof(T) == 4) w[e] = *reinterpret_cast<const uint32_t*>(v);
+          else if constexpr (sizeof(T) == 2) w[e / 2] |= (uint32_t)*reinterpret_cast<const unsigned short*>(v) << (16 * (e % 2));
+          else w[e / 4] |= (uint32_t)*reinterpret_cast<const unsigned char*>(v) << (8 * (e % 4));
+        }
+    }
+  }
+}
+
+// Word i + skip of the n words of w, for a skip of 0 to MOST (4 at most) that is known when the kernel runs; beyond them zeros.
+template <int MOST, int n>
+__device__ __forceinline__ uint32_t word_from(const uint32_t (&w)[n], int i, int skip) {
+  const uint32_t x0 = i < n ? w[i < n ? i : 0] : 0u, x1 = i + 1 < n ? w[i + 1 < n ? i + 1 : 0] : 0u, x2 = i + 2 < n ? w[i + 2 < n ? i + 2 : 0] : 0u,
+                 x3 = i + 3 < n ? w[i + 3 < n ? i + 3 : 0] : 0u, x4 = i + 4 < n ? w[i + 4 < n ? i + 4 : 0] : 0u;
+  const uint32_t lo = skip & 1 ? x1 : x0, hi = skip & 1 ? x3 : x2;
+  const uint32_t up = MOST < 2 ? lo : skip & 2 ? hi : lo;
+  return MOST < 4 ? up : skip & 4 ? x4 : up;
+}
+// N words from byte `first` on (a multiple of the values' size, 4 MOST + 3 at most).
+template <typename T, int MOST, int N, int M>
+__device__ __forceinline__ void bytes_from(const uint32_t (&w)[M], int first, uint32_t (&out)[N]) {
+  uint32_t a = word_from<MOST>(w, 0, first >> 2);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const uint32_t b = sizeof(T) < 4 || i + 1 < N ? word_from<MOST>(w, i + 1, first >> 2) : 0u;
+    out[i] = sizeof(T) == 4 ? a : __funnelshift_r(a, b, 8 * (first & 3));
+    a = b;
+  }
+}
+// The octet's own words.
+template <typename T, bool VEC>
+__device__ __forceinline__ void words_of(const Fetched<T, VEC>& f, int shift, uint32_t (&w)[Octet<T>::WORDS]) {
+  if constexpr (VEC) {
+#pragma unroll
+    for (int i = 0; i < Octet<T>::WORDS; ++i) w[i] = f.w[i];
   } else {
-    const uint4 u = *reinterpret_cast<const uint4*>(row + c);
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+    bytes_from<T, Octet<T>::PIECE - 1>(f.w, shift * (int)sizeof(T), w);
+  }
+}
+template <typename T>
+__device__ __forceinline__ void floats_of(const uint32_t (&w)[Octet<T>::WORDS], float (&f)[8]) {
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = __uint_as_float(w[e]);
+  } else {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       if constexpr (std::is_same<T, bf16>::value) {
@@ -38,17 +134,12 @@ __device__ __forceinline__ void load8(const T* row, int c, int C, float (&f)[8])
     }
   }
 }
-template <typename T, bool VEC>
-__device__ __forceinline__ void store8(T* row, int c, int C, const float (&f)[8]) {
-  if constexpr (!VEC) {
+template <typename T>
+__device__ __forceinline__ void words_for(const float (&f)[8], uint32_t (&w)[Octet<T>::WORDS]) {
+  if constexpr (sizeof(T) == 4) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (c + e < C) row[c + e] = from_f<T>(f[e]);
-  } else if constexpr (sizeof(T) == 4) {
-    *reinterpret_cast<float4*>(row + c) = make_float4(f[0], f[1], f[2], f[3]);
-    if (c + 4 < C) *reinterpret_cast<float4*>(row + c + 4) = make_float4(f[4], f[5], f[6], f[7]);
+    for (int e = 0; e < 8; ++e) w[e] = __float_as_uint(f[e]);
   } else {
-    uint32_t w[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       if constexpr (std::is_same<T, bf16>::value) {
@@ -59,64 +150,152 @@ __device__ __forceinline__ void store8(T* row, int c, int C, const float (&f)[8]
         w[i] = *reinterpret_cast<const uint32_t*>(&v);
       }
     }
-    *reinterpret_cast<uint4*>(row + c) = make_uint4(w[0], w[1], w[2], w[3]);
   }
 }
+// The octet's values as floats: zeros where `in` is false and from C on.  CLEAN = false: whatever, there.
+template <typename T, bool VEC, bool CLEAN = true>
+__device__ __forceinline__ void values_of(const Fetched<T, VEC>& f, const T* row, int c, int C, bool in, float (&v)[8]) {
+  uint32_t w[Octet<T>::WORDS];
+  words_of<T, VEC>(f, shift_of<T, VEC>(row), w);
+  if constexpr (CLEAN && !VEC) {                             // (VEC: pieces that are not there are zeros already)
+    const int bits = in ? 8 * (int)sizeof(T) * min(8, C - c) : 0;
+#pragma unroll
+    for (int i = 0; i < Octet<T>::WORDS; ++i) {
+      if constexpr (sizeof(T) == 4) w[i] = bits > 32 * i ? w[i] : 0u;
+      else w[i] = bits - 32 * i >= 32 ? w[i] : w[i] & ((1u << max(bits - 32 * i, 0)) - 1u);
+    }
+  }
+  floats_of<T>(w, v);
+}
 
-// A weight of floats, or of the activations' type.
+// Values from `from` to until - 1 of a piece.
+template <typename T, int PIECE>
+__device__ __forceinline__ void store_values(T* to, const uint32_t (&w)[PIECE], int from, int until) {
+#pragma unroll
+  for (int e = 0; e < 4 * PIECE / (int)sizeof(T); ++e) {
+    if (e < from || e >= until) continue;
+    if constexpr (sizeof(T) == 4) *reinterpret_cast<uint32_t*>(to + e) = w[e];
+    else if constexpr (sizeof(T) == 2) *reinterpret_cast<unsigned short*>(to + e) = (unsigned short)(w[e / 2] >> (16 * (e % 2)));
+    else *reinterpret_cast<unsigned char*>(to + e) = (unsigned char)(w[e / 4] >> (8 * (e % 4)));
+  }
+}
+// An octet to memory: values c to c + 7 of the row, those below C, of the lanes whose `in` says so.  Of rows at any alignment a lane writes the pieces from the boundary
+// before its octet on, as far as the next lane's, with what the lane before it has of them; what is left at the ends of a row and of a warp goes value by value.  All lanes of
+// the warp take part, and the octets of a row are those of neighbouring lanes.
+template <typename T, bool VEC>
+__device__ __forceinline__ void store8(T* row, int c, int C, bool in, const uint32_t (&w)[Octet<T>::WORDS]) {
+  constexpr int N = Octet<T>::WORDS, PIECE = Octet<T>::PIECE, PER = Octet<T>::PER;
+  const auto whole = [](T* to, const uint32_t* w) {
+    if constexpr (PIECE == 4) *reinterpret_cast<uint4*>(to) = make_uint4(w[0], w[1], w[2], w[3]);
+    else *reinterpret_cast<uint2*>(to) = make_uint2(w[0], w[1]);
+  };
+  if constexpr (VEC) {
+#pragma unroll
+    for (int i = 0; i < N / PIECE; ++i)
+      if (in && c + i * PER < C) whole(row + c + i * PER, w + PIECE * i);
+  } else {
+    uint32_t all[PIECE + N];                                 // a piece's worth of the lane before, and the octet
+#pragma unroll
+    for (int i = 0; i < PIECE; ++i) all[i] = __shfl_up_sync(0xffffffffu, w[N - PIECE + i], 1);
+#pragma unroll
+    for (int i = 0; i < N; ++i) all[PIECE + i] = w[i];
+    const int lane = threadIdx.x & 31, follows = __shfl_down_sync(0xffffffffu, (int)(in && c > 0), 1);
+    if (!in) return;
+    const int shift = shift_of<T, false>(row);
+    uint32_t out[N + PIECE];
+    bytes_from<T, PIECE>(all, 4 * PIECE - shift * (int)sizeof(T), out);
+    // `out` lies from the boundary on; of its values those from lo to hi - 1 are this lane's to write: whole pieces, and what is left of one at either end.
+    const int lo = c == 0 || lane == 0 ? shift : 0, hi = follows && lane < 31 ? 8 : shift + min(8, C - c);
+    T* to = row + (c - shift);
+    uint32_t rest[PIECE];
+    int from = 0, until = 0, at = 0;
+#pragma unroll
+    for (int i = 0; i < N / PIECE + 1; ++i) {
+      if (lo <= i * PER && (i + 1) * PER <= hi) {
+        whole(to + i * PER, out + PIECE * i);
+      } else if (lo < (i + 1) * PER && i * PER < hi) {
+        if (until) store_values(to + at, rest, from, until); // (a lane with two such ends: rows of one octet, and ends of warps)
+        from = max(lo - i * PER, 0); until = min(hi - i * PER, PER); at = i * PER;
+#pragma unroll
+        for (int k = 0; k < PIECE; ++k) rest[k] = out[PIECE * i + k];
+      }
+    }
+    if (until) store_values(to + at, rest, from, until);
+  }
+}
+template <typename T, bool VEC>
+__device__ __forceinline__ void store8(T* row, int c, int C, bool in, const float (&f)[8]) {
+  uint32_t w[Octet<T>::WORDS];
+  words_for<T>(f, w);
+  store8<T, VEC>(row, c, C, in, w);
+}
+
+// A weight of floats, or of the activations' type; read value by value where it is not aligned as its rows are.
 struct Weight {
   const void* p;                   // null: ones
   int f32;
+  template <typename P, bool VEC>
+  __device__ __forceinline__ void load_as(int c, int C, float (&f)[8]) const {
+    const P* q = static_cast<const P*>(p) + c;
+    if constexpr (VEC) {
+      Fetched<P, true> t;
+      const Rows r = {};
+      fetch8<P, true>(r, static_cast<const P*>(p), 0, c, C, c < C, t);
+      values_of<P, true>(t, static_cast<const P*>(p), c, C, c < C, f);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] = c + e < C ? to_f(q[e]) : 0.f;
+    }
+  }
   template <typename T, bool VEC>
   __device__ __forceinline__ void load(int c, int C, float (&f)[8]) const {
     if (!p) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) f[e] = 1.f;
     } else if (sizeof(T) == 4 || f32) {
-      load8<float, VEC>(static_cast<const float*>(p), c, C, f);
+      load_as<float, VEC>(c, C, f);
     } else {
-      load8<T, VEC>(static_cast<const T*>(p), c, C, f);
+      load_as<T, VEC>(c, C, f);
     }
   }
 };
 
 // ---- the mask
 
+// How a kernel gets its key: no mask, from the host, or with a number in device memory (which the compiler does not know to be the same in all lanes: it keeps the rounds' keys
+// in registers of each).
+enum { DROP_NONE = 0, DROP_HOST = 1, DROP_DEVICE = 2 };
+
 struct Drop {
   uint32_t bound, last;            // T - 1 of the header's T: its upper half with all bits below it set, and its lower half
   uint32_t k0, k1;
   const unsigned long long* add;
   float scale;                     // 1 / (1 - p)
-  int on;
-  long per;                        // rows of a mask row
-  // the key, when the kernel runs
+  int how;
+  Divisor per;                     // rows of a mask row
+  template <int HOW>
   __device__ __forceinline__ uint2 key() const {
-    if (!add) return make_uint2(k0, k1);
+    if (HOW != DROP_DEVICE) return make_uint2(k0, k1);
     const unsigned long long s = ((unsigned long long)k1 << 32 | k0) + *add;
     return make_uint2((uint32_t)s, (uint32_t)(s >> 32));
   }
-  __device__ __forceinline__ long mask_row(long row) const { return per == 1 ? row : row / per; }
+  __device__ __forceinline__ unsigned long long first_block(long row, int octets) const { return (unsigned long long)per((uint32_t)row) * (uint32_t)octets; }
 };
 
-// What the mask leaves of an octet.  dropped where u <= T - 1: decided by the upper halves, except where one equals T - 1's, which about one octet of 8192 meets: then
-// the lower halves are drawn too.
-__device__ __forceinline__ void drop8(const Drop& d, uint2 key, unsigned long long block, float (&f)[8]) {
+// Which values of an octet are dropped: where u <= T - 1.  The upper halves decide, except where one equals T - 1's, which about one octet of 8192 meets: then the lower halves
+// are drawn too.
+__device__ __forceinline__ void mask8(const Drop& d, uint2 key, unsigned long long block, bool (&gone)[8]) {
   const uint4 u = philox4x32_10((uint32_t)block, (uint32_t)(block >> 32), key.x, key.y, 3u);
   const uint32_t w[4] = {u.x, u.y, u.z, u.w};
   const uint32_t top = d.bound >> 16, twice = top * 0x10001u;
-  uint32_t tie = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t x = w[i] ^ twice;
-    tie |= (x - 0x00010001u) & ~x & 0x80008000u;             // a half of zeros
-  }
-  bool gone[8];
+  // the least half of what differs: zero where one is the border
+  const uint32_t off = __vminu2(__vminu2(w[0] ^ twice, w[1] ^ twice), __vminu2(w[2] ^ twice, w[3] ^ twice));
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     gone[2 * i] = (w[i] << 16) <= d.bound;
     gone[2 * i + 1] = w[i] <= d.bound;
   }
-  if (tie && d.last != 0xffffu) {
+  if (((off - 0x00010001u) & ~off & 0x80008000u) != 0 && d.last != 0xffffu) {
     const uint4 lower = philox4x32_10((uint32_t)block, (uint32_t)(block >> 32), key.x, key.y, 4u);
     const uint32_t l[4] = {lower.x, lower.y, lower.z, lower.w};
 #pragma unroll
@@ -125,8 +304,6 @@ __device__ __forceinline__ void drop8(const Drop& d, uint2 key, unsigned long lo
       if ((w[i] >> 16) == top) gone[2 * i + 1] = (l[i] >> 16) <= d.last;
     }
   }
-#pragma unroll
-  for (int e = 0; e < 8; ++e) f[e] = gone[e] ? 0.f : f[e] * d.scale;
 }
 
 // ---- over the threads of a row: `group` of them, a power of two up to 32, or all of the block
@@ -160,21 +337,53 @@ __device__ __forceinline__ uint32_t row_max(uint32_t v, int group, uint32_t* buf
 
 // ---- host side
 
+// The rows of a tensor of `size` bytes a value.
+inline Rows rows_of(const void* p, long rows, int C, long stride, size_t size) {
+  const char* q = static_cast<const char*>(p);
+  const long bytes = stride * (long)size;
+  return {q, bytes, q ? q + (rows - 1) * bytes + C * (long)size : nullptr, bytes >= 16 ? std::max(rows - 2, 0L) : 0L};
+}
+inline bool whole(const Rows& t, size_t a) { return !t.p || (reinterpret_cast<uintptr_t>(t.p) % a == 0 && t.stride % a == 0); }
 inline bool at(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 inline int pow2_from(long n) { int p = 1; while (p < n) p *= 2; return p; }
 
+// Threads a row and octets a thread: up to 32 octets one each, up to 64 two each of a warp, which meets no barrier; beyond, in a block of its own, one or two each,
+// whichever leaves fewer threads without an octet, and two where that is the same (half the warps at a barrier, and what threads keep beside their octets once for two).
+// V = 0: more than 512 threads hold.
+struct Team { int V, group, threads; long groups; };
+inline Team team_of(int octets) {
+  Team t = {};
+  const auto up = [](int n) { return (n + 31) / 32 * 32; };
+  if (octets <= 64) {
+    t.V = octets <= 32 ? 1 : 2;
+    t.group = octets <= 32 ? pow2_from(octets) : 32;
+    t.threads = 128;
+  } else {
+    const int one = up(octets), two = up((octets + 1) / 2);
+    t.V = one <= 512 && one < 2 * two ? 1 : two <= 512 ? 2 : 0;
+    t.group = t.threads = t.V == 1 ? one : t.V == 2 ? two : 1024;
+  }
+  t.groups = t.threads / t.group;
+  return t;
+}
 inline Drop drop_of(const xconv_rows_desc* d) {
   Drop r = {};
   const unsigned long long T = (unsigned long long)(d->p * 4294967296.0);
-  r.per = d->rows_per_mask;
-  r.on = T > 0;
-  if (!r.on) return r;
+  if (T == 0) return r;
+  r.how = d->seed_add ? DROP_DEVICE : DROP_HOST;
+  r.per = divisor((uint32_t)std::min<long>(d->rows_per_mask, 0x7fffffff));          // (rows are fewer)
   const uint32_t t = (uint32_t)(T - 1);
   r.bound = t | 0xffffu; r.last = t & 0xffffu;
   r.k0 = (uint32_t)d->seed; r.k1 = (uint32_t)(d->seed >> 32);
   r.add = d->seed_add;
   r.scale = d->p < 1.0 ? (float)(1.0 / (1.0 - d->p)) : 0.f;
   return r;
+}
+// f(VEC, how the key comes) as types.
+template <typename F>
+auto with_kinds(bool vec, int how, F&& f) {
+  const auto g = [&](auto h) { return vec ? f(std::true_type(), h) : f(std::false_type(), h); };
+  return how == DROP_NONE ? g(std::integral_constant<int, DROP_NONE>()) : how == DROP_HOST ? g(std::integral_constant<int, DROP_HOST>()) : g(std::integral_constant<int, DROP_DEVICE>());
 }
 // f(T()) with the type of the activations.
 template <typename F>
