@@ -52,10 +52,10 @@ __global__ void __launch_bounds__(256) dropout_kernel(const DropArgs a) {
   for (int i = 0; i < EACH; ++i) {
     const Unit<FLAT> n(a.units, first + 256 * i);
     float f[8], r[8];
-    values_of<T, VEC, false>(fx[i], n.template at<T>(a.X), 8 * n.k, n.C, n.in, f);
+    values_of<T, VEC, false>(fx[i], 8 * n.k, n.C, n.in, f);
 #pragma unroll
     for (int e = 0; e < 8; ++e) r[e] = 0.f;
-    if (a.R.p) values_of<T, VEC, false>(fr[i], n.template at<T>(a.R), 8 * n.k, n.C, n.in, r);
+    if (a.R.p) values_of<T, VEC, false>(fr[i], 8 * n.k, n.C, n.in, r);
     if (DROP) {
       bool gone[8];
       mask8(a.drop, key, FLAT ? (unsigned long long)n.u : a.drop.first_block(n.row, a.units.octets) + n.k, gone);
@@ -98,7 +98,7 @@ __global__ void __launch_bounds__(256) dequantize_kernel(const DequantArgs a) {
   for (int i = 0; i < EACH; ++i) {
     const Unit<FLAT> n(a.units, first + 256 * i);
     uint32_t b[2];
-    words_of<byte, VEC>(fq[i], shift_of<byte, VEC>(n.template at<byte>(a.Q)), b);
+    words_of<byte, VEC>(fq[i], b);
     float f[8];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {

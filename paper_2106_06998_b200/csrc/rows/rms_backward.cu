@@ -23,10 +23,10 @@ struct RmsBackArgs {
 
 // xh and g of an octet from what was fetched of h and dy, and its part of dw.
 template <typename T, bool VEC>
-__device__ __forceinline__ void weigh(const RmsBackArgs& a, const T* h, const T* dy, const Fetched<T, VEC>& fh, const Fetched<T, VEC>& fy, int k, bool in, float rstd,
+__device__ __forceinline__ void weigh(const RmsBackArgs& a, const Fetched<T, VEC>& fh, const Fetched<T, VEC>& fy, int k, bool in, float rstd,
                                       const float (&w)[8], float (&xh)[8], float (&g)[8], float (&dw)[8]) {
-  values_of<T, VEC>(fh, h, 8 * k, a.C, in, xh);
-  values_of<T, VEC>(fy, dy, 8 * k, a.C, in, g);
+  values_of<T, VEC>(fh, 8 * k, a.C, in, xh);
+  values_of<T, VEC>(fy, 8 * k, a.C, in, g);
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     xh[e] *= rstd;
@@ -36,18 +36,18 @@ __device__ __forceinline__ void weigh(const RmsBackArgs& a, const T* h, const T*
 }
 // dr, and dx, of an octet.
 template <typename T, bool VEC, int DROP>
-__device__ __forceinline__ void write_out(const RmsBackArgs& a, uint2 key, unsigned long long block, long row, const Fetched<T, VEC>& fd, int k, bool in, float rstd, float mean,
+__device__ __forceinline__ void write_out(const RmsBackArgs& a, uint2 key, unsigned long long block, T* dR, T* dX, const Fetched<T, VEC>& fd, int k, bool in, float rstd, float mean,
                                           const float (&xh)[8], const float (&g)[8]) {
   float d[8];
   if (a.dH.p) {
-    values_of<T, VEC>(fd, row_of<T>(a.dH, row), 8 * k, a.C, in, d);
+    values_of<T, VEC>(fd, 8 * k, a.C, in, d);
 #pragma unroll
     for (int e = 0; e < 8; ++e) d[e] = fmaf(rstd, fmaf(-xh[e], mean, g[e]), d[e]);
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e) d[e] = rstd * fmaf(-xh[e], mean, g[e]);
   }
-  if (a.dR.p) store8<T, VEC>(const_cast<T*>(row_of<T>(a.dR, row)), 8 * k, a.C, in, d);
+  if (a.dR.p) store8<T, VEC>(dR, 8 * k, a.C, in, d);
   if (a.dX.p) {
     if (DROP) {
       bool gone[8];
@@ -55,7 +55,7 @@ __device__ __forceinline__ void write_out(const RmsBackArgs& a, uint2 key, unsig
 #pragma unroll
       for (int e = 0; e < 8; ++e) d[e] = gone[e] ? 0.f : d[e] * a.drop.scale;
     }
-    store8<T, VEC>(const_cast<T*>(row_of<T>(a.dX, row)), 8 * k, a.C, in, d);
+    store8<T, VEC>(dX, 8 * k, a.C, in, d);
   }
 }
 
@@ -70,6 +70,7 @@ __global__ void __launch_bounds__(512) rms_backward_kernel(const RmsBackArgs a) 
   const uint2 key = a.drop.key<DROP>();
   const long step = (long)gridDim.x * groups;
   long row = (long)blockIdx.x * groups + own;
+  Walk<T> hs(a.H, row, step), dy(a.dY, row, step), dh(a.dH, row, step), dr(a.dR, row, step), dx(a.dX, row, step);
   Fetched<T, VEC> fh[V], fy[V], fd[V];
   float next_rstd = 0.f;
   const auto fetch = [&](long next) {
@@ -78,10 +79,11 @@ __global__ void __launch_bounds__(512) rms_backward_kernel(const RmsBackArgs a) 
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       const int k = lane + v * group;
-      fetch8<T, VEC>(a.H, row_of<T>(a.H, next), next, 8 * k, a.C, in && k < a.octets, fh[v]);
-      fetch8<T, VEC>(a.dY, row_of<T>(a.dY, next), next, 8 * k, a.C, in && k < a.octets, fy[v]);
-      if (a.dH.p) fetch8<T, VEC>(a.dH, row_of<T>(a.dH, next), next, 8 * k, a.C, in && k < a.octets, fd[v]);
+      fetch8<T, VEC>(a.H, hs.row, next, 8 * k, a.C, in && k < a.octets, fh[v]);
+      fetch8<T, VEC>(a.dY, dy.row, next, 8 * k, a.C, in && k < a.octets, fy[v]);
+      if (a.dH.p) fetch8<T, VEC>(a.dH, dh.row, next, 8 * k, a.C, in && k < a.octets, fd[v]);
     }
+    hs.next(); dy.next(); dh.next();
   };
   fetch(row);
   float dw[V][8], w[V][8];
@@ -92,7 +94,7 @@ __global__ void __launch_bounds__(512) rms_backward_kernel(const RmsBackArgs a) 
     a.w.load<T, VEC>(8 * min(lane + v * group, a.octets - 1), a.C, w[v]);
   }
   int turn = 0;
-  for (long row0 = (long)blockIdx.x * groups; row0 < a.rows; row0 += step, row += step, turn ^= 1) {
+  for (long row0 = (long)blockIdx.x * groups; row0 < a.rows; row0 += step, row += step, turn ^= 1, dr.next(), dx.next()) {
     const bool in = row < a.rows;
     const float rstd = next_rstd;
     float xh[V][8], g[V][8], s = 0.f;
@@ -100,7 +102,7 @@ __global__ void __launch_bounds__(512) rms_backward_kernel(const RmsBackArgs a) 
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       const int k = lane + v * group;
-      weigh<T, VEC>(a, row_of<T>(a.H, row), row_of<T>(a.dY, row), fh[v], fy[v], k, in && k < a.octets, rstd, w[v], xh[v], g[v], dw[v]);
+      weigh<T, VEC>(a, fh[v], fy[v], k, in && k < a.octets, rstd, w[v], xh[v], g[v], dw[v]);
 #pragma unroll
       for (int e = 0; e < 8; ++e) s = fmaf(g[v][e], xh[v][e], s);
       d[v] = fd[v];
@@ -111,7 +113,7 @@ __global__ void __launch_bounds__(512) rms_backward_kernel(const RmsBackArgs a) 
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       const int k = lane + v * group;
-      write_out<T, VEC, DROP>(a, key, block, row, d[v], k, in && k < a.octets, rstd, mean, xh[v], g[v]);
+      write_out<T, VEC, DROP>(a, key, block, dr.out(), dx.out(), d[v], k, in && k < a.octets, rstd, mean, xh[v], g[v]);
     }
   }
   if (!a.part) return;
@@ -158,7 +160,7 @@ __global__ void __launch_bounds__(1024) rms_backward_wide_kernel(const RmsBackAr
       fetch8<T, VEC>(a.dY, row_of<T>(a.dY, row), row, 8 * k, a.C, k < a.octets, fy);
       float w[8];
       a.w.load<T, VEC>(8 * min(k, a.octets - 1), a.C, w);
-      weigh<T, VEC>(a, row_of<T>(a.H, row), row_of<T>(a.dY, row), fh, fy, k, k < a.octets, rstd, w, xh, g, unused);
+      weigh<T, VEC>(a, fh, fy, k, k < a.octets, rstd, w, xh, g, unused);
     };
     for (int v = 0; v < steps; ++v) {
       read(threadIdx.x + v * 1024);
@@ -172,7 +174,7 @@ __global__ void __launch_bounds__(1024) rms_backward_wide_kernel(const RmsBackAr
       read(k);
       Fetched<T, VEC> fd;
       if (a.dH.p) fetch8<T, VEC>(a.dH, row_of<T>(a.dH, row), row, 8 * k, a.C, k < a.octets, fd);
-      write_out<T, VEC, DROP>(a, key, block, row, fd, k, k < a.octets, rstd, mean, xh, g);
+      write_out<T, VEC, DROP>(a, key, block, const_cast<T*>(row_of<T>(a.dR, row)), const_cast<T*>(row_of<T>(a.dX, row)), fd, k, k < a.octets, rstd, mean, xh, g);
     }
   }
 }

@@ -62,13 +62,12 @@ __device__ __forceinline__ uint32_t group_most(uint32_t m, int width) {
 
 // The octet of h from what was fetched of x and r.
 template <typename T, bool VEC, int DROP>
-__device__ __forceinline__ void sum_of(const RmsArgs& a, uint2 key, unsigned long long block, const T* x, const T* r, const Fetched<T, VEC>& fx, const Fetched<T, VEC>& fr, int k, bool in,
-                                       float (&h)[8]) {
-  values_of<T, VEC>(fx, x, 8 * k, a.C, in, h);
+__device__ __forceinline__ void sum_of(const RmsArgs& a, uint2 key, unsigned long long block, const Fetched<T, VEC>& fx, const Fetched<T, VEC>& fr, int k, bool in, float (&h)[8]) {
+  values_of<T, VEC>(fx, 8 * k, a.C, in, h);
   float f[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) f[e] = 0.f;
-  if (a.R.p) values_of<T, VEC>(fr, r, 8 * k, a.C, in, f);
+  if (a.R.p) values_of<T, VEC>(fr, 8 * k, a.C, in, f);
   if (DROP) {
     bool gone[8];
     mask8(a.drop, key, block + k, gone);
@@ -86,38 +85,43 @@ template <typename T, int V, bool VEC, bool Q, int DROP>
 __global__ void __launch_bounds__(512) rms_forward_kernel(const RmsArgs a) {
   __shared__ float sums[2][32];
   __shared__ uint32_t most[2][32];
+  typedef std::conditional_t<Q, unsigned char, T> Y;
   const int group = a.group, lane = group <= 32 ? threadIdx.x & (group - 1) : threadIdx.x;
   const int groups = group <= 32 ? blockDim.x / group : 1, own = group <= 32 ? threadIdx.x / group : 0;
   const uint2 key = a.drop.key<DROP>();
   const long step = (long)gridDim.x * groups;
   long row = (long)blockIdx.x * groups + own;
+  Walk<T> x(a.X, row, step), r(a.R, row, step), hs(a.H, row, step);
+  Walk<Y> ys(a.Y, row, step);
   Fetched<T, VEC> fx[V], fr[V];
   const auto fetch = [&](long next) {
     const bool in = next < a.rows;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       const int k = lane + v * group;
-      fetch8<T, VEC>(a.X, row_of<T>(a.X, next), next, 8 * k, a.C, in && k < a.octets, fx[v]);
-      if (a.R.p) fetch8<T, VEC>(a.R, row_of<T>(a.R, next), next, 8 * k, a.C, in && k < a.octets, fr[v]);
+      fetch8<T, VEC>(a.X, x.row, next, 8 * k, a.C, in && k < a.octets, fx[v]);
+      if (a.R.p) fetch8<T, VEC>(a.R, r.row, next, 8 * k, a.C, in && k < a.octets, fr[v]);
     }
+    x.next(); r.next();
   };
   fetch(row);
+  float w[8];
+  if (V == 1) a.w.load<T, VEC>(8 * min(lane, a.octets - 1), a.C, w);
   int turn = 0;
-  for (long row0 = (long)blockIdx.x * groups; row0 < a.rows; row0 += step, row += step, turn ^= 1) {
+  for (long row0 = (long)blockIdx.x * groups; row0 < a.rows; row0 += step, row += step, turn ^= 1, hs.next(), ys.next()) {
     const bool in = row < a.rows;
-    const T *x = row_of<T>(a.X, row), *r = row_of<T>(a.R, row);
     const unsigned long long block = DROP ? a.drop.first_block(row, a.octets) : 0;
     float h[V][8], ss = 0.f;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       const int k = lane + v * group;
-      sum_of<T, VEC, DROP>(a, key, block, x, r, fx[v], fr[v], k, in && k < a.octets, h[v]);
+      sum_of<T, VEC, DROP>(a, key, block, fx[v], fr[v], k, in && k < a.octets, h[v]);
     }
     fetch(row + step);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       const int k = lane + v * group;
-      if (a.H.p) store8<T, VEC>(const_cast<T*>(row_of<T>(a.H, row)), 8 * k, a.C, in && k < a.octets, h[v]);
+      if (a.H.p) store8<T, VEC>(hs.out(), 8 * k, a.C, in && k < a.octets, h[v]);
 #pragma unroll
       for (int e = 0; e < 8; ++e) ss = fmaf(h[v][e], h[v][e], ss);
     }
@@ -127,11 +131,10 @@ __global__ void __launch_bounds__(512) rms_forward_kernel(const RmsArgs a) {
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       const int k = lane + v * group;
-      float w[8];
-      a.w.load<T, VEC>(8 * min(k, a.octets - 1), a.C, w);
+      if (V > 1) a.w.load<T, VEC>(8 * min(k, a.octets - 1), a.C, w);
 #pragma unroll
       for (int e = 0; e < 8; ++e) h[v][e] *= rstd * w[e];
-      if (!Q) store8<T, VEC>(const_cast<T*>(row_of<T>(a.Y, row)), 8 * k, a.C, in && k < a.octets, h[v]);
+      if constexpr (!Q) store8<T, VEC>(ys.out(), 8 * k, a.C, in && k < a.octets, h[v]);
     }
     if constexpr (Q) {
       uint32_t m[V];
@@ -153,7 +156,7 @@ __global__ void __launch_bounds__(512) rms_forward_kernel(const RmsArgs a) {
         const bool here = in && k < a.octets;
         const float scale = q_scale(m[v], a.q);
         if (here && (a.q_group ? (8 * k) % a.q_group == 0 : k == 0)) a.scales[row * a.q_groups + (a.q_group ? 8 * k / a.q_group : 0)] = scale;
-        store8q<VEC>(const_cast<unsigned char*>(row_of<unsigned char>(a.Y, row)), 8 * k, a.C, here, h[v], 1.f / scale, a.q);
+        store8q<VEC>(ys.out(), 8 * k, a.C, here, h[v], 1.f / scale, a.q);
       }
     }
   }
@@ -175,7 +178,7 @@ __global__ void __launch_bounds__(1024) rms_forward_wide_kernel(const RmsArgs a)
       Fetched<T, VEC> fx, fr;
       fetch8<T, VEC>(a.X, x, row, 8 * k, a.C, k < a.octets, fx);
       if (a.R.p) fetch8<T, VEC>(a.R, r, row, 8 * k, a.C, k < a.octets, fr);
-      sum_of<T, VEC, DROP>(a, key, block, x, r, fx, fr, k, k < a.octets, h);
+      sum_of<T, VEC, DROP>(a, key, block, fx, fr, k, k < a.octets, h);
     };
     float ss = 0.f, y[8];
     for (int v = 0; v < steps; ++v) {

@@ -42,8 +42,18 @@ struct Octet {
 template <typename T, bool VEC>
 struct Fetched {
   uint32_t w[Octet<T>::WORDS + (VEC ? 0 : Octet<T>::PIECE)];
+  int shift;                       // (not VEC) values between the boundary before the row and the row
 };
 
+// ... as a pointer that moves on from row to row.
+template <typename T>
+struct Walk {
+  const T* row;
+  long step;                       // bytes
+  __device__ __forceinline__ Walk(const Rows& t, long first, long rows) : row(reinterpret_cast<const T*>(t.p + first * t.stride)), step(rows * t.stride) {}
+  __device__ __forceinline__ void next() { row = reinterpret_cast<const T*>(reinterpret_cast<const char*>(row) + step); }
+  __device__ __forceinline__ T* out() const { return const_cast<T*>(row); }
+};
 template <typename T>
 __device__ __forceinline__ const T* row_of(const Rows& t, long row) { return reinterpret_cast<const T*>(t.p + row * t.stride); }
 // Values between the boundary before a row and the row.
@@ -53,35 +63,38 @@ __device__ __forceinline__ int shift_of(const T* row) { return VEC ? 0 : (int)(r
 // The octet from value c on (a multiple of 8) of the n-th row, as its pieces lie in memory: pieces that are not needed (`in` false, or from C on) as zeros.
 template <typename T, bool VEC>
 __device__ __forceinline__ void fetch8(const Rows& t, const T* row, long n, int c, int C, bool in, Fetched<T, VEC>& f) {
-  constexpr int PIECE = Octet<T>::PIECE, PER = Octet<T>::PER;
-  const int shift = shift_of<T, VEC>(row);
-  const bool inner = VEC || (unsigned long)(n - 1) < (unsigned long)t.inner;
-  const char* at = reinterpret_cast<const char*>(row + (c - shift));
+  constexpr int PIECE = Octet<T>::PIECE, PER = Octet<T>::PER, PIECES = sizeof(f.w) / (4 * PIECE);
+  f.shift = shift_of<T, VEC>(row);
+  const char* at = reinterpret_cast<const char*>(row + (c - f.shift));
+  const auto needed = [&](int i) { return in && (i == 0 || c - f.shift + i * PER < C) && (i + 1 < PIECES || VEC || f.shift + 8 > i * PER); };
+  if (VEC || (unsigned long)(n - 1) < (unsigned long)t.inner) {
 #pragma unroll
-  for (int i = 0; i < (int)(sizeof(f.w) / (4 * PIECE)); ++i) {
-    const char* q = at + 4 * PIECE * i;
-    uint32_t* w = f.w + PIECE * i;
-    const bool needed = in && c - shift + i * PER < C && (VEC || i * PER < 8 + shift);
-    if (needed && (inner || (q >= t.p && q + 4 * PIECE <= t.end))) {
+    for (int i = 0; i < PIECES; ++i) {
+      uint32_t* w = f.w + PIECE * i;
       if constexpr (PIECE == 4) {
-        const uint4 u = __ldg(reinterpret_cast<const uint4*>(q));
+        uint4 u = make_uint4(0u, 0u, 0u, 0u);
+        if (needed(i)) u = __ldg(reinterpret_cast<const uint4*>(at + 4 * PIECE * i));
         w[0] = u.x; w[1] = u.y; w[2] = u.z; w[3] = u.w;
       } else {
-        const uint2 u = __ldg(reinterpret_cast<const uint2*>(q));
+        uint2 u = make_uint2(0u, 0u);
+        if (needed(i)) u = __ldg(reinterpret_cast<const uint2*>(at + 4 * PIECE * i));
         w[0] = u.x; w[1] = u.y;
       }
-    } else {
+    }
+  } else {
+    // (value by value: few rows come here)
 #pragma unroll
-      for (int k = 0; k < PIECE; ++k) w[k] = 0u;
-      if (!VEC && needed)
+    for (int i = 0; i < PIECES * PIECE; ++i) {
+      f.w[i] = 0u;
+      if (!needed(i / PIECE)) continue;
 #pragma unroll
-        for (int e = 0; e < PER; ++e) {
-          const char* v = q + e * sizeof(T);
-          if (v < t.p || v >= t.end) continue;
-          if constexpr (sizeof(T) == 4) w[e] = *reinterpret_cast<const uint32_t*>(v);
-          else if constexpr (sizeof(T) == 2) w[e / 2] |= (uint32_t)*reinterpret_cast<const unsigned short*>(v) << (16 * (e % 2));
-          else w[e / 4] |= (uint32_t)*reinterpret_cast<const unsigned char*>(v) << (8 * (e % 4));
-        }
+      for (int e = 0; e < 4 / (int)sizeof(T); ++e) {
+        const char* v = at + 4 * i + e * sizeof(T);
+        if (v < t.p || v >= t.end) continue;
+        if constexpr (sizeof(T) == 4) f.w[i] = *reinterpret_cast<const uint32_t*>(v);
+        else if constexpr (sizeof(T) == 2) f.w[i] |= (uint32_t)*reinterpret_cast<const unsigned short*>(v) << (16 * e);
+        else f.w[i] |= (uint32_t)*reinterpret_cast<const unsigned char*>(v) << (8 * e);
+      }
     }
   }
 }
@@ -108,12 +121,12 @@ __device__ __forceinline__ void bytes_from(const uint32_t (&w)[M], int first, ui
 }
 // The octet's own words.
 template <typename T, bool VEC>
-__device__ __forceinline__ void words_of(const Fetched<T, VEC>& f, int shift, uint32_t (&w)[Octet<T>::WORDS]) {
+__device__ __forceinline__ void words_of(const Fetched<T, VEC>& f, uint32_t (&w)[Octet<T>::WORDS]) {
   if constexpr (VEC) {
 #pragma unroll
     for (int i = 0; i < Octet<T>::WORDS; ++i) w[i] = f.w[i];
   } else {
-    bytes_from<T, Octet<T>::PIECE - 1>(f.w, shift * (int)sizeof(T), w);
+    bytes_from<T, Octet<T>::PIECE - 1>(f.w, f.shift * (int)sizeof(T), w);
   }
 }
 template <typename T>
@@ -154,9 +167,9 @@ __device__ __forceinline__ void words_for(const float (&f)[8], uint32_t (&w)[Oct
 }
 // The octet's values as floats: zeros where `in` is false and from C on.  CLEAN = false: whatever, there.
 template <typename T, bool VEC, bool CLEAN = true>
-__device__ __forceinline__ void values_of(const Fetched<T, VEC>& f, const T* row, int c, int C, bool in, float (&v)[8]) {
+__device__ __forceinline__ void values_of(const Fetched<T, VEC>& f, int c, int C, bool in, float (&v)[8]) {
   uint32_t w[Octet<T>::WORDS];
-  words_of<T, VEC>(f, shift_of<T, VEC>(row), w);
+  words_of<T, VEC>(f, w);
   if constexpr (CLEAN && !VEC) {                             // (VEC: pieces that are not there are zeros already)
     const int bits = in ? 8 * (int)sizeof(T) * min(8, C - c) : 0;
 #pragma unroll
@@ -168,59 +181,49 @@ __device__ __forceinline__ void values_of(const Fetched<T, VEC>& f, const T* row
   floats_of<T>(w, v);
 }
 
-// Values from `from` to until - 1 of a piece.
-template <typename T, int PIECE>
-__device__ __forceinline__ void store_values(T* to, const uint32_t (&w)[PIECE], int from, int until) {
-#pragma unroll
-  for (int e = 0; e < 4 * PIECE / (int)sizeof(T); ++e) {
-    if (e < from || e >= until) continue;
-    if constexpr (sizeof(T) == 4) *reinterpret_cast<uint32_t*>(to + e) = w[e];
-    else if constexpr (sizeof(T) == 2) *reinterpret_cast<unsigned short*>(to + e) = (unsigned short)(w[e / 2] >> (16 * (e % 2)));
-    else *reinterpret_cast<unsigned char*>(to + e) = (unsigned char)(w[e / 4] >> (8 * (e % 4)));
-  }
-}
 // An octet to memory: values c to c + 7 of the row, those below C, of the lanes whose `in` says so.  Of rows at any alignment a lane writes the pieces from the boundary
-// before its octet on, as far as the next lane's, with what the lane before it has of them; what is left at the ends of a row and of a warp goes value by value.  All lanes of
+// before its octet on that are full, the first with what the lane before it has of it; values that no such piece takes, at the ends of a row and of a warp, go one by one.  All lanes of
 // the warp take part, and the octets of a row are those of neighbouring lanes.
 template <typename T, bool VEC>
 __device__ __forceinline__ void store8(T* row, int c, int C, bool in, const uint32_t (&w)[Octet<T>::WORDS]) {
-  constexpr int N = Octet<T>::WORDS, PIECE = Octet<T>::PIECE, PER = Octet<T>::PER;
+  constexpr int N = Octet<T>::WORDS, PIECE = Octet<T>::PIECE, PER = Octet<T>::PER, PIECES = N / PIECE;
   const auto whole = [](T* to, const uint32_t* w) {
     if constexpr (PIECE == 4) *reinterpret_cast<uint4*>(to) = make_uint4(w[0], w[1], w[2], w[3]);
     else *reinterpret_cast<uint2*>(to) = make_uint2(w[0], w[1]);
   };
   if constexpr (VEC) {
 #pragma unroll
-    for (int i = 0; i < N / PIECE; ++i)
-      if (in && c + i * PER < C) whole(row + c + i * PER, w + PIECE * i);
+    for (int i = 0; i < PIECES; ++i)
+      if (in && (i == 0 || c + i * PER < C)) whole(row + c + i * PER, w + PIECE * i);
   } else {
     uint32_t all[PIECE + N];                                 // a piece's worth of the lane before, and the octet
 #pragma unroll
     for (int i = 0; i < PIECE; ++i) all[i] = __shfl_up_sync(0xffffffffu, w[N - PIECE + i], 1);
 #pragma unroll
     for (int i = 0; i < N; ++i) all[PIECE + i] = w[i];
-    const int lane = threadIdx.x & 31, follows = __shfl_down_sync(0xffffffffu, (int)(in && c > 0), 1);
     if (!in) return;
-    const int shift = shift_of<T, false>(row);
-    uint32_t out[N + PIECE];
+    const int shift = shift_of<T, false>(row), lane = threadIdx.x & 31, m = C - c;      // (values from this one on: more than 8, but for the last octet)
+    uint32_t out[N];                                         // from the boundary on
     bytes_from<T, PIECE>(all, 4 * PIECE - shift * (int)sizeof(T), out);
-    // `out` lies from the boundary on; of its values those from lo to hi - 1 are this lane's to write: whole pieces, and what is left of one at either end.
-    const int lo = c == 0 || lane == 0 ? shift : 0, hi = follows && lane < 31 ? 8 : shift + min(8, C - c);
-    T* to = row + (c - shift);
-    uint32_t rest[PIECE];
-    int from = 0, until = 0, at = 0;
+    // the octet's values that no piece takes, by bits: those of the i-th piece from the boundary on are PER of them from i PER - shift on
+    uint32_t left = m >= 8 ? 0xffu : (1u << m) - 1u;
+    T* to = row + c;
 #pragma unroll
-    for (int i = 0; i < N / PIECE + 1; ++i) {
-      if (lo <= i * PER && (i + 1) * PER <= hi) {
-        whole(to + i * PER, out + PIECE * i);
-      } else if (lo < (i + 1) * PER && i * PER < hi) {
-        if (until) store_values(to + at, rest, from, until); // (a lane with two such ends: rows of one octet, and ends of warps)
-        from = max(lo - i * PER, 0); until = min(hi - i * PER, PER); at = i * PER;
-#pragma unroll
-        for (int k = 0; k < PIECE; ++k) rest[k] = out[PIECE * i + k];
-      }
+    for (int i = 0; i < PIECES + 1; ++i) {
+      const uint32_t its = ((1u << PER) - 1u) << 8 << (i * PER) >> shift >> 8;
+      // (the piece behind the last one is the next lane's first)
+      const bool full = i < PIECES ? shift + m >= (i + 1) * PER && (i > 0 || (c > 0 && lane > 0)) : lane < 31 && shift + m - 8 >= PER;
+      if (full) left &= ~its;
+      if (i < PIECES && full) whole(to - shift + i * PER, out + PIECE * i);
     }
-    if (until) store_values(to + at, rest, from, until);
+    if (left)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (!(left >> e & 1)) continue;
+        if constexpr (sizeof(T) == 4) *reinterpret_cast<uint32_t*>(to + e) = w[e];
+        else if constexpr (sizeof(T) == 2) *reinterpret_cast<unsigned short*>(to + e) = (unsigned short)(w[e / 2] >> (16 * (e % 2)));
+        else *reinterpret_cast<unsigned char*>(to + e) = (unsigned char)(w[e / 4] >> (8 * (e % 4)));
+      }
   }
 }
 template <typename T, bool VEC>
@@ -241,7 +244,7 @@ struct Weight {
       Fetched<P, true> t;
       const Rows r = {};
       fetch8<P, true>(r, static_cast<const P*>(p), 0, c, C, c < C, t);
-      values_of<P, true>(t, static_cast<const P*>(p), c, C, c < C, f);
+      values_of<P, true>(t, c, C, c < C, f);
     } else {
 #pragma unroll
       for (int e = 0; e < 8; ++e) f[e] = c + e < C ? to_f(q[e]) : 0.f;
