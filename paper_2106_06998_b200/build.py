@@ -12,7 +12,7 @@ LIB = os.path.join(HERE, "libxconv.so")
 MARSHAL, MARSHAL_SOURCE = os.path.join(HERE, "_marshal.so"), os.path.join(HERE, "csrc", "marshal.cpp")
 SOURCES = ["api.cu", "tc_kernels.cu", "conv_tc.cu", "contract_tc.cu", "stream_tc.cu", "conv_fma.cu", "small_f32.cu", "conv_split.cu", "contract_split.cu", "gemm_split.cu",
            "static_scratch.cu", "layer_norm.cu", "api_norm.cu", "update/newton_schulz.cu", "api_update.cu",
-           "rows/rms_norm.cu", "rows/rms_backward.cu", "rows/dropout.cu", "api_rows.cu"]
+           "rows/rms_norm.cu", "rows/rms_backward.cu", "rows/rms_staged.cu", "rows/dropout.cu", "api_rows.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "--use_fast_math=false", "-Xcompiler", "-fPIC,-O2", "-cudart", "static"]
 

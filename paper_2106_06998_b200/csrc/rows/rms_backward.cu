@@ -4,6 +4,7 @@
 //
 // Memory bounds it: dy, h (and dh) are read once, dr (and dx) written once.  The threads of a block keep the same columns from row to row and carry dw in registers; blocks
 // leave a partial sum a column each, which a second kernel adds in fixed order (no atomics: the same bits every time).
+#include "rms.h"
 #include "rows.cuh"
 
 namespace xconv {
@@ -222,7 +223,7 @@ Plan plan_of(const xconv_rows_desc* d) {
 
 }  // namespace
 
-size_t rms_backward_part_bytes(const xconv_rows_desc* d) { return (size_t)plan_of(d).parts * (size_t)d->C * sizeof(float); }
+size_t rms_backward_part_bytes(const xconv_rows_desc* d) { return (size_t)std::max(plan_of(d).parts, rms_staged_backward_parts(d)) * (size_t)d->C * sizeof(float); }
 
 cudaError_t launch_rms_backward(const xconv_rows_desc* d, const void* dY, const void* H, const float* rstd, const void* weight, const void* dH, void* dX, void* dR,
                                 float* dweight, float* part, cudaStream_t st, int* launches) {
@@ -235,8 +236,11 @@ cudaError_t launch_rms_backward(const xconv_rows_desc* d, const void* dY, const 
   a.rows = d->rows; a.C = d->C; a.octets = (d->C + 7) / 8; a.group = p.team.group; a.inv_c = 1.f / (float)d->C;
   a.drop = drop_of(d);
   const bool vec = d->C % (16 / es) == 0 && whole(a.dY, 16) && whole(a.H, 16) && whole(a.dH, 16) && whole(a.dX, 16) && whole(a.dR, 16) && at(weight, 16);
+  long parts = p.parts;
   if (d->rows > 0) {
-    const cudaError_t e = with_type(d->dtype, [&](auto t) {
+    cudaError_t e;
+    if (!vec && rms_staged_backward(d, dY, H, rstd, weight, dH, dX, dR, part, &parts, st, &e)) ++*launches;
+    else e = with_type(d->dtype, [&](auto t) {
       using T = decltype(t);
       const int V = p.team.V;
       if (V || dX || dR) {
@@ -260,7 +264,7 @@ cudaError_t launch_rms_backward(const xconv_rows_desc* d, const void* dY, const 
   }
   if (!dweight) return cudaSuccess;
   ++*launches;
-  return launch_pdl(rms_sums_kernel, dim3((unsigned)((d->C + 31) / 32)), dim3(1024), 0, st, (const float*)part, (int)p.parts, (int)d->C, dweight);
+  return launch_pdl(rms_sums_kernel, dim3((unsigned)((d->C + 31) / 32)), dim3(1024), 0, st, (const float*)part, (int)parts, (int)d->C, dweight);
 }
 
 }  // namespace xconv

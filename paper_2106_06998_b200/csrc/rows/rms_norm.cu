@@ -4,6 +4,7 @@
 //
 // Memory bounds it: x and the residual are read once, h and y written once.  A row lies in the registers of `group` threads, V octets each; h stays in float for y (it
 // is rounded once, where it is written).
+#include "rms.h"
 #include "rows.cuh"
 
 namespace xconv {
@@ -235,6 +236,8 @@ cudaError_t launch_rms_forward(const xconv_rows_desc* d, const void* X, const vo
   a.q = d->q_type; a.q_group = d->q_group < d->C ? d->q_group : 0; a.q_groups = a.q_group ? (d->C + a.q_group - 1) / a.q_group : 1;
   a.drop = drop_of(d);
   const bool vec = d->C % (a.q ? 8 : 16 / es) == 0 && whole(a.X, 16) && whole(a.R, 16) && whole(a.H, 16) && whole(a.Y, a.q ? 8 : 16) && at(weight, 16);
+  cudaError_t e;
+  if (!vec && !a.q && rms_staged_forward(d, X, residual, weight, H, Y, rstd, st, &e)) return e;
   const Team p = team_of(a.octets);
   a.group = p.group;
   const long blocks = std::min((d->rows + p.groups - 1) / p.groups, (long)ROWS_SMS * std::max(1, 2048 / p.threads));

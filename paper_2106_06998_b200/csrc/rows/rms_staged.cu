@@ -1,0 +1,236 @@
+// RMS norm and its gradients of dense rows that do not begin on 16-byte boundaries (formulas: rms_norm.cu, rms_backward.cu).
+#include "rms.h"
+#include "staged.cuh"
+
+namespace xconv {
+
+namespace {
+
+struct StagedArgs {
+  Staged s;
+  const void *in[3];               // forward: x, residual; backward: h, dy, dh
+  void *out[2];                    // over the first and the second of them: y, h; dx, dr
+  const void* weight;
+  int weight_f32;
+  float* rstd;                     // (read by the backward pass)
+  float* part;
+  float eps, inv_c;
+};
+
+template <typename T, int V, bool BACK>
+__global__ void __launch_bounds__(512, V <= 4 ? 2 : 1) rms_staged_kernel(const StagedArgs a) {
+  extern __shared__ uint4 ring[];
+  __shared__ float sums[2][32];
+  constexpr int PER = 16 / sizeof(T);
+  char* const base = reinterpret_cast<char*>(ring);
+  const Staged& s = a.s;
+  unsigned char* const mask = reinterpret_cast<unsigned char*>(base + s.mask_at);
+  const int group = s.group, lane = group <= 32 ? threadIdx.x & (group - 1) : threadIdx.x, own = group <= 32 ? threadIdx.x / group : 0;
+  const int bytes = s.slots * s.slot;                          // of a stage
+  const bool drops = s.drop.how != DROP_NONE;
+  const uint2 key = s.drop.how == DROP_DEVICE ? s.drop.key<DROP_DEVICE>() : s.drop.key<DROP_HOST>();
+  const auto fetch = [&](long run, int stage) {
+    if (run < s.runs) {
+      const Run r = Run::of<PER>(s, run);
+#pragma unroll
+      for (int i = 0; i < (BACK ? 3 : 2); ++i)
+        if (a.in[i]) run_in<T>(s, r, base + stage * bytes + i * s.slot, static_cast<const T*>(a.in[i]));
+    }
+    copies_commit();
+  };
+  for (int i = 0; i < s.stages - 1; ++i) fetch(blockIdx.x + (long)i * gridDim.x, i);
+  const Pairs<T, V> pairs(lane, group, s.C, s.C & 1 ? (int)((long)blockIdx.x * s.run + own) & 1 : 0);
+  float w[V][2], dw[V][2];
+  if (sizeof(T) == 4 || a.weight_f32) pairs.template weights<float>(a.weight, w);
+  else pairs.template weights<T>(a.weight, w);
+#pragma unroll
+  for (int v = 0; v < V; ++v) dw[v][0] = dw[v][1] = 0.f;
+  int stage = 0, turn = 0;
+  uint32_t masks_from = 0xffffffffu, masks_to = 0;
+  for (long run = blockIdx.x; run < s.runs; run += gridDim.x) {
+    if (s.stages == 3) copies_wait<1>();
+    else copies_wait<0>();
+    __syncthreads();
+    // (the stage before this one was written out before the barrier)
+    fetch(run + (long)(s.stages - 1) * gridDim.x, stage == 0 ? s.stages - 1 : stage - 1);
+    const Run here = Run::of<PER>(s, run);
+    uint32_t first = 0;
+    if (drops) {
+      first = s.drop.per((uint32_t)(run * s.run));
+      const uint32_t last = s.drop.per((uint32_t)(run * s.run + here.rows - 1));
+      if (first != masks_from || last != masks_to) {           // (rows that share a mask find it there)
+        run_mask(s, mask, key, first, last);
+        masks_from = first; masks_to = last;
+        __syncthreads();
+      }
+    }
+    T* const at = reinterpret_cast<T*>(base + stage * bytes) + here.shift;
+    const int apart = s.slot / (int)sizeof(T);
+    for (int r = own; r < s.run; r += s.groups, turn ^= 1) {
+      const bool in = r < here.rows;                           // (of a row that is not there memory holds whatever: nothing of it is kept)
+      const long row = run * s.run + r;
+      T* const x = at + r * s.C;
+      const unsigned char* bits = mask + (drops && in ? s.drop.per((uint32_t)row) - first : 0u) * (uint32_t)s.pitch;
+      if constexpr (!BACK) {
+        float h[V][2], f[V][2], ss = 0.f;
+        pairs.read(x, h);
+        if (a.in[1]) pairs.read(x + apart, f);
+        else
+#pragma unroll
+          for (int v = 0; v < V; ++v) f[v][0] = f[v][1] = 0.f;
+        if (drops) {
+          bool gone[V][2];
+          pairs.gone(bits, gone);
+#pragma unroll
+          for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) h[v][k] = gone[v][k] ? f[v][k] : fmaf(h[v][k], s.drop.scale, f[v][k]);
+        } else {
+#pragma unroll
+          for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) h[v][k] += f[v][k];
+        }
+        if (a.out[1] && in) pairs.write(x + apart, h);
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+          for (int k = 0; k < 2; ++k) ss = fmaf(h[v][k], h[v][k], ss);
+        ss = row_sum(ss, group, sums[turn]);
+        const float rstd = rsqrtf(fmaf(ss, a.inv_c, a.eps));
+        if (in && lane == 0 && a.rstd) a.rstd[row] = rstd;
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+          for (int k = 0; k < 2; ++k) h[v][k] *= rstd * w[v][k];
+        if (in) pairs.write(x, h);
+      } else {
+        float xh[V][2], g[V][2], t = 0.f;
+        const float rstd = in ? __ldg(a.rstd + row) : 0.f;
+        pairs.read(x, xh);
+        pairs.read(x + apart, g);
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            xh[v][k] *= rstd;
+            if (in) dw[v][k] = fmaf(g[v][k], xh[v][k], dw[v][k]);
+            g[v][k] *= w[v][k];
+            t = fmaf(g[v][k], xh[v][k], t);
+          }
+        const float mean = row_sum(t, group, sums[turn]) * a.inv_c;
+        if (a.in[2]) {
+          float d[V][2];
+          pairs.read(x + 2 * apart, d);
+#pragma unroll
+          for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) g[v][k] = fmaf(rstd, fmaf(-xh[v][k], mean, g[v][k]), d[v][k]);
+        } else {
+#pragma unroll
+          for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) g[v][k] = rstd * fmaf(-xh[v][k], mean, g[v][k]);
+        }
+        if (a.out[1] && in) pairs.write(x + apart, g);
+        if (a.out[0]) {
+          if (drops) {
+            bool gone[V][2];
+            pairs.gone(bits, gone);
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+#pragma unroll
+              for (int k = 0; k < 2; ++k) g[v][k] = gone[v][k] ? 0.f : g[v][k] * s.drop.scale;
+          }
+          if (in) pairs.write(x, g);
+        }
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (a.out[i]) run_out<T>(here, base + stage * bytes + i * s.slot, static_cast<T*>(a.out[i]));
+    stage = stage == s.stages - 1 ? 0 : stage + 1;
+  }
+  if (!BACK || !a.part) return;
+  // The block's sums of dw: every group's side by side in shared memory, then column by column in order.
+  copies_wait<0>();
+  __syncthreads();
+  float* const cols = reinterpret_cast<float*>(ring);
+#pragma unroll
+  for (int v = 0; v < V; ++v)
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+      if (pairs.has(v, k)) cols[(size_t)own * s.C + pairs.column + 2 * v * group + k] = dw[v][k];
+  __syncthreads();
+  for (int c = threadIdx.x; c < s.C; c += blockDim.x) {
+    float t = cols[c];
+    for (int i = 1; i < s.groups; ++i) t += cols[(size_t)i * s.C + c];
+    a.part[(size_t)blockIdx.x * s.C + c] = t;
+  }
+}
+
+template <bool BACK>
+cudaError_t launch(const xconv_rows_desc* d, const StagedPlan& p, const StagedArgs& a, cudaStream_t st) {
+  return with_type(d->dtype, [&](auto t) {
+    using T = decltype(t);
+    void (*kernel)(const StagedArgs) = nullptr;
+#define XC_STAGED(N) if (p.V == N) kernel = rms_staged_kernel<T, N, BACK>;
+    XC_STAGED(1) XC_STAGED(2) XC_STAGED(3) XC_STAGED(4) XC_STAGED(5) XC_STAGED(6) XC_STAGED(7) XC_STAGED(8)
+#undef XC_STAGED
+    if (!kernel) return cudaErrorInvalidValue;
+    if (p.smem > 40 * 1024) {
+      // (the same for every size, so that no other thread finds it lowered)
+      const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, STAGED_SMEM);
+      if (e != cudaSuccess) return e;
+    }
+    kernel<<<(unsigned)p.blocks, p.threads, p.smem, st>>>(a);
+    return cudaGetLastError();
+  });
+}
+
+bool is_dense(const xconv_rows_desc* d, const void* p, int64_t stride) { return !p || (stride == d->C && at(p, 16)); }
+
+}  // namespace
+
+bool rms_staged_forward(const xconv_rows_desc* d, const void* X, const void* residual, const void* weight, void* H, void* Y, float* rstd, cudaStream_t st, cudaError_t* e) {
+  if (!is_dense(d, X, d->x_stride) || !is_dense(d, residual, d->r_stride) || !is_dense(d, H, d->h_stride) || !is_dense(d, Y, d->y_stride)) return false;
+  StagedArgs a = {};
+  a.s.drop = drop_of(d);
+  const StagedPlan p = staged_plan(d, residual || H ? 2 : 1, false, &a.s);
+  if (!p.threads) return false;
+  a.in[0] = X; a.in[1] = residual; a.out[0] = Y; a.out[1] = H;
+  a.weight = weight; a.weight_f32 = d->param_dtype == XCONV_F32; a.rstd = rstd; a.eps = d->eps; a.inv_c = 1.f / (float)d->C;
+  *e = launch<false>(d, p, a, st);
+  return true;
+}
+
+long rms_staged_backward_parts(const xconv_rows_desc* d) {
+  Staged s = {};
+  s.drop.how = DROP_HOST;
+  long most = 0;
+  // (fewer tensors need less memory, so that more blocks fit)
+  for (int slots = 2; slots <= 3; ++slots)
+    for (int how : {DROP_NONE, DROP_HOST}) {
+      s.drop.how = how;
+      const StagedPlan p = staged_plan(d, slots, true, &s);
+      if (p.threads) most = std::max(most, p.blocks);
+    }
+  return most;
+}
+
+bool rms_staged_backward(const xconv_rows_desc* d, const void* dY, const void* H, const float* rstd, const void* weight, const void* dH, void* dX, void* dR, float* part, long* parts,
+                         cudaStream_t st, cudaError_t* e) {
+  if (!is_dense(d, dY, d->y_stride) || !is_dense(d, H, d->h_stride) || !is_dense(d, dH, d->dh_stride) || !is_dense(d, dX, d->x_stride) || !is_dense(d, dR, d->r_stride)) return false;
+  StagedArgs a = {};
+  if (dX) a.s.drop = drop_of(d);
+  const StagedPlan p = staged_plan(d, dH ? 3 : 2, true, &a.s);
+  if (!p.threads) return false;
+  a.in[0] = H; a.in[1] = dY; a.in[2] = dH; a.out[0] = dX; a.out[1] = dR;
+  a.weight = weight; a.weight_f32 = d->param_dtype == XCONV_F32; a.rstd = const_cast<float*>(rstd); a.part = part; a.inv_c = 1.f / (float)d->C;
+  *parts = p.blocks;
+  *e = launch<true>(d, p, a, st);
+  return true;
+}
+
+}  // namespace xconv

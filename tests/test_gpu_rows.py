@@ -179,6 +179,21 @@ def e4m3_half_step(v):
     return torch.exp2(e - 4)
 
 
+def check_8_bits(Q, scales, y, y_off, width, M):
+    """Codes and scales of y, of `width` values a scale; returns both in 64 bits."""
+    C = y.shape[1]
+    pad = lambda v: torch.nn.functional.pad(v, (0, -C % width)).reshape(v.shape[0], -1, width)
+    most, most_off = pad(y).abs().amax(-1), pad(y_off).amax(-1)
+    got = R.last(scales)
+    R.close("scales", got, most.clamp(min=2.0 ** -100) / M, (most_off + 2.0 ** -22 * most) / M + 2.0 ** -140)
+    wide, codes = got.repeat_interleave(width, 1)[:, :C], R.last(Q.float())
+    assert float(codes.abs().max()) <= M
+    # the nearest 8-bit value: half a step, where the value before it may be off by what float arithmetic is, and by the product with 1 / scale
+    half = e4m3_half_step(codes) if M == 448.0 else torch.full_like(codes, 0.5)
+    R.close("Q", codes, y / wide, half + y_off / wide + 2.0 ** -21 * (y / wide).abs())
+    return codes, wide
+
+
 @pytest.mark.parametrize("shape,dtype,kind,own_params", cases())
 @pytest.mark.parametrize("q", [torch.float8_e4m3fn, torch.int8])
 @pytest.mark.parametrize("group", [0, 32, 64, 128])
@@ -191,18 +206,9 @@ def test_rmsnorm_in_8_bits(shape, dtype, kind, own_params, q, group):
     (y, h, s), (y_off, h_off, s_off) = R.norm(X, weight, residual, 1e-5)
     R.close("H", R.last(H), h, R.rounded(h, h_off, t))
     R.close("rstd", rstd.cpu().double().reshape(-1), s, s_off + 2.0 ** -23 * s)
-    M = 448.0 if q == torch.float8_e4m3fn else 127.0
     width = group if 0 < group < C else C
-    pad = lambda v: torch.nn.functional.pad(v, (0, -C % width)).reshape(v.shape[0], -1, width)
-    most, most_off = pad(y).abs().amax(-1), pad(y_off).amax(-1)
-    got_scales = R.last(scales)
-    R.close("scales", got_scales, most.clamp(min=2.0 ** -100) / M, (most_off + 2.0 ** -22 * most) / M + 2.0 ** -140)
-    wide = got_scales.repeat_interleave(width, 1)[:, :C]
-    codes = R.last(Q.float())
-    assert Q.dtype == q and Q.shape == X.shape and float(codes.abs().max()) <= M
-    # the nearest 8-bit value: half a step, where the value before it may be off by what float arithmetic is, and by the product with 1 / scale
-    half = e4m3_half_step(codes) if q == torch.float8_e4m3fn else torch.full_like(codes, 0.5)
-    R.close("Q", codes, y / wide, half + y_off / wide + 2.0 ** -21 * (y / wide).abs())
+    codes, wide = check_8_bits(Q, scales, y, y_off, width, 448.0 if q == torch.float8_e4m3fn else 127.0)
+    assert Q.dtype == q and Q.shape == X.shape
     for out in (torch.float32, torch.bfloat16, torch.float16):
         V = xb.xconv_dequantize(Q, scales, group=group, dtype=out)
         want = codes * wide
@@ -262,35 +268,44 @@ def test_no_rows():
 
 @pytest.mark.parametrize("C,gap", [(64, 8), (64, 3), (97, 15), (20000, 4)])
 def test_nothing_is_written_between_the_rows(C, gap):
-    """The library's calls with strided outputs: what lies between the rows and behind the last one stays."""
-    rows, wide = 13, C + gap
-    X, res = tensor((rows, C), torch.bfloat16, 1), tensor((rows, C), torch.bfloat16, 2)
+    """The library's calls with strided outputs: what lies between the rows and behind the last one stays.  (Strided rows may get their sums in another order than dense ones: the results are
+    held to the formulas, as everywhere.)"""
+    rows, wide, t = 13, C + gap, torch.bfloat16
+    X, res = tensor((rows, C), t, 1), tensor((rows, C), t, 2)
     fresh = lambda dtype=torch.bfloat16: torch.full((rows + 2, wide), 7, device="cuda", dtype=dtype)
     outside = lambda t: bool((t[rows:] == 7).all()) and bool((t[:, C:] == 7).all())
     d = xb.RowsDesc(rows=rows, C=C, dtype=xb.XCONV_BF16, eps=1e-5, x_stride=C, r_stride=C, h_stride=wide, dh_stride=C, y_stride=wide, p=0.25, seed=9, rows_per_mask=1)
     call = lambda name, *a: xb._check(getattr(xb.lib(), name)(ctypes.byref(d), *[t.data_ptr() if isinstance(t, torch.Tensor) else t for t in a], xb._stream()), name)
     Y, H, rstd = fresh(), fresh(), torch.full((rows + 2,), 7.0, device="cuda")
     call("xconv_rmsnorm_forward", X, res, None, H, Y, None, rstd)
-    want = xb.xconv_rmsnorm(X, residual=res, eps=1e-5, p=0.25, seed=9)
-    assert torch.equal(Y[:rows, :C], want[0]) and torch.equal(H[:rows, :C], want[1]) and torch.equal(rstd[:rows], want[2])
+    (y, h, s), (y_off, h_off, s_off) = R.norm(X, None, res, 1e-5, 0.25, 9)
+    R.close("Y", R.last(Y[:rows, :C]), y, R.rounded(y, y_off, t))
+    R.close("H", R.last(H[:rows, :C]), h, R.rounded(h, h_off, t))
+    R.close("rstd", rstd[:rows].cpu().double(), s, s_off + 2.0 ** -23 * s)
     assert outside(Y) and outside(H) and bool((rstd[rows:] == 7).all())
-    call("xconv_dropout", X, res, Y)
-    assert torch.equal(Y[:rows, :C], xb.xconv_dropout(X, 0.25, 9, residual=res)) and outside(Y)
+    drop = fresh()
+    call("xconv_dropout", X, res, drop)
+    R.close("dropout", R.last(drop[:rows, :C]), h, R.rounded(h, h_off, t))
+    assert outside(drop)
     d.q_type, d.q_group = xb.XCONV_Q_INT8, 32
-    Q, scales = fresh(torch.int8), torch.full((rows * -(-C // 32) + 5,), 7.0, device="cuda")
-    call("xconv_rmsnorm_forward", X, res, None, H, Q, scales, rstd)
-    q = xb.xconv_rmsnorm_quantized(X, residual=res, eps=1e-5, qdtype=torch.int8, group=32, p=0.25, seed=9)
-    assert torch.equal(Q[:rows, :C], q[0]) and torch.equal(scales[:-5], q[1].flatten()) and outside(Q) and outside(H) and bool((scales[-5:] == 7).all())
+    Q, scales, again = fresh(torch.int8), torch.full((rows * -(-C // 32) + 5,), 7.0, device="cuda"), fresh()
+    call("xconv_rmsnorm_forward", X, res, None, again, Q, scales, rstd)
+    check_8_bits(Q[:rows, :C], scales[:-5].view(rows, -1), y, y_off, 32, 127.0)
+    assert outside(Q) and outside(again) and bool((scales[-5:] == 7).all())
     d.x_stride = wide
     V = fresh()
     call("xconv_dequantize", Q, scales, V)
-    assert torch.equal(V[:rows, :C], xb.xconv_dequantize(q[0], q[1], group=32)) and outside(V)
+    want = R.last(Q[:rows, :C].float()) * R.last(scales[:-5].view(rows, -1)).repeat_interleave(32, 1)[:, :C]
+    R.close("V", R.last(V[:rows, :C]), want, R.rounded(want, 0 * want, t))
+    assert outside(V)
     d.r_stride = wide
     dX, dR, dw = fresh(), fresh(), torch.full((C + 8,), 7.0, device="cuda")
     ws = torch.empty(xb.lib().xconv_rmsnorm_workspace_bytes(ctypes.byref(d)), dtype=torch.uint8, device="cuda")
     call("xconv_rmsnorm_backward", Y, H, rstd, None, res, dX, dR, dw, ws, ws.numel())
-    back = xb.xconv_rmsnorm_backward(Y[:rows, :C], H[:rows, :C], rstd[:rows].contiguous(), dH=res, p=0.25, seed=9)
-    assert torch.equal(dX[:rows, :C], back[0]) and torch.equal(dR[:rows, :C], back[1]) and torch.equal(dw[:C], back[2])
+    (dx, dr, dweight), (x_off, r_off, w_off) = R.norm_backward(Y[:rows, :C], H[:rows, :C], rstd[:rows], None, res, 0.25, 9)
+    R.close("dX", R.last(dX[:rows, :C]), dx, R.rounded(dx, x_off, t))
+    R.close("dresidual", R.last(dR[:rows, :C]), dr, R.rounded(dr, r_off, t))
+    R.close("dweight", dw[:C].cpu().double(), dweight, w_off)
     assert outside(dX) and outside(dR) and bool((dw[C:] == 7).all())
 
 
