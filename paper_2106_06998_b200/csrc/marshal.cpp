@@ -11,6 +11,7 @@
 #include <torch/csrc/utils/object_ptr.h>
 
 #include <ATen/ATen.h>
+#include <ATen/cuda/EmptyTensor.h>
 #include <ATen/PythonTorchFunctionTLS.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/cuda/CUDAGraphsC10Utils.h>
@@ -573,11 +574,17 @@ bool group_of(PyObject* o, int32_t* group) {
 }
 int64_t groups_of(int64_t C, int32_t group) { return group > 0 && group < C ? (C + group - 1) / group : 1; }
 int q_code(at::ScalarType t) { return t == at::kFloat8_e4m3fn ? XCONV_Q_E4M3 : t == at::kChar ? XCONV_Q_INT8 : XCONV_Q_NONE; }
-at::Tensor dense_like(const at::Tensor& t, at::ScalarType type, int64_t C) {
-  const auto fmt = t.dim() == 4 ? at::MemoryFormat::ChannelsLast : t.dim() == 5 ? at::MemoryFormat::ChannelsLast3d : at::MemoryFormat::Contiguous;
-  std::vector<int64_t> sizes = t.sizes().vec();
+// Outputs straight from the allocator: through the dispatcher each takes half a microsecond more, and a call on few rows is little else.
+at::Tensor fresh(at::IntArrayRef sizes, at::ScalarType type, const at::Tensor& like, at::MemoryFormat fmt) { return at::detail::empty_cuda(sizes, type, like.device(), fmt); }
+at::MemoryFormat format_of(const at::Tensor& t) {
+  return t.dim() == 4 ? at::MemoryFormat::ChannelsLast : t.dim() == 5 ? at::MemoryFormat::ChannelsLast3d : at::MemoryFormat::Contiguous;
+}
+at::Tensor fresh_like(const at::Tensor& t) { return fresh(t.sizes(), t.scalar_type(), t, format_of(t)); }
+at::Tensor fresh_like(const at::Tensor& t, at::ScalarType type, int64_t C) {
+  int64_t sizes[5];
+  std::copy(t.sizes().begin(), t.sizes().end(), sizes);
   sizes[t.dim() >= 4 ? 1 : t.dim() - 1] = C;
-  return at::empty(sizes, t.options().dtype(type).requires_grad(false), fmt);
+  return fresh(at::IntArrayRef(sizes, (size_t)t.dim()), type, t, format_of(t));
 }
 
 // dropout(X, p, seed, residual, channels) -> Y
@@ -590,7 +597,7 @@ PyObject* dropout(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   if (C > INT32_MAX) Py_RETURN_NONE;
   xconv_rows_desc d = rows_desc(*X, C, dtype_code(*X), -1);
   if (!mask_of(a[1], a[2], a[4], shape, &d)) Py_RETURN_NONE;
-  const at::Tensor Y = dense_like(*X);
+  const at::Tensor Y = fresh_like(*X);
   const cudaStream_t stream = c10::cuda::getCurrentCUDAStream().stream();
   const void *x = X->data_ptr(), *r = address(R);
   const xconv_status s = unlocked([&] { return rows_lib.dropout(&d, x, r, Y.data_ptr(), stream); });
@@ -615,13 +622,13 @@ Normed norm_rows(PyObject* const* a, PyObject* p, PyObject* seed, PyObject* chan
   float* scales = nullptr;
   if (group >= 0) {
     d.q_type = q_code(y); d.q_group = group;
-    n.scales = dense_like(*X, at::kFloat, groups_of(C, group));
+    n.scales = fresh_like(*X, at::kFloat, groups_of(C, group));
     scales = (float*)n.scales.data_ptr();
   }
-  n.Y = dense_like(*X, group >= 0 ? y : X->scalar_type(), C);
-  n.rstd = at::empty(shape, X->options().dtype(at::kFloat).requires_grad(false));
+  n.Y = fresh_like(*X, group >= 0 ? y : X->scalar_type(), C);
+  n.rstd = fresh(shape, at::kFloat, *X, at::MemoryFormat::Contiguous);
   const bool sum = R || d.p > 0.0;
-  n.H = sum ? dense_like(*X) : *X;
+  n.H = sum ? fresh_like(*X) : *X;
   const cudaStream_t stream = c10::cuda::getCurrentCUDAStream().stream();
   const void *x = X->data_ptr(), *r = address(R), *wp = address(w);
   void *h = sum ? n.H.data_ptr() : nullptr, *yp = n.Y.data_ptr();
@@ -668,7 +675,7 @@ PyObject* rmsnorm_backward(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   xconv_rows_desc d = rows_desc(*H, C, dtype_code(*H), code);
   if (!mask_of(a[5], a[6], a[7], shape, &d)) Py_RETURN_NONE;
   const bool two = d.p > 0.0;
-  const at::Tensor dX = dense_like(*H), dR = two ? dense_like(*H) : dX, dw = at::empty({C}, H->options().dtype(at::kFloat).requires_grad(false));
+  const at::Tensor dX = fresh_like(*H), dR = two ? fresh_like(*H) : dX, dw = fresh({C}, at::kFloat, *H, at::MemoryFormat::Contiguous);
   const cudaStream_t stream = c10::cuda::getCurrentCUDAStream().stream();
   const at::Tensor ws = scratch(rows_lib.rms_workspace_bytes(&d), *H, stream);
   const void *dy = dY->data_ptr(), *h = H->data_ptr(), *wp = address(w), *dh = address(dH);
@@ -697,7 +704,7 @@ PyObject* dequantize(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   if (scales->scalar_type() != at::kFloat || scales->sizes() != at::IntArrayRef(want) || scales->device() != Q->device()) Py_RETURN_NONE;
   xconv_rows_desc d = rows_desc(*Q, C, dtype, -1);
   d.q_type = q_code(Q->scalar_type()); d.q_group = group;
-  const at::Tensor X = dense_like(*Q, type, C);
+  const at::Tensor X = fresh_like(*Q, type, C);
   const cudaStream_t stream = c10::cuda::getCurrentCUDAStream().stream();
   const void* q = Q->data_ptr();
   const float* f = (const float*)scales->data_ptr();

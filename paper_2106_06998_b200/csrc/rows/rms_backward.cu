@@ -64,7 +64,7 @@ __device__ __forceinline__ void write_out(const RmsBackArgs& a, uint2 key, unsig
 
 template <typename T, int V, bool VEC, int DROP>
 __global__ void __launch_bounds__(512) rms_backward_kernel(const RmsBackArgs a) {
-  extern __shared__ float cols[];                            // C floats a warp, in a block of several groups
+  extern __shared__ __align__(16) float cols[];                            // C floats a warp, in a block of several groups
   __shared__ float sums[2][32];
   const int group = a.group, lane = group <= 32 ? threadIdx.x & (group - 1) : threadIdx.x;
   const int groups = group <= 32 ? blockDim.x / group : 1, own = group <= 32 ? threadIdx.x / group : 0;
@@ -117,6 +117,7 @@ __global__ void __launch_bounds__(512) rms_backward_kernel(const RmsBackArgs a) 
       write_out<T, VEC, DROP>(a, key, block, dr.out(), dx.out(), d[v], k, in && k < a.octets, rstd, mean, xh[v], g[v]);
     }
   }
+  pdl_trigger();
   if (!a.part) return;
   // The groups of a warp by shuffles, the warps side by side in shared memory, then column by column in order.
   for (int o = group; o < 32; o <<= 1)
@@ -129,12 +130,18 @@ __global__ void __launch_bounds__(512) rms_backward_kernel(const RmsBackArgs a) 
   float* to = several ? cols + warp * a.C : a.part + (size_t)blockIdx.x * a.C;
   if ((threadIdx.x & 31) < group)
 #pragma unroll
-    for (int v = 0; v < V; ++v)
+    for (int v = 0; v < V; ++v) {
+      const int c = 8 * (lane + v * group);
+      if (VEC && a.C % 4 == 0) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int c = 8 * (lane + v * group) + e;
-        if (c < a.C) to[c] = dw[v][e];
+        for (int e = 0; e < 8; e += 4)
+          if (c + e < a.C) *reinterpret_cast<float4*>(to + c + e) = make_float4(dw[v][e], dw[v][e + 1], dw[v][e + 2], dw[v][e + 3]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (c + e < a.C) to[c + e] = dw[v][e];
       }
+    }
   if (!several) return;
   __syncthreads();
   for (int c = threadIdx.x; c < a.C; c += blockDim.x) {
@@ -193,49 +200,78 @@ __global__ void __launch_bounds__(256) rms_columns_kernel(const RmsBackArgs a, l
   a.part[(size_t)blockIdx.y * a.C + c] = dw;
 }
 
-// Columns' sums over the parts, 32 columns a block: each of its warps adds every 32nd part, then the warps' sums are added in order.  (No parts: zeros.)
-__global__ void __launch_bounds__(1024) rms_sums_kernel(const float* part, int parts, int C, float* dweight) {
-  __shared__ float sums[32][33];
+// Columns' sums over the parts: 16 columns a block (VEC: four a thread), of which every thread adds every GROUPS-th part -- all loads in flight at once up to 640 parts: this
+// kernel is a chain of waits for L2 -- then the threads' sums are added in order.  (No parts: zeros.)
+template <bool VEC>
+__global__ void __launch_bounds__(256) rms_sums_kernel(const float* part, int parts, int C, float* dweight) {
+  constexpr int EACH = VEC ? 4 : 1, LANES = 16 / EACH, GROUPS = 256 / LANES, DEEP = VEC ? 10 : 20;
+  __shared__ float sums[GROUPS][17];
+  const int lane = threadIdx.x % LANES, g = threadIdx.x / LANES, c = blockIdx.x * 16 + lane * EACH;
+  float own[EACH];
+#pragma unroll
+  for (int e = 0; e < EACH; ++e) own[e] = 0.f;
   pdl_wait();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const long c = (long)blockIdx.x * 32 + lane;
-  float own[4] = {0.f, 0.f, 0.f, 0.f};
-  if (c < C) sum_splits<32, 4, 4>(part + c, (size_t)C, warp, parts, own);
-  sums[warp][lane] = (own[0] + own[1]) + (own[2] + own[3]);
+  if (c < C)
+    for (int first = g; first < parts; first += GROUPS * DEEP) {
+      float v[DEEP][EACH];
+#pragma unroll
+      for (int i = 0; i < DEEP; ++i) {
+        const int n = first + i * GROUPS;
+        const float* at = part + (size_t)n * C + c;
+        if constexpr (VEC) {
+          const float4 t = n < parts ? __ldcg(reinterpret_cast<const float4*>(at)) : make_float4(0.f, 0.f, 0.f, 0.f);
+          v[i][0] = t.x; v[i][1] = t.y; v[i][2] = t.z; v[i][3] = t.w;
+        } else {
+          v[i][0] = n < parts ? __ldcg(at) : 0.f;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < DEEP; ++i)
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) own[e] += v[i][e];
+    }
+#pragma unroll
+  for (int e = 0; e < EACH; ++e) sums[g][lane * EACH + e] = own[e];
   __syncthreads();
-  float s = sums[lane][warp];                                // (column `warp` of the block's 32)
-  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-  const long col = (long)blockIdx.x * 32 + warp;
-  if (lane == 0 && col < C) dweight[col] = s;
+  // 16 threads a column
+  const int col = threadIdx.x >> 4, t = threadIdx.x & 15;
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < GROUPS / 16; ++i) s += sums[t + 16 * i][col];
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  if (t == 0 && blockIdx.x * 16 + col < C) dweight[blockIdx.x * 16 + col] = s;
 }
 
 // Rows that a block of rms_columns_kernel adds, at least, and partial sums at most.
 constexpr long WIDE_ROWS = 64, WIDE_PARTS = 512;
 
 struct Plan { Team team; long blocks, parts; };
-Plan plan_of(const xconv_rows_desc* d) {
+Plan plan_of(const xconv_rows_desc* d, bool vec) {
   Plan p = {};
-  p.team = team_of((d->C + 7) / 8);
-  p.blocks = std::min((d->rows + p.team.groups - 1) / p.team.groups, (long)ROWS_SMS * std::max(1, 512 / p.team.threads));
+  p.team = team_of((d->C + 7) / 8, d->dtype == XCONV_F32 || !vec);
+  // (at most: 1024 threads of an SM)
+  p.blocks = std::min((d->rows + p.team.groups - 1) / p.team.groups, (long)ROWS_SMS * std::max(1, 1024 / p.team.threads));
   p.parts = p.team.V ? p.blocks : std::min((d->rows + WIDE_ROWS - 1) / WIDE_ROWS, WIDE_PARTS);
   return p;
 }
 
 }  // namespace
 
-size_t rms_backward_part_bytes(const xconv_rows_desc* d) { return (size_t)std::max(plan_of(d).parts, rms_staged_backward_parts(d)) * (size_t)d->C * sizeof(float); }
+size_t rms_backward_part_bytes(const xconv_rows_desc* d) { return (size_t)std::max({plan_of(d, true).parts, plan_of(d, false).parts, rms_staged_backward_parts(d)}) * (size_t)d->C * sizeof(float); }
 
 cudaError_t launch_rms_backward(const xconv_rows_desc* d, const void* dY, const void* H, const float* rstd, const void* weight, const void* dH, void* dX, void* dR,
                                 float* dweight, float* part, cudaStream_t st, int* launches) {
-  const Plan p = plan_of(d);
   RmsBackArgs a = {};
   const size_t es = d->dtype == XCONV_F32 ? 4 : 2;
   a.dY = rows_of(dY, d->rows, d->C, d->y_stride, es); a.H = rows_of(H, d->rows, d->C, d->h_stride, es); a.dH = rows_of(dH, d->rows, d->C, d->dh_stride, es);
   a.dX = rows_of(dX, d->rows, d->C, d->x_stride, es); a.dR = rows_of(dR, d->rows, d->C, d->r_stride, es);
   a.rstd = rstd; a.w = {weight, d->param_dtype == XCONV_F32}; a.part = part;
-  a.rows = d->rows; a.C = d->C; a.octets = (d->C + 7) / 8; a.group = p.team.group; a.inv_c = 1.f / (float)d->C;
+  a.rows = d->rows; a.C = d->C; a.octets = (d->C + 7) / 8; a.inv_c = 1.f / (float)d->C;
   a.drop = drop_of(d);
   const bool vec = d->C % (16 / es) == 0 && whole(a.dY, 16) && whole(a.H, 16) && whole(a.dH, 16) && whole(a.dX, 16) && whole(a.dR, 16) && at(weight, 16);
+  const Plan p = plan_of(d, vec);
+  a.group = p.team.group;
   long parts = p.parts;
   if (d->rows > 0) {
     cudaError_t e;
@@ -251,7 +287,9 @@ cudaError_t launch_rms_backward(const xconv_rows_desc* d, const void* dY, const 
         };
         const auto kernel = with_kinds(vec, a.dX.p ? a.drop.how : DROP_NONE, pick);
         const size_t smem = V && part && p.team.group <= 32 ? (size_t)(p.team.threads / 32) * d->C * sizeof(float) : 0;
-        kernel<<<(unsigned)p.blocks, p.team.threads, smem, st>>>(a);
+        const long blocks = std::min(p.blocks, (long)ROWS_SMS * resident_blocks(kernel, p.team.threads, (int)smem));
+        if (V) parts = blocks;
+        kernel<<<(unsigned)blocks, p.team.threads, smem, st>>>(a);
         ++*launches;
       }
       if (!V && part) {
@@ -264,7 +302,7 @@ cudaError_t launch_rms_backward(const xconv_rows_desc* d, const void* dY, const 
   }
   if (!dweight) return cudaSuccess;
   ++*launches;
-  return launch_pdl(rms_sums_kernel, dim3((unsigned)((d->C + 31) / 32)), dim3(1024), 0, st, (const float*)part, (int)parts, (int)d->C, dweight);
+  return launch_pdl(d->C % 4 == 0 ? rms_sums_kernel<true> : rms_sums_kernel<false>, dim3((unsigned)((d->C + 15) / 16)), dim3(256), 0, st, (const float*)part, (int)parts, (int)d->C, dweight);
 }
 
 }  // namespace xconv

@@ -17,7 +17,7 @@ struct RmsArgs {
   float *scales, *rstd;
   long rows;
   int C, octets, group;
-  int q, q_group, q_groups;        // 8 bits: the type, values of a scale (0: the row), scales of a row
+  int q, q_group, q_shift, q_groups;       // 8 bits: the type, values of a scale (2^q_shift, or 0: the row), scales of a row
   float eps, inv_c;
   Drop drop;
 };
@@ -26,24 +26,33 @@ struct RmsArgs {
 
 constexpr float Q_LEAST = 7.888609052210118e-31f;          // 2^-100
 
-__device__ __forceinline__ float q_largest(int q) { return q == XCONV_Q_E4M3 ? 448.f : 127.f; }
-__device__ __forceinline__ uint32_t magnitude(const float (&y)[8]) {
-  uint32_t m = 0;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) m = max(m, __float_as_uint(y[e]) & 0x7fffffffu);
-  return m;
+// The largest magnitude, NaN above all.
+__device__ __forceinline__ float most_of(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
 }
-// The scale of values up to `most` (as bits: infinities and NaN stay what they are).
-__device__ __forceinline__ float q_scale(uint32_t most, int q) {
-  const float a = __uint_as_float(most);
-  return (a < Q_LEAST ? Q_LEAST : a) / q_largest(q);
+__device__ __forceinline__ float magnitude(const float (&y)[8]) {
+  float m[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) m[e] = most_of(fabsf(y[e]), fabsf(y[e + 4]));
+  return most_of(most_of(m[0], m[1]), most_of(m[2], m[3]));
+}
+// The scale of values up to a, and what they are multiplied by: the nearest floats but one, by a reciprocal within an ulp.  (NaN where a is not finite.)
+struct Scale { float scale, inv; };
+__device__ __forceinline__ Scale q_scale(float a, int q) {
+  const float M = q == XCONV_Q_E4M3 ? 448.f : 127.f, least = a < Q_LEAST ? Q_LEAST : a;
+  float r;
+  asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(least));
+  return {fmaf(least, q == XCONV_Q_E4M3 ? 1.f / 448.f : 1.f / 127.f, 0.f * least), M * r};
 }
 __device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
   unsigned short r;
   asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
   return r;
 }
-__device__ __forceinline__ uint32_t int8(float v) { return (uint32_t)max(-127, min(127, __float2int_rn(v))) & 0xffu; }
+// The nearest whole number of y * inv, at most 127 (and a little) in magnitude, in the low byte: added to 3 * 2^22, where a float's last place is one.
+__device__ __forceinline__ uint32_t int8(float y, float inv) { return __float_as_uint(fmaf(y, inv, 12582912.f)); }
 template <bool VEC>
 __device__ __forceinline__ void store8q(unsigned char* row, int c, int C, bool in, const float (&y)[8], float inv, int q) {
   uint32_t b[2];
@@ -51,14 +60,28 @@ __device__ __forceinline__ void store8q(unsigned char* row, int c, int C, bool i
   for (int i = 0; i < 2; ++i) {
     const float* v = y + 4 * i;
     b[i] = q == XCONV_Q_E4M3 ? e4m3x2(v[0] * inv, v[1] * inv) | e4m3x2(v[2] * inv, v[3] * inv) << 16
-                             : int8(v[0] * inv) | int8(v[1] * inv) << 8 | int8(v[2] * inv) << 16 | int8(v[3] * inv) << 24;
+                             : __byte_perm(__byte_perm(int8(v[0], inv), int8(v[1], inv), 0x0040), __byte_perm(int8(v[2], inv), int8(v[3], inv), 0x0040), 0x5410);
   }
   store8<unsigned char, VEC>(row, c, C, in, b);
 }
-// The scale of this lane's octet, whose largest magnitude is m (of its group of `width` values, which neighbouring lanes hold).
-__device__ __forceinline__ uint32_t group_most(uint32_t m, int width) {
-  for (int o = width >> 4; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+// The largest magnitude of the `width` values of which this lane and its neighbours hold an octet each.
+__device__ __forceinline__ float group_most(float m, int width) {
+  for (int o = width >> 4; o > 0; o >>= 1) m = most_of(m, __shfl_xor_sync(0xffffffffu, m, o));
   return m;
+}
+// (over the threads of a row, as row_sum)
+__device__ __forceinline__ float row_most(float v, int group, float* buf) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1)
+    if (o < group) v = most_of(v, __shfl_xor_sync(0xffffffffu, v, o));
+  if (group <= 32) return v;
+  const int lane = threadIdx.x & 31;
+  if (lane == 0) buf[threadIdx.x >> 5] = v;
+  __syncthreads();
+  v = lane < (group >> 5) ? buf[lane] : 0.f;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v = most_of(v, __shfl_xor_sync(0xffffffffu, v, o));
+  return v;
 }
 
 // The octet of h from what was fetched of x and r.
@@ -85,7 +108,7 @@ __device__ __forceinline__ void sum_of(const RmsArgs& a, uint2 key, unsigned lon
 template <typename T, int V, bool VEC, bool Q, int DROP>
 __global__ void __launch_bounds__(512) rms_forward_kernel(const RmsArgs a) {
   __shared__ float sums[2][32];
-  __shared__ uint32_t most[2][32];
+  __shared__ float most[2][32];
   typedef std::conditional_t<Q, unsigned char, T> Y;
   const int group = a.group, lane = group <= 32 ? threadIdx.x & (group - 1) : threadIdx.x;
   const int groups = group <= 32 ? blockDim.x / group : 1, own = group <= 32 ? threadIdx.x / group : 0;
@@ -138,7 +161,7 @@ __global__ void __launch_bounds__(512) rms_forward_kernel(const RmsArgs a) {
       if constexpr (!Q) store8<T, VEC>(ys.out(), 8 * k, a.C, in && k < a.octets, h[v]);
     }
     if constexpr (Q) {
-      uint32_t m[V];
+      float m[V];
 #pragma unroll
       for (int v = 0; v < V; ++v) m[v] = magnitude(h[v]);
       if (a.q_group) {
@@ -146,8 +169,8 @@ __global__ void __launch_bounds__(512) rms_forward_kernel(const RmsArgs a) {
         for (int v = 0; v < V; ++v) m[v] = group_most(m[v], a.q_group);
       } else {
 #pragma unroll
-        for (int v = 1; v < V; ++v) m[0] = max(m[0], m[v]);
-        m[0] = row_max(m[0], group, most[turn]);
+        for (int v = 1; v < V; ++v) m[0] = most_of(m[0], m[v]);
+        m[0] = row_most(m[0], group, most[turn]);
 #pragma unroll
         for (int v = 1; v < V; ++v) m[v] = m[0];
       }
@@ -155,9 +178,9 @@ __global__ void __launch_bounds__(512) rms_forward_kernel(const RmsArgs a) {
       for (int v = 0; v < V; ++v) {
         const int k = lane + v * group;
         const bool here = in && k < a.octets;
-        const float scale = q_scale(m[v], a.q);
-        if (here && (a.q_group ? (8 * k) % a.q_group == 0 : k == 0)) a.scales[row * a.q_groups + (a.q_group ? 8 * k / a.q_group : 0)] = scale;
-        store8q<VEC>(ys.out(), 8 * k, a.C, here, h[v], 1.f / scale, a.q);
+        const Scale f = q_scale(m[v], a.q);
+        if (here && (a.q_group ? (8 * k & (a.q_group - 1)) == 0 : k == 0)) a.scales[row * a.q_groups + (a.q_group ? 8 * k >> a.q_shift : 0)] = f.scale;
+        store8q<VEC>(ys.out(), 8 * k, a.C, here, h[v], f.inv, a.q);
       }
     }
   }
@@ -168,7 +191,7 @@ __global__ void __launch_bounds__(512) rms_forward_kernel(const RmsArgs a) {
 template <typename T, bool VEC, int DROP>
 __global__ void __launch_bounds__(1024) rms_forward_wide_kernel(const RmsArgs a) {
   __shared__ float sums[2][32];
-  __shared__ uint32_t most[2][32];
+  __shared__ float most[2][32];
   const uint2 key = a.drop.key<DROP>();
   const int steps = (a.octets + 1023) / 1024;
   int turn = 0;
@@ -199,13 +222,13 @@ __global__ void __launch_bounds__(1024) rms_forward_wide_kernel(const RmsArgs a)
 #pragma unroll
       for (int e = 0; e < 8; ++e) y[e] *= rstd * w[e];
     };
-    uint32_t m = 0;
+    float m = 0.f;
     if (a.q && !a.q_group) {
       for (int v = 0; v < steps; ++v) {
         normed(threadIdx.x + v * 1024);
-        m = max(m, magnitude(y));
+        m = most_of(m, magnitude(y));
       }
-      m = row_max(m, 1024, most[turn]);
+      m = row_most(m, 1024, most[turn]);
     }
     for (int v = 0; v < steps; ++v) {
       const int k = threadIdx.x + v * 1024;
@@ -216,9 +239,9 @@ __global__ void __launch_bounds__(1024) rms_forward_wide_kernel(const RmsArgs a)
         continue;
       }
       if (a.q_group) m = group_most(magnitude(y), a.q_group);
-      const float scale = q_scale(m, a.q);
-      if (here && (a.q_group ? (8 * k) % a.q_group == 0 : k == 0)) a.scales[row * a.q_groups + (a.q_group ? 8 * k / a.q_group : 0)] = scale;
-      store8q<VEC>(const_cast<unsigned char*>(row_of<unsigned char>(a.Y, row)), 8 * k, a.C, here, y, 1.f / scale, a.q);
+      const Scale f = q_scale(m, a.q);
+      if (here && (a.q_group ? (8 * k & (a.q_group - 1)) == 0 : k == 0)) a.scales[row * a.q_groups + (a.q_group ? 8 * k >> a.q_shift : 0)] = f.scale;
+      store8q<VEC>(const_cast<unsigned char*>(row_of<unsigned char>(a.Y, row)), 8 * k, a.C, here, y, f.inv, a.q);
     }
   }
 }
@@ -234,11 +257,12 @@ cudaError_t launch_rms_forward(const xconv_rows_desc* d, const void* X, const vo
   a.w = {weight, d->param_dtype == XCONV_F32}; a.scales = scales; a.rstd = rstd;
   a.rows = d->rows; a.C = d->C; a.octets = (d->C + 7) / 8; a.eps = d->eps; a.inv_c = 1.f / (float)d->C;
   a.q = d->q_type; a.q_group = d->q_group < d->C ? d->q_group : 0; a.q_groups = a.q_group ? (d->C + a.q_group - 1) / a.q_group : 1;
+  while (a.q_group >> a.q_shift > 1) ++a.q_shift;
   a.drop = drop_of(d);
   const bool vec = d->C % (a.q ? 8 : 16 / es) == 0 && whole(a.X, 16) && whole(a.R, 16) && whole(a.H, 16) && whole(a.Y, a.q ? 8 : 16) && at(weight, 16);
   cudaError_t e;
   if (!vec && !a.q && rms_staged_forward(d, X, residual, weight, H, Y, rstd, st, &e)) return e;
-  const Team p = team_of(a.octets);
+  const Team p = team_of(a.octets, !vec);
   a.group = p.group;
   const long blocks = std::min((d->rows + p.groups - 1) / p.groups, (long)ROWS_SMS * std::max(1, 2048 / p.threads));
   return with_type(d->dtype, [&](auto t) {

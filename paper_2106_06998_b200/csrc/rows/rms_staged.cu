@@ -153,6 +153,7 @@ __global__ void __launch_bounds__(512, V <= 4 ? 2 : 1) rms_staged_kernel(const S
     stage = stage == s.stages - 1 ? 0 : stage + 1;
   }
   if (!BACK || !a.part) return;
+  pdl_trigger();
   // The block's sums of dw: every group's side by side in shared memory, then column by column in order.
   copies_wait<0>();
   __syncthreads();
@@ -189,12 +190,14 @@ cudaError_t launch(const xconv_rows_desc* d, const StagedPlan& p, const StagedAr
   });
 }
 
+// (rows of whole pieces never come here, whatever their pointers: the scratch memory of a call is known by its sizes)
+bool is_odd(const xconv_rows_desc* d) { return d->C % (d->dtype == XCONV_F32 ? 4 : 8) != 0; }
 bool is_dense(const xconv_rows_desc* d, const void* p, int64_t stride) { return !p || (stride == d->C && at(p, 16)); }
 
 }  // namespace
 
 bool rms_staged_forward(const xconv_rows_desc* d, const void* X, const void* residual, const void* weight, void* H, void* Y, float* rstd, cudaStream_t st, cudaError_t* e) {
-  if (!is_dense(d, X, d->x_stride) || !is_dense(d, residual, d->r_stride) || !is_dense(d, H, d->h_stride) || !is_dense(d, Y, d->y_stride)) return false;
+  if (!is_odd(d) || !is_dense(d, X, d->x_stride) || !is_dense(d, residual, d->r_stride) || !is_dense(d, H, d->h_stride) || !is_dense(d, Y, d->y_stride)) return false;
   StagedArgs a = {};
   a.s.drop = drop_of(d);
   const StagedPlan p = staged_plan(d, residual || H ? 2 : 1, false, &a.s);
@@ -207,8 +210,8 @@ bool rms_staged_forward(const xconv_rows_desc* d, const void* X, const void* res
 
 long rms_staged_backward_parts(const xconv_rows_desc* d) {
   Staged s = {};
-  s.drop.how = DROP_HOST;
   long most = 0;
+  if (!is_odd(d)) return 0;
   // (fewer tensors need less memory, so that more blocks fit)
   for (int slots = 2; slots <= 3; ++slots)
     for (int how : {DROP_NONE, DROP_HOST}) {
@@ -221,7 +224,7 @@ long rms_staged_backward_parts(const xconv_rows_desc* d) {
 
 bool rms_staged_backward(const xconv_rows_desc* d, const void* dY, const void* H, const float* rstd, const void* weight, const void* dH, void* dX, void* dR, float* part, long* parts,
                          cudaStream_t st, cudaError_t* e) {
-  if (!is_dense(d, dY, d->y_stride) || !is_dense(d, H, d->h_stride) || !is_dense(d, dH, d->dh_stride) || !is_dense(d, dX, d->x_stride) || !is_dense(d, dR, d->r_stride)) return false;
+  if (!is_odd(d) || !is_dense(d, dY, d->y_stride) || !is_dense(d, H, d->h_stride) || !is_dense(d, dH, d->dh_stride) || !is_dense(d, dX, d->x_stride) || !is_dense(d, dR, d->r_stride)) return false;
   StagedArgs a = {};
   if (dX) a.s.drop = drop_of(d);
   const StagedPlan p = staged_plan(d, dH ? 3 : 2, true, &a.s);

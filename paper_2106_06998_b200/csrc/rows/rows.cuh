@@ -325,19 +325,6 @@ __device__ __forceinline__ float row_sum(float v, int group, float* buf) {
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
 }
-// (of magnitudes by their bits: a NaN is above all)
-__device__ __forceinline__ uint32_t row_max(uint32_t v, int group, uint32_t* buf) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1)
-    if (o < group) v = max(v, __shfl_xor_sync(0xffffffffu, v, o));
-  if (group <= 32) return v;
-  const int lane = threadIdx.x & 31;
-  if (lane == 0) buf[threadIdx.x >> 5] = v;
-  __syncthreads();
-  v = lane < (group >> 5) ? buf[lane] : 0u;
-  return __reduce_max_sync(0xffffffffu, v);
-}
-
 // ---- host side
 
 // The rows of a tensor of `size` bytes a value.
@@ -350,21 +337,22 @@ inline bool whole(const Rows& t, size_t a) { return !t.p || (reinterpret_cast<ui
 inline bool at(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 inline int pow2_from(long n) { int p = 1; while (p < n) p *= 2; return p; }
 
-// Threads a row and octets a thread: up to 32 octets one each, up to 64 two each of a warp, which meets no barrier; beyond, in a block of its own, one or two each,
-// whichever leaves fewer threads without an octet, and two where that is the same (half the warps at a barrier, and what threads keep beside their octets once for two).
+// Threads a row and octets a thread.  Two octets a thread: what it keeps beside them once for two, half the steps of a sum over the row, and twice the bytes on their way (gradients of
+// 131072 x 128 bf16 24 us, with one 30; of 8192 x 4096 48 us, with one 63).  One, where two of floats with all their companions do not fit the registers (`one`: gradients of 131072 x 64
+// floats 23 us, with two 26) or octets have to be in neighbouring lanes (rows at any alignment), or more threads would go without.  Rows of up to 64 octets take part of a warp each and meet no barrier; longer ones have a block of their own.
 // V = 0: more than 512 threads hold.
 struct Team { int V, group, threads; long groups; };
-inline Team team_of(int octets) {
+inline Team team_of(int octets, bool one) {
   Team t = {};
   const auto up = [](int n) { return (n + 31) / 32 * 32; };
-  if (octets <= 64) {
-    t.V = octets <= 32 ? 1 : 2;
-    t.group = octets <= 32 ? pow2_from(octets) : 32;
+  if (octets <= (one ? 32 : 64)) {
+    t.V = one || octets == 1 ? 1 : 2;
+    t.group = pow2_from((octets + t.V - 1) / t.V);
     t.threads = 128;
   } else {
-    const int one = up(octets), two = up((octets + 1) / 2);
-    t.V = one <= 512 && one < 2 * two ? 1 : two <= 512 ? 2 : 0;
-    t.group = t.threads = t.V == 1 ? one : t.V == 2 ? two : 1024;
+    const int n1 = up(octets), n2 = up((octets + 1) / 2);
+    t.V = n1 <= 512 && (one || n1 < 2 * n2) ? 1 : n2 <= 512 ? 2 : 0;
+    t.group = t.threads = t.V == 1 ? n1 : t.V == 2 ? n2 : 1024;
   }
   t.groups = t.threads / t.group;
   return t;
@@ -381,6 +369,12 @@ inline Drop drop_of(const xconv_rows_desc* d) {
   r.add = d->seed_add;
   r.scale = d->p < 1.0 ? (float)(1.0 / (1.0 - d->p)) : 0.f;
   return r;
+}
+// Blocks of a kernel that an SM holds.  (Asked once: the devices are all alike.)
+template <typename... A>
+int resident_blocks(void (*kernel)(A...), int threads, int smem) {
+  int n = 0;
+  return cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, threads, smem) == cudaSuccess ? std::max(n, 1) : 1;
 }
 // f(VEC, how the key comes) as types.
 template <typename F>
