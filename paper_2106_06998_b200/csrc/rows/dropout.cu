@@ -69,6 +69,129 @@ __global__ void __launch_bounds__(256) dropout_kernel(const DropArgs a) {
   }
 }
 
+// Dense rows that do not begin on 16-byte boundaries: whatever the rows, in pieces of 16 bytes.  A block draws the mask of its pieces' rows into shared memory, a byte an octet, and
+// every piece picks its bits from the up to three octets that it meets.  Rows that share a mask row find it drawn once a block.
+constexpr int LOOSE_EACH = 4, LOOSE_PIECES = 256 * LOOSE_EACH, LOOSE_BYTES = 24 * 1024;
+
+struct LooseArgs {
+  const void *X, *R;
+  void* Y;
+  long values;
+  int C, octets, shared;           // shared: mask rows have several rows
+  Divisor by;                      // C
+  Drop drop;
+};
+
+template <typename T, int DROP>
+__global__ void __launch_bounds__(256, 4) dropout_loose_kernel(const LooseArgs a) {
+  extern __shared__ unsigned char masks[];
+  constexpr int PER = 16 / sizeof(T);
+  const long first = (long)blockIdx.x * (LOOSE_PIECES * PER);                   // the block's first value
+  const int here = (int)min((long)(LOOSE_PIECES * PER), a.values - first);
+  const auto load = [&](const void* from, int i, uint4& u) {
+    const int at = i * PER;
+    u = make_uint4(0u, 0u, 0u, 0u);
+    if (at + PER <= here) {
+      u = __ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(from) + first + at));
+    } else {
+      uint32_t* w = &u.x;
+#pragma unroll
+      for (int e = 0; e < PER; ++e)
+        if (at + e < here) {
+          if constexpr (sizeof(T) == 4) w[e] = static_cast<const uint32_t*>(from)[first + at + e];
+          else w[e / 2] |= (uint32_t)static_cast<const unsigned short*>(from)[first + at + e] << (16 * (e % 2));
+        }
+    }
+  };
+  uint4 x[LOOSE_EACH];
+#pragma unroll
+  for (int i = 0; i < LOOSE_EACH; ++i) load(a.X, threadIdx.x + 256 * i, x[i]);
+  long row0 = 0;
+  int col0 = 0, rows = 0, origin = 0;                        // of the block's first value; rows behind its row; the byte of its row's first octet (before the masks, if these begin within the row)
+  if (DROP) {
+    const uint2 key = a.drop.key<DROP>();
+    row0 = first / a.C;
+    col0 = (int)(first - row0 * a.C);
+    rows = (int)(((long)col0 + here - 1) / a.C);
+    const uint32_t m0 = a.drop.per((uint32_t)row0), m1 = a.drop.per((uint32_t)(row0 + rows));
+    // from the octet of the first value to that of the last; of shared mask rows all octets
+    const unsigned long long begin = (unsigned long long)m0 * (uint32_t)a.octets + (a.shared ? 0 : col0 / 8);
+    const int last = (int)(((long)col0 + here - 1) - (long)rows * a.C) / 8;
+    const int count = (int)((unsigned long long)m1 * (uint32_t)a.octets + (a.shared ? a.octets - 1 : last) + 1 - begin);
+    origin = a.shared ? 0 : -(col0 / 8);
+    int k = (a.shared ? 0 : col0 / 8) + (int)threadIdx.x;
+    k %= a.octets;
+    const int step = 256 % a.octets;
+    for (int i = threadIdx.x; i < count; i += 256) {
+      const uint32_t b = mask_bits(a.drop, key, begin + i);
+      masks[i] = (unsigned char)(8 * k + 8 <= a.C ? b : b & ((1u << (a.C - 8 * k)) - 1u));
+      k += step;
+      if (k >= a.octets) k -= a.octets;
+    }
+    if (threadIdx.x < 2) masks[count + threadIdx.x] = 0;                         // (what the last pieces ask for)
+    __syncthreads();
+  }
+  uint4 r[LOOSE_EACH];
+  if (a.R)
+#pragma unroll
+    for (int i = 0; i < LOOSE_EACH; ++i) load(a.R, threadIdx.x + 256 * i, r[i]);
+#pragma unroll
+  for (int i = 0; i < LOOSE_EACH; ++i) {
+    const int at = (threadIdx.x + 256 * i) * PER;
+    if (at >= here) continue;
+    float f[PER], g[PER];
+    const auto floats = [](const uint4& u, float (&v)[PER]) {
+      const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+      if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(w[e]);
+      } else {
+        floats_of<T>(w, v);
+      }
+    };
+    floats(x[i], f);
+#pragma unroll
+    for (int e = 0; e < PER; ++e) g[e] = 0.f;
+    if (a.R) floats(r[i], g);
+    if (DROP) {
+      const uint32_t n = (uint32_t)col0 + (uint32_t)at, row = a.by(n);
+      const int c = (int)(n - row * (uint32_t)a.C), k = c >> 3;
+      const auto byte_of = [&](uint32_t r) { return (a.shared ? (int)(a.drop.per((uint32_t)row0 + r) - a.drop.per((uint32_t)row0)) : (int)r) * a.octets + origin; };
+      // the octet of the first value, the one behind it, and the one behind that
+      const int b = byte_of(row) + k, here0 = min(8, a.C - 8 * k) - (c & 7);
+      const bool more = k + 1 < a.octets;
+      const int next = a.shared && k + 2 >= a.octets ? byte_of(min(row + 1, (uint32_t)rows)) : b + (more ? 2 : 1);
+      uint32_t bits = (uint32_t)masks[b] >> (c & 7);
+      if (more) {
+        bits |= (uint32_t)masks[b + 1] << here0;
+        bits |= (uint32_t)masks[next] << min(here0 + min(8, a.C - 8 * k - 8), 31);
+      } else {
+        bits |= (uint32_t)masks[next] << here0;
+      }
+#pragma unroll
+      for (int e = 0; e < PER; ++e) f[e] = bits >> e & 1 ? g[e] : fmaf(f[e], a.drop.scale, g[e]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < PER; ++e) f[e] += g[e];
+    }
+    uint32_t w[4];
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = __float_as_uint(f[e]);
+    } else {
+      words_for<T>(f, w);
+    }
+    T* to = static_cast<T*>(a.Y) + first + at;
+    if (at + PER <= here) {
+      *reinterpret_cast<uint4*>(to) = make_uint4(w[0], w[1], w[2], w[3]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < PER; ++e)
+        if (at + e < here) to[e] = from_f<T>(f[e]);
+    }
+  }
+}
+
 struct DequantArgs {
   Rows Q, X;
   const float* scales;
@@ -132,6 +255,21 @@ cudaError_t launch_dropout(const xconv_rows_desc* d, const void* X, const void* 
   a.drop = drop_of(d);
   const bool vec = d->C % (16 / es) == 0 && whole(a.X, 16) && whole(a.R, 16) && whole(a.Y, 16);
   const bool dense = d->x_stride == d->C && (!residual || d->r_stride == d->C) && d->y_stride == d->C;
+  if (!vec && dense && d->C >= 8 && at(X, 16) && at(residual, 16) && at(Y, 16)) {
+    LooseArgs l = {};
+    l.X = X; l.R = residual; l.Y = Y; l.values = d->rows * d->C; l.C = d->C; l.octets = (d->C + 7) / 8; l.by = divisor((uint32_t)d->C); l.drop = a.drop;
+    const long values = LOOSE_PIECES * 16 / (long)es;
+    l.shared = a.drop.how && d->rows_per_mask > 1;
+    // bytes of a block's masks, at most
+    const long rows = values / d->C + 2, bytes = l.shared ? (rows / d->rows_per_mask + 2) * l.octets + 2 : values / 8 + 2 * rows + 4;
+    if (!a.drop.how || bytes <= LOOSE_BYTES)
+      return with_type(d->dtype, [&](auto t) {
+        using T = decltype(t);
+        const auto kernel = a.drop.how == DROP_NONE ? dropout_loose_kernel<T, DROP_NONE> : a.drop.how == DROP_HOST ? dropout_loose_kernel<T, DROP_HOST> : dropout_loose_kernel<T, DROP_DEVICE>;
+        kernel<<<(unsigned)((l.values + values - 1) / values), 256, a.drop.how ? (size_t)bytes : 0, st>>>(l);
+        return cudaGetLastError();
+      });
+  }
   const bool flat = vec && dense && d->C % 8 == 0 && (!a.drop.how || d->rows_per_mask == 1);
   a.units = units_of(d);
   return with_type(d->dtype, [&](auto t) {

@@ -262,7 +262,7 @@ cudaError_t launch_rms_forward(const xconv_rows_desc* d, const void* X, const vo
   const bool vec = d->C % (a.q ? 8 : 16 / es) == 0 && whole(a.X, 16) && whole(a.R, 16) && whole(a.H, 16) && whole(a.Y, a.q ? 8 : 16) && at(weight, 16);
   cudaError_t e;
   if (!vec && !a.q && rms_staged_forward(d, X, residual, weight, H, Y, rstd, st, &e)) return e;
-  const Team p = team_of(a.octets, !vec);
+  const Team p = team_of(a.octets, !vec || (a.q && es == 4));
   a.group = p.group;
   const long blocks = std::min((d->rows + p.groups - 1) / p.groups, (long)ROWS_SMS * std::max(1, 2048 / p.threads));
   return with_type(d->dtype, [&](auto t) {

@@ -28,7 +28,7 @@ __global__ void __launch_bounds__(512, V <= 4 ? 2 : 1) rms_staged_kernel(const S
   const int group = s.group, lane = group <= 32 ? threadIdx.x & (group - 1) : threadIdx.x, own = group <= 32 ? threadIdx.x / group : 0;
   const int bytes = s.slots * s.slot;                          // of a stage
   const bool drops = s.drop.how != DROP_NONE;
-  const uint2 key = s.drop.how == DROP_DEVICE ? s.drop.key<DROP_DEVICE>() : s.drop.key<DROP_HOST>();
+  const uint2 host_key = s.drop.key<DROP_HOST>(), key = s.drop.how == DROP_DEVICE ? s.drop.key<DROP_DEVICE>() : host_key;
   const auto fetch = [&](long run, int stage) {
     if (run < s.runs) {
       const Run r = Run::of<PER>(s, run);
@@ -48,22 +48,22 @@ __global__ void __launch_bounds__(512, V <= 4 ? 2 : 1) rms_staged_kernel(const S
   int stage = 0, turn = 0;
   uint32_t masks_from = 0xffffffffu, masks_to = 0;
   for (long run = blockIdx.x; run < s.runs; run += gridDim.x) {
+    const Run here = Run::of<PER>(s, run);
+    uint32_t first = 0;
+    if (drops) {                                               // (while the run is on its way; rows that share a mask find it there)
+      first = s.drop.per((uint32_t)(run * s.run));
+      const uint32_t last = s.drop.per((uint32_t)(run * s.run + here.rows - 1));
+      if (first != masks_from || last != masks_to) {
+        if (s.drop.how == DROP_HOST) run_mask(s, mask, host_key, first, last);        // (a key that all lanes share costs them nothing)
+        else run_mask(s, mask, key, first, last);
+      }
+      masks_from = first; masks_to = last;
+    }
     if (s.stages == 3) copies_wait<1>();
     else copies_wait<0>();
     __syncthreads();
     // (the stage before this one was written out before the barrier)
     fetch(run + (long)(s.stages - 1) * gridDim.x, stage == 0 ? s.stages - 1 : stage - 1);
-    const Run here = Run::of<PER>(s, run);
-    uint32_t first = 0;
-    if (drops) {
-      first = s.drop.per((uint32_t)(run * s.run));
-      const uint32_t last = s.drop.per((uint32_t)(run * s.run + here.rows - 1));
-      if (first != masks_from || last != masks_to) {           // (rows that share a mask find it there)
-        run_mask(s, mask, key, first, last);
-        masks_from = first; masks_to = last;
-        __syncthreads();
-      }
-    }
     T* const at = reinterpret_cast<T*>(base + stage * bytes) + here.shift;
     const int apart = s.slot / (int)sizeof(T);
     for (int r = own; r < s.run; r += s.groups, turn ^= 1) {

@@ -309,6 +309,33 @@ __device__ __forceinline__ void mask8(const Drop& d, uint2 key, unsigned long lo
   }
 }
 
+// The same as bits of a byte: a value is kept where its half carries out of a sum with what the border lacks to 2^32, and the carries are taken into the byte as they come (34 cycles of an SM
+// for the octets of a warp; by comparisons 47; 24 without the mask, ten rounds alone).
+__device__ __forceinline__ uint32_t mask_bits(const Drop& d, uint2 key, unsigned long long block) {
+  const uint4 u = philox4x32_10((uint32_t)block, (uint32_t)(block >> 32), key.x, key.y, 3u);
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+  const uint32_t top = d.bound >> 16, twice = top * 0x10001u, lacks = ~d.bound;
+  const uint32_t off = __vminu2(__vminu2(w[0] ^ twice, w[1] ^ twice), __vminu2(w[2] ^ twice, w[3] ^ twice));
+  uint32_t kept = 0;
+#pragma unroll
+  for (int i = 3; i >= 0; --i) {
+    uint32_t sum;
+    asm("{add.cc.u32 %1, %2, %3;\n\taddc.u32 %0, %0, %0;}" : "+r"(kept), "=r"(sum) : "r"(w[i]), "r"(lacks));
+    asm("{add.cc.u32 %1, %2, %3;\n\taddc.u32 %0, %0, %0;}" : "+r"(kept), "=r"(sum) : "r"(w[i] << 16), "r"(lacks));
+  }
+  uint32_t b = kept ^ 0xffu;
+  if (((off - 0x00010001u) & ~off & 0x80008000u) != 0 && d.last != 0xffffu) {
+    const uint4 lower = philox4x32_10((uint32_t)block, (uint32_t)(block >> 32), key.x, key.y, 4u);
+    const uint32_t l[4] = {lower.x, lower.y, lower.z, lower.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if ((w[i] & 0xffffu) == top) b = (b & ~(1u << 2 * i)) | ((l[i] & 0xffffu) <= d.last ? 1u << 2 * i : 0u);
+      if ((w[i] >> 16) == top) b = (b & ~(2u << 2 * i)) | ((l[i] >> 16) <= d.last ? 2u << 2 * i : 0u);
+    }
+  }
+  return b;
+}
+
 // ---- over the threads of a row: `group` of them, a power of two up to 32, or all of the block
 
 // buf: 32 entries that no thread uses before the next barrier but one.
@@ -339,7 +366,7 @@ inline int pow2_from(long n) { int p = 1; while (p < n) p *= 2; return p; }
 
 // Threads a row and octets a thread.  Two octets a thread: what it keeps beside them once for two, half the steps of a sum over the row, and twice the bytes on their way (gradients of
 // 131072 x 128 bf16 24 us, with one 30; of 8192 x 4096 48 us, with one 63).  One, where two of floats with all their companions do not fit the registers (`one`: gradients of 131072 x 64
-// floats 23 us, with two 26) or octets have to be in neighbouring lanes (rows at any alignment), or more threads would go without.  Rows of up to 64 octets take part of a warp each and meet no barrier; longer ones have a block of their own.
+// floats 23 us, with two 26; norm of as many into 8 bits 20, with two 23) or octets have to be in neighbouring lanes (rows at any alignment), or more threads would go without.  Rows of up to 64 octets take part of a warp each and meet no barrier; longer ones have a block of their own.
 // V = 0: more than 512 threads hold.
 struct Team { int V, group, threads; long groups; };
 inline Team team_of(int octets, bool one) {

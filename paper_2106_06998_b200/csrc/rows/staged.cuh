@@ -68,12 +68,7 @@ __device__ __forceinline__ void run_mask(const Staged& s, unsigned char* mask, u
   int m = threadIdx.x / s.octets, k = threadIdx.x - m * s.octets;
   const int dm = blockDim.x / s.octets, dk = blockDim.x - dm * s.octets;
   for (int i = threadIdx.x; i < n; i += blockDim.x) {
-    bool gone[8];
-    mask8(s.drop, key, (unsigned long long)(first + m) * (uint32_t)s.octets + k, gone);
-    uint32_t b = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) b |= gone[e] ? 1u << e : 0u;
-    mask[m * s.pitch + 4 + k] = (unsigned char)b;
+    mask[m * s.pitch + 4 + k] = (unsigned char)mask_bits(s.drop, key, (unsigned long long)(first + m) * (uint32_t)s.octets + k);
     m += dm; k += dk;
     if (k >= s.octets) { k -= s.octets; ++m; }
   }
