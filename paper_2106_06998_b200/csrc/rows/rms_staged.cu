@@ -24,11 +24,10 @@ __global__ void __launch_bounds__(512, V <= 4 ? 2 : 1) rms_staged_kernel(const S
   constexpr int PER = 16 / sizeof(T);
   char* const base = reinterpret_cast<char*>(ring);
   const Staged& s = a.s;
-  unsigned char* const mask = reinterpret_cast<unsigned char*>(base + s.mask_at);
   const int group = s.group, lane = group <= 32 ? threadIdx.x & (group - 1) : threadIdx.x, own = group <= 32 ? threadIdx.x / group : 0;
   const int bytes = s.slots * s.slot;                          // of a stage
   const bool drops = s.drop.how != DROP_NONE;
-  const uint2 host_key = s.drop.key<DROP_HOST>(), key = s.drop.how == DROP_DEVICE ? s.drop.key<DROP_DEVICE>() : host_key;
+  const uint2 key = s.drop.how == DROP_DEVICE ? s.drop.key<DROP_DEVICE>() : s.drop.key<DROP_HOST>();
   const auto fetch = [&](long run, int stage) {
     if (run < s.runs) {
       const Run r = Run::of<PER>(s, run);
@@ -46,19 +45,9 @@ __global__ void __launch_bounds__(512, V <= 4 ? 2 : 1) rms_staged_kernel(const S
 #pragma unroll
   for (int v = 0; v < V; ++v) dw[v][0] = dw[v][1] = 0.f;
   int stage = 0, turn = 0;
-  uint32_t masks_from = 0xffffffffu, masks_to = 0;
+  PairMask<V> mask;
   for (long run = blockIdx.x; run < s.runs; run += gridDim.x) {
     const Run here = Run::of<PER>(s, run);
-    uint32_t first = 0;
-    if (drops) {                                               // (while the run is on its way; rows that share a mask find it there)
-      first = s.drop.per((uint32_t)(run * s.run));
-      const uint32_t last = s.drop.per((uint32_t)(run * s.run + here.rows - 1));
-      if (first != masks_from || last != masks_to) {
-        if (s.drop.how == DROP_HOST) run_mask(s, mask, host_key, first, last);        // (a key that all lanes share costs them nothing)
-        else run_mask(s, mask, key, first, last);
-      }
-      masks_from = first; masks_to = last;
-    }
     if (s.stages == 3) copies_wait<1>();
     else copies_wait<0>();
     __syncthreads();
@@ -70,7 +59,7 @@ __global__ void __launch_bounds__(512, V <= 4 ? 2 : 1) rms_staged_kernel(const S
       const bool in = r < here.rows;                           // (of a row that is not there memory holds whatever: nothing of it is kept)
       const long row = run * s.run + r;
       T* const x = at + r * s.C;
-      const unsigned char* bits = mask + (drops && in ? s.drop.per((uint32_t)row) - first : 0u) * (uint32_t)s.pitch;
+      if (drops) mask.draw(s, key, lane, pairs.odd, s.drop.per((uint32_t)min(row, s.rows - 1)));
       if constexpr (!BACK) {
         float h[V][2], f[V][2], ss = 0.f;
         pairs.read(x, h);
@@ -80,7 +69,7 @@ __global__ void __launch_bounds__(512, V <= 4 ? 2 : 1) rms_staged_kernel(const S
           for (int v = 0; v < V; ++v) f[v][0] = f[v][1] = 0.f;
         if (drops) {
           bool gone[V][2];
-          pairs.gone(bits, gone);
+          mask.gone(s, lane, gone);
 #pragma unroll
           for (int v = 0; v < V; ++v)
 #pragma unroll
@@ -136,7 +125,7 @@ __global__ void __launch_bounds__(512, V <= 4 ? 2 : 1) rms_staged_kernel(const S
         if (a.out[0]) {
           if (drops) {
             bool gone[V][2];
-            pairs.gone(bits, gone);
+            mask.gone(s, lane, gone);
 #pragma unroll
             for (int v = 0; v < V; ++v)
 #pragma unroll

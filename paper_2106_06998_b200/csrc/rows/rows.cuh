@@ -319,9 +319,8 @@ __device__ __forceinline__ uint32_t mask_bits(const Drop& d, uint2 key, unsigned
   uint32_t kept = 0;
 #pragma unroll
   for (int i = 3; i >= 0; --i) {
-    uint32_t sum;
-    asm("{add.cc.u32 %1, %2, %3;\n\taddc.u32 %0, %0, %0;}" : "+r"(kept), "=r"(sum) : "r"(w[i]), "r"(lacks));
-    asm("{add.cc.u32 %1, %2, %3;\n\taddc.u32 %0, %0, %0;}" : "+r"(kept), "=r"(sum) : "r"(w[i] << 16), "r"(lacks));
+    asm("{.reg .u32 sum;\n\tadd.cc.u32 sum, %1, %2;\n\taddc.u32 %0, %0, %0;}" : "+r"(kept) : "r"(w[i]), "r"(lacks));
+    asm("{.reg .u32 sum;\n\tadd.cc.u32 sum, %1, %2;\n\taddc.u32 %0, %0, %0;}" : "+r"(kept) : "r"(w[i] << 16), "r"(lacks));
   }
   uint32_t b = kept ^ 0xffu;
   if (((off - 0x00010001u) & ~off & 0x80008000u) != 0 && d.last != 0xffffu) {

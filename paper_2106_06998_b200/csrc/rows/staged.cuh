@@ -12,9 +12,9 @@ namespace xconv {
 constexpr int STAGED_SMEM = 200 * 1024;
 
 struct Staged {
-  int C, group, groups, run, octets, pitch;      // threads of a row, rows of a pass and of a run; bytes of a mask row
+  int C, group, groups, run, octets;             // threads of a row, rows of a pass and of a run
   int slot, slots;                               // bytes of a tensor's run, tensors of a stage
-  int stages, mask_at;                           // (bytes)
+  int stages;
   long rows, runs, values;                       // of a tensor
   Drop drop;
 };
@@ -62,18 +62,6 @@ __device__ __forceinline__ void run_out(const Run& r, const char* at, T* tensor)
   if (head < min(first * PER, r.end)) to[head] = from[head];
   if (tail < r.end) to[tail] = from[tail];
 }
-// The mask of mask rows `first` to `last`, a bit a value: set where it is dropped.  A row's bits begin on a word of 32, behind a word of whatever.
-__device__ __forceinline__ void run_mask(const Staged& s, unsigned char* mask, uint2 key, uint32_t first, uint32_t last) {
-  const int n = (int)(last - first + 1) * s.octets;
-  int m = threadIdx.x / s.octets, k = threadIdx.x - m * s.octets;
-  const int dm = blockDim.x / s.octets, dk = blockDim.x - dm * s.octets;
-  for (int i = threadIdx.x; i < n; i += blockDim.x) {
-    mask[m * s.pitch + 4 + k] = (unsigned char)mask_bits(s.drop, key, (unsigned long long)(first + m) * (uint32_t)s.octets + k);
-    m += dm; k += dk;
-    if (k >= s.octets) { k -= s.octets; ++m; }
-  }
-}
-
 // A thread's pairs of a row: V of them, `group` pairs from one to the next.  A row with an odd number of values before it has its first one in the second place of its first pair.
 template <typename T, int V>
 struct Pairs {
@@ -117,22 +105,61 @@ struct Pairs {
       }
     }
   }
-  // Whether values are dropped, by a mask row in shared memory: two bits from the pair's first column on (-1: the last bit of the word in front).
-  __device__ __forceinline__ void gone(const unsigned char* mask, bool (&g)[V][2]) const {
-    const uint32_t* bits = reinterpret_cast<const uint32_t*>(mask + 4);
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const int c = column + 2 * v * group;
-      const uint32_t b = __funnelshift_r(bits[c >> 5], bits[(c >> 5) + 1], c & 31);
-      g[v][0] = b & 1; g[v][1] = b & 2;
-    }
-  }
   template <typename P>
   __device__ __forceinline__ void weights(const void* weight, float (&w)[V][2]) const {
 #pragma unroll
     for (int v = 0; v < V; ++v)
 #pragma unroll
       for (int k = 0; k < 2; ++k) w[v][k] = has(v, k) ? (weight ? to_f(static_cast<const P*>(weight)[column + 2 * v * group + k]) : 1.f) : 0.f;
+  }
+};
+
+// Whether a thread's values are dropped.  The lanes of a row draw an octet each for every four pairs of a thread -- the octets of the pairs that lie side by side in their lanes -- and
+// each asks the lane that has its pair's.  In an odd row a pair's second value is the first of its two in the octets' count: bytes are moved on by one, and take in the last bit of the
+// octet before.
+template <int V>
+struct PairMask {
+  static constexpr int ROUNDS = (V + 3) / 4;
+  uint32_t bits[ROUNDS];
+  uint32_t row;                    // the mask row that they are of
+  __device__ __forceinline__ PairMask() : row(0xffffffffu) {}
+  __device__ __forceinline__ void draw(const Staged& s, uint2 key, int lane, int odd, uint32_t mask_row) {
+    if (!__any_sync(0xffffffffu, mask_row != row)) return;    // (whole channels: the row before had the same)
+    row = mask_row;
+    const unsigned long long first = (unsigned long long)mask_row * (uint32_t)s.octets;
+    const int l = threadIdx.x & 31, group = s.group;
+    if (group <= 32) {
+      uint32_t last = 0;
+#pragma unroll
+      for (int j = 0; j < ROUNDS; ++j) {
+        const uint32_t b = mask_bits(s.drop, key, first + (j * group + lane));
+        uint32_t before = __shfl_up_sync(0xffffffffu, b, 1, group);
+        if (lane == 0) before = last;
+        last = __shfl_sync(0xffffffffu, b, group - 1, group);
+        bits[j] = odd ? b << 1 | before >> 7 : b;
+      }
+    } else {
+      const int apart = group >> 2, base = (int)(threadIdx.x >> 5) * 8;       // octets from a pair to the thread's next; of the warp's first one
+      uint32_t ahead = 0;          // the octet before those of the lane-th pairs
+      if (odd) ahead = mask_bits(s.drop, key, first + max(base + (l & 7) * apart - 1, 0));
+#pragma unroll
+      for (int j = 0; j < ROUNDS; ++j) {
+        const int v = 4 * j + (l >> 3);
+        const uint32_t b = mask_bits(s.drop, key, first + (base + v * apart + (l & 7)));
+        uint32_t before = __shfl_up_sync(0xffffffffu, b, 1);
+        const uint32_t other = __shfl_sync(0xffffffffu, ahead, v);
+        if ((l & 7) == 0) before = other;
+        bits[j] = odd ? b << 1 | before >> 7 : b;
+      }
+    }
+  }
+  __device__ __forceinline__ void gone(const Staged& s, int lane, bool (&g)[V][2]) const {
+    const int width = min(s.group, 32), l = lane & (width - 1), apart = width >> 2, by = 2 * (l & 3);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const uint32_t b = __shfl_sync(0xffffffffu, bits[v >> 2], (l >> 2) + (v & 3) * apart, width) >> by;
+      g[v][0] = b & 1; g[v][1] = b & 2;
+    }
   }
 };
 
@@ -153,7 +180,7 @@ inline StagedPlan staged_plan(const xconv_rows_desc* d, int slots, bool backward
   if (!best) return p;
   p.threads = s->group <= 32 ? 256 : s->group;
   s->groups = p.threads / s->group;
-  s->C = d->C; s->octets = (d->C + 7) / 8; s->pitch = 4 + (s->octets + 3) / 4 * 4;
+  s->C = d->C; s->octets = (d->C + 7) / 8;
   s->rows = d->rows; s->values = d->rows * d->C; s->slots = slots;
   // rows of a run: passes of the block's groups (an even number of rows, or one), about 6 KB a tensor, but runs for all SMs
   const long row_bytes = (long)d->C * es;
@@ -163,10 +190,8 @@ inline StagedPlan staged_plan(const xconv_rows_desc* d, int slots, bool backward
   s->runs = (d->rows + s->run - 1) / s->run;
   // (a boundary's shift in front; behind, what lanes without values of the row read)
   s->slot = (int)((s->run * row_bytes + 16 + 2 * s->group * es + 15) / 16 * 16);
-  const int mask = s->drop.how ? s->run * s->pitch + 2 * s->group * p.V / 8 + 16 : 0;
   for (s->stages = 3; s->stages >= 2; --s->stages) {
-    s->mask_at = s->stages * slots * s->slot;
-    p.smem = s->mask_at + mask;
+    p.smem = s->stages * slots * s->slot;
     if (backward) p.smem = std::max(p.smem, s->groups * d->C * 4);
     if (p.smem <= STAGED_SMEM) break;
   }
