@@ -39,6 +39,7 @@ struct DropArgs {
 
 template <typename T, bool VEC, bool FLAT, int DROP, int EACH>
 __global__ void __launch_bounds__(256) dropout_kernel(const DropArgs a) {
+  pdl_wait();
   const uint2 key = a.drop.key<DROP>();
   const long first = (long)blockIdx.x * (256 * EACH) + threadIdx.x;
   Fetched<T, VEC> fx[EACH], fr[EACH];
@@ -86,13 +87,14 @@ template <typename T, int DROP>
 __global__ void __launch_bounds__(256, 4) dropout_loose_kernel(const LooseArgs a) {
   extern __shared__ unsigned char masks[];
   constexpr int PER = 16 / sizeof(T);
+  pdl_wait();
   const long first = (long)blockIdx.x * (LOOSE_PIECES * PER);                   // the block's first value
   const int here = (int)min((long)(LOOSE_PIECES * PER), a.values - first);
   const auto load = [&](const void* from, int i, uint4& u) {
     const int at = i * PER;
     u = make_uint4(0u, 0u, 0u, 0u);
     if (at + PER <= here) {
-      u = __ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(from) + first + at));
+      u = *reinterpret_cast<const uint4*>(static_cast<const T*>(from) + first + at);
     } else {
       uint32_t* w = &u.x;
 #pragma unroll
@@ -208,6 +210,7 @@ __device__ __forceinline__ float2 from_e4m3x2(uint32_t u) {
 template <typename T, bool VEC, bool FLAT, int EACH>
 __global__ void __launch_bounds__(256) dequantize_kernel(const DequantArgs a) {
   typedef unsigned char byte;
+  pdl_wait();
   const long first = (long)blockIdx.x * (256 * EACH) + threadIdx.x;
   Fetched<byte, VEC> fq[EACH];
   float scale[EACH];
@@ -215,7 +218,7 @@ __global__ void __launch_bounds__(256) dequantize_kernel(const DequantArgs a) {
   for (int i = 0; i < EACH; ++i) {
     const Unit<FLAT> n(a.units, first + 256 * i);
     fetch8<byte, VEC>(a.Q, n.template at<byte>(a.Q), n.row, 8 * n.k, n.C, n.in, fq[i]);
-    scale[i] = n.in ? __ldg(a.scales + (FLAT ? 8 * n.u >> a.shift : n.row * a.q_groups + (a.shift ? 8 * n.k >> a.shift : 0))) : 0.f;
+    scale[i] = n.in ? a.scales[FLAT ? 8 * n.u >> a.shift : n.row * a.q_groups + (a.shift ? 8 * n.k >> a.shift : 0)] : 0.f;
   }
 #pragma unroll
   for (int i = 0; i < EACH; ++i) {
@@ -266,8 +269,7 @@ cudaError_t launch_dropout(const xconv_rows_desc* d, const void* X, const void* 
       return with_type(d->dtype, [&](auto t) {
         using T = decltype(t);
         const auto kernel = a.drop.how == DROP_NONE ? dropout_loose_kernel<T, DROP_NONE> : a.drop.how == DROP_HOST ? dropout_loose_kernel<T, DROP_HOST> : dropout_loose_kernel<T, DROP_DEVICE>;
-        kernel<<<(unsigned)((l.values + values - 1) / values), 256, a.drop.how ? (size_t)bytes : 0, st>>>(l);
-        return cudaGetLastError();
+        return launch_pdl(kernel, dim3((unsigned)((l.values + values - 1) / values)), dim3(256), a.drop.how ? (size_t)bytes : 0, st, l);
       });
   }
   const bool flat = vec && dense && d->C % 8 == 0 && (!a.drop.how || d->rows_per_mask == 1);
@@ -278,8 +280,7 @@ cudaError_t launch_dropout(const xconv_rows_desc* d, const void* X, const void* 
       if constexpr (!decltype(v)::value) return dropout_kernel<T, false, false, decltype(how)::value, 1>;
       else return flat ? dropout_kernel<T, true, true, decltype(how)::value, 2> : dropout_kernel<T, true, false, decltype(how)::value, 2>;
     });
-    kernel<<<blocks_of(a.units.count, vec ? 2 : 1), 256, 0, st>>>(a);
-    return cudaGetLastError();
+    return launch_pdl(kernel, dim3(blocks_of(a.units.count, vec ? 2 : 1)), dim3(256), 0, st, a);
   });
 }
 
@@ -296,10 +297,8 @@ cudaError_t launch_dequantize(const xconv_rows_desc* d, const void* Q, const flo
   a.units = units_of(d);
   return with_type(d->dtype, [&](auto t) {
     using T = decltype(t);
-    if (flat) dequantize_kernel<T, true, true, 4><<<blocks_of(a.units.count, 4), 256, 0, st>>>(a);
-    else if (vec) dequantize_kernel<T, true, false, 4><<<blocks_of(a.units.count, 4), 256, 0, st>>>(a);
-    else dequantize_kernel<T, false, false, 1><<<blocks_of(a.units.count, 1), 256, 0, st>>>(a);
-    return cudaGetLastError();
+    const auto kernel = flat ? dequantize_kernel<T, true, true, 4> : vec ? dequantize_kernel<T, true, false, 4> : dequantize_kernel<T, false, false, 1>;
+    return launch_pdl(kernel, dim3(blocks_of(a.units.count, vec ? 4 : 1)), dim3(256), 0, st, a);
   });
 }
 

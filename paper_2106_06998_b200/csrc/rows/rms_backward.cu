@@ -68,6 +68,7 @@ __global__ void __launch_bounds__(512) rms_backward_kernel(const RmsBackArgs a) 
   __shared__ float sums[2][32];
   const int group = a.group, lane = group <= 32 ? threadIdx.x & (group - 1) : threadIdx.x;
   const int groups = group <= 32 ? blockDim.x / group : 1, own = group <= 32 ? threadIdx.x / group : 0;
+  pdl_wait();
   const uint2 key = a.drop.key<DROP>();
   const long step = (long)gridDim.x * groups;
   long row = (long)blockIdx.x * groups + own;
@@ -76,7 +77,7 @@ __global__ void __launch_bounds__(512) rms_backward_kernel(const RmsBackArgs a) 
   float next_rstd = 0.f;
   const auto fetch = [&](long next) {
     const bool in = next < a.rows;
-    next_rstd = in ? __ldg(a.rstd + next) : 0.f;
+    next_rstd = in ? a.rstd[next] : 0.f;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       const int k = lane + v * group;
@@ -156,11 +157,12 @@ __global__ void __launch_bounds__(512) rms_backward_kernel(const RmsBackArgs a) 
 template <typename T, bool VEC, int DROP>
 __global__ void __launch_bounds__(1024) rms_backward_wide_kernel(const RmsBackArgs a) {
   __shared__ float sums[2][32];
+  pdl_wait();
   const uint2 key = a.drop.key<DROP>();
   const int steps = (a.octets + 1023) / 1024;
   int turn = 0;
   for (long row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
-    const float rstd = __ldg(a.rstd + row);
+    const float rstd = a.rstd[row];
     float xh[8], g[8], unused[8], s = 0.f;
     const auto read = [&](int k) {
       Fetched<T, VEC> fh, fy;
@@ -190,13 +192,14 @@ __global__ void __launch_bounds__(1024) rms_backward_wide_kernel(const RmsBackAr
 // dw of rows that no block holds: a thread a column, a block a run of rows.
 template <typename T>
 __global__ void __launch_bounds__(256) rms_columns_kernel(const RmsBackArgs a, long rows_per) {
+  pdl_wait();
   const int c = blockIdx.x * 256 + threadIdx.x;
   if (c >= a.C) return;
   const long r0 = (long)blockIdx.y * rows_per, r1 = min(a.rows, r0 + rows_per);
   float dw = 0.f;
 #pragma unroll 4
   for (long row = r0; row < r1; ++row)
-    dw = fmaf(to_f(row_of<T>(a.dY, row)[c]), to_f(row_of<T>(a.H, row)[c]) * __ldg(a.rstd + row), dw);
+    dw = fmaf(to_f(row_of<T>(a.dY, row)[c]), to_f(row_of<T>(a.H, row)[c]) * a.rstd[row], dw);
   a.part[(size_t)blockIdx.y * a.C + c] = dw;
 }
 
@@ -279,6 +282,7 @@ cudaError_t launch_rms_backward(const xconv_rows_desc* d, const void* dY, const 
     else e = with_type(d->dtype, [&](auto t) {
       using T = decltype(t);
       const int V = p.team.V;
+      cudaError_t e = cudaSuccess;
       if (V || dX || dR) {
         const auto pick = [&](auto v, auto dropped) -> void (*)(const RmsBackArgs) {
           constexpr bool VEC = decltype(v)::value;
@@ -289,14 +293,14 @@ cudaError_t launch_rms_backward(const xconv_rows_desc* d, const void* dY, const 
         const size_t smem = V && part && p.team.group <= 32 ? (size_t)(p.team.threads / 32) * d->C * sizeof(float) : 0;
         const long blocks = std::min(p.blocks, (long)ROWS_SMS * resident_blocks(kernel, p.team.threads, (int)smem));
         if (V) parts = blocks;
-        kernel<<<(unsigned)blocks, p.team.threads, smem, st>>>(a);
+        e = launch_pdl(kernel, dim3((unsigned)blocks), dim3(p.team.threads), smem, st, a);
         ++*launches;
       }
-      if (!V && part) {
-        rms_columns_kernel<T><<<dim3((unsigned)((d->C + 255) / 256), (unsigned)p.parts), 256, 0, st>>>(a, (d->rows + p.parts - 1) / p.parts);
+      if (e == cudaSuccess && !V && part) {
+        e = launch_pdl(rms_columns_kernel<T>, dim3((unsigned)((d->C + 255) / 256), (unsigned)p.parts), dim3(256), 0, st, a, (d->rows + p.parts - 1) / p.parts);
         ++*launches;
       }
-      return cudaGetLastError();
+      return e;
     });
     if (e != cudaSuccess) return e;
   }

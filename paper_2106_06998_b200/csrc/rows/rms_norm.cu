@@ -112,6 +112,7 @@ __global__ void __launch_bounds__(512) rms_forward_kernel(const RmsArgs a) {
   typedef std::conditional_t<Q, unsigned char, T> Y;
   const int group = a.group, lane = group <= 32 ? threadIdx.x & (group - 1) : threadIdx.x;
   const int groups = group <= 32 ? blockDim.x / group : 1, own = group <= 32 ? threadIdx.x / group : 0;
+  pdl_wait();
   const uint2 key = a.drop.key<DROP>();
   const long step = (long)gridDim.x * groups;
   long row = (long)blockIdx.x * groups + own;
@@ -192,6 +193,7 @@ template <typename T, bool VEC, int DROP>
 __global__ void __launch_bounds__(1024) rms_forward_wide_kernel(const RmsArgs a) {
   __shared__ float sums[2][32];
   __shared__ float most[2][32];
+  pdl_wait();
   const uint2 key = a.drop.key<DROP>();
   const int steps = (a.octets + 1023) / 1024;
   int turn = 0;
@@ -275,8 +277,7 @@ cudaError_t launch_rms_forward(const xconv_rows_desc* d, const void* X, const vo
       return p.V == 1 ? rms_forward_kernel<T, 1, VEC, false, DROP> : rms_forward_kernel<T, 2, VEC, false, DROP>;
     };
     const auto kernel = with_kinds(vec, a.drop.how, pick);
-    kernel<<<(unsigned)blocks, p.threads, 0, st>>>(a);
-    return cudaGetLastError();
+    return launch_pdl(kernel, dim3((unsigned)blocks), dim3(p.threads), 0, st, a);
   });
 }
 

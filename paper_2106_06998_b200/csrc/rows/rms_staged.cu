@@ -27,6 +27,7 @@ __global__ void __launch_bounds__(512, V <= 4 ? 2 : 1) rms_staged_kernel(const S
   const int group = s.group, lane = group <= 32 ? threadIdx.x & (group - 1) : threadIdx.x, own = group <= 32 ? threadIdx.x / group : 0;
   const int bytes = s.slots * s.slot;                          // of a stage
   const bool drops = s.drop.how != DROP_NONE;
+  pdl_wait();
   const uint2 key = s.drop.how == DROP_DEVICE ? s.drop.key<DROP_DEVICE>() : s.drop.key<DROP_HOST>();
   const auto fetch = [&](long run, int stage) {
     if (run < s.runs) {
@@ -95,7 +96,7 @@ __global__ void __launch_bounds__(512, V <= 4 ? 2 : 1) rms_staged_kernel(const S
         if (in) pairs.write(x, h);
       } else {
         float xh[V][2], g[V][2], t = 0.f;
-        const float rstd = in ? __ldg(a.rstd + row) : 0.f;
+        const float rstd = in ? a.rstd[row] : 0.f;
         pairs.read(x, xh);
         pairs.read(x + apart, g);
 #pragma unroll
@@ -174,8 +175,7 @@ cudaError_t launch(const xconv_rows_desc* d, const StagedPlan& p, const StagedAr
       const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, STAGED_SMEM);
       if (e != cudaSuccess) return e;
     }
-    kernel<<<(unsigned)p.blocks, p.threads, p.smem, st>>>(a);
-    return cudaGetLastError();
+    return launch_pdl(kernel, dim3((unsigned)p.blocks), dim3(p.threads), p.smem, st, a);
   });
 }
 
