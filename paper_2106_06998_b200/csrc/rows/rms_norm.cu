@@ -84,19 +84,17 @@ __device__ __forceinline__ float row_most(float v, int group, float* buf) {
   return v;
 }
 
-// The octet of h from what was fetched of x and r.
+// The octet of h from what was fetched of x and r, and which of x's values are dropped, by bits.
 template <typename T, bool VEC, int DROP>
-__device__ __forceinline__ void sum_of(const RmsArgs& a, uint2 key, unsigned long long block, const Fetched<T, VEC>& fx, const Fetched<T, VEC>& fr, int k, bool in, float (&h)[8]) {
+__device__ __forceinline__ void sum_of(const RmsArgs& a, uint32_t dropped, const Fetched<T, VEC>& fx, const Fetched<T, VEC>& fr, int k, bool in, float (&h)[8]) {
   values_of<T, VEC>(fx, 8 * k, a.C, in, h);
   float f[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) f[e] = 0.f;
   if (a.R.p) values_of<T, VEC>(fr, 8 * k, a.C, in, f);
   if (DROP) {
-    bool gone[8];
-    mask8(a.drop, key, block + k, gone);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) h[e] = gone[e] ? f[e] : fmaf(h[e], a.drop.scale, f[e]);
+    for (int e = 0; e < 8; ++e) h[e] = dropped & 1u << e ? f[e] : fmaf(h[e], a.drop.scale, f[e]);
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e) h[e] += f[e];
@@ -129,20 +127,31 @@ __global__ void __launch_bounds__(512) rms_forward_kernel(const RmsArgs a) {
     }
     x.next(); r.next();
   };
+  // (the next row's mask, too: there are loads to wait for meanwhile)
+  uint32_t dropped[V];
+  const auto draw = [&](long next) {
+    if (!DROP) return;
+    const unsigned long long block = a.drop.first_block(next, a.octets);
+#pragma unroll
+    for (int v = 0; v < V; ++v) dropped[v] = mask_bits(a.drop, key, block + lane + v * group);
+  };
+#pragma unroll
+  for (int v = 0; v < V; ++v) dropped[v] = 0;
   fetch(row);
+  draw(row);
   float w[8];
   if (V == 1) a.w.load<T, VEC>(8 * min(lane, a.octets - 1), a.C, w);
   int turn = 0;
   for (long row0 = (long)blockIdx.x * groups; row0 < a.rows; row0 += step, row += step, turn ^= 1, hs.next(), ys.next()) {
     const bool in = row < a.rows;
-    const unsigned long long block = DROP ? a.drop.first_block(row, a.octets) : 0;
     float h[V][8], ss = 0.f;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       const int k = lane + v * group;
-      sum_of<T, VEC, DROP>(a, key, block, fx[v], fr[v], k, in && k < a.octets, h[v]);
+      sum_of<T, VEC, DROP>(a, dropped[v], fx[v], fr[v], k, in && k < a.octets, h[v]);
     }
     fetch(row + step);
+    draw(row + step);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       const int k = lane + v * group;
@@ -204,7 +213,7 @@ __global__ void __launch_bounds__(1024) rms_forward_wide_kernel(const RmsArgs a)
       Fetched<T, VEC> fx, fr;
       fetch8<T, VEC>(a.X, x, row, 8 * k, a.C, k < a.octets, fx);
       if (a.R.p) fetch8<T, VEC>(a.R, r, row, 8 * k, a.C, k < a.octets, fr);
-      sum_of<T, VEC, DROP>(a, key, block, fx, fr, k, k < a.octets, h);
+      sum_of<T, VEC, DROP>(a, DROP ? mask_bits(a.drop, key, block + k) : 0, fx, fr, k, k < a.octets, h);
     };
     float ss = 0.f, y[8];
     for (int v = 0; v < steps; ++v) {
