@@ -207,6 +207,20 @@ __device__ __forceinline__ float2 from_e4m3x2(uint32_t u) {
   return __half22float2(*reinterpret_cast<const __half2*>(&h));
 }
 
+__device__ __forceinline__ void codes_of(const uint2& u, int q, float (&f)[8]) {
+  const uint32_t b[2] = {u.x, u.y};
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    if (q == XCONV_Q_E4M3) {
+      const float2 lo = from_e4m3x2(b[h] & 0xffffu), hi = from_e4m3x2(b[h] >> 16);
+      f[4 * h] = lo.x; f[4 * h + 1] = lo.y; f[4 * h + 2] = hi.x; f[4 * h + 3] = hi.y;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) f[4 * h + e] = (float)(int)(signed char)(b[h] >> (8 * e));
+    }
+  }
+}
+
 template <typename T, bool VEC, bool FLAT, int EACH>
 __global__ void __launch_bounds__(256) dequantize_kernel(const DequantArgs a) {
   typedef unsigned char byte;
@@ -226,19 +240,67 @@ __global__ void __launch_bounds__(256) dequantize_kernel(const DequantArgs a) {
     uint32_t b[2];
     words_of<byte, VEC>(fq[i], b);
     float f[8];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      if (a.q == XCONV_Q_E4M3) {
-        const float2 lo = from_e4m3x2(b[h] & 0xffffu), hi = from_e4m3x2(b[h] >> 16);
-        f[4 * h] = lo.x; f[4 * h + 1] = lo.y; f[4 * h + 2] = hi.x; f[4 * h + 3] = hi.y;
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) f[4 * h + e] = (float)(int)(signed char)(b[h] >> (8 * e));
-      }
-    }
+    codes_of(make_uint2(b[0], b[1]), a.q, f);
 #pragma unroll
     for (int e = 0; e < 8; ++e) f[e] *= scale[i];
     store8<T, VEC>(n.template at<T>(a.X), 8 * n.k, n.C, n.in, f);
+  }
+}
+
+// Dense rows that do not begin on boundaries, whatever the rows, in pieces of eight values, which meet up to three scales; these lie in the order of the values.
+struct LooseDequantArgs {
+  const unsigned char* Q;
+  void* X;
+  const float* scales;
+  long values, count;              // count: scales
+  int C, q, group, q_groups;       // group: values of a scale (C: the row)
+  Divisor by;                      // C
+};
+template <typename T>
+__global__ void __launch_bounds__(256) dequantize_loose_kernel(const LooseDequantArgs a) {
+  pdl_wait();
+  const long first = (long)blockIdx.x * (LOOSE_PIECES * 8);
+  const int here = (int)min((long)(LOOSE_PIECES * 8), a.values - first);
+  const long row0 = first / a.C;
+  const int col0 = (int)(first - row0 * a.C);
+  uint2 q[LOOSE_EACH];
+#pragma unroll
+  for (int i = 0; i < LOOSE_EACH; ++i) {
+    const int at = (threadIdx.x + 256 * i) * 8;
+    q[i] = make_uint2(0u, 0u);
+    if (at + 8 <= here) {
+      q[i] = *reinterpret_cast<const uint2*>(a.Q + first + at);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (at + e < here) (e < 4 ? q[i].x : q[i].y) |= (uint32_t)a.Q[first + at + e] << (8 * (e % 4));
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < LOOSE_EACH; ++i) {
+    const int at = (threadIdx.x + 256 * i) * 8;
+    if (at >= here) continue;
+    const uint32_t n = (uint32_t)col0 + (uint32_t)at, row = a.by(n);
+    const int c = (int)(n - row * (uint32_t)a.C), g = a.q_groups == 1 ? 0 : c / a.group;
+    // the values of the first scale, and of the first two
+    const int one = min((g + 1) * a.group, a.C) - c, two = one + (c + one < a.C ? min(a.group, a.C - c - one) : a.group);
+    const long s = (row0 + row) * a.q_groups + g;
+    const float s0 = a.scales[s], s1 = a.scales[min(s + 1, a.count - 1)], s2 = a.scales[min(s + 2, a.count - 1)];
+    float f[8];
+    codes_of(q[i], a.q, f);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] *= e < one ? s0 : e < two ? s1 : s2;
+    uint32_t w[Octet<T>::WORDS];
+    words_for<T>(f, w);
+    T* to = static_cast<T*>(a.X) + first + at;
+    if (at + 8 <= here) {
+#pragma unroll
+      for (int k = 0; k < Octet<T>::WORDS; k += 4) reinterpret_cast<uint4*>(to)[k / 4] = make_uint4(w[k], w[k + 1], w[k + 2], w[k + 3]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (at + e < here) to[e] = from_f<T>(f[e]);
+    }
   }
 }
 
@@ -293,7 +355,17 @@ cudaError_t launch_dequantize(const xconv_rows_desc* d, const void* Q, const flo
   while (group && (1 << a.shift) < group) ++a.shift;
   a.q_groups = group ? (d->C + group - 1) / group : 1;
   const bool vec = d->C % 8 == 0 && whole(a.Q, 8) && whole(a.X, 16);
-  const bool flat = vec && group && d->C % group == 0 && d->x_stride == d->C && d->y_stride == d->C;
+  const bool dense = d->x_stride == d->C && d->y_stride == d->C;
+  if (!vec && dense && d->C >= 8 && at(Q, 8) && at(X, 16)) {
+    LooseDequantArgs l = {};
+    l.Q = static_cast<const unsigned char*>(Q); l.X = X; l.scales = scales; l.values = d->rows * d->C; l.C = d->C; l.q = d->q_type;
+    l.group = group ? group : d->C; l.q_groups = a.q_groups; l.count = d->rows * a.q_groups; l.by = divisor((uint32_t)d->C);
+    return with_type(d->dtype, [&](auto t) {
+      using T = decltype(t);
+      return launch_pdl(dequantize_loose_kernel<T>, dim3((unsigned)((l.values + LOOSE_PIECES * 8 - 1) / (LOOSE_PIECES * 8))), dim3(256), 0, st, l);
+    });
+  }
+  const bool flat = vec && dense && group && d->C % group == 0;
   a.units = units_of(d);
   return with_type(d->dtype, [&](auto t) {
     using T = decltype(t);

@@ -4,8 +4,8 @@
 //
 // Memory bounds it: x and the residual are read once, h and y written once.  A row lies in the registers of `group` threads, V octets each; h stays in float for y (it
 // is rounded once, where it is written).
+#include "eight_bits.cuh"
 #include "rms.h"
-#include "rows.cuh"
 
 namespace xconv {
 
@@ -22,37 +22,6 @@ struct RmsArgs {
   Drop drop;
 };
 
-// ---- 8 bits
-
-constexpr float Q_LEAST = 7.888609052210118e-31f;          // 2^-100
-
-// The largest magnitude, NaN above all.
-__device__ __forceinline__ float most_of(float a, float b) {
-  float r;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-  return r;
-}
-__device__ __forceinline__ float magnitude(const float (&y)[8]) {
-  float m[4];
-#pragma unroll
-  for (int e = 0; e < 4; ++e) m[e] = most_of(fabsf(y[e]), fabsf(y[e + 4]));
-  return most_of(most_of(m[0], m[1]), most_of(m[2], m[3]));
-}
-// The scale of values up to a, and what they are multiplied by: the nearest floats but one, by a reciprocal within an ulp.  (NaN where a is not finite.)
-struct Scale { float scale, inv; };
-__device__ __forceinline__ Scale q_scale(float a, int q) {
-  const float M = q == XCONV_Q_E4M3 ? 448.f : 127.f, least = a < Q_LEAST ? Q_LEAST : a;
-  float r;
-  asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(least));
-  return {fmaf(least, q == XCONV_Q_E4M3 ? 1.f / 448.f : 1.f / 127.f, 0.f * least), M * r};
-}
-__device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
-  unsigned short r;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
-  return r;
-}
-// The nearest whole number of y * inv, at most 127 (and a little) in magnitude, in the low byte: added to 3 * 2^22, where a float's last place is one.
-__device__ __forceinline__ uint32_t int8(float y, float inv) { return __float_as_uint(fmaf(y, inv, 12582912.f)); }
 template <bool VEC>
 __device__ __forceinline__ void store8q(unsigned char* row, int c, int C, bool in, const float (&y)[8], float inv, int q) {
   uint32_t b[2];
@@ -69,21 +38,6 @@ __device__ __forceinline__ float group_most(float m, int width) {
   for (int o = width >> 4; o > 0; o >>= 1) m = most_of(m, __shfl_xor_sync(0xffffffffu, m, o));
   return m;
 }
-// (over the threads of a row, as row_sum)
-__device__ __forceinline__ float row_most(float v, int group, float* buf) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1)
-    if (o < group) v = most_of(v, __shfl_xor_sync(0xffffffffu, v, o));
-  if (group <= 32) return v;
-  const int lane = threadIdx.x & 31;
-  if (lane == 0) buf[threadIdx.x >> 5] = v;
-  __syncthreads();
-  v = lane < (group >> 5) ? buf[lane] : 0.f;
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v = most_of(v, __shfl_xor_sync(0xffffffffu, v, o));
-  return v;
-}
-
 // The octet of h from what was fetched of x and r, and which of x's values are dropped, by bits.
 template <typename T, bool VEC, int DROP>
 __device__ __forceinline__ void sum_of(const RmsArgs& a, uint32_t dropped, const Fetched<T, VEC>& fx, const Fetched<T, VEC>& fr, int k, bool in, float (&h)[8]) {
@@ -272,7 +226,7 @@ cudaError_t launch_rms_forward(const xconv_rows_desc* d, const void* X, const vo
   a.drop = drop_of(d);
   const bool vec = d->C % (a.q ? 8 : 16 / es) == 0 && whole(a.X, 16) && whole(a.R, 16) && whole(a.H, 16) && whole(a.Y, a.q ? 8 : 16) && at(weight, 16);
   cudaError_t e;
-  if (!vec && !a.q && rms_staged_forward(d, X, residual, weight, H, Y, rstd, st, &e)) return e;
+  if (!vec && rms_staged_forward(d, X, residual, weight, H, Y, scales, rstd, st, &e)) return e;
   const Team p = team_of(a.octets, !vec || (a.q && es == 4));
   a.group = p.group;
   return with_type(d->dtype, [&](auto t) {

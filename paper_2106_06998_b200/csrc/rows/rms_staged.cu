@@ -1,4 +1,5 @@
 // RMS norm and its gradients of dense rows that do not begin on 16-byte boundaries (formulas: rms_norm.cu, rms_backward.cu).
+#include "eight_bits.cuh"
 #include "rms.h"
 #include "staged.cuh"
 
@@ -12,6 +13,8 @@ struct StagedArgs {
   void *out[2];                    // over the first and the second of them: y, h; dx, dr
   const void* weight;
   int weight_f32;
+  int q;                           // forward: y in 8 bits, a scale a row
+  float* scales;
   float* rstd;                     // (read by the backward pass)
   float* part;
   float eps, inv_c;
@@ -20,7 +23,7 @@ struct StagedArgs {
 template <typename T, int V, bool BACK>
 __global__ void __launch_bounds__(512, V <= 4 ? 2 : 1) rms_staged_kernel(const StagedArgs a) {
   extern __shared__ uint4 ring[];
-  __shared__ float sums[2][32];
+  __shared__ float sums[2][32], most[2][32];
   constexpr int PER = 16 / sizeof(T);
   char* const base = reinterpret_cast<char*>(ring);
   const Staged& s = a.s;
@@ -56,6 +59,8 @@ __global__ void __launch_bounds__(512, V <= 4 ? 2 : 1) rms_staged_kernel(const S
     fetch(run + (long)(s.stages - 1) * gridDim.x, stage == 0 ? s.stages - 1 : stage - 1);
     T* const at = reinterpret_cast<T*>(base + stage * bytes) + here.shift;
     const int apart = s.slot / (int)sizeof(T);
+    unsigned char* const codes = reinterpret_cast<unsigned char*>(base + s.stages * bytes);
+    const Run eight = Run::of<16>(s, run);                     // (of a tensor of bytes)
     for (int r = own; r < s.run; r += s.groups, turn ^= 1) {
       const bool in = r < here.rows;                           // (of a row that is not there memory holds whatever: nothing of it is kept)
       const long row = run * s.run + r;
@@ -93,7 +98,23 @@ __global__ void __launch_bounds__(512, V <= 4 ? 2 : 1) rms_staged_kernel(const S
         for (int v = 0; v < V; ++v)
 #pragma unroll
           for (int k = 0; k < 2; ++k) h[v][k] *= rstd * w[v][k];
-        if (in) pairs.write(x, h);
+        if (!a.q) {
+          if (in) pairs.write(x, h);
+        } else {
+          float m = 0.f;
+#pragma unroll
+          for (int v = 0; v < V; ++v) m = most_of(m, most_of(fabsf(h[v][0]), fabsf(h[v][1])));
+          const Scale f = q_scale(row_most(m, group, most[turn]), a.q);
+          if (in && lane == 0) a.scales[row] = f.scale;
+          unsigned char* const to = codes + eight.shift + r * s.C + pairs.column;
+          if (in)
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+              const uint32_t b = a.q == XCONV_Q_E4M3 ? e4m3x2(h[v][0] * f.inv, h[v][1] * f.inv) : __byte_perm(int8(h[v][0], f.inv), int8(h[v][1], f.inv), 0x0040);
+              if (pairs.has(v, 0)) to[2 * v * group] = (unsigned char)b;
+              if (pairs.has(v, 1)) to[2 * v * group + 1] = (unsigned char)(b >> 8);
+            }
+        }
       } else {
         float xh[V][2], g[V][2], t = 0.f;
         const float rstd = in ? a.rstd[row] : 0.f;
@@ -137,8 +158,9 @@ __global__ void __launch_bounds__(512, V <= 4 ? 2 : 1) rms_staged_kernel(const S
       }
     }
     __syncthreads();
+    if (!BACK && a.q) run_out<unsigned char>(eight, reinterpret_cast<const char*>(codes), static_cast<unsigned char*>(a.out[0]));
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = !BACK && a.q ? 1 : 0; i < 2; ++i)
       if (a.out[i]) run_out<T>(here, base + stage * bytes + i * s.slot, static_cast<T*>(a.out[i]));
     stage = stage == s.stages - 1 ? 0 : stage + 1;
   }
@@ -185,13 +207,14 @@ bool is_dense(const xconv_rows_desc* d, const void* p, int64_t stride) { return 
 
 }  // namespace
 
-bool rms_staged_forward(const xconv_rows_desc* d, const void* X, const void* residual, const void* weight, void* H, void* Y, float* rstd, cudaStream_t st, cudaError_t* e) {
+bool rms_staged_forward(const xconv_rows_desc* d, const void* X, const void* residual, const void* weight, void* H, void* Y, float* scales, float* rstd, cudaStream_t st, cudaError_t* e) {
+  if (d->q_type && d->q_group > 0 && d->q_group < d->C) return false;
   if (!is_odd(d) || !is_dense(d, X, d->x_stride) || !is_dense(d, residual, d->r_stride) || !is_dense(d, H, d->h_stride) || !is_dense(d, Y, d->y_stride)) return false;
   StagedArgs a = {};
   a.s.drop = drop_of(d);
-  const StagedPlan p = staged_plan(d, residual || H ? 2 : 1, false, &a.s);
+  const StagedPlan p = staged_plan(d, residual || H ? 2 : 1, false, d->q_type != 0, &a.s);
   if (!p.threads) return false;
-  a.in[0] = X; a.in[1] = residual; a.out[0] = Y; a.out[1] = H;
+  a.in[0] = X; a.in[1] = residual; a.out[0] = Y; a.out[1] = H; a.q = d->q_type; a.scales = scales;
   a.weight = weight; a.weight_f32 = d->param_dtype == XCONV_F32; a.rstd = rstd; a.eps = d->eps; a.inv_c = 1.f / (float)d->C;
   *e = launch<false>(d, p, a, st);
   return true;
@@ -205,7 +228,7 @@ long rms_staged_backward_parts(const xconv_rows_desc* d) {
   for (int slots = 2; slots <= 3; ++slots)
     for (int how : {DROP_NONE, DROP_HOST}) {
       s.drop.how = how;
-      const StagedPlan p = staged_plan(d, slots, true, &s);
+      const StagedPlan p = staged_plan(d, slots, true, false, &s);
       if (p.threads) most = std::max(most, p.blocks);
     }
   return most;
@@ -216,7 +239,7 @@ bool rms_staged_backward(const xconv_rows_desc* d, const void* dY, const void* H
   if (!is_odd(d) || !is_dense(d, dY, d->y_stride) || !is_dense(d, H, d->h_stride) || !is_dense(d, dH, d->dh_stride) || !is_dense(d, dX, d->x_stride) || !is_dense(d, dR, d->r_stride)) return false;
   StagedArgs a = {};
   if (dX) a.s.drop = drop_of(d);
-  const StagedPlan p = staged_plan(d, dH ? 3 : 2, true, &a.s);
+  const StagedPlan p = staged_plan(d, dH ? 3 : 2, true, false, &a.s);
   if (!p.threads) return false;
   a.in[0] = H; a.in[1] = dY; a.in[2] = dH; a.out[0] = dX; a.out[1] = dR;
   a.weight = weight; a.weight_f32 = d->param_dtype == XCONV_F32; a.rstd = const_cast<float*>(rstd); a.part = part; a.inv_c = 1.f / (float)d->C;

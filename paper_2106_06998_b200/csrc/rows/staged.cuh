@@ -165,9 +165,9 @@ struct PairMask {
 
 // ---- host side
 
-// slots: tensors that are read or written.  threads = 0: rows that do not fit.
+// slots: tensors that are read or written; eight: and one of bytes.  threads = 0: rows that do not fit.
 struct StagedPlan { int V, threads, smem; long blocks; };
-inline StagedPlan staged_plan(const xconv_rows_desc* d, int slots, bool backward, Staged* s) {
+inline StagedPlan staged_plan(const xconv_rows_desc* d, int slots, bool backward, bool eight, Staged* s) {
   StagedPlan p = {};
   const int es = d->dtype == XCONV_F32 ? 4 : 2, pairs = d->C / 2 + (d->C & 1);       // (of even and odd rows the same)
   // threads of a row: as few idle ones as possible, then as few threads
@@ -191,7 +191,7 @@ inline StagedPlan staged_plan(const xconv_rows_desc* d, int slots, bool backward
   // (a boundary's shift in front; behind, what lanes without values of the row read)
   s->slot = (int)((s->run * row_bytes + 16 + 2 * s->group * es + 15) / 16 * 16);
   for (s->stages = 3; s->stages >= 2; --s->stages) {
-    p.smem = s->stages * slots * s->slot;
+    p.smem = s->stages * slots * s->slot + (eight ? (s->run * d->C + 15 + 15) / 16 * 16 : 0);
     if (backward) p.smem = std::max(p.smem, s->groups * d->C * 4);
     if (p.smem <= STAGED_SMEM) break;
   }
