@@ -338,11 +338,16 @@ cudaError_t launch_dropout(const xconv_rows_desc* d, const void* X, const void* 
   a.units = units_of(d);
   return with_type(d->dtype, [&](auto t) {
     using T = decltype(t);
+    // Octets a thread: 64 bytes of a tensor, where there are enough for all SMs (512 x 256 x 28 x 28 bf16 100 us, with half as many 103, with one octet 116).
+    constexpr int MOST = sizeof(T) == 2 ? 4 : 2;
+    const int each = vec && a.units.count >= 2L * ROWS_SMS * 2048 ? MOST : 1;
     const auto kernel = with_kinds(vec, a.drop.how, [&](auto v, auto how) -> void (*)(const DropArgs) {
-      if constexpr (!decltype(v)::value) return dropout_kernel<T, false, false, decltype(how)::value, 1>;
-      else return flat ? dropout_kernel<T, true, true, decltype(how)::value, 2> : dropout_kernel<T, true, false, decltype(how)::value, 2>;
+      constexpr int HOW = decltype(how)::value;
+      if constexpr (!decltype(v)::value) return dropout_kernel<T, false, false, HOW, 1>;
+      else if (each == 1) return flat ? dropout_kernel<T, true, true, HOW, 1> : dropout_kernel<T, true, false, HOW, 1>;
+      else return flat ? dropout_kernel<T, true, true, HOW, MOST> : dropout_kernel<T, true, false, HOW, MOST>;
     });
-    return launch_pdl(kernel, dim3(blocks_of(a.units.count, vec ? 2 : 1)), dim3(256), 0, st, a);
+    return launch_pdl(kernel, dim3(blocks_of(a.units.count, each)), dim3(256), 0, st, a);
   });
 }
 
@@ -370,7 +375,7 @@ cudaError_t launch_dequantize(const xconv_rows_desc* d, const void* Q, const flo
   return with_type(d->dtype, [&](auto t) {
     using T = decltype(t);
     const auto kernel = flat ? dequantize_kernel<T, true, true, 4> : vec ? dequantize_kernel<T, true, false, 4> : dequantize_kernel<T, false, false, 1>;
-    return launch_pdl(kernel, dim3(blocks_of(a.units.count, vec ? 4 : 1)), dim3(256), 0, st, a);
+    return launch_pdl(kernel, dim3(blocks_of(a.units.count, vec ? 2 : 1)), dim3(256), 0, st, a);
   });
 }
 
