@@ -227,7 +227,7 @@ cudaError_t launch_rms_forward(const xconv_rows_desc* d, const void* X, const vo
   const bool vec = d->C % (a.q ? 8 : 16 / es) == 0 && whole(a.X, 16) && whole(a.R, 16) && whole(a.H, 16) && whole(a.Y, a.q ? 8 : 16) && at(weight, 16);
   cudaError_t e;
   if (!vec && rms_staged_forward(d, X, residual, weight, H, Y, scales, rstd, st, &e)) return e;
-  const Team p = team_of(a.octets, !vec || (a.q && es == 4));
+  const Team p = team_of(a.octets, !vec || (a.q && es == 4), vec && es == 2);
   a.group = p.group;
   return with_type(d->dtype, [&](auto t) {
     using T = decltype(t);
@@ -235,6 +235,8 @@ cudaError_t launch_rms_forward(const xconv_rows_desc* d, const void* X, const vo
       constexpr bool VEC = decltype(v)::value;
       constexpr int DROP = decltype(dropped)::value;
       if (p.V == 0) return rms_forward_wide_kernel<T, VEC, DROP>;
+      if constexpr (VEC && sizeof(T) == 2)
+        if (p.V == 4) return a.q ? rms_forward_kernel<T, 4, VEC, true, DROP> : rms_forward_kernel<T, 4, VEC, false, DROP>;
       if (a.q) return p.V == 1 ? rms_forward_kernel<T, 1, VEC, true, DROP> : rms_forward_kernel<T, 2, VEC, true, DROP>;
       return p.V == 1 ? rms_forward_kernel<T, 1, VEC, false, DROP> : rms_forward_kernel<T, 2, VEC, false, DROP>;
     };

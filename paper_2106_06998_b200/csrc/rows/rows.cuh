@@ -369,9 +369,9 @@ inline int pow2_from(long n) { int p = 1; while (p < n) p *= 2; return p; }
 // Threads a row and octets a thread.  Two octets a thread: what it keeps beside them once for two, half the steps of a sum over the row, and twice the bytes on their way (gradients of
 // 131072 x 128 bf16 24 us, with one 30; of 8192 x 4096 48 us, with one 63).  One, where two of floats with all their companions do not fit the registers (`one`: gradients of 131072 x 64
 // floats 23 us, with two 26; norm of as many into 8 bits 20, with two 23) or octets have to be in neighbouring lanes (rows at any alignment), or more threads would go without.  Rows of up to 64 octets take part of a warp each and meet no barrier; longer ones have a block of their own.
-// V = 0: more than 512 threads hold.
+// Four, where `four` says so, of rows that 512 threads with two do not hold.  V = 0: more than they hold.
 struct Team { int V, group, threads; long groups; };
-inline Team team_of(int octets, bool one) {
+inline Team team_of(int octets, bool one, bool four = false) {
   Team t = {};
   const auto up = [](int n) { return (n + 31) / 32 * 32; };
   if (octets <= (one ? 32 : 64)) {
@@ -380,8 +380,9 @@ inline Team team_of(int octets, bool one) {
     t.threads = 128;
   } else {
     const int n1 = up(octets), n2 = up((octets + 1) / 2);
-    t.V = n1 <= 512 && (one || n1 < 2 * n2) ? 1 : n2 <= 512 ? 2 : 0;
-    t.group = t.threads = t.V == 1 ? n1 : t.V == 2 ? n2 : 1024;
+    const int n4 = up((octets + 3) / 4);
+    t.V = n1 <= 512 && (one || n1 < 2 * n2) ? 1 : n2 <= 512 ? 2 : four && n4 <= 512 ? 4 : 0;
+    t.group = t.threads = t.V == 1 ? n1 : t.V == 2 ? n2 : t.V == 4 ? n4 : 1024;
   }
   t.groups = t.threads / t.group;
   return t;

@@ -130,6 +130,35 @@ def test_values_that_pass_32_bits():
     assert torch.equal((Y[first:] != 0).cpu(), R.kept(25, 17, 0.5, 3, first=first))
 
 
+@pytest.mark.parametrize("C", [16, 17])
+def test_norms_of_values_that_pass_32_bits(C):
+    """The last rows of more than 2^31 values, and the columns' sums over all of them (of ones: their number, which floats hold)."""
+    rows, t = 2 ** 27 + 6, torch.bfloat16
+    X = torch.ones(rows, C, dtype=t, device="cuda")
+    tail = tensor((20, C), t, 1)
+    X[-20:] = tail
+    Y, H, rstd = xb.xconv_rmsnorm(X, p=0.25, seed=3)
+    mask = R.kept(20, C, 0.25, 3, first=rows - 20)
+    x = torch.where(mask, R.last(tail) / 0.75, torch.zeros((), dtype=torch.float64))
+    (y, h, s), (y_off, h_off, s_off) = R.norm(x, None, None, 1e-6)
+    R.close("H", R.last(H[-20:]), h, R.rounded(h, h_off, t))
+    R.close("Y", R.last(Y[-20:]), y, R.rounded(y, y_off + h_off * s[:, None], t))
+    del Y, H
+    Q, scales, _, _ = xb.xconv_rmsnorm_quantized(X, qdtype=torch.int8)
+    (y, _, _), (y_off, _, _) = R.norm(tail, None, None, 1e-6)
+    codes, wide = check_8_bits(Q[-20:], scales[-20:], y, y_off, C, 127.0)
+    V = xb.xconv_dequantize(Q, scales, dtype=t)
+    R.close("V", R.last(V[-20:]), codes * wide, R.rounded(codes * wide, 0 * wide, t))
+    del Q, V
+    ones = torch.ones(rows, device="cuda")
+    dX, _, dw = xb.xconv_rmsnorm_backward(X, X, ones)
+    (dx, _, _), (x_off, _, _) = R.norm_backward(X[-20:], X[-20:], ones[-20:], None, None)
+    R.close("dX", R.last(dX[-20:]), dx, R.rounded(dx, x_off, t))
+    want = rows - 20 + R.last(tail).square().sum(0)
+    # (threads add some 2^27 / 2^15 numbers one after another, each with a rounding of 2^-24 of what is there by then)
+    R.close("dweight", dw.cpu().double(), want, 2.0 ** -11 * want)
+
+
 def _seed_tensor(v):
     return torch.tensor([v], dtype=torch.int64, device="cuda")
 
@@ -359,7 +388,65 @@ def test_a_block_as_it_is_used():
     assert rel(Y2, want) < 2.0 ** -4
 
 
-def test_calls_on_two_streams_and_an_odd_stream():
+@pytest.mark.parametrize("dtype", list(T))
+def test_rows_that_are_one_row_and_weights_at_any_address(dtype):
+    """A row that is broadcast to all (stride 0), and weights that do not begin on a boundary."""
+    t = T[dtype]
+    for C in (8, 40, 97, 1024):
+        X = tensor((1, C), t, 1, scale=2.0).expand(33, C)
+        res = tensor((33, C), t, 2)
+        w = tensor((C + 1,), t, 3)[1:]
+        Y, H, rstd = xb.xconv_rmsnorm(X, w, residual=res, p=0.3, seed=SEED)
+        (y, h, s), (y_off, h_off, _) = R.norm(X, w, res, 1e-6, 0.3, SEED)
+        R.close("Y", R.last(Y), y, R.rounded(y, y_off, t))
+        R.close("H", R.last(H), h, R.rounded(h, h_off, t))
+        dX, dR, dw = xb.xconv_rmsnorm_backward(X, H, rstd, w, dH=X, p=0.3, seed=SEED)
+        (dx, dr, dweight), (x_off, r_off, w_off) = R.norm_backward(X, H, rstd, w, X, 0.3, SEED)
+        R.close("dX", R.last(dX), dx, R.rounded(dx, x_off, t))
+        R.close("dresidual", R.last(dR), dr, R.rounded(dr, r_off, t))
+        R.close("dweight", dw.cpu().double(), dweight, w_off + 2.0 ** -24 * dweight.abs())
+        D = xb.xconv_dropout(X, 0.3, SEED, residual=res)
+        R.close("D", R.last(D), h, R.rounded(h, h_off, t))
+
+
+def test_two_graphs_and_two_threads():
+    """Gradients of two sizes in two captured graphs that are replayed together, and from two host threads: each has scratch memory of its own."""
+    import threading
+    sets = []
+    for rows, C in ((3000, 1024), (2000, 97)):
+        H, dY = tensor((rows, C), torch.bfloat16, 1), tensor((rows, C), torch.bfloat16, 2)
+        _, _, rstd = xb.xconv_rmsnorm(H)
+        sets.append((dY, H, rstd, xb.xconv_rmsnorm_backward(dY, H, rstd)))
+    torch.cuda.synchronize()
+    graphs = []
+    for dY, H, rstd, _ in sets:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            out = xb.xconv_rmsnorm_backward(dY, H, rstd)
+        graphs.append((g, out, torch.cuda.Stream()))
+    for _ in range(10):
+        for g, _, stream in graphs:
+            with torch.cuda.stream(stream):
+                g.replay()
+    torch.cuda.synchronize()
+    for (_, _, _, want), (_, out, _) in zip(sets, graphs):
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
+    bad = []
+
+    def work(dY, H, rstd, want):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(50):
+                got = xb.xconv_rmsnorm_backward(dY, H, rstd)
+                torch.cuda.current_stream().synchronize()
+                if not all(torch.equal(a, b) for a, b in zip(got, want)):
+                    bad.append(1)
+
+    threads = [threading.Thread(target=work, args=s) for s in sets]
+    [t.start() for t in threads]; [t.join() for t in threads]
+    assert not bad
+
+
+def test_calls_on_two_streams():
     X, dY, w = tensor((512, 1024), torch.bfloat16, 1), tensor((512, 1024), torch.bfloat16, 2), tensor((1024,), torch.float32, 3)
     _, H, rstd = xb.xconv_rmsnorm(X, w)
     want = xb.xconv_rmsnorm_backward(dY, H, rstd, w)
