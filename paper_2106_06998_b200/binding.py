@@ -184,7 +184,7 @@ def _load_native():
     L = lib()                                   # (before `_native` is set)
     try:
         from . import _marshal
-        if getattr(_marshal, "key", None) != marshal_key():
+        if getattr(_marshal, "key", None) != marshal_key() or not hasattr(_marshal, "use_rows"):
             raise ImportError(f"it was not compiled as {marshal_key()}")
     except ImportError as e:
         warnings.warn(f"{os.path.join(_HERE, '_marshal.so')} cannot be loaded ({e}): calls go through ctypes, which takes some 10 us more of the host each; "

@@ -252,7 +252,7 @@ constexpr long WIDE_ROWS = 64, WIDE_PARTS = 512;
 struct Plan { Team team; long blocks, parts; };
 Plan plan_of(const xconv_rows_desc* d, bool vec) {
   Plan p = {};
-  p.team = team_of((d->C + 7) / 8, d->dtype == XCONV_F32 || !vec);
+  p.team = team_of((d->C + 7) / 8, d->dtype == XCONV_F32 || !vec, vec && d->dtype != XCONV_F32);
   // (at most: 1024 threads of an SM)
   p.blocks = std::min((d->rows + p.team.groups - 1) / p.team.groups, (long)ROWS_SMS * std::max(1, 1024 / p.team.threads));
   p.parts = p.team.V ? p.blocks : std::min((d->rows + WIDE_ROWS - 1) / WIDE_ROWS, WIDE_PARTS);
@@ -287,6 +287,8 @@ cudaError_t launch_rms_backward(const xconv_rows_desc* d, const void* dY, const 
         const auto pick = [&](auto v, auto dropped) -> void (*)(const RmsBackArgs) {
           constexpr bool VEC = decltype(v)::value;
           constexpr int DROP = decltype(dropped)::value;
+          if constexpr (VEC && sizeof(T) == 2)
+            if (V == 4) return rms_backward_kernel<T, 4, VEC, DROP>;
           return V == 0 ? rms_backward_wide_kernel<T, VEC, DROP> : V == 1 ? rms_backward_kernel<T, 1, VEC, DROP> : rms_backward_kernel<T, 2, VEC, DROP>;
         };
         const auto kernel = with_kinds(vec, a.dX.p ? a.drop.how : DROP_NONE, pick);
