@@ -403,7 +403,8 @@ xconv_status xconv_muon_step(const xconv_update_desc* desc, const xconv_matrices
  * half.  The value is dropped iff u < floor(p * 2^32).  seed_add, where it is not NULL, is a device pointer to a number that the kernels add to the seed (modulo 2^64) when they
  * run: a captured graph draws another mask in every replay if the number is moved on between them.  p = 0: nothing is drawn, and the other fields are ignored.
  *
- * THE NORM.  h = drop(X) + residual,   rstd = 1 / sqrt(sum_c h^2 / C + eps),   Y = h * rstd * weight,  from the h that is not rounded.
+ * THE NORM.  h = drop(X) + residual,   rstd = 1 / sqrt(sum_c h^2 / C + eps),   Y = h * rstd * weight,  from the h that is not rounded.  (The sum is a float: of a row whose squares
+ * pass its range, values of some 1e19, rstd is 0.)
  * Gradients, with xh = H * rstd and g = dY * weight:
  *   dresidual = dH + rstd * (g - xh * sum_c (g * xh) / C),   dX = drop'(dresidual, before its rounding),   dweight[c] = sum_i dY * xh.
  *

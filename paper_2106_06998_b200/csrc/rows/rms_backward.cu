@@ -4,6 +4,10 @@
 //
 // Memory bounds it: dy, h (and dh) are read once, dr (and dx) written once.  The threads of a block keep the same columns from row to row and carry dw in registers; blocks
 // leave a partial sum a column each, which a second kernel adds in fixed order (no atomics: the same bits every time).
+//
+// Measured (B200, copy rate 6.57 TB/s; replayed from a graph, with dh): 8192 x 4096 bf16, 268 MB, 47.2 us = 5.7 TB/s, of which the columns' sums 3; 8192 x 4096 floats 88.5 us
+// = 6.1 TB/s; 131072 x 128 bf16 27 us, with one octet a thread 33.  Registers (126 a thread) hold 512 threads an SM, whose loads for the next row are on their way during a sum.
+// One cluster of eight blocks that adds its own sums (a launch less) was slower wherever rows take more than two rounds (1568 x 96 floats 7.0 us, 4.2 by two kernels).
 #include "rms.h"
 #include "rows.cuh"
 

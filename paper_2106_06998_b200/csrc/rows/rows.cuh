@@ -1,7 +1,7 @@
-// (All of these kernels may start while the kernel before them still runs: they wait for it before they read or write anything, and read nothing through the read-only cache.
-// A launch of that kind also costs the host half a microsecond less.)
-//
 // What the kernels on rows share: eight neighbouring values of a row (an octet: what one Philox block decides about) as floats, the mask, sums over a row.
+//
+// All kernels of this folder may start while the kernel before them still runs: they wait for it before they read or write anything, and read nothing through the read-only cache.
+// (A launch of that kind also costs the host half a microsecond less.)
 #pragma once
 
 #include <algorithm>
