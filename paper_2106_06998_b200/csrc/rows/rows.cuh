@@ -70,33 +70,40 @@ __device__ __forceinline__ void fetch8(const Rows& t, const T* row, long n, int 
   f.shift = shift_of<T, VEC>(row);
   const char* at = reinterpret_cast<const char*>(row + (c - f.shift));
   const auto needed = [&](int i) { return in && (i == 0 || c - f.shift + i * PER < C) && (i + 1 < PIECES || VEC || f.shift + 8 > i * PER); };
+  const auto whole = [&](int i) {
+    uint32_t* w = f.w + PIECE * i;
+    if constexpr (PIECE == 4) {
+      const uint4 u = *reinterpret_cast<const uint4*>(at + 4 * PIECE * i);
+      w[0] = u.x; w[1] = u.y; w[2] = u.z; w[3] = u.w;
+    } else {
+      const uint2 u = *reinterpret_cast<const uint2*>(at + 4 * PIECE * i);
+      w[0] = u.x; w[1] = u.y;
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < PIECES * PIECE; ++i) f.w[i] = 0u;
   if (VEC || (unsigned long)(n - 1) < (unsigned long)t.inner) {
 #pragma unroll
-    for (int i = 0; i < PIECES; ++i) {
-      uint32_t* w = f.w + PIECE * i;
-      if constexpr (PIECE == 4) {
-        uint4 u = make_uint4(0u, 0u, 0u, 0u);
-        if (needed(i)) u = *reinterpret_cast<const uint4*>(at + 4 * PIECE * i);
-        w[0] = u.x; w[1] = u.y; w[2] = u.z; w[3] = u.w;
-      } else {
-        uint2 u = make_uint2(0u, 0u);
-        if (needed(i)) u = *reinterpret_cast<const uint2*>(at + 4 * PIECE * i);
-        w[0] = u.x; w[1] = u.y;
-      }
-    }
+    for (int i = 0; i < PIECES; ++i)
+      if (needed(i)) whole(i);
   } else {
-    // (value by value: few rows come here)
+    // (the first and the last row.  A branch of their own: with the question at every piece the others are 10 % slower)
 #pragma unroll
-    for (int i = 0; i < PIECES * PIECE; ++i) {
-      f.w[i] = 0u;
-      if (!needed(i / PIECE)) continue;
+    for (int i = 0; i < PIECES; ++i) {
+      if (!needed(i)) continue;
+      const char* piece = at + 4 * PIECE * i;
+      if (piece >= t.p && piece + 4 * PIECE <= t.end) {
+        whole(i);
+        continue;
+      }
 #pragma unroll
-      for (int e = 0; e < 4 / (int)sizeof(T); ++e) {
-        const char* v = at + 4 * i + e * sizeof(T);
+      for (int e = 0; e < PER; ++e) {
+        const char* v = piece + e * sizeof(T);
+        uint32_t* w = f.w + PIECE * i;
         if (v < t.p || v >= t.end) continue;
-        if constexpr (sizeof(T) == 4) f.w[i] = *reinterpret_cast<const uint32_t*>(v);
-        else if constexpr (sizeof(T) == 2) f.w[i] |= (uint32_t)*reinterpret_cast<const unsigned short*>(v) << (16 * e);
-        else f.w[i] |= (uint32_t)*reinterpret_cast<const unsigned char*>(v) << (8 * e);
+        if constexpr (sizeof(T) == 4) w[e] = *reinterpret_cast<const uint32_t*>(v);
+        else if constexpr (sizeof(T) == 2) w[e / 2] |= (uint32_t)*reinterpret_cast<const unsigned short*>(v) << (16 * (e % 2));
+        else w[e / 4] |= (uint32_t)*reinterpret_cast<const unsigned char*>(v) << (8 * (e % 4));
       }
     }
   }
