@@ -203,7 +203,7 @@ struct DequantArgs {
   Rows Q, X;
   const float* scales;
   Units units;
-  int q, shift, q_groups;          // values of a scale: 2^shift, or (0) a row
+  int shift, q_groups;             // values of a scale: 2^shift, or (0) a row
 };
 
 __device__ __forceinline__ float2 from_e4m3x2(uint32_t u) {
@@ -212,21 +212,23 @@ __device__ __forceinline__ float2 from_e4m3x2(uint32_t u) {
   return __half22float2(*reinterpret_cast<const __half2*>(&h));
 }
 
-__device__ __forceinline__ void codes_of(const uint2& u, int q, float (&f)[8]) {
-  const uint32_t b[2] = {u.x, u.y};
+template <int Q>
+__device__ __forceinline__ void codes_of(uint32_t lo, uint32_t hi, float (&f)[8]) {
+  const uint32_t b[2] = {lo, hi};
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    if (q == XCONV_Q_E4M3) {
-      const float2 lo = from_e4m3x2(b[h] & 0xffffu), hi = from_e4m3x2(b[h] >> 16);
-      f[4 * h] = lo.x; f[4 * h + 1] = lo.y; f[4 * h + 2] = hi.x; f[4 * h + 3] = hi.y;
+    if constexpr (Q == XCONV_Q_E4M3) {
+      const float2 x = from_e4m3x2(b[h] & 0xffffu), y = from_e4m3x2(b[h] >> 16);
+      f[4 * h] = x.x; f[4 * h + 1] = x.y; f[4 * h + 2] = y.x; f[4 * h + 3] = y.y;
     } else {
+      // (a byte moved up by 128 as the last one of 2^23 and so much: a conversion would take the unit that makes a quarter as many)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) f[4 * h + e] = (float)(int)(signed char)(b[h] >> (8 * e));
+      for (int e = 0; e < 4; ++e) f[4 * h + e] = __uint_as_float(__byte_perm(b[h] ^ 0x80808080u, 0x4b000000u, 0x7650 + e)) - 8388736.f;
     }
   }
 }
 
-template <typename T, bool VEC, bool FLAT, int EACH>
+template <typename T, bool VEC, bool FLAT, int Q, int EACH>
 __global__ void __launch_bounds__(256) dequantize_kernel(const DequantArgs a) {
   typedef unsigned char byte;
   pdl_wait();
@@ -245,7 +247,7 @@ __global__ void __launch_bounds__(256) dequantize_kernel(const DequantArgs a) {
     uint32_t b[2];
     words_of<byte, VEC>(fq[i], b);
     float f[8];
-    codes_of(make_uint2(b[0], b[1]), a.q, f);
+    codes_of<Q>(b[0], b[1], f);
 #pragma unroll
     for (int e = 0; e < 8; ++e) f[e] *= scale[i];
     store8<T, VEC>(n.template at<T>(a.X), 8 * n.k, n.C, n.in, f);
@@ -258,10 +260,10 @@ struct LooseDequantArgs {
   void* X;
   const float* scales;
   long values, count;              // count: scales
-  int C, q, group, q_groups;       // group: values of a scale (C: the row)
+  int C, group, q_groups;          // group: values of a scale (C: the row)
   Divisor by;                      // C
 };
-template <typename T>
+template <typename T, int Q>
 __global__ void __launch_bounds__(256) dequantize_loose_kernel(const LooseDequantArgs a) {
   pdl_wait();
   const long first = (long)blockIdx.x * (LOOSE_PIECES * 8);
@@ -292,7 +294,7 @@ __global__ void __launch_bounds__(256) dequantize_loose_kernel(const LooseDequan
     const long s = (row0 + row) * a.q_groups + g;
     const float s0 = a.scales[s], s1 = a.scales[min(s + 1, a.count - 1)], s2 = a.scales[min(s + 2, a.count - 1)];
     float f[8];
-    codes_of(q[i], a.q, f);
+    codes_of<Q>(q[i].x, q[i].y, f);
 #pragma unroll
     for (int e = 0; e < 8; ++e) f[e] *= e < one ? s0 : e < two ? s1 : s2;
     uint32_t w[Octet<T>::WORDS];
@@ -360,7 +362,7 @@ cudaError_t launch_dequantize(const xconv_rows_desc* d, const void* Q, const flo
   DequantArgs a = {};
   const size_t es = d->dtype == XCONV_F32 ? 4 : 2;
   a.Q = rows_of(Q, d->rows, d->C, d->y_stride, 1); a.X = rows_of(X, d->rows, d->C, d->x_stride, es);
-  a.scales = scales; a.q = d->q_type;
+  a.scales = scales; 
   const int group = d->q_group < d->C ? d->q_group : 0;
   while (group && (1 << a.shift) < group) ++a.shift;
   a.q_groups = group ? (d->C + group - 1) / group : 1;
@@ -368,18 +370,22 @@ cudaError_t launch_dequantize(const xconv_rows_desc* d, const void* Q, const flo
   const bool dense = d->x_stride == d->C && d->y_stride == d->C;
   if (!vec && dense && d->C >= 8 && at(Q, 8) && at(X, 16)) {
     LooseDequantArgs l = {};
-    l.Q = static_cast<const unsigned char*>(Q); l.X = X; l.scales = scales; l.values = d->rows * d->C; l.C = d->C; l.q = d->q_type;
+    l.Q = static_cast<const unsigned char*>(Q); l.X = X; l.scales = scales; l.values = d->rows * d->C; l.C = d->C;
     l.group = group ? group : d->C; l.q_groups = a.q_groups; l.count = d->rows * a.q_groups; l.by = divisor((uint32_t)d->C);
     return with_type(d->dtype, [&](auto t) {
       using T = decltype(t);
-      return launch_pdl(dequantize_loose_kernel<T>, dim3((unsigned)((l.values + LOOSE_PIECES * 8 - 1) / (LOOSE_PIECES * 8))), dim3(256), 0, st, l);
+      return launch_pdl(d->q_type == XCONV_Q_E4M3 ? dequantize_loose_kernel<T, XCONV_Q_E4M3> : dequantize_loose_kernel<T, XCONV_Q_INT8>, dim3((unsigned)((l.values + LOOSE_PIECES * 8 - 1) / (LOOSE_PIECES * 8))), dim3(256), 0, st, l);
     });
   }
   const bool flat = vec && dense && group && d->C % group == 0;
   a.units = units_of(d);
   return with_type(d->dtype, [&](auto t) {
     using T = decltype(t);
-    const auto kernel = flat ? dequantize_kernel<T, true, true, 4> : vec ? dequantize_kernel<T, true, false, 4> : dequantize_kernel<T, false, false, 1>;
+    const auto pick = [&](auto q) {
+      constexpr int Q = decltype(q)::value;
+      return flat ? dequantize_kernel<T, true, true, Q, 4> : vec ? dequantize_kernel<T, true, false, Q, 4> : dequantize_kernel<T, false, false, Q, 1>;
+    };
+    const auto kernel = d->q_type == XCONV_Q_E4M3 ? pick(std::integral_constant<int, XCONV_Q_E4M3>()) : pick(std::integral_constant<int, XCONV_Q_INT8>());
     return launch_pdl(kernel, dim3(blocks_of(a.units.count, vec ? 2 : 1)), dim3(256), 0, st, a);
   });
 }
