@@ -410,7 +410,7 @@ xconv_status xconv_muon_step(const xconv_update_desc* desc, const xconv_matrices
  *
  * 8 BITS.  q_type other than XCONV_Q_NONE: Y is stored in one byte a value, for every `q_group` neighbouring values of a row (0, or C and more: the row; 32, 64, 128; a row's last group may
  * be shorter) with a scale = max(their largest magnitude, 2^-100) / M, M = 448 (XCONV_Q_E4M3: four-bit exponent, three-bit mantissa) or 127 (XCONV_Q_INT8):
- * Y = the nearest to y * (1 / scale), ties to even.  A group with a value that is not finite comes back as NaN.  scales [rows][ceil(C / q_group)], or [rows]. */
+ * Y = the nearest to M * (h * weight) / max |h * weight|, ties to even; the product and the quotient are floats, each the nearest one (the quotient but for some 2^-46 of it).  A group with a value that is not finite comes back as NaN.  scales [rows][ceil(C / q_group)], or [rows]. */
 typedef enum { XCONV_Q_NONE = 0, XCONV_Q_E4M3 = 1, XCONV_Q_INT8 = 2 } xconv_qtype;
 typedef struct {
   int64_t rows;

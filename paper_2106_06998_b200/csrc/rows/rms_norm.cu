@@ -7,7 +7,7 @@
 //
 // Measured (B200, copy rate 6.57 TB/s; replayed from a graph, with a residual): 8192 x 4096 bf16, 268 MB, 44.8 us = 6.0 TB/s; 8192 x 4096 floats 85.5 us = 6.3 TB/s; 125000 x 128 bf16
 // 19.4 us; with dropout 8192 x 4096 bf16 51.7 us (a Philox block costs 24 cycles of an SM for 32 octets, and 122 registers hold half the threads); into e4m3 with a scale
-// for 128 values, 235 MB, 8192 x 4096 bf16 46 us (issue slots 75 %); one row 2.5 us, a launch.  Rows that do not begin on 16-byte boundaries: rms_staged.cu.
+// for 128 values, 235 MB, 8192 x 4096 bf16 47 us (issue slots 75 %); one row 2.5 us, a launch.  Rows that do not begin on 16-byte boundaries: rms_staged.cu.
 #include "eight_bits.cuh"
 #include "rms.h"
 
@@ -27,13 +27,12 @@ struct RmsArgs {
 };
 
 template <bool VEC>
-__device__ __forceinline__ void store8q(unsigned char* row, int c, int C, bool in, const float (&y)[8], float inv, int q) {
+__device__ __forceinline__ void store8q(unsigned char* row, int c, int C, bool in, const float (&u)[8], const Scale& f, int q) {
   uint32_t b[2];
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    const float* v = y + 4 * i;
-    b[i] = q == XCONV_Q_E4M3 ? e4m3x2(v[0] * inv, v[1] * inv) | e4m3x2(v[2] * inv, v[3] * inv) << 16
-                             : __byte_perm(__byte_perm(int8(v[0], inv), int8(v[1], inv), 0x0040), __byte_perm(int8(v[2], inv), int8(v[3], inv), 0x0040), 0x5410);
+    const float2 v = q_of(u[4 * i], u[4 * i + 1], f), w = q_of(u[4 * i + 2], u[4 * i + 3], f);
+    b[i] = q == XCONV_Q_E4M3 ? e4m3x2(v) | e4m3x2(w) << 16 : __byte_perm(int8x2(v), int8x2(w), 0x5410);
   }
   store8<unsigned char, VEC>(row, c, C, in, b);
 }
@@ -61,8 +60,9 @@ __device__ __forceinline__ void sum_of(const RmsArgs& a, uint32_t dropped, const
 
 // ---- rows in registers, V octets a thread; the next row is fetched while this one is worked on
 
+// (Two octets into 8 bits: 64 registers, at which an SM holds 1024 threads; with the 69 that the compiler would take 8192 x 4096 bf16 takes 50.1 us, not 47.1.)
 template <typename T, int V, bool VEC, bool Q, int DROP>
-__global__ void __launch_bounds__(512) rms_forward_kernel(const RmsArgs a) {
+__global__ void __launch_bounds__(512, Q && VEC && V == 2 && sizeof(T) == 2 && DROP == DROP_NONE ? 2 : 0) rms_forward_kernel(const RmsArgs a) {
   __shared__ float sums[2][32];
   __shared__ float most[2][32];
   typedef std::conditional_t<Q, unsigned char, T> Y;
@@ -120,12 +120,14 @@ __global__ void __launch_bounds__(512) rms_forward_kernel(const RmsArgs a) {
     ss = row_sum(ss, group, sums[turn]);
     const float rstd = rsqrtf(fmaf(ss, a.inv_c, a.eps));
     if (in && lane == 0 && a.rstd) a.rstd[row] = rstd;
+    const Root root = root_of(rstd);
+    const float by = Q ? root.power : rstd;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       const int k = lane + v * group;
       if (V > 1) a.w.load<T, VEC>(8 * min(k, a.octets - 1), a.C, w);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) h[v][e] *= rstd * w[e];
+      for (int e = 0; e < 8; ++e) h[v][e] *= by * w[e];
       if constexpr (!Q) store8<T, VEC>(ys.out(), 8 * k, a.C, in && k < a.octets, h[v]);
     }
     if constexpr (Q) {
@@ -146,9 +148,9 @@ __global__ void __launch_bounds__(512) rms_forward_kernel(const RmsArgs a) {
       for (int v = 0; v < V; ++v) {
         const int k = lane + v * group;
         const bool here = in && k < a.octets;
-        const Scale f = q_scale(m[v], a.q);
+        const Scale f = q_scale(m[v], root, a.q);
         if (here && (a.q_group ? (8 * k & (a.q_group - 1)) == 0 : k == 0)) a.scales[row * a.q_groups + (a.q_group ? 8 * k >> a.q_shift : 0)] = f.scale;
-        store8q<VEC>(ys.out(), 8 * k, a.C, here, h[v], f.inv, a.q);
+        store8q<VEC>(ys.out(), 8 * k, a.C, here, h[v], f, a.q);
       }
     }
   }
@@ -184,12 +186,14 @@ __global__ void __launch_bounds__(1024) rms_forward_wide_kernel(const RmsArgs a)
     ss = row_sum(ss, 1024, sums[turn]);
     const float rstd = rsqrtf(fmaf(ss, a.inv_c, a.eps));
     if (threadIdx.x == 0 && a.rstd) a.rstd[row] = rstd;
+    const Root root = root_of(rstd);
+    const float by = a.q ? root.power : rstd;
     const auto normed = [&](int k) {
       sum(k, y);
       float w[8];
       a.w.load<T, VEC>(8 * min(k, a.octets - 1), a.C, w);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] *= rstd * w[e];
+      for (int e = 0; e < 8; ++e) y[e] *= by * w[e];
     };
     float m = 0.f;
     if (a.q && !a.q_group) {
@@ -208,9 +212,9 @@ __global__ void __launch_bounds__(1024) rms_forward_wide_kernel(const RmsArgs a)
         continue;
       }
       if (a.q_group) m = group_most(magnitude(y), a.q_group);
-      const Scale f = q_scale(m, a.q);
+      const Scale f = q_scale(m, root, a.q);
       if (here && (a.q_group ? (8 * k & (a.q_group - 1)) == 0 : k == 0)) a.scales[row * a.q_groups + (a.q_group ? 8 * k >> a.q_shift : 0)] = f.scale;
-      store8q<VEC>(const_cast<unsigned char*>(row_of<unsigned char>(a.Y, row)), 8 * k, a.C, here, y, f.inv, a.q);
+      store8q<VEC>(const_cast<unsigned char*>(row_of<unsigned char>(a.Y, row)), 8 * k, a.C, here, y, f, a.q);
     }
   }
 }

@@ -98,23 +98,26 @@ __global__ void __launch_bounds__(512, V <= 4 ? 2 : 1) rms_staged_kernel(const S
         ss = row_sum(ss, group, sums[turn]);
         const float rstd = rsqrtf(fmaf(ss, a.inv_c, a.eps));
         if (in && lane == 0 && a.rstd) a.rstd[row] = rstd;
+        const Root root = root_of(rstd);
+        const float by = a.q ? root.power : rstd;
 #pragma unroll
         for (int v = 0; v < V; ++v)
 #pragma unroll
-          for (int k = 0; k < 2; ++k) h[v][k] *= rstd * w[v][k];
+          for (int k = 0; k < 2; ++k) h[v][k] *= by * w[v][k];
         if (!a.q) {
           if (in) pairs.write(x, h);
         } else {
           float m = 0.f;
 #pragma unroll
           for (int v = 0; v < V; ++v) m = most_of(m, most_of(fabsf(h[v][0]), fabsf(h[v][1])));
-          const Scale f = q_scale(row_most(m, group, most[turn]), a.q);
+          const Scale f = q_scale(row_most(m, group, most[turn]), root, a.q);
           if (in && lane == 0) a.scales[row] = f.scale;
           unsigned char* const to = codes + eight.shift + r * s.C + pairs.column;
           if (in)
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-              const uint32_t b = a.q == XCONV_Q_E4M3 ? e4m3x2(h[v][0] * f.inv, h[v][1] * f.inv) : __byte_perm(int8(h[v][0], f.inv), int8(h[v][1], f.inv), 0x0040);
+              const float2 t = q_of(h[v][0], h[v][1], f);
+              const uint32_t b = a.q == XCONV_Q_E4M3 ? e4m3x2(t) : int8x2(t);
               if (pairs.has(v, 0)) to[2 * v * group] = (unsigned char)b;
               if (pairs.has(v, 1)) to[2 * v * group + 1] = (unsigned char)(b >> 8);
             }
