@@ -7,7 +7,7 @@
 //
 // Measured (B200, copy rate 6.57 TB/s; replayed from a graph): 512 x 256 x 28 x 28 bf16 with a residual, 617 MB, 100 us = 6.2 TB/s (108 in a long loop, at lower clocks); 8192 x 4096 floats
 // 60 us, as a copy; gradients of 16 M bf16 values 16 us (floor 9.7); rows at any alignment: 164948 x 97 bf16 23 us (floor 14.6), by octets cut out in registers 37, whole
-// channels of 47250 x 97 float16 4.5 us (floor 2.8), 10.7; back from int8, 8192 x 4096 into bf16 19.5 us (floor 15.3).
+// channels of 47250 x 97 float16 4.5 us (floor 2.8), 10.7; back from int8, 8192 x 4096 into bf16 18.4 us (floor 15.3).
 #include "rows.cuh"
 
 namespace xconv {
@@ -228,6 +228,9 @@ __device__ __forceinline__ void codes_of(uint32_t lo, uint32_t hi, float (&f)[8]
   }
 }
 
+// Octets a thread of aligned rows: two (32 x 4096 e4m3 into bf16 1.5 us, 8192 x 4096 17.7, into floats 36.5, 131072 x 64 int8 into bf16 6.0) or four (1.9, 18.0, 38.0, 5.9).
+constexpr int DEQUANTIZE_EACH = 2;
+
 template <typename T, bool VEC, bool FLAT, int Q, int EACH>
 __global__ void __launch_bounds__(256) dequantize_kernel(const DequantArgs a) {
   typedef unsigned char byte;
@@ -383,10 +386,10 @@ cudaError_t launch_dequantize(const xconv_rows_desc* d, const void* Q, const flo
     using T = decltype(t);
     const auto pick = [&](auto q) {
       constexpr int Q = decltype(q)::value;
-      return flat ? dequantize_kernel<T, true, true, Q, 4> : vec ? dequantize_kernel<T, true, false, Q, 4> : dequantize_kernel<T, false, false, Q, 1>;
+      return flat ? dequantize_kernel<T, true, true, Q, DEQUANTIZE_EACH> : vec ? dequantize_kernel<T, true, false, Q, DEQUANTIZE_EACH> : dequantize_kernel<T, false, false, Q, 1>;
     };
     const auto kernel = d->q_type == XCONV_Q_E4M3 ? pick(std::integral_constant<int, XCONV_Q_E4M3>()) : pick(std::integral_constant<int, XCONV_Q_INT8>());
-    return launch_pdl(kernel, dim3(blocks_of(a.units.count, vec ? 2 : 1)), dim3(256), 0, st, a);
+    return launch_pdl(kernel, dim3(blocks_of(a.units.count, vec ? DEQUANTIZE_EACH : 1)), dim3(256), 0, st, a);
   });
 }
 
