@@ -31,21 +31,23 @@ static xconv_status validate_q(const xconv_rows_desc* d) {
   if (d->q_group < 0) return XCONV_ERR_INVALID_ARG;
   return d->q_group < d->C && d->q_group != 0 && d->q_group != 32 && d->q_group != 64 && d->q_group != 128 ? XCONV_ERR_UNSUPPORTED : XCONV_OK;
 }
+namespace {
 // A tensor that is there, or may be missing.
-struct Rows {
+struct RowTensor {
   const void* p;
   int64_t stride;
   size_t size;
   bool out, must;
 };
+}  // namespace
 template <int N>
-static xconv_status validate_tensors(const xconv_rows_desc* d, const Rows (&tensors)[N]) {
+static xconv_status validate_tensors(const xconv_rows_desc* d, const RowTensor (&tensors)[N]) {
   const int64_t most = 1L << 60;
-  for (const Rows& t : tensors)
+  for (const RowTensor& t : tensors)
     if ((t.must && !t.p) || (t.p && (t.stride < 0 || (t.out && t.stride < d->C)))) return XCONV_ERR_INVALID_ARG;
-  for (const Rows& t : tensors)
+  for (const RowTensor& t : tensors)
     if (t.p && d->rows > 0 && t.stride > most / d->rows) return XCONV_ERR_UNSUPPORTED;
-  for (const Rows& t : tensors)
+  for (const RowTensor& t : tensors)
     if (off(t.p, t.size)) return XCONV_ERR_ALIGNMENT;
   return XCONV_OK;
 }
