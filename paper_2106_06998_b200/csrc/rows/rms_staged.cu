@@ -232,12 +232,10 @@ long rms_staged_backward_parts(const xconv_rows_desc* d) {
   long most = 0;
   if (!is_odd(d)) return 0;
   // (fewer tensors need less memory, so that more blocks fit)
-  for (int slots = 2; slots <= 3; ++slots)
-    for (int how : {DROP_NONE, DROP_HOST}) {
-      s.drop.how = how;
-      const StagedPlan p = staged_plan(d, slots, true, false, &s);
-      if (p.threads) most = std::max(most, p.blocks);
-    }
+  for (int slots = 2; slots <= 3; ++slots) {
+    const StagedPlan p = staged_plan(d, slots, true, false, &s);
+    if (p.threads) most = std::max(most, p.blocks);
+  }
   return most;
 }
 
