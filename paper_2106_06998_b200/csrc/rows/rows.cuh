@@ -376,8 +376,8 @@ inline int pow2_from(long n) { int p = 1; while (p < n) p *= 2; return p; }
 // Threads a row and octets a thread.  Two octets a thread: what it keeps beside them once for two, half the steps of a sum over the row, and twice the bytes on their way (gradients of
 // 131072 x 128 bf16 24 us, with one 30; of 8192 x 4096 48 us, with one 63).  One, where two of floats with all their companions do not fit the registers (`one`: gradients of 131072 x 64
 // floats 23 us, with two 26; norm of as many into 8 bits 20, with two 23) or octets have to be in neighbouring lanes (rows at any alignment), or more threads would go without.  Rows of up to 64 octets take part of a warp each and meet no barrier; longer ones have a block of their own.
-// Four, where `four` says so, of rows that 512 threads with two do not hold (4096 x 12288 bf16: norm 69 us, read again for every step 113; gradients, though a third of what a thread keeps
-// is then in local memory, 156 and 199).  V = 0: more than they hold.
+// Four, where `four` says so, of rows that 512 threads with two do not hold (4096 x 12288 bf16: norm 69 us, read again for every step 113; gradients, by a kernel of their own, 97
+// and 199).  V = 0: more than they hold.
 struct Team { int V, group, threads; long groups; };
 inline Team team_of(int octets, bool one, bool four = false) {
   Team t = {};
