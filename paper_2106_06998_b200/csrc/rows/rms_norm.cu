@@ -5,8 +5,8 @@
 // Memory bounds it: x and the residual are read once, h and y written once.  A row lies in the registers of `group` threads, V octets each; h stays in float for y (it
 // is rounded once, where it is written).  Blocks go from row to row, and a row's loads are under way while the one before is summed and written; nothing is staged.
 //
-// Measured (B200, copy rate 6.57 TB/s; replayed from a graph, with a residual): 8192 x 4096 bf16, 268 MB, 44.8 us = 6.0 TB/s; 8192 x 4096 floats 85.5 us = 6.3 TB/s; 125000 x 128 bf16
-// 19.4 us; with dropout 8192 x 4096 bf16 51.7 us (a Philox block costs 24 cycles of an SM for 32 octets, and 122 registers hold half the threads); into e4m3 with a scale
+// Measured (B200, copy rate 6.57 TB/s; replayed from a graph, with a residual): 8192 x 4096 bf16, 268 MB, 44.5 us = 6.0 TB/s; 8192 x 4096 floats 85.6 us = 6.3 TB/s; 125000 x 128 bf16
+// 23.0 us; with dropout 8192 x 4096 bf16 53.3 us (a Philox block costs 24 cycles of an SM for 32 octets, and 122 registers hold half the threads); into e4m3 with a scale
 // for 128 values, 235 MB, 8192 x 4096 bf16 47 us (issue slots 75 %); one row 2.5 us, a launch.  Rows that do not begin on 16-byte boundaries: rms_staged.cu.
 #include "eight_bits.cuh"
 #include "rms.h"
@@ -259,8 +259,8 @@ cudaError_t launch_rms_forward(const xconv_rows_desc* d, const void* X, const vo
     };
     const auto kernel = with_kinds(vec, a.drop.how, pick);
     // As many blocks as the SMs hold, or several times as many: the later ones' rows begin as the first ones' end, at different times, which serves where memory alone bounds them (four
-    // times: 125000 x 128 floats 42 us, once 48; twice: 8192 x 4096 bf16 44.5 us, once 47) and costs where threads have much to set up for little (125000 x 128 bf16 21 us, once
-    // 19.4; 8192 x 4096 bf16 with dropout 54 us, once 52).
+    // times: 125000 x 128 floats 42.0 us, once 48.1; twice: 8192 x 4096 bf16 44.1 us, once 46.9) and costs where threads have much to set up for little (8192 x 4096 bf16 with dropout: four times
+    // 55.2 us, once 53.2; of 125000 x 128 bf16 four times would be 22.2 us, once is 23.2).
     const int waves = es == 4 ? 4 : a.drop.how == DROP_NONE && p.group > 32 ? 2 : 1;
     const long blocks = std::min((d->rows + p.groups - 1) / p.groups, (long)ROWS_SMS * waves * resident_blocks(kernel, p.threads, 0));
     return launch_pdl(kernel, dim3((unsigned)blocks), dim3(p.threads), 0, st, a);

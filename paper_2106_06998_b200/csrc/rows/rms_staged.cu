@@ -1,7 +1,8 @@
 // RMS norm and its gradients of dense rows that do not begin on 16-byte boundaries (formulas: rms_norm.cu, rms_backward.cu).
 //
-// Instructions bound it.  Measured (B200; replayed from a graph): 47250 x 97 float16 with residual and dropout 16.4 us (floor of bytes 5.6), by octets cut out in registers 23; gradients
-// with dh 21.5 us (floor 7.0), 31; 164948 x 97 bf16 without dropout 39 us (floor 19.5), 59, with it 53, 67.  Masks drawn into shared memory by all threads before a run's
+// Too few warps bound it: 16 an SM or fewer, which fill 62 to 64 % of the issue slots (a row's pairs take the registers of more).  Measured (B200; replayed from a graph): 47250 x 97 float16 with
+// residual and dropout 17 to 18 us (floor of bytes 5.6), by octets cut out in registers 23; gradients
+// with dh 21.5 us (floor 7.0), 31; 164948 x 97 bf16 without dropout 39 us (floor 19.5), 59, with it 54, 67; 8192 x 4097 bf16 100 us, gradients 124 (floors 40.9).  Masks drawn into shared memory by all threads before a run's
 // rows: 58 instead of 53.
 #include "eight_bits.cuh"
 #include "rms.h"

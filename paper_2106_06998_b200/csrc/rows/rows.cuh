@@ -374,8 +374,8 @@ inline bool at(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) 
 inline int pow2_from(long n) { int p = 1; while (p < n) p *= 2; return p; }
 
 // Threads a row and octets a thread.  Two octets a thread: what it keeps beside them once for two, half the steps of a sum over the row, and twice the bytes on their way (gradients of
-// 131072 x 128 bf16 24 us, with one 30; of 8192 x 4096 48 us, with one 63).  One, where two of floats with all their companions do not fit the registers (`one`: gradients of 131072 x 64
-// floats 23 us, with two 26; norm of as many into 8 bits 20, with two 23) or octets have to be in neighbouring lanes (rows at any alignment), or more threads would go without.  Rows of up to 64 octets take part of a warp each and meet no barrier; longer ones have a block of their own.
+// 131072 x 128 bf16 26 us, with one 30; of 8192 x 4096 47 us, with one 59).  One, where two of floats with all their companions do not fit the registers (`one`: gradients of 131072 x 64
+// floats 26 us, with two 30; norm of as many into 8 bits 19, with two 22) or octets have to be in neighbouring lanes (rows at any alignment), or more threads would go without.  Rows of up to 64 octets take part of a warp each and meet no barrier; longer ones have a block of their own.
 // Four, where `four` says so, of rows that 512 threads with two do not hold (4096 x 12288 bf16: norm 69 us, read again for every step 113; gradients, by a kernel of their own, 97
 // and 199).  V = 0: more than they hold.
 struct Team { int V, group, threads; long groups; };
@@ -408,7 +408,7 @@ inline Drop drop_of(const xconv_rows_desc* d) {
   r.scale = d->p < 1.0 ? (float)(1.0 / (1.0 - d->p)) : 0.f;
   return r;
 }
-// Blocks of a kernel that an SM holds.  (Asked once: the devices are all alike.)
+// Blocks of a kernel that an SM of the current device holds.  (Asked in every launch: nothing is kept between calls.)
 template <typename... A>
 int resident_blocks(void (*kernel)(A...), int threads, int smem) {
   int n = 0;

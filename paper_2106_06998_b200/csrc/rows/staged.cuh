@@ -1,7 +1,7 @@
 // Dense rows that do not begin on 16-byte boundaries, by runs of rows through shared memory: what the forward and the backward kernel share.
 //
 // A run's bytes are copied as whole pieces of 16 bytes (asynchronously, stages - 1 runs ahead) to a place in shared memory that has the same position about a boundary, worked on there two
-// values at a time, neighbouring lanes on neighbouring pairs, and results go back over the inputs and out in pieces again.  Instructions bound such rows: a thread's rows are all
+// values at a time, neighbouring lanes on neighbouring pairs, and results go back over the inputs and out in pieces again.  Instructions count for such rows: a thread's rows are all
 // even or all odd in number, so that what of its pairs is the row's is known before the first one.
 #pragma once
 
